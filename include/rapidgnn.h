@@ -12,6 +12,10 @@
  *              fallback pull of the misses from the remote store
  * and two companions: rg_mean_aggregate (Eq. 1 with AGG = mean over a sampled block, the consumer of the
  * gathered rows) and rg_cache_hit_curve (Section V: remote fetches against cache size).
+ * Line 15, the training step on a gathered batch, has its operators as well: feature rows of 4-bit numbers that the steps
+ * above move as they are (rg_mx4_quantize, rg_mx4_dequantize), their product with a weight and its gradient (rg_mx4_matmul,
+ * rg_mx4_matmul_grad), layer norm (rg_layer_norm, rg_layer_norm_grad), and clipping by the norm of all gradients
+ * (rg_clip_grad_norm).
  * Every step runs in HIP kernels on the device; there is no CPU fallback.
  *
  * Conventions
@@ -426,6 +430,85 @@ RG_API rg_status rg_gather_features_static(rg_ctx* ctx, const int32_t* input_nod
 RG_API rg_status rg_mean_aggregate(rg_ctx* ctx, const int32_t* indptr, const int32_t* nbr_local, int64_t n_dst,
                                    const int32_t* n_dst_dev, const float* feat, int64_t feat_stride, int32_t dim,
                                    float* agg, int64_t agg_stride, void* stream);
+
+/* ---- rows of numbers, and the types they come in ------------------------------------------------
+ * The operators below take rows of 32- or 16-bit numbers: strides are in numbers of the array's type, a
+ * row needs no more alignment than its numbers, and what lies behind a row's own numbers is neither
+ * read nor written.  n is at most 2^31 - 1; n_dev is an optional device count as for
+ * rg_access_histogram (rows beyond min(n, *n_dev) are neither read nor written and add to no sum).  Every
+ * sum is kept in 32 bits or more; a 16-bit result is rounded once, to the nearest.  Results do not
+ * depend on timing: the same call gives the same bits.  Inputs and outputs do not overlap unless a
+ * call says that they may. */
+typedef enum { RG_F32 = 0, RG_BF16 = 1, RG_F16 = 2 } rg_dtype;
+
+/* ---- packed rows: 4-bit numbers with a scale per group of 32 -------------------------------------
+ * A packed row of dim numbers is rg_mx4_row_words(dim) words of 32 bits, so that the stores, the cache
+ * and the gather hold and move it as a row of that many floats (bits are copied as they are): 256 floats
+ * of 1024 bytes become 34 words of 136.  With G = ceil(dim / 32): 16 G bytes of codes (number 2i in the
+ * low half of byte i, 2i + 1 in the high half; codes behind the row's own numbers are 0), then G scale bytes,
+ * then zero bytes up to a whole word.  A code is a sign bit (8) and a magnitude of
+ * 0, 0.5, 1, 1.5, 2, 3, 4, 6; scale byte s stands for 2^(s - 127), 255 for "not a number".
+ * Quantisation: s = max(0, floor(log2 max|x|) - 2 + 127) over the group, each x / 2^(s - 127) goes to the
+ * nearest magnitude (halves to the even code, above 6 to 6, the sign of what becomes 0 is kept).  A group
+ * that holds a NaN or an infinity gets s = 255 and codes 0: all of it reads as NaN.
+ * 1 <= dim <= RG_MX4_MAX_DIM; packed strides are in words of 32 bits. */
+#define RG_MX4_MAX_DIM 65536
+RG_API int64_t rg_mx4_row_words(int32_t dim);      /* 0 if dim is out of range */
+/* x and packed may be mapped memory: a remote store can be packed where it lies. */
+RG_API rg_status rg_mx4_quantize(rg_ctx* ctx, const void* x, rg_dtype x_type, int64_t x_stride, int64_t n, const int32_t* n_dev,
+                                 int32_t dim, void* packed, int64_t packed_stride, void* stream);
+RG_API rg_status rg_mx4_dequantize(rg_ctx* ctx, const void* packed, int64_t packed_stride, int64_t n, const int32_t* n_dev,
+                                   int32_t dim, void* x, rg_dtype x_type, int64_t x_stride, void* stream);
+
+/* y[i][j] = sum_k rows[i][k] weight[j][k] for j < out_dim: the projection of packed rows by packed weight rows
+ * (Eq. 1's matrix).  rows: device, n packed rows; weight: device, out_dim packed rows; y: device.  Products of 4-bit
+ * numbers are exact; the sums are the matrix unit's, in 32 bits.  1 <= out_dim <= RG_MX4_MAX_DIM. */
+RG_API rg_status rg_mx4_matmul(rg_ctx* ctx, const void* rows, int64_t rows_stride, int64_t n, const int32_t* n_dev,
+                               const void* weight, int64_t weight_stride, int32_t out_dim, int32_t dim, void* y,
+                               rg_dtype y_type, int64_t y_stride, void* stream);
+/* grad[j][k] = sum_i dy[i][j] rows[i][k]: the gradient of that product to its weight (taken as the numbers it
+ * was rounded from: the rounding passes the gradient on).  dy keeps all its bits: a 32-bit number goes through
+ * the matrix unit in three parts, one of 16 bits in one or two.  grad: device float[out_dim * grad_stride], overwritten
+ * (zeros where there are no rows). */
+RG_API rg_status rg_mx4_matmul_grad(rg_ctx* ctx, const void* dy, rg_dtype dy_type, int64_t dy_stride, const void* rows,
+                                    int64_t rows_stride, int64_t n, const int32_t* n_dev, int32_t out_dim, int32_t dim,
+                                    float* grad, int64_t grad_stride, void* stream);
+
+/* ---- layer norm ----------------------------------------------------------------------------------
+ * mean_i = sum_k x[i][k] / dim, rstd_i = 1 / sqrt(sum_k (x[i][k] - mean_i)^2 / dim + eps),
+ * y[i][k] = (x[i][k] - mean_i) rstd_i gamma[k] + beta[k].
+ * x and y: device, of type `type`, and y may be x itself (same stride); gamma, beta: device float[dim], or NULL for 1 and
+ * 0; mean, rstd: device float[n], or NULL where no backward pass follows.  eps >= 0. */
+#define RG_NORM_MAX_DIM 65536
+RG_API rg_status rg_layer_norm(rg_ctx* ctx, const void* x, rg_dtype type, int64_t x_stride, int64_t n, const int32_t* n_dev,
+                               int32_t dim, const float* gamma, const float* beta, float eps, void* y, int64_t y_stride,
+                               float* mean, float* rstd, void* stream);
+/* Its backward pass.  With h[i][k] = (x[i][k] - mean_i) rstd_i and g[i][k] = dy[i][k] gamma[k]:
+ * dx[i][k] = rstd_i (g[i][k] - sum_k g[i][k] / dim - h[i][k] sum_k g[i][k] h[i][k] / dim),
+ * dgamma[k] = sum_i dy[i][k] h[i][k], dbeta[k] = sum_i dy[i][k].
+ * dy, x, dx: device, of type `type`; dx may be dy or x itself (same stride).  gamma as above; mean and rstd are the forward
+ * pass's.  dx, dgamma, dbeta: each may be NULL (not wanted); dgamma and dbeta: device float[dim], overwritten (zeros where
+ * there are no rows). */
+RG_API rg_status rg_layer_norm_grad(rg_ctx* ctx, const void* dy, int64_t dy_stride, const void* x, int64_t x_stride,
+                                    rg_dtype type, int64_t n, const int32_t* n_dev, int32_t dim, const float* gamma,
+                                    const float* mean, const float* rstd, void* dx, int64_t dx_stride, float* dgamma,
+                                    float* dbeta, void* stream);
+
+/* ---- the norm of all gradients, and clipping -----------------------------------------------------
+ * norm = sqrt(sum of the squares of every number of every tensor); where norm is finite and larger than max_norm
+ * every number g becomes g max_norm / norm, else it stays.  (A step whose norm is not finite is the caller's to
+ * skip.)  The squares are summed in 64 bits, so that no finite gradient's norm overflows on the way.
+ * tensors: host array[count] of contiguous device arrays; `out` may be `in` itself or another array that overlaps
+ * none of the call's; count >= 0, numbers in all < 2^40.  norm: device float, written.  max_norm >= 0, or infinity to
+ * measure only (numbers are copied where out is another array). */
+typedef struct {
+    const void* in;
+    void* out;
+    int64_t size;          /* numbers; 0 is allowed (and the pointers then not looked at) */
+    rg_dtype type;
+} rg_tensor;
+RG_API rg_status rg_clip_grad_norm(rg_ctx* ctx, const rg_tensor* tensors, int32_t count, float max_norm, float* norm,
+                                   void* stream);
 
 /* ---- kernel timing for the benchmark ------------------------------------------------------
  * With profiling on, every launch of the listed kernels is bracketed by hipEvents on its own

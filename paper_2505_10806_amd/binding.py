@@ -22,7 +22,11 @@ RG_GATHER_TICKETS = 8
 RG_ORDER_ASCENDING, RG_ORDER_FIRST_SEEN = 0, 1
 RG_STATIC_GATHER_MAX_ROWS = 1 << 20
 RG_GATHER_PART_HBM, RG_GATHER_PART_MISS = 1, 2
+RG_F32, RG_BF16, RG_F16 = range(3)
+RG_MX4_MAX_DIM = RG_NORM_MAX_DIM = 65536
 RG_K_GATHER_HBM, RG_K_GATHER_MISS, RG_K_SAMPLE, RG_K_HISTOGRAM, RG_K_CACHE_FILL, RG_K_AGGREGATE = range(6)
+
+_TYPES = {torch.float32: RG_F32, torch.bfloat16: RG_BF16, torch.float16: RG_F16}
 
 _STATUS_NAMES = {0: "RG_OK", 1: "RG_ERR_INVALID_ARG", 2: "RG_ERR_CAPACITY", 3: "RG_ERR_OOM",
                  4: "RG_ERR_HIP", 5: "RG_ERR_STATE"}
@@ -57,6 +61,10 @@ class rg_cache(ctypes.Structure):
 
 class rg_prefetch_plan(ctypes.Structure):
     _fields_ = [("list", c_p), ("list_capacity", c_i64), ("offsets", c_p), ("num_batches", c_i32)]
+
+
+class rg_tensor(ctypes.Structure):
+    _fields_ = [("in_", c_p), ("out", c_p), ("size", c_i64), ("type", c_i32)]
 
 
 def _load():
@@ -98,6 +106,15 @@ def _load():
                                      c_i32, c_p, c_i64, c_p, c_p, c_p]
     L.rg_gather_features_static.argtypes = L.rg_gather_features.argtypes
     L.rg_gather_run_part.argtypes = [c_p, c_i32, c_i32, c_i64, c_p, ctypes.POINTER(rg_cache), c_p, c_i64, c_p, c_i64, c_i32, c_p, c_i64, c_p]
+    L.rg_mx4_row_words.argtypes = [c_i32]
+    L.rg_mx4_row_words.restype = c_i64
+    L.rg_mx4_quantize.argtypes = [c_p, c_p, c_i32, c_i64, c_i64, c_p, c_i32, c_p, c_i64, c_p]
+    L.rg_mx4_dequantize.argtypes = [c_p, c_p, c_i64, c_i64, c_p, c_i32, c_p, c_i32, c_i64, c_p]
+    L.rg_mx4_matmul.argtypes = [c_p, c_p, c_i64, c_i64, c_p, c_p, c_i64, c_i32, c_i32, c_p, c_i32, c_i64, c_p]
+    L.rg_mx4_matmul_grad.argtypes = [c_p, c_p, c_i32, c_i64, c_p, c_i64, c_i64, c_p, c_i32, c_i32, c_p, c_i64, c_p]
+    L.rg_layer_norm.argtypes = [c_p, c_p, c_i32, c_i64, c_i64, c_p, c_i32, c_p, c_p, ctypes.c_float, c_p, c_i64, c_p, c_p, c_p]
+    L.rg_layer_norm_grad.argtypes = [c_p, c_p, c_i64, c_p, c_i64, c_i32, c_i64, c_p, c_i32, c_p, c_p, c_p, c_p, c_i64, c_p, c_p, c_p]
+    L.rg_clip_grad_norm.argtypes = [c_p, ctypes.POINTER(rg_tensor), c_i32, ctypes.c_float, c_p, c_p]
     L.rg_profile_enable.argtypes = [c_p, ctypes.c_int]
     L.rg_profile_reset.argtypes = [c_p]
     L.rg_profile_select.argtypes = [c_p, ctypes.c_uint32]
@@ -106,7 +123,9 @@ def _load():
                  "rg_access_histogram", "rg_access_histogram_epoch", "rg_access_histogram_sampled", "rg_build_cache", "rg_cache_hit_curve",
                  "rg_prefetch_cache_rows", "rg_plan_prefetch", "rg_plan_sampled", "rg_prefetch_planned", "rg_gather_features",
                  "rg_gather_features_static", "rg_gather_prepare", "rg_gather_run", "rg_mean_aggregate", "rg_profile_enable",
-                 "rg_profile_reset", "rg_profile_read", "rg_profile_select", "rg_stream_create", "rg_stream_destroy", "rg_gather_run_part"):
+                 "rg_profile_reset", "rg_profile_read", "rg_profile_select", "rg_stream_create", "rg_stream_destroy", "rg_gather_run_part",
+                 "rg_mx4_quantize", "rg_mx4_dequantize", "rg_mx4_matmul", "rg_mx4_matmul_grad", "rg_layer_norm", "rg_layer_norm_grad",
+                 "rg_clip_grad_norm"):
         getattr(L, name).restype = ctypes.c_int
     return L
 
@@ -119,7 +138,9 @@ EXPORTED_SYMBOLS = ["rg_create", "rg_destroy", "rg_last_error", "rg_version", "r
                     "rg_build_cache", "rg_cache_hit_curve", "rg_prefetch_cache_rows", "rg_plan_prefetch",
                     "rg_plan_sampled", "rg_prefetch_planned", "rg_gather_features", "rg_gather_features_static",
                     "rg_stream_create", "rg_stream_destroy", "rg_gather_prepare", "rg_gather_run_part",
-                    "rg_gather_run", "rg_mean_aggregate", "rg_profile_enable", "rg_profile_select", "rg_profile_reset", "rg_profile_read"]
+                    "rg_gather_run", "rg_mean_aggregate", "rg_mx4_row_words", "rg_mx4_quantize", "rg_mx4_dequantize",
+                    "rg_mx4_matmul", "rg_mx4_matmul_grad", "rg_layer_norm", "rg_layer_norm_grad", "rg_clip_grad_norm",
+                    "rg_profile_enable", "rg_profile_select", "rg_profile_reset", "rg_profile_read"]
 
 
 def _ptr(t, dtype=None, device_type=None, name="tensor"):
@@ -137,6 +158,38 @@ def _ptr(t, dtype=None, device_type=None, name="tensor"):
     if not t.is_contiguous():
         raise ValueError(f"{name}: tensor must be contiguous")
     return t.data_ptr()
+
+
+def _rows(t, n, width, dtype=None, device_type="cuda", name="tensor"):
+    """(address, row stride) of a tensor of at least n rows with at least `width` numbers side by side (None -> NULL)."""
+    if t is None:
+        return None, 0
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
+    if device_type == "cuda" and not t.is_cuda:
+        raise ValueError(f"{name}: expected a cuda tensor, got {t.device}")
+    if device_type == "mapped" and not t.is_cuda and not t.is_pinned():
+        raise ValueError(f"{name}: host tensor must be pinned to be read from the device")
+    if t.dim() != 2 or t.shape[0] < n or t.shape[1] < width or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name}: expected rows of at least {width} numbers side by side, {n} of them; got shape {tuple(t.shape)}, "
+                         f"strides {t.stride()}")
+    # (the stride of a single row says nothing)
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def _numbers(t, n, dtype, name):
+    """Address of at least n numbers one behind the other (None -> NULL)."""
+    p = _ptr(t, dtype, "cuda", name)
+    if t is not None and t.numel() < n:
+        raise ValueError(f"{name}: {t.numel()} numbers, {n} required")
+    return p
+
+
+def _type(t, name):
+    try:
+        return _TYPES[t.dtype]
+    except KeyError:
+        raise TypeError(f"{name}: expected float32, bfloat16 or float16, got {t.dtype}") from None
 
 
 # The current stream's handle without a Stream object around it (0.2 us instead of 2.7: a call of one launch took 9.2 us, now 5.9).
@@ -365,6 +418,69 @@ class Context:
             _ptr(feat, torch.float32, "cuda", "feat"), feat.stride(0), int(dim),
             _ptr(agg, torch.float32, "cuda", "agg"), agg.stride(0), _stream_handle(stream)))
 
+    # -- rg_mx4_*
+    def mx4_quantize(self, x, n, dim, packed, n_dev=None, stream=None):
+        """x: [>= n, >= dim] float32, bfloat16 or float16; packed: float32 [>= n, >= mx4_row_words(dim)] (see mx4_rows).  Either may
+        be pinned host memory."""
+        px, sx = _rows(x, n, dim, None, "mapped", "x")
+        pp, sp = _rows(packed, n, mx4_row_words(dim), torch.float32, "mapped", "packed")
+        self._check(_lib.rg_mx4_quantize(self._h, px, _type(x, "x"), sx, int(n), _ptr(n_dev, torch.int32, "cuda", "n_dev"), int(dim), pp, sp,
+                                         _stream_handle(stream)))
+        return packed
+
+    def mx4_dequantize(self, packed, n, dim, x, n_dev=None, stream=None):
+        px, sx = _rows(x, n, dim, None, "mapped", "x")
+        pp, sp = _rows(packed, n, mx4_row_words(dim), torch.float32, "mapped", "packed")
+        self._check(_lib.rg_mx4_dequantize(self._h, pp, sp, int(n), _ptr(n_dev, torch.int32, "cuda", "n_dev"), int(dim), px, _type(x, "x"), sx,
+                                           _stream_handle(stream)))
+        return x
+
+    def mx4_matmul(self, rows, n, weight, out_dim, dim, y, n_dev=None, stream=None):
+        """y[:n, :out_dim] = rows . weight^T of packed rows; y: float32, bfloat16 or float16."""
+        words = mx4_row_words(dim)
+        pr, sr = _rows(rows, n, words, torch.float32, "cuda", "rows")
+        pw, sw = _rows(weight, out_dim, words, torch.float32, "cuda", "weight")
+        py, sy = _rows(y, n, out_dim, None, "cuda", "y")
+        self._check(_lib.rg_mx4_matmul(self._h, pr, sr, int(n), _ptr(n_dev, torch.int32, "cuda", "n_dev"), pw, sw, int(out_dim), int(dim), py,
+                                       _type(y, "y"), sy, _stream_handle(stream)))
+        return y
+
+    def mx4_matmul_grad(self, dy, rows, n, out_dim, dim, grad, n_dev=None, stream=None):
+        """grad[:out_dim, :dim] = dy^T . rows; grad: float32."""
+        pd, sd = _rows(dy, n, out_dim, None, "cuda", "dy")
+        pr, sr = _rows(rows, n, mx4_row_words(dim), torch.float32, "cuda", "rows")
+        pg, sg = _rows(grad, out_dim, dim, torch.float32, "cuda", "grad")
+        self._check(_lib.rg_mx4_matmul_grad(self._h, pd, _type(dy, "dy"), sd, pr, sr, int(n), _ptr(n_dev, torch.int32, "cuda", "n_dev"),
+                                            int(out_dim), int(dim), pg, sg, _stream_handle(stream)))
+        return grad
+
+    # -- rg_layer_norm / rg_layer_norm_grad
+    def layer_norm(self, x, n, dim, gamma, beta, eps, y, mean=None, rstd=None, n_dev=None, stream=None):
+        px, sx = _rows(x, n, dim, None, "cuda", "x")
+        py, sy = _rows(y, n, dim, x.dtype, "cuda", "y")
+        f32 = torch.float32
+        self._check(_lib.rg_layer_norm(self._h, px, _type(x, "x"), sx, int(n), _ptr(n_dev, torch.int32, "cuda", "n_dev"), int(dim),
+                                       _numbers(gamma, dim, f32, "gamma"), _numbers(beta, dim, f32, "beta"), float(eps), py, sy,
+                                       _numbers(mean, n, f32, "mean"), _numbers(rstd, n, f32, "rstd"), _stream_handle(stream)))
+        return y
+
+    def layer_norm_grad(self, dy, x, n, dim, gamma, mean, rstd, dx, dgamma, dbeta, n_dev=None, stream=None):
+        pd, sd = _rows(dy, n, dim, x.dtype, "cuda", "dy")
+        px, sx = _rows(x, n, dim, None, "cuda", "x")
+        pg, sg = _rows(dx, n, dim, x.dtype, "cuda", "dx")
+        f32 = torch.float32
+        self._check(_lib.rg_layer_norm_grad(self._h, pd, sd, px, sx, _type(x, "x"), int(n), _ptr(n_dev, torch.int32, "cuda", "n_dev"), int(dim),
+                                            _numbers(gamma, dim, f32, "gamma"), _numbers(mean, n, f32, "mean"),
+                                            _numbers(rstd, n, f32, "rstd"), pg, sg, _numbers(dgamma, dim, f32, "dgamma"),
+                                            _numbers(dbeta, dim, f32, "dbeta"), _stream_handle(stream)))
+
+    # -- rg_clip_grad_norm
+    def clip_grad_norm(self, tensors, max_norm, norm, stream=None):
+        """tensors: TensorList; norm: float32 cuda tensor [1], written."""
+        self._check(_lib.rg_clip_grad_norm(self._h, tensors.c_array, tensors.count, float(max_norm),
+                                           _numbers(norm, 1, torch.float32, "norm"), _stream_handle(stream)))
+        return norm
+
     # -- rg_profile_*
     def profile_enable(self, on=True):
         self._check(_lib.rg_profile_enable(self._h, 1 if on else 0))
@@ -394,6 +510,36 @@ def blocks_bounds(num_nodes, num_edges, num_seeds, fanouts):
     if st != RG_OK:
         raise RgError(st, "rg_blocks_bounds: invalid argument")
     return list(fub), list(eub)
+
+
+def mx4_row_words(dim):
+    """Words of 32 bits in a packed row of dim numbers: the `dim` that the gather and the cache see."""
+    words = _lib.rg_mx4_row_words(int(dim))
+    if words == 0:
+        raise ValueError(f"mx4_row_words: dim = {dim} not in [1, {RG_MX4_MAX_DIM}]")
+    return words
+
+
+def mx4_rows(n, dim, device, pin_memory=False):
+    """Room for n packed rows of dim numbers, each on 16 bytes (so that the gather moves them 16 at a time)."""
+    return torch.zeros(max(int(n), 1), -(-mx4_row_words(dim) // 4) * 4, dtype=torch.float32, device=device, pin_memory=pin_memory)
+
+
+class TensorList:
+    """rg_tensor[] over contiguous cuda tensors (kept alive by this object); out: as many, or None to work in place."""
+
+    def __init__(self, tensors, out=None):
+        self.tensors = list(tensors)
+        self.out = self.tensors if out is None else list(out)
+        if len(self.out) != len(self.tensors):
+            raise ValueError(f"TensorList: {len(self.tensors)} tensors and {len(self.out)} to write")
+        self.count = len(self.tensors)
+        self.c_array = (rg_tensor * max(self.count, 1))()
+        for c, t, o in zip(self.c_array, self.tensors, self.out):
+            if o.numel() != t.numel():
+                raise ValueError(f"TensorList: {t.numel()} numbers and {o.numel()} to write")
+            c.in_, c.out, c.size = _ptr(t, None, "cuda", "tensors"), _ptr(o, t.dtype, "cuda", "out"), t.numel()
+            c.type = _type(t, "tensors")
 
 
 def version():

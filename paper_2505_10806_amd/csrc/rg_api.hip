@@ -49,6 +49,19 @@ rg_status rg_ensure(rg_ctx* ctx, RgBuf& buf, size_t bytes, bool zero_new) {
     return RG_OK;
 }
 
+rg_status rg_scratch(rg_ctx* ctx, RgBuf& buf, size_t bytes, hipStream_t s, const char* who) {
+    if (bytes <= buf.bytes) return RG_OK;
+    if (rg_capturing(s))
+        return rg_set_error(ctx, RG_ERR_STATE, "%s: %zu bytes of scratch are needed and %zu are there, and the stream records a graph: make "
+                            "a call of this size before the recording", who, bytes, buf.bytes);
+    RgBuf larger;
+    const rg_status st = rg_ensure(ctx, larger, std::max(bytes, buf.bytes + buf.bytes / 2));
+    if (st != RG_OK) return st;
+    if (buf.p) ctx->outgrown.push_back(buf.p);
+    buf = larger;
+    return RG_OK;
+}
+
 rg_status rg_check_device_readable(rg_ctx* ctx, const void* p, const char* what) {
     hipPointerAttribute_t attr;
     const hipError_t e = hipPointerGetAttributes(&attr, p);
@@ -191,7 +204,7 @@ void rg_destroy(rg_ctx* ctx) {
     (void)hipDeviceSynchronize();
     RgBuf* bufs[] = {&ctx->visited, &ctx->marked, &ctx->slice_marks, &ctx->pos, &ctx->chunk_sum, &ctx->row_start, &ctx->row_deg, &ctx->first_key, &ctx->seen, &ctx->sched_pairs, &ctx->sched_late, &ctx->sched_buckets,
                      &ctx->hist_bounds, &ctx->topk_ctl, &ctx->topk_blk, &ctx->topk_caps, &ctx->pf_list, &ctx->pf_ctl, &ctx->plan_cursor, &ctx->claim_bits, &ctx->claim_blk, &ctx->gather_src, &ctx->miss_list,
-                     &ctx->gather_ctl};
+                     &ctx->gather_ctl, &ctx->mx4_parts, &ctx->norm_parts, &ctx->clip_parts};
     for (RgBuf* b : bufs)
         if (b->p) (void)hipFree(b->p);
     for (RgBuf& b : ctx->rank)

@@ -1,0 +1,84 @@
+// Rows of 32- or 16-bit numbers, as the training step's kernels read and write them: numbers are worked on in 32 bits and rounded
+// once, to the nearest (halves to even), where a 16-bit result is stored.
+#pragma once
+
+#include "rg_internal.h"
+
+// Rows start where their stride puts them, so vectors are declared with their elements' alignment only: the device's memory
+// instructions take 16 bytes from any element's address.
+template <typename T, int N> struct RgPack;
+template <int N> struct RgPack<float, N> { typedef float type __attribute__((ext_vector_type(N), aligned(4))); };
+template <int N> struct RgPack<__bf16, N> { typedef __bf16 type __attribute__((ext_vector_type(N), aligned(2))); };
+template <int N> struct RgPack<_Float16, N> { typedef _Float16 type __attribute__((ext_vector_type(N), aligned(2))); };
+typedef uint32_t rg_u32x4 __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t rg_u32x2 __attribute__((ext_vector_type(2), aligned(4)));
+
+// N numbers from p, in 32 bits.
+template <int N, typename T>
+__device__ __forceinline__ void rg_load(const T* p, float (&v)[N]) {
+    if constexpr (sizeof(T) * N <= 16) {
+        const typename RgPack<T, N>::type a = *(const typename RgPack<T, N>::type*)p;
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = (float)a[i];
+    } else {
+        constexpr int H = 16 / sizeof(T);
+#pragma unroll
+        for (int h = 0; h < N / H; ++h) {
+            const typename RgPack<T, H>::type a = ((const typename RgPack<T, H>::type*)p)[h];
+#pragma unroll
+            for (int i = 0; i < H; ++i) v[h * H + i] = (float)a[i];
+        }
+    }
+}
+
+// The same of the first `live` of them (less than N: one by one), the others 0.
+template <int N, typename T>
+__device__ __forceinline__ void rg_load_head(const T* p, int live, float (&v)[N]) {
+    if (live >= N) { rg_load<N>(p, v); return; }
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = i < live ? (float)p[i] : 0.0f;
+}
+
+template <int N, typename T>
+__device__ __forceinline__ void rg_store(T* p, const float (&v)[N]) {
+    constexpr int H = sizeof(T) * N <= 16 ? N : 16 / (int)sizeof(T);
+#pragma unroll
+    for (int h = 0; h < N / H; ++h) {
+        typename RgPack<T, H>::type a;
+#pragma unroll
+        for (int i = 0; i < H; ++i) a[i] = (T)v[h * H + i];
+        ((typename RgPack<T, H>::type*)p)[h] = a;
+    }
+}
+
+template <int N, typename T>
+__device__ __forceinline__ void rg_store_live(T* p, int live, const float (&v)[N]) {
+    if (live >= N) { rg_store<N>(p, v); return; }
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        if (i < live) p[i] = (T)v[i];
+}
+
+__device__ __forceinline__ int64_t rg_least(int64_t a, int64_t b) { return a < b ? a : b; }
+
+// min(n, *n_dev): the rows a batch really has.
+__device__ __forceinline__ int64_t rg_rows(int64_t n, const int32_t* n_dev) {
+    if (!n_dev) return n;
+    const int64_t d = *n_dev;
+    return d < n ? (d < 0 ? 0 : d) : n;
+}
+
+// i / d for i < 2^16 and d < 2^14; m = rg_inverse(d).
+static inline uint32_t rg_inverse(uint32_t d) { return d <= 1 ? 0 : (uint32_t)(((1ull << 32) + d - 1) / d); }
+__device__ __forceinline__ uint32_t rg_divide(uint32_t i, uint32_t m) { return m ? __umulhi(i, m) : i; }
+
+static inline int rg_type_bytes(rg_dtype t) { return t == RG_F32 ? 4 : 2; }
+static inline bool rg_type_known(rg_dtype t) { return t == RG_F32 || t == RG_BF16 || t == RG_F16; }
+
+// Runs `...` with the element type of `t` as T.
+#define RG_FOR_TYPE(t, ...)                                     \
+    do {                                                        \
+        if ((t) == RG_F32) { typedef float T; __VA_ARGS__; }    \
+        else if ((t) == RG_BF16) { typedef __bf16 T; __VA_ARGS__; } \
+        else { typedef _Float16 T; __VA_ARGS__; }               \
+    } while (0)

@@ -94,6 +94,9 @@ struct rg_ctx {
     void* static_scratch = nullptr;   // device address of the library's file-scope gather scratch on ctx->device
     std::vector<hipStream_t> streams;   // streams made by rg_stream_create and not yet destroyed (rg_destroy takes the rest)
 
+    // training-step scratch: sums of parts of the rows, or of the tensors, that a second launch joins
+    RgBuf mx4_parts, norm_parts, clip_parts;
+
     // profiling
     bool profiling = false;
     uint32_t prof_mask = 0xFFFFFFFFu;  // bit k: launches of kernel id k are bracketed while profiling is on
@@ -105,6 +108,9 @@ struct rg_ctx {
 
 rg_status rg_set_error(rg_ctx* ctx, rg_status code, const char* fmt, ...);
 rg_status rg_ensure(rg_ctx* ctx, RgBuf& buf, size_t bytes, bool zero_new = false);
+// At least `bytes` of scratch.  Work under way and graphs keep the allocations they were given (rg_destroy frees them); while s records
+// a graph nothing can be allocated (RG_ERR_STATE: the same call made once before the recording leaves scratch enough).
+rg_status rg_scratch(rg_ctx* ctx, RgBuf& buf, size_t bytes, hipStream_t s, const char* who);
 // RG_OK if kernels on the ctx's device may dereference p (device, managed or pinned/registered host memory).
 rg_status rg_check_device_readable(rg_ctx* ctx, const void* p, const char* what);
 // True while s records a graph: nothing may be allocated then.  (The NULL stream cannot; the question costs 0.3 us.)

@@ -1,0 +1,436 @@
+// Layer norm of rows and its backward pass.
+#include "rg_elements.h"
+
+namespace {
+
+// A row lies in the registers of L = 2^log2L lanes: lane l holds chunks l, l + L, ... (NC of them) of V numbers, 16 bytes each.
+template <typename T> struct Chunk { static constexpr int V = 16 / (int)sizeof(T); };
+// Numbers of each of its rows that a lane holds at most: rows of up to 64 times as many stay in registers, longer ones are read again.
+constexpr int kHeld = 32, kHeldGrad = 16;
+
+__device__ __forceinline__ float group_sum(float x, int log2L) {
+    for (int off = 1 << log2L >> 1; off > 0; off >>= 1) x += __shfl_xor(x, off, RG_WAVE);
+    return x;
+}
+
+// Sum over a workgroup of NW wavefronts; smem holds NW floats.  Contains barriers.
+template <int NW>
+__device__ __forceinline__ float block_sum(float x, float* smem) {
+    x = group_sum(x, 6);
+    __syncthreads();
+    if (rg_lane() == 0) smem[threadIdx.x >> 6] = x;
+    __syncthreads();
+    float sum = 0.0f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) sum += smem[w];
+    return sum;
+}
+
+template <int V>
+__device__ __forceinline__ void load_params(const float* p, int live, float absent, float (&v)[V]) {
+    if (p) rg_load_head<V>(p, live, v);
+    else {
+#pragma unroll
+        for (int j = 0; j < V; ++j) v[j] = absent;
+    }
+}
+
+template <typename T, int NC>
+__global__ void __launch_bounds__(256) k_layer_norm(const T* x, int64_t x_stride, int64_t n, const int32_t* __restrict__ n_dev, int dim,
+                                                    const float* __restrict__ gamma, const float* __restrict__ beta, float eps, T* y,
+                                                    int64_t y_stride, float* __restrict__ mean, float* __restrict__ rstd, int log2L) {
+    constexpr int V = Chunk<T>::V;
+    const int64_t n_act = rg_rows(n, n_dev);
+    const int lane = rg_lane(), L = 1 << log2L, R = RG_WAVE >> log2L, l = lane & (L - 1);
+    const int64_t wave = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) >> 6, waves = ((int64_t)gridDim.x * blockDim.x) >> 6;
+    for (int64_t row0 = wave * R; row0 < n_act; row0 += waves * R) {
+        const int64_t row = row0 + (lane >> log2L);
+        const bool live_row = row < n_act;
+        const T* src = x + (live_row ? row : n_act - 1) * x_stride;
+        float v[NC][V];
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < NC; ++i) {
+            const int col = (l + i * L) * V;
+            rg_load_head<V>(src + col, dim - col, v[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < NC; ++i)
+#pragma unroll
+            for (int j = 0; j < V; ++j) sum += v[i][j];
+        const float m = group_sum(sum, log2L) / (float)dim;
+        float square = 0.0f;
+#pragma unroll
+        for (int i = 0; i < NC; ++i) {
+            const int col = (l + i * L) * V;
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                v[i][j] -= m;
+                if (col + j < dim) square += v[i][j] * v[i][j];
+            }
+        }
+        const float s = 1.0f / sqrtf(group_sum(square, log2L) / (float)dim + eps);
+        if (!live_row) continue;
+        T* dst = y + row * y_stride;
+#pragma unroll
+        for (int i = 0; i < NC; ++i) {
+            const int col = (l + i * L) * V;
+            if (col >= dim) continue;
+            float g[V], b[V];
+            load_params<V>(gamma ? gamma + col : nullptr, dim - col, 1.0f, g);
+            load_params<V>(beta ? beta + col : nullptr, dim - col, 0.0f, b);
+#pragma unroll
+            for (int j = 0; j < V; ++j) v[i][j] = v[i][j] * s * g[j] + b[j];
+            rg_store_live<V>(dst + col, dim - col, v[i]);
+        }
+        if (l == 0) {
+            if (mean) mean[row] = m;
+            if (rstd) rstd[row] = s;
+        }
+    }
+}
+
+// Rows too long for a wavefront's registers: a workgroup each, read three times.
+template <typename T>
+__global__ void __launch_bounds__(256) k_layer_norm_long(const T* x, int64_t x_stride, int64_t n, const int32_t* __restrict__ n_dev, int dim,
+                                                         const float* __restrict__ gamma, const float* __restrict__ beta, float eps, T* y,
+                                                         int64_t y_stride, float* __restrict__ mean, float* __restrict__ rstd) {
+    constexpr int V = Chunk<T>::V;
+    __shared__ float smem[4];
+    const int64_t n_act = rg_rows(n, n_dev);
+    for (int64_t row = blockIdx.x; row < n_act; row += gridDim.x) {
+        const T* src = x + row * x_stride;
+        float sum = 0.0f, square = 0.0f, v[V];
+        for (int col = threadIdx.x * V; col < dim; col += 256 * V) {
+            rg_load_head<V>(src + col, dim - col, v);
+#pragma unroll
+            for (int j = 0; j < V; ++j) sum += v[j];
+        }
+        const float m = block_sum<4>(sum, smem) / (float)dim;
+        for (int col = threadIdx.x * V; col < dim; col += 256 * V) {
+            rg_load_head<V>(src + col, dim - col, v);
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                if (col + j < dim) square += (v[j] - m) * (v[j] - m);
+        }
+        const float s = 1.0f / sqrtf(block_sum<4>(square, smem) / (float)dim + eps);
+        for (int col = threadIdx.x * V; col < dim; col += 256 * V) {
+            float g[V], b[V];
+            rg_load_head<V>(src + col, dim - col, v);
+            load_params<V>(gamma ? gamma + col : nullptr, dim - col, 1.0f, g);
+            load_params<V>(beta ? beta + col : nullptr, dim - col, 0.0f, b);
+#pragma unroll
+            for (int j = 0; j < V; ++j) v[j] = (v[j] - m) * s * g[j] + b[j];
+            rg_store_live<V>(y + row * y_stride + col, dim - col, v);
+        }
+        if (threadIdx.x == 0) {
+            if (mean) mean[row] = m;
+            if (rstd) rstd[row] = s;
+        }
+    }
+}
+
+// ---------------------------------------------------------------- backward
+// Every lane adds up dy h and dy of its columns over the rows it meets; a workgroup's sums go to its own part, which a second launch
+// joins in the order of the workgroups.
+constexpr int kGradThreads = 512, kGradWaves = kGradThreads / RG_WAVE;
+
+template <typename T, int NC, bool SUMS>
+__global__ void __launch_bounds__(kGradThreads) k_layer_norm_grad(const T* dy, int64_t dy_stride, const T* x, int64_t x_stride, int64_t n,
+                                                                  const int32_t* __restrict__ n_dev, int dim, const float* __restrict__ gamma,
+                                                                  const float* __restrict__ mean, const float* __restrict__ rstd, T* dx,
+                                                                  int64_t dx_stride, float* __restrict__ parts, int log2L) {
+    constexpr int V = Chunk<T>::V;
+    extern __shared__ float wave_sums[];                   // [kGradWaves][dim]
+    const int64_t n_act = rg_rows(n, n_dev);
+    const int lane = rg_lane(), L = 1 << log2L, R = RG_WAVE >> log2L, l = lane & (L - 1);
+    const int64_t wave = (int64_t)blockIdx.x * kGradWaves + (threadIdx.x >> 6), waves = (int64_t)gridDim.x * kGradWaves;
+    float g[NC][V], by_gamma[NC][V], by_beta[NC][V];
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+        const int col = (l + i * L) * V;
+        load_params<V>(gamma ? gamma + col : nullptr, dim - col, 1.0f, g[i]);
+#pragma unroll
+        for (int j = 0; j < V; ++j) by_gamma[i][j] = by_beta[i][j] = 0.0f;
+    }
+    for (int64_t row0 = wave * R; row0 < n_act; row0 += waves * R) {
+        const int64_t row = row0 + (lane >> log2L);
+        const bool live_row = row < n_act;
+        const int64_t at = live_row ? row : n_act - 1;
+        float h[NC][V], d[NC][V];
+#pragma unroll
+        for (int i = 0; i < NC; ++i) {
+            const int col = (l + i * L) * V;
+            rg_load_head<V>(x + at * x_stride + col, dim - col, h[i]);
+            rg_load_head<V>(dy + at * dy_stride + col, live_row ? dim - col : 0, d[i]);
+        }
+        const float m = mean[at], s = rstd[at];
+        float along = 0.0f, all = 0.0f;
+#pragma unroll
+        for (int i = 0; i < NC; ++i) {
+            const int col = (l + i * L) * V;
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const bool in = live_row && col + j < dim;
+                h[i][j] = in ? (h[i][j] - m) * s : 0.0f;
+                if (SUMS) {
+                    by_gamma[i][j] += d[i][j] * h[i][j];
+                    by_beta[i][j] += d[i][j];
+                }
+                d[i][j] *= g[i][j];
+                along += d[i][j] * h[i][j];
+                all += d[i][j];
+            }
+        }
+        if (!dx) continue;
+        along = group_sum(along, log2L) / (float)dim;
+        all = group_sum(all, log2L) / (float)dim;
+        if (!live_row) continue;
+#pragma unroll
+        for (int i = 0; i < NC; ++i) {
+            const int col = (l + i * L) * V;
+            if (col >= dim) continue;
+#pragma unroll
+            for (int j = 0; j < V; ++j) d[i][j] = s * (d[i][j] - all - h[i][j] * along);
+            rg_store_live<V>(dx + row * dx_stride + col, dim - col, d[i]);
+        }
+    }
+    if (!SUMS) return;
+#pragma unroll 1
+    for (int which = 0; which < 2; ++which) {
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < NC; ++i)
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const int col = (l + i * L) * V + j;
+                float sum = which ? by_beta[i][j] : by_gamma[i][j];
+                for (int off = L; off < RG_WAVE; off <<= 1) sum += __shfl_xor(sum, off, RG_WAVE);
+                if (lane < L && col < dim) wave_sums[(threadIdx.x >> 6) * dim + col] = sum;
+            }
+        __syncthreads();
+        for (int col = threadIdx.x; col < dim; col += kGradThreads) {
+            float sum = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kGradWaves; ++w) sum += wave_sums[w * dim + col];
+            parts[((int64_t)blockIdx.x * 2 + which) * dim + col] = sum;
+        }
+    }
+}
+
+// Column sums of `count` parts: 64 columns to a workgroup, 16 runs of parts side by side.
+__global__ void __launch_bounds__(1024) k_norm_join(const float* __restrict__ parts, int count, int dim, float* __restrict__ dgamma,
+                                                    float* __restrict__ dbeta) {
+    __shared__ float runs[16][64];
+    const int lane = threadIdx.x & 63, run = threadIdx.x >> 6;
+    const int col = blockIdx.x * 64 + lane;                // of both rows of a part, one behind the other
+    const int per_run = (count + 15) / 16, first = run * per_run, last = min(first + per_run, count);
+    float sum = 0.0f;
+    if (col < 2 * dim) {
+#pragma unroll 8
+        for (int b = first; b < last; ++b) sum += parts[(int64_t)b * 2 * dim + col];
+    }
+    runs[run][lane] = sum;
+    __syncthreads();
+    if (run != 0 || col >= 2 * dim) return;
+    sum = 0.0f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) sum += runs[r][lane];
+    if (col < dim) {
+        if (dgamma) dgamma[col] = sum;
+    } else if (dbeta) dbeta[col - dim] = sum;
+}
+
+// Longer rows: a workgroup to a row for dx ...
+template <typename T>
+__global__ void __launch_bounds__(256) k_layer_norm_grad_long(const T* dy, int64_t dy_stride, const T* x, int64_t x_stride, int64_t n,
+                                                              const int32_t* __restrict__ n_dev, int dim, const float* __restrict__ gamma,
+                                                              const float* __restrict__ mean, const float* __restrict__ rstd, T* dx,
+                                                              int64_t dx_stride) {
+    constexpr int V = Chunk<T>::V;
+    __shared__ float smem[4];
+    const int64_t n_act = rg_rows(n, n_dev);
+    for (int64_t row = blockIdx.x; row < n_act; row += gridDim.x) {
+        const float m = mean[row], s = rstd[row];
+        float along = 0.0f, all = 0.0f, h[V], d[V], g[V];
+        for (int col = threadIdx.x * V; col < dim; col += 256 * V) {
+            rg_load_head<V>(x + row * x_stride + col, dim - col, h);
+            rg_load_head<V>(dy + row * dy_stride + col, dim - col, d);
+            load_params<V>(gamma ? gamma + col : nullptr, dim - col, 1.0f, g);
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                along += col + j < dim ? d[j] * g[j] * ((h[j] - m) * s) : 0.0f;
+                all += d[j] * g[j];
+            }
+        }
+        along = block_sum<4>(along, smem) / (float)dim;
+        all = block_sum<4>(all, smem) / (float)dim;
+        for (int col = threadIdx.x * V; col < dim; col += 256 * V) {
+            rg_load_head<V>(x + row * x_stride + col, dim - col, h);
+            rg_load_head<V>(dy + row * dy_stride + col, dim - col, d);
+            load_params<V>(gamma ? gamma + col : nullptr, dim - col, 1.0f, g);
+#pragma unroll
+            for (int j = 0; j < V; ++j) d[j] = s * (d[j] * g[j] - all - (h[j] - m) * s * along);
+            rg_store_live<V>(dx + row * dx_stride + col, dim - col, d);
+        }
+    }
+}
+
+// ... and, before dx takes their place, a workgroup to 64 chunks of columns and a range of the rows for the sums.
+template <typename T>
+__global__ void __launch_bounds__(256) k_layer_norm_sums_long(const T* __restrict__ dy, int64_t dy_stride, const T* __restrict__ x, int64_t x_stride,
+                                                              int64_t n, const int32_t* __restrict__ n_dev, int dim, const float* __restrict__ mean,
+                                                              const float* __restrict__ rstd, float* __restrict__ parts) {
+    constexpr int V = Chunk<T>::V;
+    __shared__ float runs[2][4][64 * V];
+    const int64_t n_act = rg_rows(n, n_dev);
+    const int lane = rg_lane(), wave = threadIdx.x >> 6;
+    const int col = (blockIdx.x * 64 + lane) * V;
+    float by_gamma[V], by_beta[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) by_gamma[j] = by_beta[j] = 0.0f;
+    for (int64_t row = blockIdx.y * 4 + wave; row < n_act; row += gridDim.y * 4) {
+        float h[V], d[V];
+        rg_load_head<V>(x + row * x_stride + col, dim - col, h);
+        rg_load_head<V>(dy + row * dy_stride + col, dim - col, d);
+        const float m = mean[row], s = rstd[row];
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            by_gamma[j] += d[j] * ((h[j] - m) * s);
+            by_beta[j] += d[j];
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        runs[0][wave][lane * V + j] = by_gamma[j];
+        runs[1][wave][lane * V + j] = by_beta[j];
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < 64 * V; i += 256) {
+        const int at = blockIdx.x * 64 * V + i;
+        if (at >= dim) continue;
+#pragma unroll
+        for (int which = 0; which < 2; ++which)
+            parts[((int64_t)blockIdx.y * 2 + which) * dim + at] =
+                (runs[which][0][i] + runs[which][1][i]) + (runs[which][2][i] + runs[which][3][i]);
+    }
+}
+
+// Lanes to a row and chunks to a lane: the smallest number of lane slots that holds the row's chunks.
+struct Shape {
+    int log2L, chunks;         // chunks = 0: too long to be held
+};
+
+Shape row_shape(int dim, int V, int held) {
+    const int total = (int)rg_div_up(dim, V);
+    Shape best = {6, 0};
+    int slots = 1 << 30;
+    for (int log2L = 6; log2L >= 0; --log2L) {
+        int per = (int)rg_div_up(total, 1 << log2L);
+        if (per > 4) per = per <= held / V ? held / V : 0;          // 1, 2, 3, 4 or as many as are held
+        if (per == 0 || per * V > held) continue;
+        if (per << log2L < slots) { slots = per << log2L; best = {log2L, per}; }
+    }
+    return best;
+}
+
+#define RG_FOR_CHUNKS(shape, most, ...)                                            \
+    do {                                                                        \
+        if ((shape).chunks == 1) { constexpr int NC = 1; __VA_ARGS__; }         \
+        else if ((shape).chunks == 2) { constexpr int NC = 2; __VA_ARGS__; }    \
+        else if ((shape).chunks == 3) { constexpr int NC = (most) < 3 ? (most) : 3; __VA_ARGS__; }    \
+        else if ((shape).chunks == 4) { constexpr int NC = (most) < 4 ? (most) : 4; __VA_ARGS__; }    \
+        else { constexpr int NC = (most); __VA_ARGS__; }                        \
+    } while (0)
+
+bool aligned(const void* p, int bytes) { return (uintptr_t)p % (uintptr_t)bytes == 0; }
+
+}  // namespace
+
+extern "C" {
+
+rg_status rg_layer_norm(rg_ctx* ctx, const void* x, rg_dtype type, int64_t x_stride, int64_t n, const int32_t* n_dev, int32_t dim,
+                        const float* gamma, const float* beta, float eps, void* y, int64_t y_stride, float* mean, float* rstd, void* stream) {
+    if (!ctx) return RG_ERR_INVALID_ARG;
+    RG_REQUIRE(ctx, n >= 0 && n <= (1ll << 31) - 1, "rg_layer_norm: n = %lld out of range", (long long)n);
+    RG_REQUIRE(ctx, dim >= 1 && dim <= RG_NORM_MAX_DIM, "rg_layer_norm: dim = %d not in [1,%d]", dim, RG_NORM_MAX_DIM);
+    RG_REQUIRE(ctx, rg_type_known(type), "rg_layer_norm: unknown type %d", (int)type);
+    RG_REQUIRE(ctx, x_stride >= dim && y_stride >= dim, "rg_layer_norm: bad stride");
+    RG_REQUIRE(ctx, eps >= 0.0f, "rg_layer_norm: eps is negative or not a number");
+    if (n == 0) return RG_OK;
+    RG_REQUIRE(ctx, x && y, "rg_layer_norm: null pointer");
+    RG_REQUIRE(ctx, x != y || x_stride == y_stride, "rg_layer_norm: y is x with another stride");
+    RG_REQUIRE(ctx, aligned(x, rg_type_bytes(type)) && aligned(y, rg_type_bytes(type)) && aligned(gamma, 4) && aligned(beta, 4) &&
+               aligned(mean, 4) && aligned(rstd, 4), "rg_layer_norm: pointer not aligned to its numbers");
+    RG_HIP(ctx, hipSetDevice(ctx->device));
+    hipStream_t s = (hipStream_t)stream;
+    RG_FOR_TYPE(type, {
+        const Shape shape = row_shape(dim, Chunk<T>::V, kHeld);
+        if (shape.chunks == 0) {
+            k_layer_norm_long<T><<<(unsigned)rg_min64(n, (int64_t)ctx->num_cus * 32), 256, 0, s>>>((const T*)x, x_stride, n, n_dev, dim, gamma,
+                                                                                                  beta, eps, (T*)y, y_stride, mean, rstd);
+        } else {
+            const unsigned grid = (unsigned)rg_min64(rg_div_up(n, 4 * (RG_WAVE >> shape.log2L)), (int64_t)ctx->num_cus * 64);
+            RG_FOR_CHUNKS(shape, kHeld / Chunk<T>::V, k_layer_norm<T, NC><<<grid, 256, 0, s>>>((const T*)x, x_stride, n, n_dev, dim, gamma, beta, eps, (T*)y,
+                                                                                      y_stride, mean, rstd, shape.log2L));
+        }
+    });
+    RG_LAUNCH_CHECK(ctx, "k_layer_norm");
+    return RG_OK;
+}
+
+rg_status rg_layer_norm_grad(rg_ctx* ctx, const void* dy, int64_t dy_stride, const void* x, int64_t x_stride, rg_dtype type, int64_t n,
+                             const int32_t* n_dev, int32_t dim, const float* gamma, const float* mean, const float* rstd, void* dx,
+                             int64_t dx_stride, float* dgamma, float* dbeta, void* stream) {
+    if (!ctx) return RG_ERR_INVALID_ARG;
+    RG_REQUIRE(ctx, n >= 0 && n <= (1ll << 31) - 1, "rg_layer_norm_grad: n = %lld out of range", (long long)n);
+    RG_REQUIRE(ctx, dim >= 1 && dim <= RG_NORM_MAX_DIM, "rg_layer_norm_grad: dim = %d not in [1,%d]", dim, RG_NORM_MAX_DIM);
+    RG_REQUIRE(ctx, rg_type_known(type), "rg_layer_norm_grad: unknown type %d", (int)type);
+    RG_REQUIRE(ctx, dy_stride >= dim && x_stride >= dim && (!dx || dx_stride >= dim), "rg_layer_norm_grad: bad stride");
+    RG_REQUIRE(ctx, n == 0 || (dy && x && mean && rstd), "rg_layer_norm_grad: null pointer");
+    RG_REQUIRE(ctx, !dx || ((dx != x || dx_stride == x_stride) && (dx != dy || dx_stride == dy_stride)),
+               "rg_layer_norm_grad: dx is an input with another stride");
+    const int b = rg_type_bytes(type);
+    RG_REQUIRE(ctx, aligned(dy, b) && aligned(x, b) && aligned(dx, b) && aligned(gamma, 4) && aligned(mean, 4) && aligned(rstd, 4) &&
+               aligned(dgamma, 4) && aligned(dbeta, 4), "rg_layer_norm_grad: pointer not aligned to its numbers");
+    const bool sums = dgamma || dbeta;
+    if (!sums && (!dx || n == 0)) return RG_OK;
+    RG_HIP(ctx, hipSetDevice(ctx->device));
+    hipStream_t s = (hipStream_t)stream;
+    int64_t blocks = 0;
+    RG_FOR_TYPE(type, {
+        constexpr int V = Chunk<T>::V;
+        const Shape shape = row_shape(dim, V, kHeldGrad);
+        const int64_t stripes = rg_div_up(dim, 64 * V);
+        if (shape.chunks == 0) blocks = rg_max64(1, rg_min64(rg_div_up(n, 16), rg_div_up((int64_t)ctx->num_cus * 8, stripes)));
+        else blocks = rg_max64(1, rg_min64(rg_div_up(n, kGradWaves * (RG_WAVE >> shape.log2L)), (int64_t)ctx->num_cus * 2));
+        if (sums) {
+            const rg_status st = rg_scratch(ctx, ctx->norm_parts, (size_t)blocks * 2 * dim * 4, s, "rg_layer_norm_grad");
+            if (st != RG_OK) return st;
+        }
+        float* parts = (float*)ctx->norm_parts.p;
+        if (shape.chunks == 0) {
+            if (sums)
+                k_layer_norm_sums_long<T><<<dim3((unsigned)stripes, (unsigned)blocks), 256, 0, s>>>((const T*)dy, dy_stride, (const T*)x, x_stride, n,
+                                                                                               n_dev, dim, mean, rstd, parts);
+            if (dx && n > 0)
+                k_layer_norm_grad_long<T><<<(unsigned)rg_min64(n, (int64_t)ctx->num_cus * 32), 256, 0, s>>>(
+                    (const T*)dy, dy_stride, (const T*)x, x_stride, n, n_dev, dim, gamma, mean, rstd, (T*)dx, dx_stride);
+        } else if (sums) {
+            const size_t lds = (size_t)kGradWaves * dim * 4;
+            RG_FOR_CHUNKS(shape, kHeldGrad / V, k_layer_norm_grad<T, NC, true><<<(unsigned)blocks, kGradThreads, lds, s>>>(
+                (const T*)dy, dy_stride, (const T*)x, x_stride, n, n_dev, dim, gamma, mean, rstd, (T*)dx, dx_stride, parts, shape.log2L));
+        } else {
+            RG_FOR_CHUNKS(shape, kHeldGrad / V, k_layer_norm_grad<T, NC, false><<<(unsigned)blocks, kGradThreads, 0, s>>>(
+                (const T*)dy, dy_stride, (const T*)x, x_stride, n, n_dev, dim, gamma, mean, rstd, (T*)dx, dx_stride, nullptr, shape.log2L));
+        }
+        RG_LAUNCH_CHECK(ctx, "k_layer_norm_grad");
+    });
+    if (sums) {
+        k_norm_join<<<(unsigned)rg_div_up(2ll * dim, 64), 1024, 0, s>>>((const float*)ctx->norm_parts.p, (int)blocks, dim, dgamma, dbeta);
+        RG_LAUNCH_CHECK(ctx, "k_norm_join");
+    }
+    return RG_OK;
+}
+
+}  // extern "C"

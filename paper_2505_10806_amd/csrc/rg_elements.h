@@ -68,6 +68,13 @@ __device__ __forceinline__ int64_t rg_rows(int64_t n, const int32_t* n_dev) {
     return d < n ? (d < 0 ? 0 : d) : n;
 }
 
+// Workgroups are dealt to the 8 XCDs in turn: the place of workgroup `block` of `grid` in an order in which neighbours share an XCD
+// (and its L2).
+__device__ __forceinline__ int rg_xcd_block(int block, int grid) {
+    const int xcd = block & 7, per = grid >> 3, more = grid & 7;
+    return xcd * per + min(xcd, more) + (block >> 3);
+}
+
 // i / d for i < 2^16 and d < 2^14; m = rg_inverse(d).
 static inline uint32_t rg_inverse(uint32_t d) { return d <= 1 ? 0 : (uint32_t)(((1ull << 32) + d - 1) / d); }
 __device__ __forceinline__ uint32_t rg_divide(uint32_t i, uint32_t m) { return m ? __umulhi(i, m) : i; }

@@ -204,22 +204,44 @@ __device__ __forceinline__ float bf16_rest(float x) {
 template <typename T> struct Parts { static constexpr int count = sizeof(T) == 4 ? 3 : 2; };
 template <> struct Parts<__bf16> { static constexpr int count = 1; };
 
-// Four neighbouring numbers of dy (fewer at the row's end: zeros).
-template <typename T> struct Dy4 { T v[4]; };
-template <typename T>
-__device__ __forceinline__ void load_dy(const T* p, int live, Dy4<T>& d) {
-    if (live >= 4) {
-        const typename RgPack<T, 4>::type a = *(const typename RgPack<T, 4>::type*)p;
+// What a lane holds of 32 rows: COLS neighbouring numbers of dy, the word of codes and the word of scales of its 8 rows.
+template <typename T, int COLS> struct GradStep {
+    typedef T Vec __attribute__((ext_vector_type(COLS)));
+    Vec d[8];
+    uint32_t code[8], scale[8];
+};
+
+template <typename T, int COLS>
+__device__ __forceinline__ typename GradStep<T, COLS>::Vec load_columns(const T* p) {
+    typename GradStep<T, COLS>::Vec v;
+    if constexpr (COLS == 1) v[0] = *p;
+    else {
+        const typename RgPack<T, COLS>::type a = *(const typename RgPack<T, COLS>::type*)p;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) d.v[i] = a[i];
+        for (int i = 0; i < COLS; ++i) v[i] = a[i];
+    }
+    return v;
+}
+
+// The columns of a lane that reaches over the end of a row, which were loaded `over` columns further left (0: as they are; what
+// comes in from the right is not used).
+template <typename T, int COLS>
+__device__ __forceinline__ typename GradStep<T, COLS>::Vec move_columns(typename GradStep<T, COLS>::Vec v, int over) {
+    if constexpr (COLS == 1) return v;
+    else if constexpr (COLS * sizeof(T) == 8 && COLS == 4) {
+        uint64_t w;
+        __builtin_memcpy(&w, &v, 8);
+        w >>= (16 * over) & 63;
+        __builtin_memcpy(&v, &w, 8);
+        return v;
     } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) d.v[i] = i < live ? p[i] : (T)0.0f;
+        static_assert(COLS == 2, "two columns, or four of 16 bits");
+        v[0] = over ? v[1] : v[0];
+        return v;
     }
 }
 
-// Part p of column t of eight rows' numbers, as a fragment; f32 and f16 numbers lose that part.
-template <typename T>
+// Part p of one column of eight rows' numbers, as a fragment; the numbers lose that part.
 __device__ __forceinline__ void turn_column(float (&x)[8], Frag& f, bool last) {
 #pragma unroll
     for (int j = 0; j < 8; j += 2) f.w[j / 2] = __builtin_amdgcn_perm(__float_as_uint(x[j + 1]), __float_as_uint(x[j]), kHighHalves);
@@ -229,69 +251,140 @@ __device__ __forceinline__ void turn_column(float (&x)[8], Frag& f, bool last) {
     }
 }
 
-// Workgroup (tile of 64 WH outputs x 128 WF columns, split of the rows); its wavefronts are WH x WF, each 64 outputs x 128 columns.
-template <typename T, int WH, int WF>
-__global__ void __launch_bounds__(64 * WH * WF, 1) k_mx4_grad(const T* __restrict__ dy, int64_t dy_stride, const uint32_t* __restrict__ rows,
-                                                           int64_t rows_stride, int64_t n, const int32_t* __restrict__ n_dev, int out_dim,
-                                                           int dim, int64_t rows_per_split, float* __restrict__ grad, int64_t grad_stride,
-                                                           int64_t split_stride, int tiles_h, int tiles_f) {
+// A wavefront makes a tile of 16 COLS outputs x 128 columns from rows of its own, WAVES of them (a workgroup) the same tile from
+// neighbouring rows, and adds theirs up in LDS; so the parts that a second launch joins are few.  The next 32 rows are on their
+// way while the matrix unit works on these.  out_dim >= COLS.  Workgroups of one range of rows follow each other on one XCD: they read the same rows.
+constexpr int kGradWaves = 8;
+
+template <typename T, int COLS>
+__global__ void __launch_bounds__(64 * kGradWaves, 2) k_mx4_grad(const T* __restrict__ dy, int64_t dy_stride, const uint32_t* __restrict__ rows,
+                                                              int64_t rows_stride, int64_t n, const int32_t* __restrict__ n_dev, int out_dim,
+                                                              int dim, int64_t rows_per_wave, float* __restrict__ grad, int64_t grad_stride,
+                                                              int64_t split_stride, int tiles_h, int tiles) {
+    __shared__ v4f sums[kGradWaves / 2][COLS * 8][64];
     const int64_t n_act = rg_rows(n, n_dev);
     const int lane = rg_lane(), c = lane & 15, q = lane >> 4;
     const int wave = threadIdx.x >> 6;
-    const int tile = blockIdx.x % (tiles_h * tiles_f);
-    const int64_t split = blockIdx.x / (tiles_h * tiles_f);
-    const int h0 = (tile % tiles_h) * (64 * WH) + (wave % WH) * 64;
-    const int f0 = (tile / tiles_h) * (128 * WF) + (wave / WH) * 128;
-    if (h0 >= out_dim || f0 >= dim) return;
+    const int block = rg_xcd_block(blockIdx.x, gridDim.x);
+    const int tile = block % tiles;
+    const int64_t split = block / tiles;
+    const int h0 = (tile % tiles_h) * (16 * COLS), f0 = (tile / tiles_h) * 128;
     const int groups = (dim + kGroup - 1) / kGroup;
-    const int h = h0 + 4 * c, col = f0 + 8 * c;
-    const bool wide = col < dim;                           // this lane's word of codes is there
-    const int word = wide ? col >> 3 : 0, group = wide ? col >> 5 : 0;
-    v4f acc[4][8];
+    const int h = h0 + COLS * c, col = f0 + 8 * c;
+    const int h_at = min(h, out_dim - COLS), over = h - h_at;
+    const int shift = 8 * (c >> 2);
+    v4f acc[COLS][8];
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
+    for (int t = 0; t < COLS; ++t)
 #pragma unroll
         for (int u = 0; u < 8; ++u) acc[t][u] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-    const int64_t first = split * rows_per_split, last = rg_least(first + rows_per_split, n_act);
-    for (int64_t i0 = first; i0 < last; i0 += 32) {
-        Dy4<T> d[8];
-        uint32_t code[8], scale[8];
+
+    const int64_t first = (split * kGradWaves + wave) * rows_per_wave, last = rg_least(first + rows_per_wave, n_act);
+    const T* pd = dy + (first + 8 * q) * dy_stride + h_at;
+    const uint32_t* px = rows + (first + 8 * q) * rows_stride + min(col >> 3, 4 * groups - 1);
+    const uint32_t* ps = rows + (first + 8 * q) * rows_stride + 4 * groups + (f0 >> 7);
+
+    const auto load = [&](GradStep<T, COLS>& s) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const int64_t i = i0 + 8 * q + j;
-            const bool live = i < last;
-            const int64_t at = live ? i : last - 1;
-            load_dy<T>(dy + at * dy_stride + h, live ? out_dim - h : 0, d[j]);
-            const uint32_t* row = rows + at * rows_stride;
-            code[j] = live ? row[word] : 0u;
-            scale[j] = live ? ((const uint8_t*)(row + 4 * groups))[group] : 0u;
+            s.d[j] = load_columns<T, COLS>(pd + j * dy_stride);
+            s.code[j] = px[j * rows_stride];
+            s.scale[j] = ps[j * rows_stride];
         }
-        Frag b[8];
-        turn_codes(code, scale, b);
+        pd += 32 * dy_stride;
+        px += 32 * rows_stride;
+        ps += 32 * rows_stride;
+    };
+    const auto multiply = [&](const GradStep<T, COLS>& s) {
+        uint32_t scale[8];
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
+        for (int j = 0; j < 8; ++j) scale[j] = (s.scale[j] >> shift) & 255u;
+        Frag b[8];
+        turn_codes(s.code, scale, b);
+        typename GradStep<T, COLS>::Vec d[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) d[j] = move_columns<T, COLS>(s.d[j], over);
+#pragma unroll
+        for (int t = 0; t < COLS; ++t) {
             float x[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = (float)d[j].v[t];
+            for (int j = 0; j < 8; ++j) x[j] = (float)d[j][t];
 #pragma unroll
             for (int p = 0; p < Parts<T>::count; ++p) {
                 Frag a;
-                turn_column<T>(x, a, p + 1 == Parts<T>::count);
+                turn_column(x, a, p + 1 == Parts<T>::count);
 #pragma unroll
                 for (int u = 0; u < 8; ++u) acc[t][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, b[u].v, acc[t][u], 0, 0, 0);
             }
         }
+    };
+
+    const int steps = last > first ? (int)((last - first) >> 5) : 0;
+    if (steps > 0) {
+        GradStep<T, COLS> even, odd;
+        load(even);
+        for (int k = 0; k + 2 <= steps; k += 2) {
+            load(odd);
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(even);
+            // (behind the last whole step the same rows once more, which nothing uses)
+            const int64_t back = k + 2 < steps ? 0 : 32;
+            pd -= back * dy_stride;
+            px -= back * rows_stride;
+            ps -= back * rows_stride;
+            load(even);
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(odd);
+        }
+        if (steps & 1) multiply(even);
     }
+    const int64_t i = first + 32ll * steps;
+    if (i < last) {                                        // fewer than 32 rows: the others are zeros
+        GradStep<T, COLS> s;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const bool live = i + 8 * q + j < last;
+            typename GradStep<T, COLS>::Vec none = (typename GradStep<T, COLS>::Vec)(T)0.0f;
+            s.d[j] = none;
+            s.code[j] = s.scale[j] = 0u;
+            if (live) {
+                s.d[j] = load_columns<T, COLS>(pd + j * dy_stride);
+                s.code[j] = px[j * rows_stride];
+                s.scale[j] = ps[j * rows_stride];
+            }
+        }
+        multiply(s);
+    }
+
+    // half of the wavefronts hand their sums to the other half, until one is left
+#pragma unroll
+    for (int half = kGradWaves / 2; half > 0; half >>= 1) {
+        __syncthreads();
+        if (wave >= half && wave < 2 * half) {
+#pragma unroll
+            for (int t = 0; t < COLS; ++t)
+#pragma unroll
+                for (int u = 0; u < 8; ++u) sums[wave - half][t * 8 + u][lane] = acc[t][u];
+        }
+        __syncthreads();
+        if (wave < half) {
+#pragma unroll
+            for (int t = 0; t < COLS; ++t)
+#pragma unroll
+                for (int u = 0; u < 8; ++u) acc[t][u] += sums[wave][t * 8 + u][lane];
+        }
+    }
+    if (wave != 0 || col >= dim) return;
     float* out = grad + split * split_stride;
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
+    for (int t = 0; t < COLS; ++t)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int row = h0 + 4 * (4 * q + i) + t;
-            if (row >= out_dim || !wide) continue;
+        for (int r = 0; r < 4; ++r) {
+            const int row = h0 + COLS * (4 * q + r) + t;
+            if (row >= out_dim) continue;
             float v[8];
 #pragma unroll
-            for (int u = 0; u < 8; ++u) v[u] = acc[t][u][i];
+            for (int u = 0; u < 8; ++u) v[u] = acc[t][u][r];
             rg_store_live<8>(out + row * grad_stride + col, dim - col, v);
         }
 }
@@ -400,12 +493,13 @@ rg_status rg_mx4_matmul_grad(rg_ctx* ctx, const void* dy, rg_dtype dy_type, int6
     RG_REQUIRE(ctx, aligned(rows, 4) && aligned(dy, rg_type_bytes(dy_type)) && aligned(grad, 4), "rg_mx4_matmul_grad: pointer not aligned to its numbers");
     RG_HIP(ctx, hipSetDevice(ctx->device));
     hipStream_t s = (hipStream_t)stream;
-    const bool flat = dim <= 128;
-    const int tiles_h = (int)rg_div_up(out_dim, flat ? 256 : 128), tiles_f = (int)rg_div_up(dim, flat ? 128 : 256);
-    const int64_t tiles = (int64_t)tiles_h * tiles_f;
-    const int64_t most = rg_max64(1, 2ll * ctx->num_cus / tiles);
-    const int64_t per_split = rg_max64(256, rg_div_up(rg_div_up(n, most), 32) * 32);
-    const int64_t splits = rg_max64(1, rg_div_up(n, per_split));
+    const int cols = out_dim < 4 ? 1 : dy_type == RG_BF16 ? 4 : 2;
+    const int tile_h = 16 * cols;
+    const int tiles_h = (int)rg_div_up(out_dim, tile_h);
+    const int64_t tiles = (int64_t)tiles_h * rg_div_up(dim, 128);
+    const int64_t most = rg_max64(1, ctx->num_cus / tiles);
+    const int64_t per_wave = rg_max64(1, rg_div_up(rg_div_up(n, most * kGradWaves), 32)) * 32;
+    const int64_t splits = rg_max64(1, rg_div_up(n, per_wave * kGradWaves));
     float* parts = grad;
     int64_t parts_stride = grad_stride, split_stride = 0;
     if (splits > 1) {
@@ -417,12 +511,10 @@ rg_status rg_mx4_matmul_grad(rg_ctx* ctx, const void* dy, rg_dtype dy_type, int6
     }
     const unsigned grid = (unsigned)(tiles * splits);
     RG_FOR_TYPE(dy_type, {
-        if (flat)
-            k_mx4_grad<T, 4, 1><<<grid, 256, 0, s>>>((const T*)dy, dy_stride, (const uint32_t*)rows, rows_stride, n, n_dev, out_dim, dim, per_split,
-                                                     parts, parts_stride, split_stride, tiles_h, tiles_f);
-        else
-            k_mx4_grad<T, 2, 2><<<grid, 256, 0, s>>>((const T*)dy, dy_stride, (const uint32_t*)rows, rows_stride, n, n_dev, out_dim, dim, per_split,
-                                                     parts, parts_stride, split_stride, tiles_h, tiles_f);
+        constexpr int COLS = Parts<T>::count > 1 ? 2 : 4;
+        const auto kernel = cols == 1 ? k_mx4_grad<T, 1> : k_mx4_grad<T, COLS>;
+        kernel<<<grid, 64 * kGradWaves, 0, s>>>((const T*)dy, dy_stride, (const uint32_t*)rows, rows_stride, n, n_dev, out_dim, dim, per_wave,
+                                                parts, parts_stride, split_stride, tiles_h, (int)tiles);
     });
     RG_LAUNCH_CHECK(ctx, "k_mx4_grad");
     if (splits > 1) {

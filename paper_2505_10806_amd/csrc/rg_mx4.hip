@@ -2,7 +2,7 @@
 // packed weight, and the gradient of that product to its weight.
 #include "rg_elements.h"
 
-#include <algorithm>
+#include <type_traits>
 
 namespace {
 
@@ -163,11 +163,10 @@ __global__ void __launch_bounds__(256) k_mx4_matmul(const uint32_t* __restrict__
 }
 
 // ---------------------------------------------------------------- grad = dy^T . rows
-// The contraction runs over the rows, so both operands are needed column by column.  They are turned in registers: a lane loads four
-// neighbouring columns of eight rows of dy and eight neighbouring columns (one word of codes) of the same rows, and the pairs of rows that
-// the 16 x 16 x 32 bf16 matrix instruction wants side by side are put together by byte permutations; which column a lane's row of
-// the tile stands for is free.  4-bit numbers times their scale are bf16 numbers exactly.  Numbers of dy are cut into PARTS bf16 numbers
-// that sum to them exactly (1 for bf16, 2 for f16, 3 for f32).
+// The contraction runs over the rows, so the matrix unit wants both operands column by column, eight rows of one column side by side.
+// Threads turn them on their way into LDS: one loads four neighbouring columns of eight rows of dy, or one word of codes (eight
+// columns) of eight rows, and puts pairs of rows together by byte permutations.  4-bit numbers times their scale are bf16 numbers
+// exactly; numbers of dy are cut into bf16 numbers that sum to them exactly (one for bf16, two for f16, three for f32).
 
 constexpr uint32_t kLowHalves = 0x05040100u, kHighHalves = 0x07060302u;   // of (later, earlier) as {earlier, later}
 
@@ -178,90 +177,356 @@ union Frag {
     v8bf v;
 };
 
-// Fragments u = 0 .. 7 of eight rows' words of codes: fragment u holds number u of each word's eight.
-__device__ __forceinline__ void turn_codes(const uint32_t (&code)[8], const uint32_t (&scale)[8], Frag (&f)[8]) {
+// Fragments 2 BYTE and 2 BYTE + 1 of eight rows' words of codes: fragment u holds number u of each word's eight.
+template <int BYTE>
+__device__ __forceinline__ void turn_byte(const uint32_t (&code)[8], const float (&scale)[8], Frag& even, Frag& odd) {
 #pragma unroll
     for (int j = 0; j < 8; j += 2) {
-        const float s0 = scale_bits(scale[j]), s1 = scale_bits(scale[j + 1]);
-#define RG_TURN_BYTE(B)                                                                                                              \
-        {                                                                                                                            \
-            const uint32_t p0 = bits(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code[j], s0, B));                                     \
-            const uint32_t p1 = bits(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code[j + 1], s1, B));                                 \
-            f[2 * B].w[j / 2] = __builtin_amdgcn_perm(p1, p0, kLowHalves);                                                           \
-            f[2 * B + 1].w[j / 2] = __builtin_amdgcn_perm(p1, p0, kHighHalves);                                                      \
-        }
-        RG_TURN_BYTE(0) RG_TURN_BYTE(1) RG_TURN_BYTE(2) RG_TURN_BYTE(3)
-#undef RG_TURN_BYTE
+        const uint32_t p0 = bits(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code[j], scale[j], BYTE));
+        const uint32_t p1 = bits(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code[j + 1], scale[j + 1], BYTE));
+        even.w[j / 2] = __builtin_amdgcn_perm(p1, p0, kLowHalves);
+        odd.w[j / 2] = __builtin_amdgcn_perm(p1, p0, kHighHalves);
     }
 }
 
-// x less its leading bf16 part (cut off, not rounded): exact.  Infinities have no rest.
-__device__ __forceinline__ float bf16_rest(float x) {
-    const float head = __uint_as_float(__float_as_uint(x) & 0xFFFF0000u);
-    return x == head ? 0.0f : x - head;
-}
+// x less its leading bf16 part (cut off, not rounded): exact, but NaN for infinities.
+__device__ __forceinline__ float bf16_rest(float x) { return x - __uint_as_float(__float_as_uint(x) & 0xFFFF0000u); }
 
 template <typename T> struct Parts { static constexpr int count = sizeof(T) == 4 ? 3 : 2; };
 template <> struct Parts<__bf16> { static constexpr int count = 1; };
 
-// What a lane holds of 32 rows: COLS neighbouring numbers of dy, the word of codes and the word of scales of its 8 rows.
-template <typename T, int COLS> struct GradStep {
-    typedef T Vec __attribute__((ext_vector_type(COLS)));
-    Vec d[8];
-    uint32_t code[8], scale[8];
-};
-
-template <typename T, int COLS>
-__device__ __forceinline__ typename GradStep<T, COLS>::Vec load_columns(const T* p) {
-    typename GradStep<T, COLS>::Vec v;
-    if constexpr (COLS == 1) v[0] = *p;
-    else {
-        const typename RgPack<T, COLS>::type a = *(const typename RgPack<T, COLS>::type*)p;
+// Eight numbers cut into their parts, each as a fragment, handed to put(part, fragment).
+template <int P, typename F>
+__device__ __forceinline__ void cut(float (&x)[8], F put) {
+    float whole[8], most = 0.0f;
 #pragma unroll
-        for (int i = 0; i < COLS; ++i) v[i] = a[i];
+    for (int j = 0; j < 8; ++j) {
+        whole[j] = x[j];
+        most = fmaxf(most, fabsf(x[j]));
     }
-    return v;
-}
-
-// The columns of a lane that reaches over the end of a row, which were loaded `over` columns further left (0: as they are; what
-// comes in from the right is not used).
-template <typename T, int COLS>
-__device__ __forceinline__ typename GradStep<T, COLS>::Vec move_columns(typename GradStep<T, COLS>::Vec v, int over) {
-    if constexpr (COLS == 1) return v;
-    else if constexpr (COLS * sizeof(T) == 8 && COLS == 4) {
-        uint64_t w;
-        __builtin_memcpy(&w, &v, 8);
-        w >>= (16 * over) & 63;
-        __builtin_memcpy(&v, &w, 8);
-        return v;
-    } else {
-        static_assert(COLS == 2, "two columns, or four of 16 bits");
-        v[0] = over ? v[1] : v[0];
-        return v;
-    }
-}
-
-// Part p of one column of eight rows' numbers, as a fragment; the numbers lose that part.
-__device__ __forceinline__ void turn_column(float (&x)[8], Frag& f, bool last) {
+    const bool endless = __any(__builtin_isinf(most));
 #pragma unroll
-    for (int j = 0; j < 8; j += 2) f.w[j / 2] = __builtin_amdgcn_perm(__float_as_uint(x[j + 1]), __float_as_uint(x[j]), kHighHalves);
-    if (!last) {
+    for (int p = 0; p < P; ++p) {
+        Frag f;
+#pragma unroll
+        for (int j = 0; j < 8; j += 2) f.w[j / 2] = __builtin_amdgcn_perm(__float_as_uint(x[j + 1]), __float_as_uint(x[j]), kHighHalves);
+        put(p, f);
+        if (p + 1 == P) break;
 #pragma unroll
         for (int j = 0; j < 8; ++j) x[j] = bf16_rest(x[j]);
+        if (endless) {                                     // infinities have no rest (NaN has, and stays one)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = __builtin_isinf(whole[j]) ? 0.0f : x[j];
+        }
     }
 }
 
-// A wavefront makes a tile of 16 COLS outputs x 128 columns from rows of its own, WAVES of them (a workgroup) the same tile from
-// neighbouring rows, and adds theirs up in LDS; so the parts that a second launch joins are few.  The next 32 rows are on their
-// way while the matrix unit works on these.  out_dim >= COLS.  Workgroups of one range of rows follow each other on one XCD: they read the same rows.
-constexpr int kGradWaves = 8;
+// The number in the low or the high half of a word.
+template <typename T>
+__device__ __forceinline__ float half_number(uint32_t word, int high) {
+    const uint16_t h = (uint16_t)(word >> (16 * high));
+    T v;
+    __builtin_memcpy(&v, &h, 2);
+    return (float)v;
+}
 
-template <typename T, int COLS>
-__global__ void __launch_bounds__(64 * kGradWaves, 2) k_mx4_grad(const T* __restrict__ dy, int64_t dy_stride, const uint32_t* __restrict__ rows,
+// Every wavefront's LDS accesses done, and everyone here.  (Loads from memory stay on their way.)
+__device__ __forceinline__ void lds_barrier() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+constexpr int kGradThreads = 512;
+
+// A workgroup's tile of 64 TH outputs x 128 TF columns, ROWS rows at a time; its eight wavefronts are WH x WF x WK of them, each with
+// 64 x 16 FRAGS of the tile and 32 of the rows.
+template <typename T, int TF_> struct GradShape {
+    static constexpr int TH = 2, TF = TF_, P = Parts<T>::count;
+    static constexpr int FRAGS = 4 * TF;
+    static constexpr int WH = TH, WF = 8 * TF / FRAGS, WK = 8 / (WH * WF), ROWS = 32 * WK, GROUPS = ROWS / 8;
+    static constexpr int kDy = GROUPS * 128 * TF;          // pieces of 16 bytes (eight rows of a column): codes first, then the parts of dy
+    static constexpr int kPieces = kDy + P * GROUPS * 64 * TH;
+    static constexpr int kSums = 4 * 4 * FRAGS * 64;       // what four wavefronts hand to the others at the end
+    static constexpr int kLds = 2 * kPieces > kSums ? 2 * kPieces : kSums;
+    static_assert(GROUPS * 16 * TH <= 256 && GROUPS * 16 * TF <= 256, "a thread loads one item of a step");
+};
+
+// Four wavefronts load dy, the others codes; all of them multiply.  While step s is multiplied from one half of LDS the other half
+// is free for step s + 1, whose rows, and those of s + 2, are on their way: one barrier a step.  The WK sums of a piece of the tile are added up in LDS
+// at the end, the ranges' of the rows by a second launch in their order.
+// Workgroups of one range of rows follow each other on one XCD, whose L2 serves all but the first.
+template <typename S, typename T>
+__global__ void __launch_bounds__(kGradThreads, 2) k_mx4_grad(const T* __restrict__ dy, int64_t dy_stride, const uint32_t* __restrict__ rows,
+                                                             int64_t rows_stride, int64_t n, const int32_t* __restrict__ n_dev, int out_dim,
+                                                             int dim, int64_t rows_per_split, float* __restrict__ grad, int64_t grad_stride,
+                                                             int64_t split_stride, int tiles_h, int tiles) {
+    constexpr int P = S::P, W4 = sizeof(T), FRAGS = S::FRAGS;                    // W4: words of four numbers of dy
+    __shared__ Frag lds[S::kLds];
+    const int64_t n_act = rg_rows(n, n_dev);
+    const int lane = rg_lane(), c = lane & 15, q = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);      // (the same in every lane, which the compiler may know)
+    const int block = rg_xcd_block(blockIdx.x, gridDim.x);
+    const int tile = block % tiles;
+    const int64_t split = block / tiles;
+    const int h0 = (tile % tiles_h) * (64 * S::TH), f0 = (tile / tiles_h) * (128 * S::TF);
+    const int groups = (dim + kGroup - 1) / kGroup;
+    const int64_t first = split * rows_per_split, last = rg_least(first + rows_per_split, n_act);
+    const int64_t steps = last > first ? (last - first) / S::ROWS : 0;
+    const int rest = last > first ? (int)((last - first) - steps * S::ROWS) : 0;
+
+    // this wavefront's piece of the tile
+    const int wf = wave % S::WF, wh = wave / S::WF % S::WH, wk = wave / (S::WF * S::WH);
+    const Frag* from_x = lds + (4 * wk + q) * (128 * S::TF) + 16 * FRAGS * wf + c;
+    const Frag* from_dy = lds + S::kDy + (4 * wk + q) * (64 * S::TH) + 64 * wh + c;
+    v4f acc[4][FRAGS];
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int u = 0; u < FRAGS; ++u) acc[t][u] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    const auto multiply = [&](int half) {
+        Frag b[FRAGS];
+#pragma unroll
+        for (int u = 0; u < FRAGS; ++u) b[u] = from_x[half * S::kPieces + 16 * u];
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                const Frag a = from_dy[half * S::kPieces + p * S::GROUPS * 64 * S::TH + 16 * t];
+#pragma unroll
+                for (int u = 0; u < FRAGS; ++u) acc[t][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, b[u].v, acc[t][u], 0, 0, 0);
+            }
+    };
+
+    // ROLE: loads dy (its four columns k) or codes (its word w) of the eight rows of group g.
+    const auto run = [&](auto role, int item) {
+        constexpr bool DY = decltype(role)::value;
+        constexpr int PER = DY ? 16 * S::TH : 16 * S::TF;
+        const int g = item / PER, k = item % PER;
+        const int h = h0 + 4 * k, h_at = min(h, out_dim - 4), over = h - h_at;
+        const bool ragged = h0 + 64 * S::TH > out_dim;
+        const int group = min((f0 >> 5) + (k >> 2), groups - 1);
+        const T* pd = dy + (first + 8 * g) * dy_stride + h_at;
+        const uint32_t* px = rows + (first + 8 * g) * rows_stride + min((f0 >> 3) + k, 4 * groups - 1);
+        const uint8_t* ps = (const uint8_t*)(rows + (first + 8 * g) * rows_stride + 4 * groups) + group;
+        struct Raw {
+            uint32_t w[DY ? 8 * W4 : 16];
+        };
+        // row `at` (of those from the thread's first on) as the j-th of eight
+        const auto load_row = [&](Raw& raw, int j, int64_t at) {
+            if constexpr (!DY) {
+                raw.w[j] = px[at * rows_stride];
+                raw.w[8 + j] = ps[4 * at * rows_stride];
+            } else {
+                typedef uint32_t Words __attribute__((ext_vector_type(sizeof(T) == 4 ? 4 : 2), aligned(2)));
+                const Words v = *(const Words*)(pd + at * dy_stride);
+#pragma unroll
+                for (int t = 0; t < W4; ++t) raw.w[j * W4 + t] = v[t];
+            }
+        };
+        // step s (behind the last whole one: that one again, which nothing uses)
+        const auto load = [&](Raw& raw, int64_t s) {
+            if (s >= steps) {
+                pd -= S::ROWS * dy_stride;
+                px -= S::ROWS * rows_stride;
+                ps -= 4 * S::ROWS * rows_stride;
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) load_row(raw, j, j);
+            pd += S::ROWS * dy_stride;
+            px += S::ROWS * rows_stride;
+            ps += 4 * S::ROWS * rows_stride;
+        };
+        // into one half of LDS; of the last, not whole step `live` rows, the others as zeros
+        const auto turn = [&](Raw& raw, int half, int live) {
+            Frag* to = lds + half * S::kPieces;
+            if constexpr (!DY) {
+                uint32_t code[8];
+                float scale[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    code[j] = j < live ? raw.w[j] : 0u;
+                    scale[j] = scale_bits(j < live ? raw.w[8 + j] : 0u);
+                }
+                Frag f[8];
+                turn_byte<0>(code, scale, f[0], f[1]);
+                turn_byte<1>(code, scale, f[2], f[3]);
+                turn_byte<2>(code, scale, f[4], f[5]);
+                turn_byte<3>(code, scale, f[6], f[7]);
+#pragma unroll
+                for (int u = 0; u < 8; ++u) to[g * (128 * S::TF) + u * PER + k] = f[u];
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+#pragma unroll
+                    for (int t = 0; t < W4; ++t) raw.w[j * W4 + t] = j < live ? raw.w[j * W4 + t] : 0u;
+                if (ragged) {                              // columns that were loaded from further left
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        if constexpr (W4 == 2) {
+                            const uint64_t x = (((uint64_t)raw.w[2 * j + 1] << 32) | raw.w[2 * j]) >> ((16 * over) & 63);
+                            raw.w[2 * j] = (uint32_t)x;
+                            raw.w[2 * j + 1] = (uint32_t)(x >> 32);
+                        } else {
+                            const uint32_t x0 = raw.w[4 * j], x1 = raw.w[4 * j + 1], x2 = raw.w[4 * j + 2], x3 = raw.w[4 * j + 3];
+                            raw.w[4 * j] = over == 0 ? x0 : over == 1 ? x1 : over == 2 ? x2 : x3;
+                            raw.w[4 * j + 1] = over == 0 ? x1 : over == 1 ? x2 : x3;
+                            raw.w[4 * j + 2] = over == 0 ? x2 : x3;
+                        }
+                    }
+                }
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    Frag* column = to + S::kDy + g * (64 * S::TH) + t * PER + k;
+                    if constexpr (P == 1) {
+                        Frag f;
+#pragma unroll
+                        for (int j = 0; j < 8; j += 2)
+                            f.w[j / 2] = __builtin_amdgcn_perm(raw.w[(j + 1) * W4 + (t >> 1)], raw.w[j * W4 + (t >> 1)],
+                                                               t & 1 ? kHighHalves : kLowHalves);
+                        *column = f;
+                    } else {
+                        float x[8];
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            if constexpr (W4 == 4) x[j] = __uint_as_float(raw.w[4 * j + t]);
+                            else x[j] = half_number<T>(raw.w[2 * j + (t >> 1)], t & 1);
+                        }
+                        cut<P>(x, [&](int p, const Frag& f) { column[p * S::GROUPS * 64 * S::TH] = f; });
+                    }
+                }
+            }
+        };
+        if (steps > 0) {
+            if constexpr (P == 1) {                        // two steps' rows are on their way
+                Raw even, odd;
+                load(even, 0);
+                load(odd, 1);
+                int64_t s = 0;
+                for (; s + 2 <= steps; s += 2) {
+                    turn(even, 0, 8);
+                    load(even, s + 2);
+                    __builtin_amdgcn_sched_barrier(0);
+                    lds_barrier();
+                    multiply(0);
+                    turn(odd, 1, 8);
+                    load(odd, s + 3);
+                    __builtin_amdgcn_sched_barrier(0);
+                    lds_barrier();
+                    multiply(1);
+                }
+                if (s < steps) {
+                    turn(even, 0, 8);
+                    lds_barrier();
+                    multiply(0);
+                }
+            } else {                                       // dy's parts take longer to make: of the two wavefronts of a SIMD one does it
+                Raw raw;                                   // while the other one multiplies; registers for one step's rows are left
+                load(raw, 0);
+                turn(raw, 0, 8);
+                load(raw, 1);
+                for (int64_t s = 0; s < steps; ++s) {
+                    lds_barrier();
+                    if (!DY) multiply((int)(s & 1));
+                    if (s + 1 < steps) turn(raw, (int)(s + 1) & 1, 8);
+                    load(raw, s + 2);
+                    __builtin_amdgcn_sched_barrier(0);
+                    if (DY) multiply((int)(s & 1));
+                }
+            }
+        }
+        if (rest > 0) {
+            Raw raw;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) load_row(raw, j, min(j, rest - 1 - 8 * g));
+            turn(raw, (int)(steps & 1), rest - 8 * g);
+            lds_barrier();
+            multiply((int)(steps & 1));
+        }
+    };
+    if (wave < S::GROUPS * S::TH / 4) run(std::true_type(), threadIdx.x);
+    else if (wave >= 4 && wave < 4 + S::GROUPS * S::TF / 4) run(std::false_type(), threadIdx.x - 256);
+    else                                                   // (nothing left to load)
+        for (int64_t s = 0; s < steps + (rest > 0); ++s) {
+            lds_barrier();
+            multiply((int)(s & 1));
+        }
+
+    // the sums over wk, half of the wavefronts giving theirs to the other half (wk is the slowest of a wavefront's coordinates)
+    v4f* sums = (v4f*)lds;
+    for (int half = 4; half >= S::WH * S::WF; half >>= 1) {
+        __syncthreads();
+        if (wave >= half && wave < 2 * half) {
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int u = 0; u < FRAGS; ++u) sums[((wave - half) * (4 * FRAGS) + t * FRAGS + u) * 64 + lane] = acc[t][u];
+        }
+        __syncthreads();
+        if (wave < half) {
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int u = 0; u < FRAGS; ++u) acc[t][u] += sums[(wave * (4 * FRAGS) + t * FRAGS + u) * 64 + lane];
+        }
+    }
+    if (wk != 0) return;
+    // fragment i of the codes' 8 TF: number i / TF of words 16 (i % TF) + 0 .. 15; of dy's 4 TH: columns 4 (16 (i % TH) + 0 .. 15) + i / TH
+    float* out = grad + split * split_stride;
+    constexpr int RUN = FRAGS / S::TF;                     // neighbouring numbers of a word
+#pragma unroll
+    for (int word = 0; word < S::TF; ++word) {
+        const int col = f0 + 8 * (16 * word + c) + RUN * wf;
+        if (col >= dim) continue;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int piece = 4 * wh + t;
+                const int row = h0 + 4 * (16 * (piece % S::TH) + 4 * q + r) + piece / S::TH;
+                if (row >= out_dim) continue;
+                float v[RUN];
+#pragma unroll
+                for (int u = 0; u < RUN; ++u) v[u] = acc[t][u * S::TF + word][r];
+                rg_store_live<RUN>(out + row * grad_stride + col, dim - col, v);
+            }
+    }
+}
+
+// A wavefront makes a tile of 16 COLS outputs x 128 columns from rows of its own, the eight of a workgroup the same tile from
+// neighbouring rows, and adds theirs up in LDS; so the parts that a second launch joins are few.  A row of the tile is 128 bytes of dy,
+// 64 of codes and 4 of scales each: a wavefront loads them 16 bytes a lane and turns them round by way of LDS of its own (without a barrier), and
+// the next 32 rows are on their way meanwhile.  (Loaded as the lanes need them, 24 accesses of 4 and 8 bytes to a step instead of 7, a step
+// took a compute unit 400 to 540 cycles.)
+// Workgroups of one range of rows follow each other on one XCD, whose L2 serves all but the first.
+// NARROW: rows of dy are shorter than 16 bytes.
+constexpr int kFewWaves = 8;
+
+// (Four columns of three parts each would leave no registers for the rows on their way.)
+template <typename T> struct FewTile {
+    static constexpr int COLS = sizeof(T) == 4 ? 2 : 4;
+    static constexpr int E = 16 / sizeof(T);               // numbers of dy in 16 bytes
+    static constexpr int PIECES = COLS * sizeof(T);        // 16 bytes each, of a tile's row of dy
+    static constexpr int LOADS = PIECES / 2;               // for 32 rows
+};
+
+template <typename T> struct FewLds {
+    rg_u32x4 dy[32][FewTile<T>::PIECES];
+    rg_u32x4 code[32][4];
+    float scale[32][4];
+};
+
+template <typename T, bool NARROW>
+__global__ void __launch_bounds__(64 * kFewWaves, 2) k_mx4_grad_few(const T* __restrict__ dy, int64_t dy_stride, const uint32_t* __restrict__ rows,
                                                               int64_t rows_stride, int64_t n, const int32_t* __restrict__ n_dev, int out_dim,
                                                               int dim, int64_t rows_per_wave, float* __restrict__ grad, int64_t grad_stride,
                                                               int64_t split_stride, int tiles_h, int tiles) {
-    __shared__ v4f sums[kGradWaves / 2][COLS * 8][64];
+    constexpr int COLS = FewTile<T>::COLS, E = FewTile<T>::E, P = Parts<T>::count;
+    constexpr int PIECES = FewTile<T>::PIECES, LOADS = FewTile<T>::LOADS, BY = 32 / LOADS;
+    __shared__ union {
+        FewLds<T> rows[kFewWaves];
+        v4f sums[kFewWaves / 2][COLS * 8][64];
+    } lds;
     const int64_t n_act = rg_rows(n, n_dev);
     const int lane = rg_lane(), c = lane & 15, q = lane >> 4;
     const int wave = threadIdx.x >> 6;
@@ -270,110 +535,171 @@ __global__ void __launch_bounds__(64 * kGradWaves, 2) k_mx4_grad(const T* __rest
     const int64_t split = block / tiles;
     const int h0 = (tile % tiles_h) * (16 * COLS), f0 = (tile / tiles_h) * 128;
     const int groups = (dim + kGroup - 1) / kGroup;
-    const int h = h0 + COLS * c, col = f0 + 8 * c;
-    const int h_at = min(h, out_dim - COLS), over = h - h_at;
-    const int shift = 8 * (c >> 2);
+    const int64_t first = (split * kFewWaves + wave) * rows_per_wave, last = rg_least(first + rows_per_wave, n_act);
+
+    // what this lane loads: 16 bytes of dy of every BY-th row (from further left where the row ends before them, and moved behind the
+    // load), a group's codes of rows lane / 4 + 0, 16, the scales of row lane % 32
+    const int dy_row = lane / PIECES, dy_piece = lane % PIECES;
+    const int piece = h0 + dy_piece * E, piece_at = NARROW ? piece : min(piece, out_dim - E), over = piece - piece_at;
+    const bool ragged = h0 + 16 * COLS > out_dim;
+    const T* pd = dy + (first + dy_row) * dy_stride + piece_at;
+    const uint32_t* px = rows + (first + (lane >> 2)) * rows_stride + 4 * min((f0 >> 5) + (lane & 3), groups - 1);
+    const uint32_t* ps = rows + (first + (lane & 31)) * rows_stride + 4 * groups + (f0 >> 7);
+    FewLds<T>& mine = lds.rows[wave];
+
+    struct Step {
+        rg_u32x4 d[LOADS], code[2];
+        uint32_t scale;
+    };
+    // the next 32 rows, of which `left` are there: those behind read the last one
+    const auto load = [&](Step& s, int left) {
+        const bool whole = left >= 32;
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const T* p = pd + (whole ? BY * i : min(BY * i, left - 1 - dy_row)) * dy_stride;
+            if constexpr (NARROW) {
+                T v[E];
+#pragma unroll
+                for (int e = 0; e < E; ++e) v[e] = piece + e < out_dim ? p[e] : (T)0.0f;
+                __builtin_memcpy(&s.d[i], v, 16);
+            } else {
+                typedef uint32_t Any __attribute__((ext_vector_type(4), aligned(2)));
+                s.d[i] = *(const Any*)p;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) s.code[i] = *(const rg_u32x4*)(px + (whole ? 16 * i : min(16 * i, left - 1 - (lane >> 2))) * rows_stride);
+        s.scale = ps[(whole ? 0 : min(0, left - 1 - (lane & 31))) * rows_stride];
+        pd += 32 * dy_stride;
+        px += 32 * rows_stride;
+        ps += 32 * rows_stride;
+    };
+    // them into LDS, those behind the last as zeros
+    const auto place = [&](Step& s, int left) {
+        if (left < 32) {
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i)
+                if (BY * i + dy_row >= left) s.d[i] = rg_u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                if (16 * i + (lane >> 2) >= left) s.code[i] = rg_u32x4{0u, 0u, 0u, 0u};
+            if ((lane & 31) >= left) s.scale = 0u;
+        }
+        if (!NARROW && ragged) {
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) {
+                uint32_t w0 = s.d[i][0], w1 = s.d[i][1], w2 = s.d[i][2], w3 = s.d[i][3];
+                const int by = over * (int)sizeof(T);
+                if (by & 8) { w0 = w2; w1 = w3; }
+                if (by & 4) { w0 = w1; w1 = w2; w2 = w3; }
+                if (sizeof(T) == 2 && (by & 2)) {
+                    w0 = __builtin_amdgcn_alignbyte(w1, w0, 2);
+                    w1 = __builtin_amdgcn_alignbyte(w2, w1, 2);
+                    w2 = __builtin_amdgcn_alignbyte(w3, w2, 2);
+                    w3 >>= 16;
+                }
+                s.d[i] = rg_u32x4{w0, w1, w2, w3};
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) mine.dy[BY * i + dy_row][dy_piece] = s.d[i];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) mine.code[16 * i + (lane >> 2)][lane & 3] = s.code[i];
+        if (lane < 32) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) mine.scale[lane][i] = scale_bits((s.scale >> (8 * i)) & 255u);
+        }
+    };
+
     v4f acc[COLS][8];
 #pragma unroll
     for (int t = 0; t < COLS; ++t)
 #pragma unroll
         for (int u = 0; u < 8; ++u) acc[t][u] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-
-    const int64_t first = (split * kGradWaves + wave) * rows_per_wave, last = rg_least(first + rows_per_wave, n_act);
-    const T* pd = dy + (first + 8 * q) * dy_stride + h_at;
-    const uint32_t* px = rows + (first + 8 * q) * rows_stride + min(col >> 3, 4 * groups - 1);
-    const uint32_t* ps = rows + (first + 8 * q) * rows_stride + 4 * groups + (f0 >> 7);
-
-    const auto load = [&](GradStep<T, COLS>& s) {
+    // lane 16 q + c: rows 4 j + q, columns COLS c .. of dy, word c of the codes
+    const auto multiply = [&] {
+        __builtin_amdgcn_wave_barrier();
+        uint32_t code[8];
+        float scale[8];
+        struct alignas(COLS * sizeof(T)) Cols { uint32_t w[COLS * sizeof(T) / 4]; };
+        Cols d[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            s.d[j] = load_columns<T, COLS>(pd + j * dy_stride);
-            s.code[j] = px[j * rows_stride];
-            s.scale[j] = ps[j * rows_stride];
+            d[j] = ((const Cols*)mine.dy[4 * j + q])[c];
+            code[j] = ((const uint32_t*)mine.code[4 * j + q])[c];
+            scale[j] = mine.scale[4 * j + q][c >> 2];
         }
-        pd += 32 * dy_stride;
-        px += 32 * rows_stride;
-        ps += 32 * rows_stride;
-    };
-    const auto multiply = [&](const GradStep<T, COLS>& s) {
-        uint32_t scale[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) scale[j] = (s.scale[j] >> shift) & 255u;
-        Frag b[8];
-        turn_codes(s.code, scale, b);
-        typename GradStep<T, COLS>::Vec d[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) d[j] = move_columns<T, COLS>(s.d[j], over);
+        __builtin_amdgcn_wave_barrier();
+        Frag a[P][COLS];
 #pragma unroll
         for (int t = 0; t < COLS; ++t) {
-            float x[8];
+            if constexpr (P == 1) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = (float)d[j][t];
+                for (int j = 0; j < 8; j += 2)
+                    a[0][t].w[j / 2] = __builtin_amdgcn_perm(d[j + 1].w[t >> 1], d[j].w[t >> 1], t & 1 ? kHighHalves : kLowHalves);
+            } else {
+                float x[8];
 #pragma unroll
-            for (int p = 0; p < Parts<T>::count; ++p) {
-                Frag a;
-                turn_column(x, a, p + 1 == Parts<T>::count);
-#pragma unroll
-                for (int u = 0; u < 8; ++u) acc[t][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, b[u].v, acc[t][u], 0, 0, 0);
+                for (int j = 0; j < 8; ++j) {
+                    if constexpr (sizeof(T) == 4) x[j] = __uint_as_float(d[j].w[t]);
+                    else x[j] = half_number<T>(d[j].w[t >> 1], t & 1);
+                }
+                cut<P>(x, [&](int p, const Frag& f) { a[p][t] = f; });
             }
         }
+#define RG_MULTIPLY_BYTE(B)                                                                                                              \
+        {                                                                                                                                \
+            Frag even, odd;                                                                                                              \
+            turn_byte<B>(code, scale, even, odd);                                                                                       \
+            _Pragma("unroll") for (int p = 0; p < P; ++p)                                                                                \
+                _Pragma("unroll") for (int t = 0; t < COLS; ++t) {                                                                       \
+                    acc[t][2 * B] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[p][t].v, even.v, acc[t][2 * B], 0, 0, 0);                  \
+                    acc[t][2 * B + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[p][t].v, odd.v, acc[t][2 * B + 1], 0, 0, 0);           \
+                }                                                                                                                        \
+        }
+        RG_MULTIPLY_BYTE(0) RG_MULTIPLY_BYTE(1) RG_MULTIPLY_BYTE(2) RG_MULTIPLY_BYTE(3)
+#undef RG_MULTIPLY_BYTE
     };
 
     const int steps = last > first ? (int)((last - first) >> 5) : 0;
+    const int rest = last > first ? (int)(last - first) & 31 : 0;
+    Step s;
     if (steps > 0) {
-        GradStep<T, COLS> even, odd;
-        load(even);
-        for (int k = 0; k + 2 <= steps; k += 2) {
-            load(odd);
+        load(s, 32);
+        for (int k = 0; k + 1 < steps; ++k) {
+            place(s, 32);
+            load(s, 32);
             __builtin_amdgcn_sched_barrier(0);
-            multiply(even);
-            // (behind the last whole step the same rows once more, which nothing uses)
-            const int64_t back = k + 2 < steps ? 0 : 32;
-            pd -= back * dy_stride;
-            px -= back * rows_stride;
-            ps -= back * rows_stride;
-            load(even);
-            __builtin_amdgcn_sched_barrier(0);
-            multiply(odd);
+            multiply();
         }
-        if (steps & 1) multiply(even);
+        place(s, 32);
+        multiply();
     }
-    const int64_t i = first + 32ll * steps;
-    if (i < last) {                                        // fewer than 32 rows: the others are zeros
-        GradStep<T, COLS> s;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const bool live = i + 8 * q + j < last;
-            typename GradStep<T, COLS>::Vec none = (typename GradStep<T, COLS>::Vec)(T)0.0f;
-            s.d[j] = none;
-            s.code[j] = s.scale[j] = 0u;
-            if (live) {
-                s.d[j] = load_columns<T, COLS>(pd + j * dy_stride);
-                s.code[j] = px[j * rows_stride];
-                s.scale[j] = ps[j * rows_stride];
-            }
-        }
-        multiply(s);
+    if (rest > 0) {
+        load(s, rest);
+        place(s, rest);
+        multiply();
     }
 
     // half of the wavefronts hand their sums to the other half, until one is left
 #pragma unroll
-    for (int half = kGradWaves / 2; half > 0; half >>= 1) {
+    for (int half = kFewWaves / 2; half > 0; half >>= 1) {
         __syncthreads();
         if (wave >= half && wave < 2 * half) {
 #pragma unroll
             for (int t = 0; t < COLS; ++t)
 #pragma unroll
-                for (int u = 0; u < 8; ++u) sums[wave - half][t * 8 + u][lane] = acc[t][u];
+                for (int u = 0; u < 8; ++u) lds.sums[wave - half][t * 8 + u][lane] = acc[t][u];
         }
         __syncthreads();
         if (wave < half) {
 #pragma unroll
             for (int t = 0; t < COLS; ++t)
 #pragma unroll
-                for (int u = 0; u < 8; ++u) acc[t][u] += sums[wave][t * 8 + u][lane];
+                for (int u = 0; u < 8; ++u) acc[t][u] += lds.sums[wave][t * 8 + u][lane];
         }
     }
+    const int col = f0 + 8 * c;
     if (wave != 0 || col >= dim) return;
     float* out = grad + split * split_stride;
 #pragma unroll
@@ -389,15 +715,33 @@ __global__ void __launch_bounds__(64 * kGradWaves, 2) k_mx4_grad(const T* __rest
         }
 }
 
-// grad = the sum of the splits' parts, in their order.
-__global__ void __launch_bounds__(256) k_mx4_grad_join(const float* __restrict__ parts, int splits, int64_t split_stride, int out_dim, int dim,
-                                                       float* __restrict__ grad, int64_t grad_stride) {
-    const int64_t total = (int64_t)out_dim * dim;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-        float sum = 0.0f;
-        for (int s = 0; s < splits; ++s) sum += parts[s * split_stride + i];
-        grad[(i / dim) * grad_stride + i % dim] = sum;
+// grad = the sum of the splits' parts: a workgroup 64 chunks of 4 numbers, 16 runs of the parts side by side, in one order.
+__global__ void __launch_bounds__(1024) k_mx4_grad_join(const float* __restrict__ parts, int splits, int64_t split_stride, int out_dim, int dim,
+                                                        float* __restrict__ grad, int64_t grad_stride) {
+    __shared__ float runs[16][256];
+    const int lane = rg_lane(), run = threadIdx.x >> 6;
+    const int64_t total = (int64_t)out_dim * dim, at = ((int64_t)blockIdx.x * 64 + lane) * 4;
+    const int per_run = (splits + 15) >> 4, first = run * per_run, last = min(first + per_run, splits);
+    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (at < total) {
+#pragma unroll 4
+        for (int s = first; s < last; ++s) {
+            float v[4];
+            rg_load_head<4>(parts + s * split_stride + at, (int)rg_least(4, total - at), v);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum[i] += v[i];
+        }
     }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) runs[run][i * 64 + lane] = sum[i];
+    __syncthreads();
+    if (threadIdx.x >= 256) return;
+    const int64_t to = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (to >= total) return;
+    float all = 0.0f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) all += runs[r][(threadIdx.x & 3) * 64 + (threadIdx.x >> 2)];
+    grad[to / dim * grad_stride + to % dim] = all;
 }
 
 bool aligned(const void* p, int bytes) { return (uintptr_t)p % (uintptr_t)bytes == 0; }
@@ -493,13 +837,14 @@ rg_status rg_mx4_matmul_grad(rg_ctx* ctx, const void* dy, rg_dtype dy_type, int6
     RG_REQUIRE(ctx, aligned(rows, 4) && aligned(dy, rg_type_bytes(dy_type)) && aligned(grad, 4), "rg_mx4_matmul_grad: pointer not aligned to its numbers");
     RG_HIP(ctx, hipSetDevice(ctx->device));
     hipStream_t s = (hipStream_t)stream;
-    const int cols = out_dim < 4 ? 1 : dy_type == RG_BF16 ? 4 : 2;
-    const int tile_h = 16 * cols;
+    const bool few = out_dim <= 64;
+    const int tile_h = few ? (dy_type == RG_F32 ? 32 : 64) : 128, tile_f = few || dim <= 128 ? 128 : 256;
+    const int waves = few ? kFewWaves : 1, step = few ? 32 : 64;                  // ranges of rows to a workgroup, rows of a step
     const int tiles_h = (int)rg_div_up(out_dim, tile_h);
-    const int64_t tiles = (int64_t)tiles_h * rg_div_up(dim, 128);
+    const int64_t tiles = (int64_t)tiles_h * rg_div_up(dim, tile_f);
     const int64_t most = rg_max64(1, ctx->num_cus / tiles);
-    const int64_t per_wave = rg_max64(1, rg_div_up(rg_div_up(n, most * kGradWaves), 32)) * 32;
-    const int64_t splits = rg_max64(1, rg_div_up(n, per_wave * kGradWaves));
+    const int64_t per_range = rg_max64(1, rg_div_up(rg_div_up(n, most * waves), step)) * step;
+    const int64_t splits = rg_max64(1, rg_div_up(n, per_range * waves));
     float* parts = grad;
     int64_t parts_stride = grad_stride, split_stride = 0;
     if (splits > 1) {
@@ -511,15 +856,14 @@ rg_status rg_mx4_matmul_grad(rg_ctx* ctx, const void* dy, rg_dtype dy_type, int6
     }
     const unsigned grid = (unsigned)(tiles * splits);
     RG_FOR_TYPE(dy_type, {
-        constexpr int COLS = Parts<T>::count > 1 ? 2 : 4;
-        const auto kernel = cols == 1 ? k_mx4_grad<T, 1> : k_mx4_grad<T, COLS>;
-        kernel<<<grid, 64 * kGradWaves, 0, s>>>((const T*)dy, dy_stride, (const uint32_t*)rows, rows_stride, n, n_dev, out_dim, dim, per_wave,
-                                                parts, parts_stride, split_stride, tiles_h, (int)tiles);
+        const auto kernel = !few ? (dim > 128 ? k_mx4_grad<GradShape<T, 2>, T> : k_mx4_grad<GradShape<T, 1>, T>)
+                                 : out_dim < FewTile<T>::E ? k_mx4_grad_few<T, true> : k_mx4_grad_few<T, false>;
+        kernel<<<grid, 512, 0, s>>>((const T*)dy, dy_stride, (const uint32_t*)rows, rows_stride, n, n_dev, out_dim, dim, per_range, parts, parts_stride,
+                                    split_stride, tiles_h, (int)tiles);
     });
     RG_LAUNCH_CHECK(ctx, "k_mx4_grad");
     if (splits > 1) {
-        const int64_t blocks = rg_min64(rg_div_up(split_stride, 256), (int64_t)ctx->num_cus * 32);
-        k_mx4_grad_join<<<(unsigned)blocks, 256, 0, s>>>(parts, (int)splits, split_stride, out_dim, dim, grad, grad_stride);
+        k_mx4_grad_join<<<(unsigned)rg_div_up(split_stride, 256), 1024, 0, s>>>(parts, (int)splits, split_stride, out_dim, dim, grad, grad_stride);
         RG_LAUNCH_CHECK(ctx, "k_mx4_grad_join");
     }
     return RG_OK;

@@ -11,6 +11,7 @@ typedef float v4f __attribute__((ext_vector_type(4)));
 typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
 typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
 
+typedef uint32_t rg_u32x4a __attribute__((ext_vector_type(4)));
 constexpr int kGroup = 32;
 constexpr uint32_t kScaleNan = 255;
 
@@ -159,6 +160,136 @@ __global__ void __launch_bounds__(256) k_mx4_matmul(const uint32_t* __restrict__
             }
         }
     }
+    }
+}
+
+// The same for many rows: a wavefront keeps the weight of 16 FRAGS outputs (STEPS of 128 numbers) in registers and goes over tiles of 16
+// rows, whose codes are loaded a tile ahead; a workgroup's wavefronts share rows (through L1) where there are outputs for them, and take
+// different rows where there are not.  Bound by the rows' traffic: results go by way of LDS, so that a wavefront's stores cover
+// whole lines (stored as the matrix unit leaves them, 64 bytes of a row at a time, 794 k rows of 256 numbers times 256 outputs took 176 us
+// instead of 126).  Where rows of y follow each other without a gap and end inside 16 bytes (`run_on`), a tile is stored as one run.
+constexpr int kKeptThreads = 256, kKeptWaves = kKeptThreads / RG_WAVE;
+
+template <typename T, int STEPS, int FRAGS>
+__global__ void __launch_bounds__(kKeptThreads, STEPS > 5 ? 2 : 1) k_mx4_matmul_kept(
+    const uint32_t* __restrict__ rows, int64_t rows_stride, int64_t n, const int32_t* __restrict__ n_dev, const uint32_t* __restrict__ weight,
+    int64_t weight_stride, int out_dim, int groups, T* __restrict__ y, int64_t y_stride, int slices, int slice_groups, int run_on,
+    uint32_t inv_last) {
+    constexpr bool WIDE = sizeof(T) == 4;
+    constexpr int OUTS = 16 * FRAGS, E = 16 / sizeof(T), PITCH = OUTS * (int)sizeof(T) + 16;   // numbers in 16 bytes; bytes of a row in LDS
+    __shared__ rg_u32x4a stage[kKeptWaves][PITCH];
+    const int64_t n_act = rg_rows(n, n_dev);
+    const int lane = rg_lane(), c = lane & 15, q = lane >> 4;
+    const int wave = threadIdx.x >> 6;
+    // `slices` (1, 2 or 4) times OUTS outputs to a workgroup, slice_groups workgroups side by side on the same rows
+    const int block = rg_xcd_block(blockIdx.x, gridDim.x);
+    const int h0 = ((block % slice_groups) * slices + wave % slices) * OUTS;
+    if (h0 >= out_dim) return;
+    const int apart = kKeptWaves / slices;                 // row tiles of a workgroup side by side
+    const int64_t first = (int64_t)(block / slice_groups) * apart + wave / slices, stride = (int64_t)(gridDim.x / slice_groups) * apart;
+
+    // row r of fragment t: of 32 bits output 16 t + r; of 16 bits, so that two fragments make 16 neighbouring bytes of a lane, output
+    // 32 (t / 2) + 8 (r / 4) + 4 (t % 2) + r % 4
+    const auto output = [](int t, int r) { return WIDE ? 16 * t + r : 32 * (t >> 1) + 8 * (r >> 2) + 4 * (t & 1) + (r & 3); };
+    rg_u32x4 wc[FRAGS][STEPS];
+    uint32_t ws[FRAGS][(STEPS + 3) / 4];
+#pragma unroll
+    for (int t = 0; t < FRAGS; ++t) {
+        const uint32_t* w = weight + (int64_t)min(h0 + output(t, c), out_dim - 1) * weight_stride;
+#pragma unroll
+        for (int k = 0; k < (STEPS + 3) / 4; ++k) ws[t][k] = 0;
+#pragma unroll
+        for (int k = 0; k < STEPS; ++k) {
+            const int g = 4 * k + q;
+            const bool live = g < groups;
+            wc[t][k] = rg_u32x4{0u, 0u, 0u, 0u};
+            if (live) wc[t][k] = *(const rg_u32x4*)(w + 4 * g);
+            const uint32_t s = live ? (w[4 * groups + k] >> (8 * q)) & 255u : 127u;
+            ws[t][k >> 2] |= s << (8 * (k & 3));
+        }
+    }
+
+    struct Tile {
+        rg_u32x4 code[STEPS];
+        uint32_t scale[STEPS];
+    };
+    const auto load = [&](Tile& x, int64_t tile) {
+        const uint32_t* row = rows + rg_least(16 * tile + c, n_act - 1) * rows_stride;
+#pragma unroll
+        for (int k = 0; k < STEPS; ++k) {
+            x.code[k] = *(const rg_u32x4*)(row + 4 * min(4 * k + q, groups - 1));   // (what is behind the last group meets zeros)
+            x.scale[k] = row[4 * groups + min(k, (groups - 1) >> 2)];
+        }
+    };
+    const int64_t tiles = (n_act + 15) >> 4;
+    if (first >= tiles) return;
+    // how this wavefront's part of a tile lies in LDS and is stored: `width` numbers of a row, in pieces of 16 bytes
+    const int width = min(OUTS, out_dim - h0);
+    const int pitch = run_on ? width * (int)sizeof(T) : PITCH, lanes = (width + E - 1) / E;
+    char* const mine = (char*)stage[wave];
+    Tile next;
+    load(next, first);
+    for (int64_t tile = first; tile < tiles; tile += stride) {
+        const Tile x = next;
+        load(next, rg_least(tile + stride, tiles - 1));
+        v4f acc[FRAGS];
+#pragma unroll
+        for (int t = 0; t < FRAGS; ++t) acc[t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int k = 0; k < STEPS; ++k) {
+            const uint32_t s = 4 * k + q < groups ? x.scale[k] >> (8 * q) : 127u;
+            const v8i b = v8i{(int)x.code[k][0], (int)x.code[k][1], (int)x.code[k][2], (int)x.code[k][3], 0, 0, 0, 0};
+#pragma unroll
+            for (int t = 0; t < FRAGS; ++t) {
+                const v8i a = v8i{(int)wc[t][k][0], (int)wc[t][k][1], (int)wc[t][k][2], (int)wc[t][k][3], 0, 0, 0, 0};
+                if ((k & 3) == 0) acc[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, acc[t], 4, 4, 0, (int)ws[t][k >> 2], 0, (int)s);
+                if ((k & 3) == 1) acc[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, acc[t], 4, 4, 1, (int)ws[t][k >> 2], 0, (int)s);
+                if ((k & 3) == 2) acc[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, acc[t], 4, 4, 2, (int)ws[t][k >> 2], 0, (int)s);
+                if ((k & 3) == 3) acc[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, acc[t], 4, 4, 3, (int)ws[t][k >> 2], 0, (int)s);
+            }
+        }
+        T* const to = (T*)(mine + c * pitch);
+        if (run_on) {                                      // number by number: rows start anywhere
+#pragma unroll
+            for (int t = 0; t < FRAGS; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int at = output(t, 4 * q) + r;
+                    if (at < width) to[at] = (T)acc[t][r];
+                }
+        } else if constexpr (WIDE) {
+#pragma unroll
+            for (int t = 0; t < FRAGS; ++t) *(v4f*)(to + 16 * t + 4 * q) = acc[t];
+        } else {
+#pragma unroll
+            for (int t = 0; t < FRAGS; t += 2) {
+                typename RgPack<T, 8>::type v;
+#pragma unroll
+                for (int r = 0; r < 8; ++r) v[r] = (T)acc[t + (r >> 2)][r & 3];
+                *(rg_u32x4a*)(to + 16 * t + 8 * q) = __builtin_bit_cast(rg_u32x4a, v);
+            }
+        }
+        __builtin_amdgcn_wave_barrier();
+        const int live = (int)rg_least(16, n_act - 16 * tile);
+        const int numbers = run_on ? live * width : width, pieces = run_on ? (numbers + E - 1) / E : live * lanes;
+        T* const out = y + 16 * tile * y_stride + h0;
+#pragma unroll
+        for (int p0 = 0; p0 < 16 * OUTS / E; p0 += RG_WAVE) {
+            const int p = p0 + lane;
+            if (p >= pieces) continue;
+            const int r = run_on ? 0 : width == OUTS ? p / (OUTS / E) : (int)rg_divide(p, inv_last);
+            const int at = (p - r * lanes) * E, left = numbers - at;
+            const rg_u32x4a v = *(const rg_u32x4a*)(mine + r * pitch + at * sizeof(T));
+            T* const there = out + r * y_stride + at;
+            if (left >= E) *(typename RgPack<T, E>::type*)there = __builtin_bit_cast(typename RgPack<T, E>::type, v);
+            else {
+                const auto e = __builtin_bit_cast(typename RgPack<T, E>::type, v);
+#pragma unroll
+                for (int i = 0; i < E; ++i)
+                    if (i < left) there[i] = e[i];
+            }
+        }
+        __builtin_amdgcn_wave_barrier();
     }
 }
 
@@ -811,14 +942,36 @@ rg_status rg_mx4_matmul(rg_ctx* ctx, const void* rows, int64_t rows_stride, int6
     RG_HIP(ctx, hipSetDevice(ctx->device));
     hipStream_t s = (hipStream_t)stream;
     const int groups = (dim + kGroup - 1) / kGroup;
+    const int steps = (groups + 3) / 4;
     RG_FOR_TYPE(y_type, {
-        if (n <= 256) {
-            const dim3 grid(1, (unsigned)rg_div_up(out_dim, 16));
-            k_mx4_matmul<T, 1, 1><<<dim3((unsigned)rg_div_up(n, 64), grid.y), 256, 0, s>>>((const uint32_t*)rows, rows_stride, n, n_dev, (const uint32_t*)weight,
-                                                                               weight_stride, out_dim, groups, (T*)y, y_stride);
+        if (n > 256 && steps <= 8) {
+            const bool many = steps <= 2 && out_dim > 64;  // registers for 128 outputs
+            const int outs = many ? 128 : 64;
+            const int slices = out_dim > 2 * outs ? 4 : out_dim > outs ? 2 : 1;
+            const int slice_groups = (int)rg_div_up(out_dim, outs * slices);
+            // Two workgroups to a compute unit, four where registers hold up to 64 outputs of up to 384 numbers (1.5 M rows of 100 numbers times 47
+            // outputs of f16: 58 / 50 / 59 us with 2 / 4 / 8; 794 k of 256 times 256 of bf16: 102 / 115 / 141), and as many whole turns of
+            // the compute units as leave three tiles to a wavefront that has fetched the weight (100 k of 602 times 41: 15 us, 20 with one more).
+            const int64_t tiles = rg_div_up(rg_div_up(n, 16), kKeptWaves / slices);
+            const int64_t turns = rg_min64(out_dim <= 64 && steps <= 3 ? 4 : 2, rg_max64(1, tiles / (3 * ctx->num_cus)));
+            const int64_t row_groups = rg_min64(tiles, rg_max64(1, turns * ctx->num_cus / slice_groups));
+            const unsigned grid = (unsigned)(row_groups * slice_groups);
+            const int last = out_dim % outs, last_bytes = last * (int)sizeof(T);
+            const int run_on = out_dim <= outs && y_stride == out_dim && last_bytes % 16 != 0;
+            const auto kernel = steps == 1 ? (many ? k_mx4_matmul_kept<T, 1, 8> : k_mx4_matmul_kept<T, 1, 4>)
+                                : steps == 2 ? (many ? k_mx4_matmul_kept<T, 2, 8> : k_mx4_matmul_kept<T, 2, 4>)
+                                : steps == 3 ? k_mx4_matmul_kept<T, 3, 4> : steps == 4 ? k_mx4_matmul_kept<T, 4, 4>
+                                : steps == 5 ? k_mx4_matmul_kept<T, 5, 4> : k_mx4_matmul_kept<T, 8, 4>;
+            kernel<<<grid, kKeptThreads, 0, s>>>((const uint32_t*)rows, rows_stride, n, n_dev, (const uint32_t*)weight, weight_stride, out_dim, groups,
+                                                 (T*)y, y_stride, slices, slice_groups, run_on, rg_inverse((uint32_t)rg_div_up(last_bytes, 16)));
+        } else if (n <= 256) {
+            const dim3 grid((unsigned)rg_div_up(n, 64), (unsigned)rg_div_up(out_dim, 16));
+            k_mx4_matmul<T, 1, 1><<<grid, 256, 0, s>>>((const uint32_t*)rows, rows_stride, n, n_dev, (const uint32_t*)weight, weight_stride, out_dim,
+                                                       groups, (T*)y, y_stride);
         } else {
-            k_mx4_matmul<T, 2, 4><<<(unsigned)rg_min64(rg_div_up(n, 128), 1 << 20), 256, 0, s>>>((const uint32_t*)rows, rows_stride, n, n_dev, (const uint32_t*)weight,
-                                                                         weight_stride, out_dim, groups, (T*)y, y_stride);
+            k_mx4_matmul<T, 2, 4><<<(unsigned)rg_min64(rg_div_up(n, 128), 1 << 20), 256, 0, s>>>((const uint32_t*)rows, rows_stride, n, n_dev,
+                                                                                                 (const uint32_t*)weight, weight_stride, out_dim,
+                                                                                                 groups, (T*)y, y_stride);
         }
     });
     RG_LAUNCH_CHECK(ctx, "k_mx4_matmul");

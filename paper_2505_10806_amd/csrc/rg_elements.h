@@ -75,7 +75,7 @@ __device__ __forceinline__ int rg_xcd_block(int block, int grid) {
     return xcd * per + min(xcd, more) + (block >> 3);
 }
 
-// i / d for i < 2^16 and d < 2^14; m = rg_inverse(d).
+// i / d for i < 2^17 and d <= 2^14; m = rg_inverse(d).
 static inline uint32_t rg_inverse(uint32_t d) { return d <= 1 ? 0 : (uint32_t)(((1ull << 32) + d - 1) / d); }
 __device__ __forceinline__ uint32_t rg_divide(uint32_t i, uint32_t m) { return m ? __umulhi(i, m) : i; }
 

@@ -20,80 +20,116 @@ constexpr uint32_t kScaleNan = 255;
 __device__ __forceinline__ float scale_bits(uint32_t s) { return __uint_as_float(s << 23); }
 
 // ---------------------------------------------------------------- numbers to packed rows
-// 16 lanes take 128 numbers of a row (four groups), 8 each: the largest magnitude of a group, as an integer (so that NaN and
-// infinities are the largest of all), goes round its four lanes; the numbers times 2^(127 - s), which is exact or far below the
-// smallest magnitude, are rounded by the conversion instruction.
+// A lane takes 16 bytes of a row (4 numbers of 32 bits, 8 of 16), so that a wavefront's loads and stores are one run of bytes; U pieces a thread
+// are on their way together.  The largest magnitude of a group, as an integer (so that NaN and infinities are the largest of all), goes round its 8 or
+// 4 lanes; the numbers times 2^(127 - s), which is exact or far below the smallest magnitude, are rounded by the conversion instruction.
+constexpr int kPiecesAhead = 4;
+
+template <int CTRL>
+__device__ __forceinline__ uint32_t max_with(uint32_t x) { return max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, false)); }
+
 template <typename T>
 __global__ void __launch_bounds__(256) k_mx4_quantize(const T* __restrict__ x, int64_t x_stride, int64_t n, const int32_t* __restrict__ n_dev,
-                                                      int dim, uint32_t* __restrict__ packed, int64_t packed_stride, int quads, uint32_t inv_quads,
+                                                      int dim, uint32_t* __restrict__ packed, int64_t packed_stride, int pieces, uint32_t inv_pieces,
                                                       int rows_per_block) {
+    constexpr int V = 16 / sizeof(T), U = kPiecesAhead;
     const int64_t n_act = rg_rows(n, n_dev);
     const int64_t row0 = (int64_t)blockIdx.x * rows_per_block;
     if (row0 >= n_act) return;
-    const int items = (int)rg_least(rows_per_block, n_act - row0) * quads;
+    const int items = (int)rg_least(rows_per_block, n_act - row0) * pieces;      // a multiple of a group's lanes: groups are in one wavefront
     const int groups = (dim + kGroup - 1) / kGroup;
-    const int sub = threadIdx.x & 15;
-    for (int it = threadIdx.x >> 4; it < items; it += 16) {
-        const int r = (int)rg_divide((uint32_t)it, inv_quads);
-        const int quad = it - r * quads;
-        const int col = quad * 128 + sub * 8;
-        float v[8];
-        rg_load_head<8>(x + (row0 + r) * x_stride + col, dim - col, v);
-        uint32_t top = 0;
+    for (int it0 = threadIdx.x; it0 < items; it0 += 256 * U) {
+        float v[U][V];
+        int r[U], piece[U];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[i]) & 0x7FFFFFFFu);
-        top = max(top, (uint32_t)__shfl_xor((int)top, 1, RG_WAVE));
-        top = max(top, (uint32_t)__shfl_xor((int)top, 2, RG_WAVE));
-        const uint32_t e = top >> 23;
-        const bool good = e < 255;
-        const uint32_t s = good ? (e > 2 ? e - 2 : 0) : kScaleNan;
-        const float f = __uint_as_float((254u - s) << 23);
-        uint32_t word = 0;
-        word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, v[0] * f, v[1] * f, 1.0f, 0);
-        word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, v[2] * f, v[3] * f, 1.0f, 1);
-        word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, v[4] * f, v[5] * f, 1.0f, 2);
-        word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, v[6] * f, v[7] * f, 1.0f, 3);
-        if (!good) word = 0;
-        uint32_t* row = packed + (row0 + r) * packed_stride;
-        const int group = quad * 4 + (sub >> 2);
-        if (group < groups) row[quad * 16 + sub] = word;
-        if ((sub & 3) == 0) ((uint8_t*)(row + 4 * groups))[group] = group < groups ? (uint8_t)s : 0;
+        for (int u = 0; u < U; ++u) {
+            const int it = it0 + 256 * u;
+            r[u] = (int)rg_divide((uint32_t)it, inv_pieces);
+            piece[u] = it - r[u] * pieces;
+            if (it < items) rg_load_head<V>(x + (row0 + r[u]) * x_stride + piece[u] * V, dim - piece[u] * V, v[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (it0 + 256 * u >= items) break;
+            uint32_t top = 0;
+#pragma unroll
+            for (int i = 0; i < V; ++i) top = max(top, __float_as_uint(v[u][i]) & 0x7FFFFFFFu);
+            top = max_with<0xB1>(top);                     // lanes 1, 0, 3, 2 of four; 2, 3, 0, 1; of eight the other four
+            top = max_with<0x4E>(top);
+            if (V == 4) top = max_with<0x141>(top);
+            const uint32_t e = top >> 23;
+            const bool good = e < 255;
+            const uint32_t s = good ? (e > 2 ? e - 2 : 0) : kScaleNan;
+            const float f = __uint_as_float((254u - s) << 23);
+            uint32_t word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0, v[u][0] * f, v[u][1] * f, 1.0f, 0);
+            word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, v[u][2] * f, v[u][3] * f, 1.0f, 1);
+            if constexpr (V == 8) {
+                word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, v[u][4] * f, v[u][5] * f, 1.0f, 2);
+                word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, v[u][6] * f, v[u][7] * f, 1.0f, 3);
+            }
+            if (!good) word = 0;
+            uint32_t* row = packed + (row0 + r[u]) * packed_stride;
+            if constexpr (V == 8) row[piece[u]] = word;
+            else ((uint16_t*)row)[piece[u]] = (uint16_t)word;
+            constexpr int LANES = kGroup / V;
+            if (piece[u] % LANES == 0) {
+                const int group = piece[u] / LANES;
+                uint8_t* scales = (uint8_t*)(row + 4 * groups);
+                scales[group] = (uint8_t)s;
+                if (group == groups - 1)
+                    for (int i = groups; i & 3; ++i) scales[i] = 0;
+            }
+        }
     }
 }
 
 // ---------------------------------------------------------------- packed rows to numbers
-// A lane takes one word of codes, 8 numbers of one group.
+// A lane makes 16 bytes of a row.
 template <typename T>
 __global__ void __launch_bounds__(256) k_mx4_dequantize(const uint32_t* __restrict__ packed, int64_t packed_stride, int64_t n,
-                                                        const int32_t* __restrict__ n_dev, int dim, T* __restrict__ x, int64_t x_stride, int words,
-                                                        uint32_t inv_words, int rows_per_block) {
+                                                        const int32_t* __restrict__ n_dev, int dim, T* __restrict__ x, int64_t x_stride, int pieces,
+                                                        uint32_t inv_pieces, int rows_per_block) {
+    constexpr int V = 16 / sizeof(T), U = kPiecesAhead;
+    typedef float v2f __attribute__((ext_vector_type(2)));
     const int64_t n_act = rg_rows(n, n_dev);
     const int64_t row0 = (int64_t)blockIdx.x * rows_per_block;
     if (row0 >= n_act) return;
-    const int items = (int)rg_least(rows_per_block, n_act - row0) * words;
+    const int items = (int)rg_least(rows_per_block, n_act - row0) * pieces;
     const int groups = (dim + kGroup - 1) / kGroup;
-    for (int it = threadIdx.x; it < items; it += 256) {
-        const int r = (int)rg_divide((uint32_t)it, inv_words);
-        const int w = it - r * words;
-        const uint32_t* row = packed + (row0 + r) * packed_stride;
-        const uint32_t code = row[w];
-        const float scale = scale_bits(((const uint8_t*)(row + 4 * groups))[w >> 2]);
-        float v[8];
-        typedef float v2f __attribute__((ext_vector_type(2)));
-        const v2f a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, scale, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, scale, 1);
-        const v2f c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, scale, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, scale, 3);
-        v[0] = a.x; v[1] = a.y; v[2] = b.x; v[3] = b.y; v[4] = c.x; v[5] = c.y; v[6] = d.x; v[7] = d.y;
-        rg_store_live<8>(x + (row0 + r) * x_stride + w * 8, dim - w * 8, v);
+    for (int it0 = threadIdx.x; it0 < items; it0 += 256 * U) {
+        uint32_t code[U], scale[U];
+        int r[U], piece[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int it = min(it0 + 256 * u, items - 1);
+            r[u] = (int)rg_divide((uint32_t)it, inv_pieces);
+            piece[u] = it - r[u] * pieces;
+            const uint32_t* row = packed + (row0 + r[u]) * packed_stride;
+            code[u] = V == 8 ? row[piece[u]] : ((const uint16_t*)row)[piece[u]];
+            scale[u] = ((const uint8_t*)(row + 4 * groups))[piece[u] / (kGroup / V)];
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (it0 + 256 * u >= items) break;
+            const float s = scale_bits(scale[u]);
+            float v[V];
+            const v2f a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[u], s, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[u], s, 1);
+            v[0] = a.x; v[1] = a.y; v[2] = b.x; v[3] = b.y;
+            if constexpr (V == 8) {
+                const v2f c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[u], s, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[u], s, 3);
+                v[4] = c.x; v[5] = c.y; v[6] = d.x; v[7] = d.y;
+            }
+            rg_store_live<V>(x + (row0 + r[u]) * x_stride + piece[u] * V, dim - piece[u] * V, v);
+        }
     }
 }
 
-// Rows that a workgroup takes when each is `per_row` units of work and it does `per_step` units at a time: several steps where
-// there are rows enough for all compute units.
-int rows_per_group(const rg_ctx* ctx, int64_t n, int per_row, int per_step, int steps) {
-    const int64_t total = n * per_row;
-    int64_t units = total >= (int64_t)ctx->num_cus * 8 * per_step * steps ? (int64_t)per_step * steps : per_step;
-    units = rg_max64(units, total >> 22);                  // (a launch has less than 2^32 threads)
-    return (int)rg_max64(1, units / per_row);
+// Rows to a workgroup of 256 threads when each is `pieces` pieces: kPiecesAhead to a thread where there are rows enough for all compute units.
+int rows_per_group(const rg_ctx* ctx, int64_t n, int pieces) {
+    const int64_t total = n * pieces, full = 256 * kPiecesAhead;
+    int64_t items = total >= (int64_t)ctx->num_cus * 8 * full ? full : 256;
+    items = rg_max64(items, total >> 22);                  // (a launch has less than 2^32 threads)
+    return (int)rg_max64(1, items / pieces);
 }
 
 // ---------------------------------------------------------------- y = rows . weight^T
@@ -899,10 +935,10 @@ rg_status rg_mx4_quantize(rg_ctx* ctx, const void* x, rg_dtype x_type, int64_t x
     RG_REQUIRE(ctx, aligned(x, rg_type_bytes(x_type)) && aligned(packed, 4), "rg_mx4_quantize: pointer not aligned to its numbers");
     RG_HIP(ctx, hipSetDevice(ctx->device));
     hipStream_t s = (hipStream_t)stream;
-    const int quads = (dim + 127) / 128;
-    const int rows = rows_per_group(ctx, n, quads, 16, 4);
+    const int pieces = (int)rg_div_up(dim, kGroup) * (kGroup * rg_type_bytes(x_type) / 16);
+    const int rows = rows_per_group(ctx, n, pieces);
     RG_FOR_TYPE(x_type, k_mx4_quantize<T><<<(unsigned)rg_div_up(n, rows), 256, 0, s>>>((const T*)x, x_stride, n, n_dev, dim, (uint32_t*)packed,
-                                                                                  packed_stride, quads, rg_inverse(quads), rows));
+                                                                                  packed_stride, pieces, rg_inverse(pieces), rows));
     RG_LAUNCH_CHECK(ctx, "k_mx4_quantize");
     return RG_OK;
 }
@@ -919,10 +955,10 @@ rg_status rg_mx4_dequantize(rg_ctx* ctx, const void* packed, int64_t packed_stri
     RG_REQUIRE(ctx, aligned(x, rg_type_bytes(x_type)) && aligned(packed, 4), "rg_mx4_dequantize: pointer not aligned to its numbers");
     RG_HIP(ctx, hipSetDevice(ctx->device));
     hipStream_t s = (hipStream_t)stream;
-    const int words = (dim + 7) / 8;
-    const int rows = rows_per_group(ctx, n, words, 256, 4);
+    const int pieces = (int)rg_div_up((int64_t)dim * rg_type_bytes(x_type), 16);
+    const int rows = rows_per_group(ctx, n, pieces);
     RG_FOR_TYPE(x_type, k_mx4_dequantize<T><<<(unsigned)rg_div_up(n, rows), 256, 0, s>>>((const uint32_t*)packed, packed_stride, n, n_dev, dim,
-                                                                                    (T*)x, x_stride, words, rg_inverse(words), rows));
+                                                                                    (T*)x, x_stride, pieces, rg_inverse(pieces), rows));
     RG_LAUNCH_CHECK(ctx, "k_mx4_dequantize");
     return RG_OK;
 }

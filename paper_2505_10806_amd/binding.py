@@ -164,25 +164,35 @@ def _rows(t, n, width, dtype=None, device_type="cuda", name="tensor"):
     """(address, row stride) of a tensor of at least n rows with at least `width` numbers side by side (None -> NULL)."""
     if t is None:
         return None, 0
+    shape, strides = t.shape, t.stride()                  # (each asked for once: they cost as much as the rest of a call)
+    if len(shape) == 2:
+        have, wide = shape
+        stride, step = strides
+        if (have >= n and wide >= width and (step == 1 or wide <= 1) and (dtype is None or t.dtype is dtype)
+                and (t.is_cuda or (device_type == "mapped" and t.is_pinned()))):
+            # (the stride of a single row says nothing)
+            return t.data_ptr(), stride if have > 1 else max(stride, wide)
     if dtype is not None and t.dtype != dtype:
         raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
     if device_type == "cuda" and not t.is_cuda:
         raise ValueError(f"{name}: expected a cuda tensor, got {t.device}")
     if device_type == "mapped" and not t.is_cuda and not t.is_pinned():
         raise ValueError(f"{name}: host tensor must be pinned to be read from the device")
-    if t.dim() != 2 or t.shape[0] < n or t.shape[1] < width or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise ValueError(f"{name}: expected rows of at least {width} numbers side by side, {n} of them; got shape {tuple(t.shape)}, "
-                         f"strides {t.stride()}")
-    # (the stride of a single row says nothing)
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+    raise ValueError(f"{name}: expected rows of at least {width} numbers side by side, {n} of them; got shape {tuple(shape)}, "
+                     f"strides {tuple(strides)}")
 
 
 def _numbers(t, n, dtype, name):
     """Address of at least n numbers one behind the other (None -> NULL)."""
-    p = _ptr(t, dtype, "cuda", name)
-    if t is not None and t.numel() < n:
+    if t is None:
+        return None
+    if t.numel() < n:
         raise ValueError(f"{name}: {t.numel()} numbers, {n} required")
-    return p
+    return _ptr(t, dtype, "cuda", name)
+
+
+def _count(n_dev):
+    return None if n_dev is None else _ptr(n_dev, torch.int32, "cuda", "n_dev")
 
 
 def _type(t, name):
@@ -424,14 +434,14 @@ class Context:
         be pinned host memory."""
         px, sx = _rows(x, n, dim, None, "mapped", "x")
         pp, sp = _rows(packed, n, mx4_row_words(dim), torch.float32, "mapped", "packed")
-        self._check(_lib.rg_mx4_quantize(self._h, px, _type(x, "x"), sx, int(n), _ptr(n_dev, torch.int32, "cuda", "n_dev"), int(dim), pp, sp,
+        self._check(_lib.rg_mx4_quantize(self._h, px, _type(x, "x"), sx, int(n), _count(n_dev), int(dim), pp, sp,
                                          _stream_handle(stream)))
         return packed
 
     def mx4_dequantize(self, packed, n, dim, x, n_dev=None, stream=None):
         px, sx = _rows(x, n, dim, None, "mapped", "x")
         pp, sp = _rows(packed, n, mx4_row_words(dim), torch.float32, "mapped", "packed")
-        self._check(_lib.rg_mx4_dequantize(self._h, pp, sp, int(n), _ptr(n_dev, torch.int32, "cuda", "n_dev"), int(dim), px, _type(x, "x"), sx,
+        self._check(_lib.rg_mx4_dequantize(self._h, pp, sp, int(n), _count(n_dev), int(dim), px, _type(x, "x"), sx,
                                            _stream_handle(stream)))
         return x
 
@@ -441,7 +451,7 @@ class Context:
         pr, sr = _rows(rows, n, words, torch.float32, "cuda", "rows")
         pw, sw = _rows(weight, out_dim, words, torch.float32, "cuda", "weight")
         py, sy = _rows(y, n, out_dim, None, "cuda", "y")
-        self._check(_lib.rg_mx4_matmul(self._h, pr, sr, int(n), _ptr(n_dev, torch.int32, "cuda", "n_dev"), pw, sw, int(out_dim), int(dim), py,
+        self._check(_lib.rg_mx4_matmul(self._h, pr, sr, int(n), _count(n_dev), pw, sw, int(out_dim), int(dim), py,
                                        _type(y, "y"), sy, _stream_handle(stream)))
         return y
 
@@ -450,7 +460,7 @@ class Context:
         pd, sd = _rows(dy, n, out_dim, None, "cuda", "dy")
         pr, sr = _rows(rows, n, mx4_row_words(dim), torch.float32, "cuda", "rows")
         pg, sg = _rows(grad, out_dim, dim, torch.float32, "cuda", "grad")
-        self._check(_lib.rg_mx4_matmul_grad(self._h, pd, _type(dy, "dy"), sd, pr, sr, int(n), _ptr(n_dev, torch.int32, "cuda", "n_dev"),
+        self._check(_lib.rg_mx4_matmul_grad(self._h, pd, _type(dy, "dy"), sd, pr, sr, int(n), _count(n_dev),
                                             int(out_dim), int(dim), pg, sg, _stream_handle(stream)))
         return grad
 
@@ -459,7 +469,7 @@ class Context:
         px, sx = _rows(x, n, dim, None, "cuda", "x")
         py, sy = _rows(y, n, dim, x.dtype, "cuda", "y")
         f32 = torch.float32
-        self._check(_lib.rg_layer_norm(self._h, px, _type(x, "x"), sx, int(n), _ptr(n_dev, torch.int32, "cuda", "n_dev"), int(dim),
+        self._check(_lib.rg_layer_norm(self._h, px, _type(x, "x"), sx, int(n), _count(n_dev), int(dim),
                                        _numbers(gamma, dim, f32, "gamma"), _numbers(beta, dim, f32, "beta"), float(eps), py, sy,
                                        _numbers(mean, n, f32, "mean"), _numbers(rstd, n, f32, "rstd"), _stream_handle(stream)))
         return y
@@ -469,7 +479,7 @@ class Context:
         px, sx = _rows(x, n, dim, None, "cuda", "x")
         pg, sg = _rows(dx, n, dim, x.dtype, "cuda", "dx")
         f32 = torch.float32
-        self._check(_lib.rg_layer_norm_grad(self._h, pd, sd, px, sx, _type(x, "x"), int(n), _ptr(n_dev, torch.int32, "cuda", "n_dev"), int(dim),
+        self._check(_lib.rg_layer_norm_grad(self._h, pd, sd, px, sx, _type(x, "x"), int(n), _count(n_dev), int(dim),
                                             _numbers(gamma, dim, f32, "gamma"), _numbers(mean, n, f32, "mean"),
                                             _numbers(rstd, n, f32, "rstd"), pg, sg, _numbers(dgamma, dim, f32, "dgamma"),
                                             _numbers(dbeta, dim, f32, "dbeta"), _stream_handle(stream)))
@@ -514,10 +524,10 @@ def blocks_bounds(num_nodes, num_edges, num_seeds, fanouts):
 
 def mx4_row_words(dim):
     """Words of 32 bits in a packed row of dim numbers: the `dim` that the gather and the cache see."""
-    words = _lib.rg_mx4_row_words(int(dim))
-    if words == 0:
+    if not 1 <= dim <= RG_MX4_MAX_DIM:
         raise ValueError(f"mx4_row_words: dim = {dim} not in [1, {RG_MX4_MAX_DIM}]")
-    return words
+    groups = (int(dim) + 31) >> 5                          # (rg_mx4_row_words, without a foreign call)
+    return 4 * groups + ((groups + 3) >> 2)
 
 
 def mx4_rows(n, dim, device, pin_memory=False):

@@ -7,89 +7,97 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kMostTensors = 64;       // that a launch's arguments describe
-constexpr int kChunk = 8192;           // numbers a workgroup takes at a time
 constexpr int kMostParts = 2048;       // workgroups of a launch
 
 struct ClipList {
     const void* in[kMostTensors];
     void* out[kMostTensors];
     int64_t size[kMostTensors];
-    int64_t first[kMostTensors + 1];   // chunks in front of each tensor
-    uint8_t type[kMostTensors];
-    int count;
+    int32_t first[kMostTensors];       // chunks in front of each tensor (of those that are not there: as many as there can be)
+    int32_t type[kMostTensors];        // (words: scalar loads drop the last two bits of each part of an address, and the compiler shares parts)
+    int32_t chunks;
+    int32_t log2_chunk;                // numbers of a chunk
 };
 
-// The tensor that chunk `at` belongs to (the last with first <= at: empty ones own none).
-__device__ __forceinline__ int tensor_of(const ClipList& list, int64_t at) {
-    int lo = 0, hi = list.count;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (list.first[mid] <= at) lo = mid;
-        else hi = mid;
-    }
-    return lo;
+// The tensor that chunk `at` belongs to: every lane looks at one.
+__device__ __forceinline__ int tensor_of(const ClipList& list, int at) {
+    static_assert(kMostTensors == RG_WAVE, "a lane for a tensor");
+    return __popcll(__ballot(list.first[rg_lane()] <= at)) - 1;
 }
 
-// f(numbers, place) on every 16 bytes of the chunk, f(number, place) one by one at its end.
+// f(numbers, place, how many) on every 16 bytes of the chunk that begins at p.
 template <typename T, typename F>
-__device__ __forceinline__ void for_chunk(const T* p, int64_t left, F f) {
+__device__ __forceinline__ void for_chunk(const T* p, int64_t left, int log2_chunk, F f) {
     constexpr int V = 16 / (int)sizeof(T);
-    const int n = (int)rg_least(left, kChunk);
-#pragma unroll
-    for (int i = 0; i < kChunk / (kThreads * V); ++i) {
-        const int at = (i * kThreads + (int)threadIdx.x) * V;
+    const int n = (int)rg_least(left, 1 << log2_chunk);
+#pragma unroll 4
+    for (int at = (int)threadIdx.x * V; at < n; at += kThreads * V) {
         float v[V];
-        if (at < n) {
-            rg_load_head<V>(p + at, n - at, v);
-            f(v, at, n - at);
-        }
+        rg_load_head<V>(p + at, n - at, v);
+        f(v, at, n - at);
     }
 }
 
+template <int NW>
 __device__ __forceinline__ double block_sum(double x, double* smem) {
 #pragma unroll
     for (int off = RG_WAVE / 2; off > 0; off >>= 1) x += __shfl_xor(x, off, RG_WAVE);
     __syncthreads();
     if (rg_lane() == 0) smem[threadIdx.x >> 6] = x;
     __syncthreads();
-    return (smem[0] + smem[1]) + (smem[2] + smem[3]);
+    x = 0.0;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) x += smem[w];
+    return x;
+}
+
+// The factor that takes a gradient of this norm to max_norm, in two: a norm beyond the 32-bit range would leave one of few bits.
+struct Scale {
+    float coarse, fine;
+    bool clipped;
+};
+__device__ __forceinline__ Scale scale_of(double norm, float max_norm) {
+    Scale s;
+    s.clipped = norm > (double)max_norm && norm <= 1.7976931348623157e308;
+    const double scale = s.clipped ? (double)max_norm / norm : 1.0;
+    s.coarse = scale < 0x1p-64 ? 0x1p-64f : 1.0f;
+    s.fine = (float)(scale / (double)s.coarse);
+    return s;
 }
 
 // parts[workgroup] = the sum of the squares of its chunks.
 __global__ void __launch_bounds__(kThreads) k_squares(ClipList list, double* __restrict__ parts) {
     __shared__ double smem[kThreads / RG_WAVE];
     double sum = 0.0;
-    for (int64_t at = blockIdx.x; at < list.first[list.count]; at += gridDim.x) {
+    for (int at = blockIdx.x; at < list.chunks; at += gridDim.x) {
         const int t = tensor_of(list, at);
-        const int64_t begin = (at - list.first[t]) * kChunk;
-        RG_FOR_TYPE(list.type[t], for_chunk((const T*)list.in[t] + begin, list.size[t] - begin, [&](const auto& v, int, int) {
+        const int64_t begin = (int64_t)(at - list.first[t]) << list.log2_chunk;
+        RG_FOR_TYPE((rg_dtype)list.type[t], for_chunk((const T*)list.in[t] + begin, list.size[t] - begin, list.log2_chunk, [&](const auto& v, int, int) {
             for (float x : v) sum += (double)x * (double)x;
         }));
     }
-    sum = block_sum(sum, smem);
+    sum = block_sum<kThreads / RG_WAVE>(sum, smem);
     if (threadIdx.x == 0) parts[blockIdx.x] = sum;
 }
 
-// Every workgroup adds up the parts (in one order) and scales its chunks.
+// Every workgroup adds up the parts (in one order) and scales its chunks, the last ones first: the device's last level of cache still holds what
+// was read last.
 __global__ void __launch_bounds__(kThreads) k_clip(ClipList list, const double* __restrict__ parts, int num_parts, float max_norm,
                                                    float* __restrict__ norm_out) {
     __shared__ double smem[kThreads / RG_WAVE];
     double sum = 0.0;
     for (int i = threadIdx.x; i < num_parts; i += kThreads) sum += parts[i];
-    const double norm = sqrt(block_sum(sum, smem));
+    const double norm = sqrt(block_sum<kThreads / RG_WAVE>(sum, smem));
     if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = (float)norm;
-    const bool clipped = norm > (double)max_norm && norm <= 1.7976931348623157e308;
-    // in two factors, so that a norm beyond the 32-bit range does not leave a scale of few bits
-    const double scale = clipped ? (double)max_norm / norm : 1.0;
-    const float coarse = scale < 0x1p-64 ? 0x1p-64f : 1.0f, fine = (float)(scale / (double)coarse);
-    for (int64_t at = blockIdx.x; at < list.first[list.count]; at += gridDim.x) {
+    const Scale scale = scale_of(norm, max_norm);
+    for (int at = list.chunks - 1 - (int)blockIdx.x; at >= 0; at -= gridDim.x) {
         const int t = tensor_of(list, at);
-        if (!clipped && list.in[t] == list.out[t]) continue;
-        const int64_t begin = (at - list.first[t]) * kChunk;
-        RG_FOR_TYPE(list.type[t], {
+        if (!scale.clipped && list.in[t] == list.out[t]) continue;
+        const int64_t begin = (int64_t)(at - list.first[t]) << list.log2_chunk;
+        RG_FOR_TYPE((rg_dtype)list.type[t], {
             T* out = (T*)list.out[t] + begin;
-            for_chunk((const T*)list.in[t] + begin, list.size[t] - begin, [&](auto& v, int place, int live) {
-                for (float& x : v) x = x * coarse * fine;
+            for_chunk((const T*)list.in[t] + begin, list.size[t] - begin, list.log2_chunk, [&](auto& v, int place, int live) {
+                for (float& x : v) x = x * scale.coarse * scale.fine;
                 rg_store_live<16 / (int)sizeof(T)>(out + place, live, v);
             });
         });
@@ -116,37 +124,46 @@ extern "C" rg_status rg_clip_grad_norm(rg_ctx* ctx, const rg_tensor* tensors, in
     }
     RG_HIP(ctx, hipSetDevice(ctx->device));
     hipStream_t s = (hipStream_t)stream;
-    const int64_t lists = rg_max64(1, rg_div_up(count, kMostTensors));
-    rg_status st = rg_scratch(ctx, ctx->clip_parts, (size_t)(lists * kMostParts) * sizeof(double), s, "rg_clip_grad_norm");
-    if (st != RG_OK) return st;
-    double* parts = (double*)ctx->clip_parts.p;
-    ClipList list;
-    const auto fill = [&](int64_t which) {
-        list.count = 0;
-        list.first[0] = 0;
-        for (int64_t i = which * kMostTensors; i < rg_min64(count, (which + 1) * kMostTensors); ++i) {
-            const rg_tensor& t = tensors[i];
+    // the tensors that hold something, kMostTensors to a launch, in chunks of 2^log2_chunk numbers
+    const auto fill = [&](ClipList& list, int32_t& next, int log2_chunk) {
+        int64_t chunks = 0;
+        int at = 0;
+        for (; next < count && at < kMostTensors; ++next) {
+            const rg_tensor& t = tensors[next];
             if (t.size == 0) continue;
-            const int at = list.count++;
             list.in[at] = t.in;
             list.out[at] = t.out;
             list.size[at] = t.size;
-            list.type[at] = (uint8_t)t.type;
-            list.first[at + 1] = list.first[at] + rg_div_up(t.size, kChunk);
+            list.type[at] = (int32_t)t.type;
+            list.first[at++] = (int32_t)chunks;
+            chunks += (t.size + (1ll << log2_chunk) - 1) >> log2_chunk;
         }
-        return (unsigned)rg_max64(1, rg_min64(list.first[list.count], kMostParts));
+        for (; at < kMostTensors; ++at) list.first[at] = INT32_MAX;
+        list.chunks = (int32_t)chunks;
+        list.log2_chunk = log2_chunk;
     };
+    ClipList list;
+    int32_t next = 0;
+    // chunks small enough for all compute units, or large enough to be worth looking up
+    const int log2_chunk = numbers < (1 << 23) ? 11 : 13;
+    const int64_t lists = rg_max64(1, rg_div_up(count, kMostTensors));
+    const rg_status st = rg_scratch(ctx, ctx->clip_parts, (size_t)(lists * kMostParts) * sizeof(double), s, "rg_clip_grad_norm");
+    if (st != RG_OK) return st;
+    double* parts = (double*)ctx->clip_parts.p;
     int num_parts = 0;
-    for (int64_t w = 0; w < lists; ++w) {
-        const unsigned grid = fill(w);
-        k_squares<<<grid, kThreads, 0, s>>>(list, parts + num_parts);
+    const auto grid_of = [](const ClipList& l) { return (unsigned)rg_max64(1, rg_min64(l.chunks, kMostParts)); };
+    for (next = 0; next < count;) {
+        fill(list, next, log2_chunk);
+        k_squares<<<grid_of(list), kThreads, 0, s>>>(list, parts + num_parts);
         RG_LAUNCH_CHECK(ctx, "k_squares");
-        num_parts += (int)grid;
+        num_parts += (int)grid_of(list);
     }
-    for (int64_t w = 0; w < lists; ++w) {
-        const unsigned grid = lists > 1 ? fill(w) : (unsigned)rg_max64(1, rg_min64(list.first[list.count], kMostParts));
-        k_clip<<<grid, kThreads, 0, s>>>(list, parts, num_parts, max_norm, w == 0 ? norm : nullptr);
+    const bool single = lists == 1;
+    for (next = single ? count : 0; single || next < count;) {
+        if (!single) fill(list, next, log2_chunk);
+        k_clip<<<grid_of(list), kThreads, 0, s>>>(list, parts, num_parts, max_norm, next == count ? norm : nullptr);
         RG_LAUNCH_CHECK(ctx, "k_clip");
+        if (single) break;
     }
     return RG_OK;
 }

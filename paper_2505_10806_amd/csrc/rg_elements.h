@@ -39,6 +39,16 @@ __device__ __forceinline__ void rg_load_head(const T* p, int live, float (&v)[N]
     for (int i = 0; i < N; ++i) v[i] = i < live ? (float)p[i] : 0.0f;
 }
 
+// The first `live` numbers of N from p as they are, the others 0.
+template <int N, typename T>
+__device__ __forceinline__ typename RgPack<T, N>::type rg_load_raw(const T* p, int live) {
+    if (live >= N) return *(const typename RgPack<T, N>::type*)p;
+    typename RgPack<T, N>::type a;
+#pragma unroll
+    for (int i = 0; i < N; ++i) a[i] = i < live ? p[i] : (T)0.0f;
+    return a;
+}
+
 template <int N, typename T>
 __device__ __forceinline__ void rg_store(T* p, const float (&v)[N]) {
     constexpr int H = sizeof(T) * N <= 16 ? N : 16 / (int)sizeof(T);

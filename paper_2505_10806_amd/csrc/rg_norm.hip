@@ -8,9 +8,32 @@ template <typename T> struct Chunk { static constexpr int V = 16 / (int)sizeof(T
 // Numbers of each of its rows that a lane holds at most: rows of up to 64 times as many stay in registers, longer ones are read again.
 constexpr int kHeld = 32, kHeldGrad = 16;
 
+// What another lane of the row of 16 holds.
+template <int CTRL>
+__device__ __forceinline__ float lane_of(float x) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xF, 0xF, false));
+}
+
+// Sums over groups of 2^log2L lanes, the same in each of them.  Between vector registers alone: by way of LDS a step of such a sum takes 120 cycles.
+// After a step the lanes of half a group hold the same, so that mirrored lanes do for the other half.
+template <int N>
+__device__ __forceinline__ void group_sums(float (&x)[N], int log2L) {
+#define RG_STEP(LOG2, ...) if (log2L >= LOG2) { _Pragma("unroll") for (int i = 0; i < N; ++i) { __VA_ARGS__; } }
+    RG_STEP(1, x[i] += lane_of<0xB1>(x[i]))                // lanes 1, 0, 3, 2 of four
+    RG_STEP(2, x[i] += lane_of<0x4E>(x[i]))                // 2, 3, 0, 1
+    RG_STEP(3, x[i] += lane_of<0x141>(x[i]))               // 7, 6, .. 0 of eight
+    RG_STEP(4, x[i] += lane_of<0x140>(x[i]))               // 15, 14, .. 0 of sixteen
+    RG_STEP(5, const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x[i]), __float_as_uint(x[i]), false, false);
+            x[i] = __uint_as_float(r[0]) + __uint_as_float(r[1]))
+    RG_STEP(6, const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x[i]), __float_as_uint(x[i]), false, false);
+            x[i] = __uint_as_float(r[0]) + __uint_as_float(r[1]))
+#undef RG_STEP
+}
+
 __device__ __forceinline__ float group_sum(float x, int log2L) {
-    for (int off = 1 << log2L >> 1; off > 0; off >>= 1) x += __shfl_xor(x, off, RG_WAVE);
-    return x;
+    float v[1] = {x};
+    group_sums(v, log2L);
+    return v[0];
 }
 
 // Sum over a workgroup of NW wavefronts; smem holds NW floats.  Contains barriers.
@@ -66,7 +89,7 @@ __global__ void __launch_bounds__(256) k_layer_norm(const T* x, int64_t x_stride
 #pragma unroll
             for (int j = 0; j < V; ++j) {
                 v[i][j] -= m;
-                if (col + j < dim) square += v[i][j] * v[i][j];
+                if ((i + 1 < NC && NC <= 4) || col + j < dim) square += v[i][j] * v[i][j];
             }
         }
         const float s = 1.0f / sqrtf(group_sum(square, log2L) / (float)dim + eps);
@@ -153,39 +176,49 @@ __global__ void __launch_bounds__(kGradThreads) k_layer_norm_grad(const T* dy, i
 #pragma unroll
         for (int j = 0; j < V; ++j) by_gamma[i][j] = by_beta[i][j] = 0.0f;
     }
+    // the next row is on its way while this one is worked on
+    struct Row {
+        typename RgPack<T, V>::type x[NC], d[NC];
+        float mean, rstd;
+    };
+    const auto load = [&](Row& r, int64_t row) {
+        row = rg_least(row, n_act - 1);
+#pragma unroll
+        for (int i = 0; i < NC; ++i) {
+            const int col = (l + i * L) * V;
+            r.x[i] = rg_load_raw<V>(x + row * x_stride + col, dim - col);
+            r.d[i] = rg_load_raw<V>(dy + row * dy_stride + col, dim - col);
+        }
+        r.mean = mean[row];
+        r.rstd = rstd[row];
+    };
+    Row next;
+    if (wave * R < n_act) load(next, wave * R + (lane >> log2L));
     for (int64_t row0 = wave * R; row0 < n_act; row0 += waves * R) {
         const int64_t row = row0 + (lane >> log2L);
-        const bool live_row = row < n_act;
-        const int64_t at = live_row ? row : n_act - 1;
+        const Row r = next;
+        load(next, row + waves * R);
+        if (row >= n_act) continue;
         float h[NC][V], d[NC][V];
+        const float m = r.mean, s = r.rstd;
+        float sums[2] = {0.0f, 0.0f};                      // of g h and of g
 #pragma unroll
-        for (int i = 0; i < NC; ++i) {
-            const int col = (l + i * L) * V;
-            rg_load_head<V>(x + at * x_stride + col, dim - col, h[i]);
-            rg_load_head<V>(dy + at * dy_stride + col, live_row ? dim - col : 0, d[i]);
-        }
-        const float m = mean[at], s = rstd[at];
-        float along = 0.0f, all = 0.0f;
+        for (int i = 0; i < NC; ++i)
 #pragma unroll
-        for (int i = 0; i < NC; ++i) {
-            const int col = (l + i * L) * V;
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                const bool in = live_row && col + j < dim;
-                h[i][j] = in ? (h[i][j] - m) * s : 0.0f;
+            for (int j = 0; j < V; ++j) {                  // (behind the row's end dy was loaded as 0)
+                h[i][j] = ((float)r.x[i][j] - m) * s;
+                d[i][j] = (float)r.d[i][j];
                 if (SUMS) {
                     by_gamma[i][j] += d[i][j] * h[i][j];
                     by_beta[i][j] += d[i][j];
                 }
                 d[i][j] *= g[i][j];
-                along += d[i][j] * h[i][j];
-                all += d[i][j];
+                sums[0] += d[i][j] * h[i][j];
+                sums[1] += d[i][j];
             }
-        }
         if (!dx) continue;
-        along = group_sum(along, log2L) / (float)dim;
-        all = group_sum(all, log2L) / (float)dim;
-        if (!live_row) continue;
+        group_sums(sums, log2L);
+        const float along = sums[0] / (float)dim, all = sums[1] / (float)dim;
 #pragma unroll
         for (int i = 0; i < NC; ++i) {
             const int col = (l + i * L) * V;

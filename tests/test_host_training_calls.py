@@ -172,10 +172,10 @@ def test_calls_without_memory_fail_and_work_again():
     run(r'''
 held = rt.memory_held()
 rt.limit_memory(held)
-for call in (lambda: matmul_grad(n=2_000_000, out_dim=900, dy_stride=900), norm_grad, clip):
+for call in (lambda: matmul_grad(n=2_000_000, out_dim=900, dy_stride=900), norm_grad, lambda: clip(sizes=(100_000,))):
     assert call() == OOM and not kernels(), message()
 rt.limit_memory((1 << 64) - 1)
-for call in (lambda: matmul_grad(n=2_000_000, out_dim=900, dy_stride=900), norm_grad, clip):
+for call in (lambda: matmul_grad(n=2_000_000, out_dim=900, dy_stride=900), norm_grad, lambda: clip(sizes=(100_000,))):
     assert call() == OK
 ''')
 
@@ -197,3 +197,13 @@ for line in log("launch"):
     x, y, block, lds = (int(v) for v in at[1:5])
     assert 1 <= x < 1 << 31 and 1 <= y <= 65535 and x * block < 1 << 32 and lds <= 65536, line
 ''')
+
+
+def test_binding_counts_the_words_of_a_row_as_the_library_does():
+    from paper_2505_10806_amd import binding as B
+    for dim in list(range(1, 700)) + [1024, 65535, 65536]:
+        assert B.mx4_row_words(dim) == B._lib.rg_mx4_row_words(dim)
+    for dim in (0, -3, 65537):
+        assert B._lib.rg_mx4_row_words(dim) == 0
+        with pytest.raises(ValueError):
+            B.mx4_row_words(dim)

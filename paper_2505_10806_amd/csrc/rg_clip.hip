@@ -152,18 +152,18 @@ extern "C" rg_status rg_clip_grad_norm(rg_ctx* ctx, const rg_tensor* tensors, in
     double* parts = (double*)ctx->clip_parts.p;
     int num_parts = 0;
     const auto grid_of = [](const ClipList& l) { return (unsigned)rg_max64(1, rg_min64(l.chunks, kMostParts)); };
-    for (next = 0; next < count;) {
+    do {                                                   // (no tensor at all is a list of none)
         fill(list, next, log2_chunk);
         k_squares<<<grid_of(list), kThreads, 0, s>>>(list, parts + num_parts);
         RG_LAUNCH_CHECK(ctx, "k_squares");
         num_parts += (int)grid_of(list);
-    }
+    } while (next < count);
     const bool single = lists == 1;
-    for (next = single ? count : 0; single || next < count;) {
+    if (!single) next = 0;
+    do {
         if (!single) fill(list, next, log2_chunk);
         k_clip<<<grid_of(list), kThreads, 0, s>>>(list, parts, num_parts, max_norm, next == count ? norm : nullptr);
         RG_LAUNCH_CHECK(ctx, "k_clip");
-        if (single) break;
-    }
+    } while (next < count);
     return RG_OK;
 }

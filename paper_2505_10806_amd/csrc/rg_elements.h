@@ -13,40 +13,49 @@ template <int N> struct RgPack<_Float16, N> { typedef _Float16 type __attribute_
 typedef uint32_t rg_u32x4 __attribute__((ext_vector_type(4), aligned(4)));
 typedef uint32_t rg_u32x2 __attribute__((ext_vector_type(2), aligned(4)));
 
-// N numbers from p, in 32 bits.
-template <int N, typename T>
-__device__ __forceinline__ void rg_load(const T* p, float (&v)[N]) {
-    if constexpr (sizeof(T) * N <= 16) {
-        const typename RgPack<T, N>::type a = *(const typename RgPack<T, N>::type*)p;
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = (float)a[i];
-    } else {
-        constexpr int H = 16 / sizeof(T);
-#pragma unroll
-        for (int h = 0; h < N / H; ++h) {
-            const typename RgPack<T, H>::type a = ((const typename RgPack<T, H>::type*)p)[h];
-#pragma unroll
-            for (int i = 0; i < H; ++i) v[h * H + i] = (float)a[i];
-        }
-    }
-}
-
-// The same of the first `live` of them (less than N: one by one), the others 0.
-template <int N, typename T>
-__device__ __forceinline__ void rg_load_head(const T* p, int live, float (&v)[N]) {
-    if (live >= N) { rg_load<N>(p, v); return; }
-#pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = i < live ? (float)p[i] : 0.0f;
-}
-
-// The first `live` numbers of N from p as they are, the others 0.
+// The first `live` numbers of N from p as they are, the others 0.  (Where not all are there, loads of the last one stand in for those that are
+// not, so that none waits for another.)
 template <int N, typename T>
 __device__ __forceinline__ typename RgPack<T, N>::type rg_load_raw(const T* p, int live) {
     if (live >= N) return *(const typename RgPack<T, N>::type*)p;
     typename RgPack<T, N>::type a;
 #pragma unroll
-    for (int i = 0; i < N; ++i) a[i] = i < live ? p[i] : (T)0.0f;
+    for (int i = 0; i < N; ++i) a[i] = (T)0.0f;
+    if (live > 0) {
+        T v[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = p[i < live ? i : live - 1];
+#pragma unroll
+        for (int i = 0; i < N; ++i) a[i] = i < live ? v[i] : (T)0.0f;
+    }
     return a;
+}
+
+// The same, in 32 bits.
+template <int N, typename T>
+__device__ __forceinline__ void rg_load_head(const T* p, int live, float (&v)[N]) {
+    const typename RgPack<T, N>::type a = rg_load_raw<N>(p, live);
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = (float)a[i];
+}
+
+// Numbers col .. col + N - 1 of a row of `dim` >= N by one load without a branch: where the row ends before them they are loaded from further left,
+// and rg_row_end puts them (those behind the end as 0) in place once they are there.
+template <int N, typename T>
+__device__ __forceinline__ typename RgPack<T, N>::type rg_load_row(const T* row, int col, int dim) {
+    return *(const typename RgPack<T, N>::type*)(row + min(col, dim - N));
+}
+template <int N, typename T>
+__device__ __forceinline__ void rg_row_end(T (&a)[N], int col, int dim) {
+    const int over = col - min(col, dim - N);
+    if (dim % N != 0) {                                    // (rows of whole vectors: all there, or none)
+#pragma unroll
+        for (int step = 1; step < N; step *= 2)
+#pragma unroll
+            for (int i = 0; i < N; ++i) a[i] = over & step ? (i + step < N ? a[(i + step) % N] : (T)0.0f) : a[i];
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) a[i] = over < N ? a[i] : (T)0.0f;
 }
 
 template <int N, typename T>
@@ -61,12 +70,36 @@ __device__ __forceinline__ void rg_store(T* p, const float (&v)[N]) {
     }
 }
 
+// The first `live` of N numbers.  Of 16 bytes: 8, 4 and 2 of them, as the bits of `live` say.
 template <int N, typename T>
 __device__ __forceinline__ void rg_store_live(T* p, int live, const float (&v)[N]) {
     if (live >= N) { rg_store<N>(p, v); return; }
+    if (live <= 0) return;
+    if constexpr (N * sizeof(T) == 16) {
+        typename RgPack<T, N>::type a;
 #pragma unroll
-    for (int i = 0; i < N; ++i)
-        if (i < live) p[i] = (T)v[i];
+        for (int i = 0; i < N; ++i) a[i] = (T)v[i];
+        typedef uint32_t Words __attribute__((ext_vector_type(4)));
+        const Words w = __builtin_bit_cast(Words, a);
+        constexpr int HALF = N / 2, WORD = 4 / sizeof(T);
+        const bool half = live & HALF;
+        typedef uint32_t Two __attribute__((ext_vector_type(2), aligned(2)));
+        typedef uint32_t One __attribute__((aligned(2)));
+        if (half) *(Two*)p = Two{w[0], w[1]};
+        T* to = p + (live & HALF);
+        uint32_t rest = half ? w[2] : w[0];
+        const uint32_t behind = half ? w[3] : w[1];
+        if (live & (HALF / 2)) *(One*)to = rest;           // a word: one number of 32 bits, two of 16
+        if constexpr (WORD == 2) {
+            to += live & 2;
+            rest = live & 2 ? behind : rest;
+            if (live & 1) *(uint16_t*)to = (uint16_t)rest;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (i < live) p[i] = (T)v[i];
+    }
 }
 
 __device__ __forceinline__ int64_t rg_least(int64_t a, int64_t b) { return a < b ? a : b; }

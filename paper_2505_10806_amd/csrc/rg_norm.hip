@@ -58,6 +58,14 @@ __device__ __forceinline__ void load_params(const float* p, int live, float abse
     }
 }
 
+// A chunk of a row in 32 bits (END: one that may reach over the row's end, or not be there, as a lane's last may).
+template <typename T, int V, bool END>
+__device__ __forceinline__ void chunk_numbers(const typename RgPack<T, V>::type& a, int col, int dim, float (&v)[V]) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) v[j] = (float)a[j];
+    if (END) rg_row_end<V>(v, col, dim);
+}
+
 template <typename T, int NC>
 __global__ void __launch_bounds__(256) k_layer_norm(const T* x, int64_t x_stride, int64_t n, const int32_t* __restrict__ n_dev, int dim,
                                                     const float* __restrict__ gamma, const float* __restrict__ beta, float eps, T* y,
@@ -66,21 +74,38 @@ __global__ void __launch_bounds__(256) k_layer_norm(const T* x, int64_t x_stride
     const int64_t n_act = rg_rows(n, n_dev);
     const int lane = rg_lane(), L = 1 << log2L, R = RG_WAVE >> log2L, l = lane & (L - 1);
     const int64_t wave = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) >> 6, waves = ((int64_t)gridDim.x * blockDim.x) >> 6;
+    if (wave * R >= n_act) return;
+    struct Row {
+        typename RgPack<T, V>::type x[NC];
+    };
+    const auto load = [&](Row& r, int64_t row) {
+        const T* src = x + rg_least(row, n_act - 1) * x_stride;
+#pragma unroll
+        for (int i = 0; i < NC; ++i) r.x[i] = rg_load_row<V>(src, (l + i * L) * V, dim);
+    };
+    Row next;
+    load(next, wave * R + (lane >> log2L));
+    float g[NC][V], b[NC][V];
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+        const int col = (l + i * L) * V;
+        load_params<V>(gamma ? gamma + col : nullptr, dim - col, 1.0f, g[i]);
+        load_params<V>(beta ? beta + col : nullptr, dim - col, 0.0f, b[i]);
+    }
     for (int64_t row0 = wave * R; row0 < n_act; row0 += waves * R) {
         const int64_t row = row0 + (lane >> log2L);
-        const bool live_row = row < n_act;
-        const T* src = x + (live_row ? row : n_act - 1) * x_stride;
+        const Row r = next;
+        load(next, row + waves * R);                       // (on its way while this one is worked on)
+        if (row >= n_act) continue;
         float v[NC][V];
         float sum = 0.0f;
 #pragma unroll
         for (int i = 0; i < NC; ++i) {
-            const int col = (l + i * L) * V;
-            rg_load_head<V>(src + col, dim - col, v[i]);
-        }
-#pragma unroll
-        for (int i = 0; i < NC; ++i)
+            if (i + 1 < NC && NC <= 4) chunk_numbers<T, V, false>(r.x[i], 0, dim, v[i]);
+            else chunk_numbers<T, V, true>(r.x[i], (l + i * L) * V, dim, v[i]);
 #pragma unroll
             for (int j = 0; j < V; ++j) sum += v[i][j];
+        }
         const float m = group_sum(sum, log2L) / (float)dim;
         float square = 0.0f;
 #pragma unroll
@@ -93,17 +118,13 @@ __global__ void __launch_bounds__(256) k_layer_norm(const T* x, int64_t x_stride
             }
         }
         const float s = 1.0f / sqrtf(group_sum(square, log2L) / (float)dim + eps);
-        if (!live_row) continue;
         T* dst = y + row * y_stride;
 #pragma unroll
         for (int i = 0; i < NC; ++i) {
             const int col = (l + i * L) * V;
             if (col >= dim) continue;
-            float g[V], b[V];
-            load_params<V>(gamma ? gamma + col : nullptr, dim - col, 1.0f, g);
-            load_params<V>(beta ? beta + col : nullptr, dim - col, 0.0f, b);
 #pragma unroll
-            for (int j = 0; j < V; ++j) v[i][j] = v[i][j] * s * g[j] + b[j];
+            for (int j = 0; j < V; ++j) v[i][j] = v[i][j] * s * g[i][j] + b[i][j];
             rg_store_live<V>(dst + col, dim - col, v[i]);
         }
         if (l == 0) {
@@ -113,7 +134,7 @@ __global__ void __launch_bounds__(256) k_layer_norm(const T* x, int64_t x_stride
     }
 }
 
-// Rows too long for a wavefront's registers: a workgroup each, read three times.
+// Rows too long for a wavefront's registers (and those of less than 16 bytes): a workgroup each, read three times.
 template <typename T>
 __global__ void __launch_bounds__(256) k_layer_norm_long(const T* x, int64_t x_stride, int64_t n, const int32_t* __restrict__ n_dev, int dim,
                                                          const float* __restrict__ gamma, const float* __restrict__ beta, float eps, T* y,
@@ -158,7 +179,7 @@ __global__ void __launch_bounds__(256) k_layer_norm_long(const T* x, int64_t x_s
 // joins in the order of the workgroups.
 constexpr int kGradThreads = 512, kGradWaves = kGradThreads / RG_WAVE;
 
-template <typename T, int NC, bool SUMS>
+template <typename T, int NC>
 __global__ void __launch_bounds__(kGradThreads) k_layer_norm_grad(const T* dy, int64_t dy_stride, const T* x, int64_t x_stride, int64_t n,
                                                                   const int32_t* __restrict__ n_dev, int dim, const float* __restrict__ gamma,
                                                                   const float* __restrict__ mean, const float* __restrict__ rstd, T* dx,
@@ -186,8 +207,8 @@ __global__ void __launch_bounds__(kGradThreads) k_layer_norm_grad(const T* dy, i
 #pragma unroll
         for (int i = 0; i < NC; ++i) {
             const int col = (l + i * L) * V;
-            r.x[i] = rg_load_raw<V>(x + row * x_stride + col, dim - col);
-            r.d[i] = rg_load_raw<V>(dy + row * dy_stride + col, dim - col);
+            r.x[i] = rg_load_row<V>(x + row * x_stride, col, dim);
+            r.d[i] = rg_load_row<V>(dy + row * dy_stride, col, dim);
         }
         r.mean = mean[row];
         r.rstd = rstd[row];
@@ -203,19 +224,24 @@ __global__ void __launch_bounds__(kGradThreads) k_layer_norm_grad(const T* dy, i
         const float m = r.mean, s = r.rstd;
         float sums[2] = {0.0f, 0.0f};                      // of g h and of g
 #pragma unroll
-        for (int i = 0; i < NC; ++i)
+        for (int i = 0; i < NC; ++i) {
+            if (i + 1 < NC) {
+                chunk_numbers<T, V, false>(r.x[i], 0, dim, h[i]);
+                chunk_numbers<T, V, false>(r.d[i], 0, dim, d[i]);
+            } else {
+                chunk_numbers<T, V, true>(r.x[i], (l + i * L) * V, dim, h[i]);
+                chunk_numbers<T, V, true>(r.d[i], (l + i * L) * V, dim, d[i]);
+            }
 #pragma unroll
-            for (int j = 0; j < V; ++j) {                  // (behind the row's end dy was loaded as 0)
-                h[i][j] = ((float)r.x[i][j] - m) * s;
-                d[i][j] = (float)r.d[i][j];
-                if (SUMS) {
-                    by_gamma[i][j] += d[i][j] * h[i][j];
-                    by_beta[i][j] += d[i][j];
-                }
+            for (int j = 0; j < V; ++j) {                  // (behind the row's end dy is 0)
+                h[i][j] = (h[i][j] - m) * s;
+                by_gamma[i][j] += d[i][j] * h[i][j];
+                by_beta[i][j] += d[i][j];
                 d[i][j] *= g[i][j];
                 sums[0] += d[i][j] * h[i][j];
                 sums[1] += d[i][j];
             }
+        }
         if (!dx) continue;
         group_sums(sums, log2L);
         const float along = sums[0] / (float)dim, all = sums[1] / (float)dim;
@@ -228,7 +254,7 @@ __global__ void __launch_bounds__(kGradThreads) k_layer_norm_grad(const T* dy, i
             rg_store_live<V>(dx + row * dx_stride + col, dim - col, d[i]);
         }
     }
-    if (!SUMS) return;
+    if (!parts) return;                                    // (not wanted; adding them up is no more than the loads leave time for)
 #pragma unroll 1
     for (int which = 0; which < 2; ++which) {
         __syncthreads();
@@ -351,12 +377,13 @@ __global__ void __launch_bounds__(256) k_layer_norm_sums_long(const T* __restric
 
 // Lanes to a row and chunks to a lane: the smallest number of lane slots that holds the row's chunks.
 struct Shape {
-    int log2L, chunks;         // chunks = 0: too long to be held
+    int log2L, chunks;         // chunks = 0: too long to be held, or too short for a load of 16 bytes
 };
 
 Shape row_shape(int dim, int V, int held) {
     const int total = (int)rg_div_up(dim, V);
     Shape best = {6, 0};
+    if (dim < V) return best;                              // (shorter than a load)
     int slots = 1 << 30;
     for (int log2L = 6; log2L >= 0; --log2L) {
         int per = (int)rg_div_up(total, 1 << log2L);
@@ -441,7 +468,7 @@ rg_status rg_layer_norm_grad(rg_ctx* ctx, const void* dy, int64_t dy_stride, con
             const rg_status st = rg_scratch(ctx, ctx->norm_parts, (size_t)blocks * 2 * dim * 4, s, "rg_layer_norm_grad");
             if (st != RG_OK) return st;
         }
-        float* parts = (float*)ctx->norm_parts.p;
+        float* parts = sums ? (float*)ctx->norm_parts.p : nullptr;
         if (shape.chunks == 0) {
             if (sums)
                 k_layer_norm_sums_long<T><<<dim3((unsigned)stripes, (unsigned)blocks), 256, 0, s>>>((const T*)dy, dy_stride, (const T*)x, x_stride, n,
@@ -449,13 +476,10 @@ rg_status rg_layer_norm_grad(rg_ctx* ctx, const void* dy, int64_t dy_stride, con
             if (dx && n > 0)
                 k_layer_norm_grad_long<T><<<(unsigned)rg_min64(n, (int64_t)ctx->num_cus * 32), 256, 0, s>>>(
                     (const T*)dy, dy_stride, (const T*)x, x_stride, n, n_dev, dim, gamma, mean, rstd, (T*)dx, dx_stride);
-        } else if (sums) {
-            const size_t lds = (size_t)kGradWaves * dim * 4;
-            RG_FOR_CHUNKS(shape, kHeldGrad / V, k_layer_norm_grad<T, NC, true><<<(unsigned)blocks, kGradThreads, lds, s>>>(
-                (const T*)dy, dy_stride, (const T*)x, x_stride, n, n_dev, dim, gamma, mean, rstd, (T*)dx, dx_stride, parts, shape.log2L));
         } else {
-            RG_FOR_CHUNKS(shape, kHeldGrad / V, k_layer_norm_grad<T, NC, false><<<(unsigned)blocks, kGradThreads, 0, s>>>(
-                (const T*)dy, dy_stride, (const T*)x, x_stride, n, n_dev, dim, gamma, mean, rstd, (T*)dx, dx_stride, nullptr, shape.log2L));
+            const size_t lds = sums ? (size_t)kGradWaves * dim * 4 : 0;
+            RG_FOR_CHUNKS(shape, kHeldGrad / V, k_layer_norm_grad<T, NC><<<(unsigned)blocks, kGradThreads, lds, s>>>(
+                (const T*)dy, dy_stride, (const T*)x, x_stride, n, n_dev, dim, gamma, mean, rstd, (T*)dx, dx_stride, parts, shape.log2L));
         }
         RG_LAUNCH_CHECK(ctx, "k_layer_norm_grad");
     });

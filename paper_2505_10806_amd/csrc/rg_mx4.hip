@@ -452,17 +452,19 @@ __global__ void __launch_bounds__(kGradThreads, 2) k_mx4_grad(const T* __restric
 #pragma unroll
         for (int u = 0; u < FRAGS; ++u) acc[t][u] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
     const auto multiply = [&](int half) {
-        Frag b[FRAGS];
+        const auto dy_frag = [&](int i) { return from_dy[half * S::kPieces + (i >> 2) * S::GROUPS * 64 * S::TH + 16 * (i & 3)]; };
+        Frag b[FRAGS], a[2];
 #pragma unroll
         for (int u = 0; u < FRAGS; ++u) b[u] = from_x[half * S::kPieces + 16 * u];
+        a[0] = dy_frag(0);
 #pragma unroll
-        for (int p = 0; p < P; ++p)
+        for (int i = 0; i < 4 * P; ++i) {                  // (the next fragment is on its way from LDS during these products)
+            if (i + 1 < 4 * P) a[(i + 1) & 1] = dy_frag(i + 1);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                const Frag a = from_dy[half * S::kPieces + p * S::GROUPS * 64 * S::TH + 16 * t];
-#pragma unroll
-                for (int u = 0; u < FRAGS; ++u) acc[t][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, b[u].v, acc[t][u], 0, 0, 0);
-            }
+            for (int u = 0; u < FRAGS; ++u) acc[i & 3][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i & 1].v, b[u].v, acc[i & 3][u], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        }
     };
 
     // ROLE: loads dy (its four columns k) or codes (its word w) of the eight rows of group g.

@@ -82,6 +82,7 @@ __global__ void __launch_bounds__(kThreads) k_squares(ClipList list, double* __r
 
 // Every workgroup adds up the parts (in one order) and scales its chunks, the last ones first: the device's last level of cache still holds what
 // was read last.
+template <bool ONCE>
 __global__ void __launch_bounds__(kThreads) k_clip(ClipList list, const double* __restrict__ parts, int num_parts, float max_norm,
                                                    float* __restrict__ norm_out) {
     __shared__ double smem[kThreads / RG_WAVE];
@@ -98,7 +99,7 @@ __global__ void __launch_bounds__(kThreads) k_clip(ClipList list, const double* 
             T* out = (T*)list.out[t] + begin;
             for_chunk((const T*)list.in[t] + begin, list.size[t] - begin, list.log2_chunk, [&](auto& v, int place, int live) {
                 for (float& x : v) x = x * scale.coarse * scale.fine;
-                rg_store_live<16 / (int)sizeof(T)>(out + place, live, v);
+                rg_store_live<16 / (int)sizeof(T), ONCE>(out + place, live, v);
             });
         });
     }
@@ -162,7 +163,8 @@ extern "C" rg_status rg_clip_grad_norm(rg_ctx* ctx, const rg_tensor* tensors, in
     if (!single) next = 0;
     do {
         if (!single) fill(list, next, log2_chunk);
-        k_clip<<<grid_of(list), kThreads, 0, s>>>(list, parts, num_parts, max_norm, next == count ? norm : nullptr);
+        const auto kernel = rg_store_once(nullptr, 16, 16, numbers / 8) ? k_clip<true> : k_clip<false>;
+        kernel<<<grid_of(list), kThreads, 0, s>>>(list, parts, num_parts, max_norm, next == count ? norm : nullptr);
         RG_LAUNCH_CHECK(ctx, "k_clip");
     } while (next < count);
     return RG_OK;

@@ -85,7 +85,7 @@ __global__ void __launch_bounds__(256) k_mx4_quantize(const T* __restrict__ x, i
 
 // ---------------------------------------------------------------- packed rows to numbers
 // A lane makes 16 bytes of a row.
-template <typename T>
+template <typename T, bool ONCE>
 __global__ void __launch_bounds__(256) k_mx4_dequantize(const uint32_t* __restrict__ packed, int64_t packed_stride, int64_t n,
                                                         const int32_t* __restrict__ n_dev, int dim, T* __restrict__ x, int64_t x_stride, int pieces,
                                                         uint32_t inv_pieces, int rows_per_block) {
@@ -119,7 +119,7 @@ __global__ void __launch_bounds__(256) k_mx4_dequantize(const uint32_t* __restri
                 const v2f c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[u], s, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[u], s, 3);
                 v[4] = c.x; v[5] = c.y; v[6] = d.x; v[7] = d.y;
             }
-            rg_store_live<V>(x + (row0 + r[u]) * x_stride + piece[u] * V, dim - piece[u] * V, v);
+            rg_store_live<V, ONCE>(x + (row0 + r[u]) * x_stride + piece[u] * V, dim - piece[u] * V, v);
         }
     }
 }
@@ -893,7 +893,7 @@ __global__ void __launch_bounds__(1024) k_mx4_grad_join(const float* __restrict_
     const int per_run = (splits + 15) >> 4, first = run * per_run, last = min(first + per_run, splits);
     float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     if (at < total) {
-#pragma unroll 4
+#pragma unroll 8
         for (int s = first; s < last; ++s) {
             float v[4];
             rg_load_head<4>(parts + s * split_stride + at, (int)rg_least(4, total - at), v);
@@ -959,8 +959,11 @@ rg_status rg_mx4_dequantize(rg_ctx* ctx, const void* packed, int64_t packed_stri
     hipStream_t s = (hipStream_t)stream;
     const int pieces = (int)rg_div_up((int64_t)dim * rg_type_bytes(x_type), 16);
     const int rows = rows_per_group(ctx, n, pieces);
-    RG_FOR_TYPE(x_type, k_mx4_dequantize<T><<<(unsigned)rg_div_up(n, rows), 256, 0, s>>>((const uint32_t*)packed, packed_stride, n, n_dev, dim,
-                                                                                    (T*)x, x_stride, pieces, rg_inverse(pieces), rows));
+    RG_FOR_TYPE(x_type, {
+        const auto kernel = rg_store_once(x, dim * sizeof(T), x_stride * sizeof(T), n) ? k_mx4_dequantize<T, true> : k_mx4_dequantize<T, false>;
+        kernel<<<(unsigned)rg_div_up(n, rows), 256, 0, s>>>((const uint32_t*)packed, packed_stride, n, n_dev, dim, (T*)x, x_stride, pieces,
+                                                           rg_inverse(pieces), rows);
+    });
     RG_LAUNCH_CHECK(ctx, "k_mx4_dequantize");
     return RG_OK;
 }

@@ -66,7 +66,7 @@ __device__ __forceinline__ void chunk_numbers(const typename RgPack<T, V>::type&
     if (END) rg_row_end<V>(v, col, dim);
 }
 
-template <typename T, int NC>
+template <typename T, int NC, bool ONCE>
 __global__ void __launch_bounds__(256) k_layer_norm(const T* x, int64_t x_stride, int64_t n, const int32_t* __restrict__ n_dev, int dim,
                                                     const float* __restrict__ gamma, const float* __restrict__ beta, float eps, T* y,
                                                     int64_t y_stride, float* __restrict__ mean, float* __restrict__ rstd, int log2L) {
@@ -125,7 +125,7 @@ __global__ void __launch_bounds__(256) k_layer_norm(const T* x, int64_t x_stride
             if (col >= dim) continue;
 #pragma unroll
             for (int j = 0; j < V; ++j) v[i][j] = v[i][j] * s * g[i][j] + b[i][j];
-            rg_store_live<V>(dst + col, dim - col, v[i]);
+            rg_store_live<V, ONCE>(dst + col, dim - col, v[i]);
         }
         if (l == 0) {
             if (mean) mean[row] = m;
@@ -179,7 +179,7 @@ __global__ void __launch_bounds__(256) k_layer_norm_long(const T* x, int64_t x_s
 // joins in the order of the workgroups.
 constexpr int kGradThreads = 512, kGradWaves = kGradThreads / RG_WAVE;
 
-template <typename T, int NC>
+template <typename T, int NC, bool ONCE>
 __global__ void __launch_bounds__(kGradThreads) k_layer_norm_grad(const T* dy, int64_t dy_stride, const T* x, int64_t x_stride, int64_t n,
                                                                   const int32_t* __restrict__ n_dev, int dim, const float* __restrict__ gamma,
                                                                   const float* __restrict__ mean, const float* __restrict__ rstd, T* dx,
@@ -251,7 +251,7 @@ __global__ void __launch_bounds__(kGradThreads) k_layer_norm_grad(const T* dy, i
             if (col >= dim) continue;
 #pragma unroll
             for (int j = 0; j < V; ++j) d[i][j] = s * (d[i][j] - all - h[i][j] * along);
-            rg_store_live<V>(dx + row * dx_stride + col, dim - col, d[i]);
+            rg_store_live<V, ONCE>(dx + row * dx_stride + col, dim - col, d[i]);
         }
     }
     if (!parts) return;                                    // (not wanted; adding them up is no more than the loads leave time for)
@@ -431,8 +431,11 @@ rg_status rg_layer_norm(rg_ctx* ctx, const void* x, rg_dtype type, int64_t x_str
                                                                                                   beta, eps, (T*)y, y_stride, mean, rstd);
         } else {
             const unsigned grid = (unsigned)rg_min64(rg_div_up(n, 4 * (RG_WAVE >> shape.log2L)), (int64_t)ctx->num_cus * 64);
-            RG_FOR_CHUNKS(shape, kHeld / Chunk<T>::V, k_layer_norm<T, NC><<<grid, 256, 0, s>>>((const T*)x, x_stride, n, n_dev, dim, gamma, beta, eps, (T*)y,
-                                                                                      y_stride, mean, rstd, shape.log2L));
+            const bool once = rg_store_once(y, dim * sizeof(T), y_stride * sizeof(T), n);
+            RG_FOR_CHUNKS(shape, kHeld / Chunk<T>::V, {
+                const auto kernel = once ? k_layer_norm<T, NC, true> : k_layer_norm<T, NC, false>;
+                kernel<<<grid, 256, 0, s>>>((const T*)x, x_stride, n, n_dev, dim, gamma, beta, eps, (T*)y, y_stride, mean, rstd, shape.log2L);
+            });
         }
     });
     RG_LAUNCH_CHECK(ctx, "k_layer_norm");
@@ -478,8 +481,12 @@ rg_status rg_layer_norm_grad(rg_ctx* ctx, const void* dy, int64_t dy_stride, con
                     (const T*)dy, dy_stride, (const T*)x, x_stride, n, n_dev, dim, gamma, mean, rstd, (T*)dx, dx_stride);
         } else {
             const size_t lds = sums ? (size_t)kGradWaves * dim * 4 : 0;
-            RG_FOR_CHUNKS(shape, kHeldGrad / V, k_layer_norm_grad<T, NC><<<(unsigned)blocks, kGradThreads, lds, s>>>(
-                (const T*)dy, dy_stride, (const T*)x, x_stride, n, n_dev, dim, gamma, mean, rstd, (T*)dx, dx_stride, parts, shape.log2L));
+            const bool once = rg_store_once(dx, dim * sizeof(T), dx_stride * sizeof(T), n);
+            RG_FOR_CHUNKS(shape, kHeldGrad / V, {
+                const auto kernel = once ? k_layer_norm_grad<T, NC, true> : k_layer_norm_grad<T, NC, false>;
+                kernel<<<(unsigned)blocks, kGradThreads, lds, s>>>((const T*)dy, dy_stride, (const T*)x, x_stride, n, n_dev, dim, gamma, mean, rstd,
+                                                                   (T*)dx, dx_stride, parts, shape.log2L);
+            });
         }
         RG_LAUNCH_CHECK(ctx, "k_layer_norm_grad");
     });

@@ -206,7 +206,7 @@ __global__ void __launch_bounds__(256) k_mx4_matmul(const uint32_t* __restrict__
 // instead of 126).  Where rows of y follow each other without a gap and end inside 16 bytes (`run_on`), a tile is stored as one run.
 constexpr int kKeptThreads = 256, kKeptWaves = kKeptThreads / RG_WAVE;
 
-template <typename T, int STEPS, int FRAGS>
+template <typename T, int STEPS, int FRAGS, bool ONCE>
 __global__ void __launch_bounds__(kKeptThreads, STEPS > 5 ? 2 : 1) k_mx4_matmul_kept(
     const uint32_t* __restrict__ rows, int64_t rows_stride, int64_t n, const int32_t* __restrict__ n_dev, const uint32_t* __restrict__ weight,
     int64_t weight_stride, int out_dim, int groups, T* __restrict__ y, int64_t y_stride, int slices, int slice_groups, int run_on,
@@ -317,9 +317,11 @@ __global__ void __launch_bounds__(kKeptThreads, STEPS > 5 ? 2 : 1) k_mx4_matmul_
             const int at = (p - r * lanes) * E, left = numbers - at;
             const rg_u32x4a v = *(const rg_u32x4a*)(mine + r * pitch + at * sizeof(T));
             T* const there = out + r * y_stride + at;
-            if (left >= E) *(typename RgPack<T, E>::type*)there = __builtin_bit_cast(typename RgPack<T, E>::type, v);
+            typedef typename RgPack<T, E>::type Piece;
+            if (ONCE) __builtin_nontemporal_store(__builtin_bit_cast(Piece, v), (Piece*)there);
+            else if (left >= E) *(Piece*)there = __builtin_bit_cast(Piece, v);
             else {
-                const auto e = __builtin_bit_cast(typename RgPack<T, E>::type, v);
+                const auto e = __builtin_bit_cast(Piece, v);
 #pragma unroll
                 for (int i = 0; i < E; ++i)
                     if (i < left) there[i] = e[i];
@@ -999,10 +1001,18 @@ rg_status rg_mx4_matmul(rg_ctx* ctx, const void* rows, int64_t rows_stride, int6
             const unsigned grid = (unsigned)(row_groups * slice_groups);
             const int last = out_dim % outs, last_bytes = last * (int)sizeof(T);
             const int run_on = out_dim <= outs && y_stride == out_dim && last_bytes % 16 != 0;
-            const auto kernel = steps == 1 ? (many ? k_mx4_matmul_kept<T, 1, 8> : k_mx4_matmul_kept<T, 1, 4>)
-                                : steps == 2 ? (many ? k_mx4_matmul_kept<T, 2, 8> : k_mx4_matmul_kept<T, 2, 4>)
-                                : steps == 3 ? k_mx4_matmul_kept<T, 3, 4> : steps == 4 ? k_mx4_matmul_kept<T, 4, 4>
-                                : steps == 5 ? k_mx4_matmul_kept<T, 5, 4> : k_mx4_matmul_kept<T, 8, 4>;
+            const auto pick = [&](auto once) {             // (ONCE: rows of whole 16 bytes)
+                constexpr bool ONCE = decltype(once)::value;
+                if (many) return steps == 1 ? k_mx4_matmul_kept<T, 1, 8, ONCE> : k_mx4_matmul_kept<T, 2, 8, ONCE>;
+                return steps == 1   ? k_mx4_matmul_kept<T, 1, 4, ONCE>
+                       : steps == 2 ? k_mx4_matmul_kept<T, 2, 4, ONCE>
+                       : steps == 3 ? k_mx4_matmul_kept<T, 3, 4, ONCE>
+                       : steps == 4 ? k_mx4_matmul_kept<T, 4, 4, ONCE>
+                       : steps == 5 ? k_mx4_matmul_kept<T, 5, 4, ONCE>
+                                    : k_mx4_matmul_kept<T, 8, 4, ONCE>;
+            };
+            const bool once = rg_store_once(y, out_dim * sizeof(T), y_stride * sizeof(T), n);
+            const auto kernel = once ? pick(std::true_type()) : pick(std::false_type());
             kernel<<<grid, kKeptThreads, 0, s>>>((const uint32_t*)rows, rows_stride, n, n_dev, (const uint32_t*)weight, weight_stride, out_dim, groups,
                                                  (T*)y, y_stride, slices, slice_groups, run_on, rg_inverse((uint32_t)rg_div_up(last_bytes, 16)));
         } else if (n <= 256) {

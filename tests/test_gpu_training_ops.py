@@ -508,6 +508,42 @@ def test_clip_what_is_not_finite_or_far(ctx):
     assert bool((g == 1).all()) and abs(norm.item() - 7 ** 0.5) < 1e-6
 
 
+# ---------------------------------------------------------------- large results
+@pytest.mark.parametrize("dtype", ref.TYPES)
+def test_results_larger_than_the_caches(ctx, dtype):
+    """More than 32 MiB of results in rows of whole 16 bytes are stored another way."""
+    from paper_2505_10806_amd import binding as B
+    n, dim = (140_007, 64) if dtype == F32 else (270_011, 64)
+    rng = np.random.default_rng(n)
+    gen = torch.Generator(device=DEV).manual_seed(n)
+    x = torch.randn(n, dim, generator=gen, device=DEV).to(dtype)
+    some = np.concatenate([np.arange(40), rng.integers(0, n, 2000), np.arange(n - 40, n)])
+    at = torch.from_numpy(some).to(DEV)
+    packed, back = B.mx4_rows(n, dim, DEV), torch.empty(n, dim, dtype=dtype, device=DEV)
+    ctx.mx4_quantize(x, n, dim, packed)
+    ctx.mx4_dequantize(packed, n, dim, back)
+    bytes_, values = ref.quantize(f64(x[at]))
+    assert np.array_equal(of_packed(packed[at], dim), bytes_) and np.array_equal(f64(back[at]), f64(torch.from_numpy(values).to(dtype)))
+    wb, wv = packed_rows(rng, dim, dim)
+    ctx.mx4_matmul(packed, n, to_packed(wb), dim, dim, back)
+    check(back[at], values @ wv.T, sum_allowed(dim, values, wv, dtype), "y")
+    y, mean, rstd = torch.empty_like(x), torch.empty(n, device=DEV), torch.empty(n, device=DEV)
+    ctx.layer_norm(x, n, dim, None, None, 1e-5, y, mean, rstd)
+    check_norm(y[at], mean[at], rstd[at], f64(x[at]), np.ones(dim), np.zeros(dim), 1e-5, dtype)
+    dy = torch.randn(n, dim, generator=gen, device=DEV).to(dtype)
+    dx, dg, db = torch.empty_like(x), torch.empty(dim, device=DEV), torch.empty(dim, device=DEV)
+    ctx.layer_norm_grad(dy, x, n, dim, None, mean, rstd, dx, dg, db)
+    check_norm_grad(dx[at], None, None, f64(dy[at]), f64(x[at]), np.ones(dim), f64(mean[at]), f64(rstd[at]), dtype)
+    check_norm_grad(None, dg, db, f64(dy), f64(x), np.ones(dim), f64(mean), f64(rstd), dtype)
+    norm, out = torch.empty(1, device=DEV), torch.empty_like(dy)
+    ctx.clip_grad_norm(B.TensorList([dy, dx], [out, back]), 7.0, norm)
+    norm64, _ = ref.clip([f64(dy), f64(dx)], 7.0)
+    check(norm, np.array([norm64]), 2.0 ** -23 * norm64, "norm")
+    for g, o in ((dy, out), (dx, back)):
+        want = f64(g[at]) * (7.0 / norm64)
+        check(o[at], want, 2.0 ** -22 * np.abs(want) + ref.stored(want, dtype), "clipped")
+
+
 # ---------------------------------------------------------------- far addresses, streams, graphs
 def test_rows_beyond_32_bits(ctx):
     """Row offsets that pass 2^32 numbers, in every array."""

@@ -8,6 +8,9 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kMostTensors = 64;       // that a launch's arguments describe
 constexpr int kMostParts = 2048;       // workgroups of a launch
+// Numbers of a chunk: 8 KB of them, two loads of 16 bytes a thread.  (The last kernel with 4, 8, 16 or 32 KB: 462 k floats 4.7 / 4.6 / 5.3 / 5.9 us,
+// 30 M 40.8 / 39.2 / 40.9 / 42.2.)
+constexpr int log2_chunk(size_t bytes) { return bytes == 4 ? 11 : 12; }
 
 struct ClipList {
     const void* in[kMostTensors];
@@ -16,7 +19,6 @@ struct ClipList {
     int32_t first[kMostTensors];       // chunks in front of each tensor (of those that are not there: as many as there can be)
     int32_t type[kMostTensors];        // (words: scalar loads drop the last two bits of each part of an address, and the compiler shares parts)
     int32_t chunks;
-    int32_t log2_chunk;                // numbers of a chunk
 };
 
 // The tensor that chunk `at` belongs to: every lane looks at one.
@@ -27,10 +29,10 @@ __device__ __forceinline__ int tensor_of(const ClipList& list, int at) {
 
 // f(numbers, place, how many) on every 16 bytes of the chunk that begins at p.
 template <typename T, typename F>
-__device__ __forceinline__ void for_chunk(const T* p, int64_t left, int log2_chunk, F f) {
+__device__ __forceinline__ void for_chunk(const T* p, int64_t left, F f) {
     constexpr int V = 16 / (int)sizeof(T);
-    const int n = (int)rg_least(left, 1 << log2_chunk);
-#pragma unroll 4
+    const int n = (int)rg_least(left, 1 << log2_chunk(sizeof(T)));
+#pragma unroll 1
     for (int at = (int)threadIdx.x * V; at < n; at += kThreads * V) {
         float v[V];
         rg_load_head<V>(p + at, n - at, v);
@@ -71,10 +73,12 @@ __global__ void __launch_bounds__(kThreads) k_squares(ClipList list, double* __r
     double sum = 0.0;
     for (int at = blockIdx.x; at < list.chunks; at += gridDim.x) {
         const int t = tensor_of(list, at);
-        const int64_t begin = (int64_t)(at - list.first[t]) << list.log2_chunk;
-        RG_FOR_TYPE((rg_dtype)list.type[t], for_chunk((const T*)list.in[t] + begin, list.size[t] - begin, list.log2_chunk, [&](const auto& v, int, int) {
-            for (float x : v) sum += (double)x * (double)x;
-        }));
+        RG_FOR_TYPE((rg_dtype)list.type[t], {
+            const int64_t begin = (int64_t)(at - list.first[t]) << log2_chunk(sizeof(T));
+            for_chunk((const T*)list.in[t] + begin, list.size[t] - begin, [&](const auto& v, int, int) {
+                for (float x : v) sum += (double)x * (double)x;
+            });
+        });
     }
     sum = block_sum<kThreads / RG_WAVE>(sum, smem);
     if (threadIdx.x == 0) parts[blockIdx.x] = sum;
@@ -94,10 +98,10 @@ __global__ void __launch_bounds__(kThreads) k_clip(ClipList list, const double* 
     for (int at = list.chunks - 1 - (int)blockIdx.x; at >= 0; at -= gridDim.x) {
         const int t = tensor_of(list, at);
         if (!scale.clipped && list.in[t] == list.out[t]) continue;
-        const int64_t begin = (int64_t)(at - list.first[t]) << list.log2_chunk;
         RG_FOR_TYPE((rg_dtype)list.type[t], {
+            const int64_t begin = (int64_t)(at - list.first[t]) << log2_chunk(sizeof(T));
             T* out = (T*)list.out[t] + begin;
-            for_chunk((const T*)list.in[t] + begin, list.size[t] - begin, list.log2_chunk, [&](auto& v, int place, int live) {
+            for_chunk((const T*)list.in[t] + begin, list.size[t] - begin, [&](auto& v, int place, int live) {
                 for (float& x : v) x = x * scale.coarse * scale.fine;
                 rg_store_live<16 / (int)sizeof(T), ONCE>(out + place, live, v);
             });
@@ -125,8 +129,8 @@ extern "C" rg_status rg_clip_grad_norm(rg_ctx* ctx, const rg_tensor* tensors, in
     }
     RG_HIP(ctx, hipSetDevice(ctx->device));
     hipStream_t s = (hipStream_t)stream;
-    // the tensors that hold something, kMostTensors to a launch, in chunks of 2^log2_chunk numbers
-    const auto fill = [&](ClipList& list, int32_t& next, int log2_chunk) {
+    // the tensors that hold something, kMostTensors to a launch
+    const auto fill = [&](ClipList& list, int32_t& next) {
         int64_t chunks = 0;
         int at = 0;
         for (; next < count && at < kMostTensors; ++next) {
@@ -137,16 +141,13 @@ extern "C" rg_status rg_clip_grad_norm(rg_ctx* ctx, const rg_tensor* tensors, in
             list.size[at] = t.size;
             list.type[at] = (int32_t)t.type;
             list.first[at++] = (int32_t)chunks;
-            chunks += (t.size + (1ll << log2_chunk) - 1) >> log2_chunk;
+            chunks += rg_div_up(t.size, 1ll << log2_chunk(rg_type_bytes(t.type)));
         }
         for (; at < kMostTensors; ++at) list.first[at] = INT32_MAX;
         list.chunks = (int32_t)chunks;
-        list.log2_chunk = log2_chunk;
     };
     ClipList list;
     int32_t next = 0;
-    // chunks small enough for all compute units, or large enough to be worth looking up
-    const int log2_chunk = numbers < (1 << 23) ? 11 : 13;
     const int64_t lists = rg_max64(1, rg_div_up(count, kMostTensors));
     const rg_status st = rg_scratch(ctx, ctx->clip_parts, (size_t)(lists * kMostParts) * sizeof(double), s, "rg_clip_grad_norm");
     if (st != RG_OK) return st;
@@ -154,7 +155,7 @@ extern "C" rg_status rg_clip_grad_norm(rg_ctx* ctx, const rg_tensor* tensors, in
     int num_parts = 0;
     const auto grid_of = [](const ClipList& l) { return (unsigned)rg_max64(1, rg_min64(l.chunks, kMostParts)); };
     do {                                                   // (no tensor at all is a list of none)
-        fill(list, next, log2_chunk);
+        fill(list, next);
         k_squares<<<grid_of(list), kThreads, 0, s>>>(list, parts + num_parts);
         RG_LAUNCH_CHECK(ctx, "k_squares");
         num_parts += (int)grid_of(list);
@@ -162,7 +163,7 @@ extern "C" rg_status rg_clip_grad_norm(rg_ctx* ctx, const rg_tensor* tensors, in
     const bool single = lists == 1;
     if (!single) next = 0;
     do {
-        if (!single) fill(list, next, log2_chunk);
+        if (!single) fill(list, next);
         const auto kernel = rg_store_once(nullptr, 16, 16, numbers / 8) ? k_clip<true> : k_clip<false>;
         kernel<<<grid_of(list), kThreads, 0, s>>>(list, parts, num_parts, max_norm, next == count ? norm : nullptr);
         RG_LAUNCH_CHECK(ctx, "k_clip");

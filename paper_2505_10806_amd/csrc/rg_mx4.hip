@@ -34,10 +34,9 @@ __global__ void __launch_bounds__(256) k_mx4_quantize(const T* __restrict__ x, i
                                                       int rows_per_block) {
     constexpr int V = 16 / sizeof(T), U = kPiecesAhead;
     const int64_t n_act = rg_rows(n, n_dev);
-    const int64_t row0 = (int64_t)blockIdx.x * rows_per_block;
-    if (row0 >= n_act) return;
-    const int items = (int)rg_least(rows_per_block, n_act - row0) * pieces;      // a multiple of a group's lanes: groups are in one wavefront
     const int groups = (dim + kGroup - 1) / kGroup;
+    for (int64_t row0 = (int64_t)blockIdx.x * rows_per_block; row0 < n_act; row0 += (int64_t)gridDim.x * rows_per_block) {
+    const int items = (int)rg_least(rows_per_block, n_act - row0) * pieces;      // a multiple of a group's lanes: groups are in one wavefront
     for (int it0 = threadIdx.x; it0 < items; it0 += 256 * U) {
         float v[U][V];
         int r[U], piece[U];
@@ -81,6 +80,7 @@ __global__ void __launch_bounds__(256) k_mx4_quantize(const T* __restrict__ x, i
             }
         }
     }
+    }
 }
 
 // ---------------------------------------------------------------- packed rows to numbers
@@ -92,10 +92,9 @@ __global__ void __launch_bounds__(256) k_mx4_dequantize(const uint32_t* __restri
     constexpr int V = 16 / sizeof(T), U = kPiecesAhead;
     typedef float v2f __attribute__((ext_vector_type(2)));
     const int64_t n_act = rg_rows(n, n_dev);
-    const int64_t row0 = (int64_t)blockIdx.x * rows_per_block;
-    if (row0 >= n_act) return;
-    const int items = (int)rg_least(rows_per_block, n_act - row0) * pieces;
     const int groups = (dim + kGroup - 1) / kGroup;
+    for (int64_t row0 = (int64_t)blockIdx.x * rows_per_block; row0 < n_act; row0 += (int64_t)gridDim.x * rows_per_block) {
+    const int items = (int)rg_least(rows_per_block, n_act - row0) * pieces;
     for (int it0 = threadIdx.x; it0 < items; it0 += 256 * U) {
         uint32_t code[U], scale[U];
         int r[U], piece[U];
@@ -122,15 +121,18 @@ __global__ void __launch_bounds__(256) k_mx4_dequantize(const uint32_t* __restri
             rg_store_live<V, ONCE>(x + (row0 + r[u]) * x_stride + piece[u] * V, dim - piece[u] * V, v);
         }
     }
+    }
 }
 
-// Rows to a workgroup of 256 threads when each is `pieces` pieces: kPiecesAhead to a thread where there are rows enough for all compute units.
+// Rows to a workgroup of 256 threads when each is `pieces` pieces: kPiecesAhead to a thread where that makes four workgroups or more for every
+// compute unit, else one (rows of 100 floats: 2.4 M of them packed and back in 464 us, 537 with one to a thread; 40 k 11.6 and 14.0; 1024 rows of 602
+// f16 5.0 and 3.3 to pack).
 int rows_per_group(const rg_ctx* ctx, int64_t n, int pieces) {
-    const int64_t total = n * pieces, full = 256 * kPiecesAhead;
-    int64_t items = total >= (int64_t)ctx->num_cus * 8 * full ? full : 256;
-    items = rg_max64(items, total >> 22);                  // (a launch has less than 2^32 threads)
-    return (int)rg_max64(1, items / pieces);
+    const int64_t full = 256 * kPiecesAhead;
+    return (int)rg_max64(1, (n * pieces >= (int64_t)ctx->num_cus * 4 * full ? full : 256) / pieces);
 }
+// Workgroups for n rows, `rows` at a time (a launch has less than 2^32 threads).
+unsigned row_groups(int64_t n, int rows) { return (unsigned)rg_min64(rg_div_up(n, rows), 1 << 23); }
 
 // ---------------------------------------------------------------- y = rows . weight^T
 // A wavefront makes a tile of 16 R rows by 16 C outputs with the scaled 16 x 16 x 128 matrix instruction: lane 16 q + c holds group
@@ -941,7 +943,7 @@ rg_status rg_mx4_quantize(rg_ctx* ctx, const void* x, rg_dtype x_type, int64_t x
     hipStream_t s = (hipStream_t)stream;
     const int pieces = (int)rg_div_up(dim, kGroup) * (kGroup * rg_type_bytes(x_type) / 16);
     const int rows = rows_per_group(ctx, n, pieces);
-    RG_FOR_TYPE(x_type, k_mx4_quantize<T><<<(unsigned)rg_div_up(n, rows), 256, 0, s>>>((const T*)x, x_stride, n, n_dev, dim, (uint32_t*)packed,
+    RG_FOR_TYPE(x_type, k_mx4_quantize<T><<<row_groups(n, rows), 256, 0, s>>>((const T*)x, x_stride, n, n_dev, dim, (uint32_t*)packed,
                                                                                   packed_stride, pieces, rg_inverse(pieces), rows));
     RG_LAUNCH_CHECK(ctx, "k_mx4_quantize");
     return RG_OK;
@@ -963,7 +965,7 @@ rg_status rg_mx4_dequantize(rg_ctx* ctx, const void* packed, int64_t packed_stri
     const int rows = rows_per_group(ctx, n, pieces);
     RG_FOR_TYPE(x_type, {
         const auto kernel = rg_store_once(x, dim * sizeof(T), x_stride * sizeof(T), n) ? k_mx4_dequantize<T, true> : k_mx4_dequantize<T, false>;
-        kernel<<<(unsigned)rg_div_up(n, rows), 256, 0, s>>>((const uint32_t*)packed, packed_stride, n, n_dev, dim, (T*)x, x_stride, pieces,
+        kernel<<<row_groups(n, rows), 256, 0, s>>>((const uint32_t*)packed, packed_stride, n, n_dev, dim, (T*)x, x_stride, pieces,
                                                            rg_inverse(pieces), rows);
     });
     RG_LAUNCH_CHECK(ctx, "k_mx4_dequantize");

@@ -135,6 +135,24 @@ def test_every_scale_and_code_of_a_packed_row_is_read(ctx):
         assert np.array_equal(f64(back), f64(torch.from_numpy(want).float().to(dtype)), equal_nan=True)
 
 
+def test_room_for_far_more_rows_than_there_are(ctx):
+    """A count of rows up to the largest that is allowed beside a small one on the device: what a workgroup works on does not grow with it."""
+    from paper_2505_10806_amd import binding as B
+    rng = np.random.default_rng(5)
+    live, dim = 40, 65_532
+    x = torch.from_numpy(rng.normal(size=(live, dim))).float()
+    want, values = ref.quantize(f64(x))
+    n_dev = torch.tensor([live], dtype=torch.int32, device=DEV)
+    most = (1 << 31) - 1
+    packed, back = torch.full((live, ref.words(dim)), PAD, device=DEV), torch.full((live, dim), PAD, device=DEV)
+    there = x.to(DEV)
+    stream = torch.cuda.current_stream().cuda_stream
+    assert B._lib.rg_mx4_quantize(ctx._h, there.data_ptr(), 0, dim, most, n_dev.data_ptr(), dim, packed.data_ptr(), ref.words(dim), stream) == 0
+    assert np.array_equal(of_packed(packed, dim), want)
+    assert B._lib.rg_mx4_dequantize(ctx._h, packed.data_ptr(), ref.words(dim), most, n_dev.data_ptr(), dim, back.data_ptr(), 0, dim, stream) == 0
+    assert np.array_equal(f64(back), values)
+
+
 @pytest.mark.parametrize("live", [0, 1, 20, 50, 51])
 def test_counts_on_the_device(ctx, live):
     """Every operator works on min(n, *n_dev) rows and leaves the others alone."""

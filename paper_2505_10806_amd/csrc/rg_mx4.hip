@@ -988,19 +988,27 @@ rg_status rg_mx4_matmul(rg_ctx* ctx, const void* rows, int64_t rows_stride, int6
     hipStream_t s = (hipStream_t)stream;
     const int groups = (dim + kGroup - 1) / kGroup;
     const int steps = (groups + 3) / 4;
+    const int64_t tiles = rg_div_up(n, 16) * rg_div_up(out_dim, 16);
     RG_FOR_TYPE(y_type, {
-        if (n > 256 && steps <= 8) {
-            const bool many = steps <= 2 && out_dim > 64;  // registers for 128 outputs
+        // Up to 32 matrix products to a compute unit each tile has a wavefront of its own: keeping the weight only pays where it is used often (1 row of
+        // 602 numbers times 41 outputs 3.1 us with the weight read by tiles, 4.7 kept; 1024 rows of 256 times 256 3.4 and 6.2; 4096 rows 5.0 and 6.1, 8192
+        // rows 7.2 and 6.7; 8192 rows of 602 times 41 5.0 and 6.6, 16384 rows 6.6 and 6.7, 32768 rows 11.0 and 9.1).
+        if (tiles * steps <= 32 * (int64_t)ctx->num_cus) {
+            const dim3 grid((unsigned)rg_div_up(n, 64), (unsigned)rg_div_up(out_dim, 16));
+            k_mx4_matmul<T, 1, 1><<<grid, 256, 0, s>>>((const uint32_t*)rows, rows_stride, n, n_dev, (const uint32_t*)weight, weight_stride, out_dim,
+                                                       groups, (T*)y, y_stride);
+        } else if (steps <= 8) {
+            // Registers hold 128 outputs of up to 256 numbers (794 k rows of 256 times 256 outputs of bf16: 99 us, 155 with 64 to a wavefront), else 64.
+            const bool many = steps <= 2 && out_dim > 64;
             const int outs = many ? 128 : 64;
             const int slices = out_dim > 2 * outs ? 4 : out_dim > outs ? 2 : 1;
             const int slice_groups = (int)rg_div_up(out_dim, outs * slices);
             // Two workgroups to a compute unit, four where registers hold up to 64 outputs of up to 384 numbers (1.5 M rows of 100 numbers times 47
             // outputs of f16: 58 / 50 / 59 us with 2 / 4 / 8; 794 k of 256 times 256 of bf16: 102 / 115 / 141), and as many whole turns of
             // the compute units as leave three tiles to a wavefront that has fetched the weight (100 k of 602 times 41: 15 us, 20 with one more).
-            const int64_t tiles = rg_div_up(rg_div_up(n, 16), kKeptWaves / slices);
-            const int64_t turns = rg_min64(out_dim <= 64 && steps <= 3 ? 4 : 2, rg_max64(1, tiles / (3 * ctx->num_cus)));
-            const int64_t row_groups = rg_min64(tiles, rg_max64(1, turns * ctx->num_cus / slice_groups));
-            const unsigned grid = (unsigned)(row_groups * slice_groups);
+            const int64_t deep = rg_div_up(rg_div_up(n, 16), kKeptWaves / slices);
+            const int64_t turns = rg_min64(out_dim <= 64 && steps <= 3 ? 4 : 2, rg_max64(1, deep / (3 * ctx->num_cus)));
+            const unsigned grid = (unsigned)(rg_min64(deep, rg_max64(1, turns * ctx->num_cus / slice_groups)) * slice_groups);
             const int last = out_dim % outs, last_bytes = last * (int)sizeof(T);
             const int run_on = out_dim <= outs && y_stride == out_dim && last_bytes % 16 != 0;
             const auto pick = [&](auto once) {             // (ONCE: rows of whole 16 bytes)
@@ -1017,14 +1025,13 @@ rg_status rg_mx4_matmul(rg_ctx* ctx, const void* rows, int64_t rows_stride, int6
             const auto kernel = once ? pick(std::true_type()) : pick(std::false_type());
             kernel<<<grid, kKeptThreads, 0, s>>>((const uint32_t*)rows, rows_stride, n, n_dev, (const uint32_t*)weight, weight_stride, out_dim, groups,
                                                  (T*)y, y_stride, slices, slice_groups, run_on, rg_inverse((uint32_t)rg_div_up(last_bytes, 16)));
-        } else if (n <= 256) {
-            const dim3 grid((unsigned)rg_div_up(n, 64), (unsigned)rg_div_up(out_dim, 16));
-            k_mx4_matmul<T, 1, 1><<<grid, 256, 0, s>>>((const uint32_t*)rows, rows_stride, n, n_dev, (const uint32_t*)weight, weight_stride, out_dim,
-                                                       groups, (T*)y, y_stride);
         } else {
-            k_mx4_matmul<T, 2, 4><<<(unsigned)rg_min64(rg_div_up(n, 128), 1 << 20), 256, 0, s>>>((const uint32_t*)rows, rows_stride, n, n_dev,
-                                                                                                 (const uint32_t*)weight, weight_stride, out_dim,
-                                                                                                 groups, (T*)y, y_stride);
+            // Longer rows, whose weight registers do not hold: read again (from L2) for every 32 rows.  (100 k rows of 1024 numbers times 256 outputs of bf16
+            // this way 131 us, kept 45; of 2048 numbers 267.)  Few rows: workgroups side by side on their outputs (2000 rows of 2048 times 256: 20 us).
+            const int64_t across = rg_min64(rg_div_up(n, 128), 1 << 20);
+            const dim3 grid((unsigned)across, (unsigned)rg_min64(rg_div_up(out_dim, 64), rg_div_up((int64_t)ctx->num_cus * 4, across)));
+            k_mx4_matmul<T, 2, 4><<<grid, 256, 0, s>>>((const uint32_t*)rows, rows_stride, n, n_dev, (const uint32_t*)weight, weight_stride, out_dim,
+                                                       groups, (T*)y, y_stride);
         }
     });
     RG_LAUNCH_CHECK(ctx, "k_mx4_matmul");

@@ -218,6 +218,22 @@ def test_product(ctx, dtype, n, dim, out):
     assert untouched(flat, y)
 
 
+@pytest.mark.parametrize("dtype", ref.TYPES)
+@pytest.mark.parametrize("n,dim,out", [(4096, 256, 250), (4097, 256, 250), (1600, 602, 250), (1650, 602, 250), (500, 1024, 500), (20, 1100, 1030),
+                                       (300, 2050, 600), (5000, 1100, 70), (20_000, 1056, 19), (30_001, 33, 65), (12_000, 602, 41), (9001, 300, 130),
+                                       (6000, 513, 72), (4100, 1024, 72), (10_001, 800, 300), (140_000, 100, 1), (70_000, 31, 23)])
+def test_product_of_many_sizes(ctx, dtype, n, dim, out):
+    """Few rows and many, rows that registers hold and longer ones, results with gaps between their rows and without."""
+    rng = np.random.default_rng(n + dim + out)
+    xb, xv = packed_rows(rng, n, dim)
+    wb, wv = packed_rows(rng, out, dim)
+    flat, y = padded(torch.zeros(n, out), dtype, n % 2 * 3, n % 2)
+    ctx.mx4_matmul(to_packed(xb), n, to_packed(wb), out, dim, y)
+    torch.cuda.synchronize()
+    check(y, xv @ wv.T, sum_allowed(dim, xv, wv, dtype), "y")
+    assert untouched(flat, y)
+
+
 def test_product_of_groups_that_are_not_numbers(ctx):
     """A NaN group of a row makes that row's results NaN and no other's; one of the weight, that output's."""
     rng = np.random.default_rng(5)

@@ -40,16 +40,27 @@ __device__ __forceinline__ void for_chunk(const T* p, int64_t left, F f) {
     }
 }
 
-template <int NW>
+// What another lane of the row of 16 holds.
+template <int CTRL>
+__device__ __forceinline__ double lane_of(double x) {
+    const uint64_t u = __double_as_longlong(x);
+    const uint32_t low = __builtin_amdgcn_update_dpp(0, (int)u, CTRL, 0xF, 0xF, false);
+    const uint32_t high = __builtin_amdgcn_update_dpp(0, (int)(u >> 32), CTRL, 0xF, 0xF, false);
+    return __longlong_as_double((int64_t)((uint64_t)high << 32 | low));
+}
+
+// Sum over the workgroup, the same in each thread; smem holds a double for every 16 of them.  Contains a barrier.
 __device__ __forceinline__ double block_sum(double x, double* smem) {
-#pragma unroll
-    for (int off = RG_WAVE / 2; off > 0; off >>= 1) x += __shfl_xor(x, off, RG_WAVE);
-    __syncthreads();
-    if (rg_lane() == 0) smem[threadIdx.x >> 6] = x;
+    // (between vector registers alone; after a step the lanes of half a group hold the same, so that mirrored lanes do for the other half)
+    x += lane_of<0xB1>(x);                                 // lanes 1, 0, 3, 2 of four
+    x += lane_of<0x4E>(x);                                 // 2, 3, 0, 1
+    x += lane_of<0x141>(x);                                // 7, 6, .. 0 of eight
+    x += lane_of<0x140>(x);                                // 15, 14, .. 0 of sixteen
+    if (rg_lane() % 16 == 0) smem[threadIdx.x >> 4] = x;
     __syncthreads();
     x = 0.0;
 #pragma unroll
-    for (int w = 0; w < NW; ++w) x += smem[w];
+    for (int i = 0; i < kThreads / 16; ++i) x += smem[i];
     return x;
 }
 
@@ -69,7 +80,7 @@ __device__ __forceinline__ Scale scale_of(double norm, float max_norm) {
 
 // parts[workgroup] = the sum of the squares of its chunks.
 __global__ void __launch_bounds__(kThreads) k_squares(ClipList list, double* __restrict__ parts) {
-    __shared__ double smem[kThreads / RG_WAVE];
+    __shared__ double smem[kThreads / 16];
     double sum = 0.0;
     for (int at = blockIdx.x; at < list.chunks; at += gridDim.x) {
         const int t = tensor_of(list, at);
@@ -80,7 +91,7 @@ __global__ void __launch_bounds__(kThreads) k_squares(ClipList list, double* __r
             });
         });
     }
-    sum = block_sum<kThreads / RG_WAVE>(sum, smem);
+    sum = block_sum(sum, smem);
     if (threadIdx.x == 0) parts[blockIdx.x] = sum;
 }
 
@@ -89,10 +100,17 @@ __global__ void __launch_bounds__(kThreads) k_squares(ClipList list, double* __r
 template <bool ONCE>
 __global__ void __launch_bounds__(kThreads) k_clip(ClipList list, const double* __restrict__ parts, int num_parts, float max_norm,
                                                    float* __restrict__ norm_out) {
-    __shared__ double smem[kThreads / RG_WAVE];
+    __shared__ double smem[kThreads / 16];
     double sum = 0.0;
-    for (int i = threadIdx.x; i < num_parts; i += kThreads) sum += parts[i];
-    const double norm = sqrt(block_sum<kThreads / RG_WAVE>(sum, smem));
+    constexpr int U = 8;                                   // on their way together
+    for (int i0 = threadIdx.x; i0 < num_parts; i0 += kThreads * U) {
+        double v[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) v[u] = parts[min(i0 + kThreads * u, num_parts - 1)];
+#pragma unroll
+        for (int u = 0; u < U; ++u) sum += i0 + kThreads * u < num_parts ? v[u] : 0.0;
+    }
+    const double norm = sqrt(block_sum(sum, smem));
     if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = (float)norm;
     const Scale scale = scale_of(norm, max_norm);
     for (int at = list.chunks - 1 - (int)blockIdx.x; at >= 0; at -= gridDim.x) {

@@ -466,7 +466,9 @@ rg_status rg_layer_norm_grad(rg_ctx* ctx, const void* dy, int64_t dy_stride, con
         const Shape shape = row_shape(dim, V, kHeldGrad);
         const int64_t stripes = rg_div_up(dim, 64 * V);
         if (shape.chunks == 0) blocks = rg_max64(1, rg_min64(rg_div_up(n, 16), rg_div_up((int64_t)ctx->num_cus * 8, stripes)));
-        else blocks = rg_max64(1, rg_min64(rg_div_up(n, kGradWaves * (RG_WAVE >> shape.log2L)), (int64_t)ctx->num_cus * 2));
+        // Two workgroups to a compute unit (794 k rows of 256 numbers of bf16 229 / 215 / 239 / 231 us with 1 / 2 / 3 / 4), one where lanes hold several
+        // chunks of a row, whose sums take longer to join (200 k rows of 602 numbers: of bf16 170 / 175 / 180 / 184, of f32 260 / 272 / 271 / 271).
+        else blocks = rg_max64(1, rg_min64(rg_div_up(n, kGradWaves * (RG_WAVE >> shape.log2L)), (int64_t)ctx->num_cus * (shape.chunks > 1 ? 1 : 2)));
         if (sums) {
             const rg_status st = rg_scratch(ctx, ctx->norm_parts, (size_t)blocks * 2 * dim * 4, s, "rg_layer_norm_grad");
             if (st != RG_OK) return st;

@@ -72,7 +72,8 @@ typedef enum {
     RG_ERR_CAPACITY = 2,      /* an output buffer is smaller than the static bound (see rg_blocks_bounds) */
     RG_ERR_OOM = 3,           /* scratch allocation failed */
     RG_ERR_HIP = 4,           /* a HIP runtime call failed; message in rg_last_error */
-    RG_ERR_STATE = 5          /* call not valid in the ctx's current state (rg_gather_run on an unprepared ticket) */
+    RG_ERR_STATE = 5          /* call not valid in the ctx's current state (rg_gather_run on an unprepared ticket; scratch that
+                                * would have to grow while the stream records a graph) */
 } rg_status;
 
 #define RG_TAG_LOCAL 0u
@@ -438,7 +439,10 @@ RG_API rg_status rg_mean_aggregate(rg_ctx* ctx, const int32_t* indptr, const int
  * rg_access_histogram (rows beyond min(n, *n_dev) are neither read nor written and add to no sum).  Every
  * sum is kept in 32 bits or more; a 16-bit result is rounded once, to the nearest.  Results do not
  * depend on timing: the same call gives the same bits.  Inputs and outputs do not overlap unless a
- * call says that they may. */
+ * call says that they may.  rg_mx4_matmul_grad, rg_layer_norm_grad and rg_clip_grad_norm keep partial sums in
+ * scratch of the ctx that grows on demand: calls of one of them are ordered by the caller (one stream does),
+ * and a call that needs more than there is while its stream records a graph returns RG_ERR_STATE and
+ * launches nothing: the same call once before the recording makes room. */
 typedef enum { RG_F32 = 0, RG_BF16 = 1, RG_F16 = 2 } rg_dtype;
 
 /* ---- packed rows: 4-bit numbers with a scale per group of 32 -------------------------------------

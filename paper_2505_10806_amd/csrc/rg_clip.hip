@@ -1,4 +1,6 @@
-// The norm of all gradients together, and clipping by it.
+// The norm of all gradients together, and clipping by it: scale = max_norm / norm where the norm is larger.  Squares are added up in 64 bits.  The norm is
+// known when all numbers have been read, so they are read twice where they are scaled: three passes over memory.  246 M floats: 158 us for the norm (6.2
+// TB/s), 343 for the scaling (5.7 TB/s, reading and writing).  Few numbers: two launches of 3.4 and 4.4 us (462 k); one workgroup in a single launch took 16.
 #include "rg_elements.h"
 
 #include <math.h>
@@ -7,7 +9,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kMostTensors = 64;       // that a launch's arguments describe
-constexpr int kMostParts = 2048;       // workgroups of a launch
+constexpr int kMostParts = 2048;       // workgroups of a launch (246 M floats' norm 321 / 202 / 158 us with 512 / 1024 / 2048)
 // Numbers of a chunk: 8 KB of them, two loads of 16 bytes a thread.  (The last kernel with 4, 8, 16 or 32 KB: 462 k floats 4.7 / 4.6 / 5.3 / 5.9 us,
 // 30 M 40.8 / 39.2 / 40.9 / 42.2.)
 constexpr int log2_chunk(size_t bytes) { return bytes == 4 ? 11 : 12; }

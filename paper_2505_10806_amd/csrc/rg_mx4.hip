@@ -431,7 +431,7 @@ template <typename T, int TF_> struct GradShape {
     static_assert(GROUPS * 16 * TH <= 256 && GROUPS * 16 * TF <= 256, "a thread loads one item of a step");
 };
 
-// Bound by everything at once: 794 k rows, 256 x 256, bf16: 121 us; on copies of an earlier form (137 us) without the loads 99, without the products 106, without the turning
+// Bound by everything at once: 794 k rows, 256 x 256, bf16: 122 us; on copies of an earlier form (137 us) without the loads 99, without the products 106, without the turning
 // 120 (62 at the rate of a large library product, 84 for the bytes).  100 k rows, 256 x 602, f32 (three parts of dy): 100 us, 69 without the products
 // (which are 55 at that rate), 89 without the cutting and turning, 93 without the loads.  Smaller tiles of 128 x 128 took 165 and 114 us (with the join).
 // Four wavefronts load dy, the others codes; all of them multiply.  While step s is multiplied from one half of LDS the other half

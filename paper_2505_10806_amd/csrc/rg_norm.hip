@@ -239,8 +239,8 @@ __global__ void __launch_bounds__(kGradThreads) k_layer_norm_grad(const T* dy, i
                 chunk_numbers<T, V, true>(r.d[i], (l + i * L) * V, dim, d[i]);
             }
 #pragma unroll
-            for (int j = 0; j < V; ++j) {                  // (behind the row's end dy is 0)
-                h[i][j] = (h[i][j] - m) * s;
+            for (int j = 0; j < V; ++j) {                  // (behind the row's end dy is 0, and h: m s alone may be infinite where the row's own h are not)
+                h[i][j] = i + 1 < NC || (l + i * L) * V + j < dim ? (h[i][j] - m) * s : 0.0f;
                 by_gamma[i][j] += d[i][j] * h[i][j];
                 by_beta[i][j] += d[i][j];
                 d[i][j] *= g[i][j];

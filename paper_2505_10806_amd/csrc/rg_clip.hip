@@ -66,7 +66,9 @@ __device__ __forceinline__ double block_sum(double x, double* smem) {
     return x;
 }
 
-// The factor that takes a gradient of this norm to max_norm, in two: a norm beyond the 32-bit range would leave one of few bits.
+// The factor that takes a gradient of this norm to max_norm, in two where it is small: the power of two below it (down to the smallest there is, which is
+// enough for factors that leave anything of a 32-bit number) and a rest of at most 1, so that neither has few bits and what is multiplied by the first is no
+// smaller than the result.
 struct Scale {
     float coarse, fine;
     bool clipped;
@@ -75,7 +77,8 @@ __device__ __forceinline__ Scale scale_of(double norm, float max_norm) {
     Scale s;
     s.clipped = norm > (double)max_norm && norm <= 1.7976931348623157e308;
     const double scale = s.clipped ? (double)max_norm / norm : 1.0;
-    s.coarse = scale < 0x1p-64 ? 0x1p-64f : 1.0f;
+    const int power = (int)(__double_as_longlong(scale) >> 52) - 1022;         // scale in [2^(power - 1), 2^power)
+    s.coarse = power < -64 && scale > 0.0 ? ldexpf(1.0f, max(power, -149)) : 1.0f;
     s.fine = (float)(scale / (double)s.coarse);
     return s;
 }

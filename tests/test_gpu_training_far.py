@@ -37,3 +37,19 @@ def test_layer_norm_gradient_of_rows_far_from_zero(ctx, dtype, dim, given):
     check(dx[far], want, 2 * s[far, None] * u * (g + g.mean(1, keepdims=True)) + ref.stored(want, dtype), "dx")
     check_norm_grad(dx[near], dg, None, dy64[near], x64[near], g64, m[near], s[near], dtype)      # (the far rows add 0 to dgamma)
     check_norm_grad(None, None, db, dy64, x64, g64, m, s, dtype)
+
+
+@pytest.mark.parametrize("dtype", [F32, torch.bfloat16])
+@pytest.mark.parametrize("largest,most", [(1e30, 1e-30), (3e38, 1e-37), (2.0 ** 100, 2.0 ** -91), (2.0 ** 127, 2.0 ** -126), (1e38, 3e-41), (1e25, 1e-20), (1e12, 1e-12)])
+def test_clip_of_norms_far_beyond_the_largest_wanted(ctx, dtype, largest, most):
+    """Factors down to 2^-270: each number within the formula's roundings, or half of the smallest 32-bit number twice where results are below 2^-126."""
+    from paper_2505_10806_amd import binding as B
+    rng = np.random.default_rng(int(np.log2(largest)))
+    grads = [torch.from_numpy(rng.uniform(-1, 1, k) * largest * 2.0 ** -rng.integers(0, 60, k)).to(dtype) for k in (1, 7, 1000, 4099)]
+    grads[0][0] = largest
+    most = float(np.float32(most))
+    norm64, want = ref.clip([f64(g) for g in grads], most)
+    norm, out = torch.empty(1, device=DEV), [torch.empty(g.shape, dtype=dtype, device=DEV) for g in grads]
+    ctx.clip_grad_norm(B.TensorList([g.to(DEV) for g in grads], out), most, norm)
+    for o, w in zip(out, want):
+        check(o, w, 2.0 ** -22 * np.abs(w) + 2.0 ** -149 + ref.stored(w, dtype), "clipped")

@@ -15,6 +15,14 @@ typedef uint32_t rg_u32x4a __attribute__((ext_vector_type(4)));
 constexpr int kGroup = 32;
 constexpr uint32_t kScaleNan = 255;
 
+// Between a wavefront's stores to LDS and its other lanes' loads of them (and the other way round): the memory's order is that of the instructions, so that
+// nothing is waited for, but only the fences keep the compiler to it.
+__device__ __forceinline__ void wave_exchange() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+}
+
 // The scale byte as the float with this exponent: what the conversion instructions read the exponent of (0 stands for 2^-127 and
 // 255 for "not a number" to them, as in the format).
 __device__ __forceinline__ float scale_bits(uint32_t s) { return __uint_as_float(s << 23); }
@@ -315,7 +323,7 @@ __global__ void __launch_bounds__(kKeptThreads, STEPS > 5 ? 2 : 1) k_mx4_matmul_
                 *(rg_u32x4a*)(to + 16 * t + 8 * q) = __builtin_bit_cast(rg_u32x4a, v);
             }
         }
-        __builtin_amdgcn_wave_barrier();
+        wave_exchange();
         const int live = (int)rg_least(16, n_act - 16 * tile);
         const int numbers = run_on ? live * width : width, pieces = run_on ? (numbers + E - 1) / E : live * lanes;
         T* const out = y + 16 * tile * y_stride + h0;
@@ -337,7 +345,7 @@ __global__ void __launch_bounds__(kKeptThreads, STEPS > 5 ? 2 : 1) k_mx4_matmul_
                     if (i < left) there[i] = e[i];
             }
         }
-        __builtin_amdgcn_wave_barrier();
+        wave_exchange();
     }
 }
 
@@ -822,7 +830,7 @@ __global__ void __launch_bounds__(64 * kFewWaves, 2) k_mx4_grad_few(const T* __r
         for (int u = 0; u < 8; ++u) acc[t][u] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
     // lane 16 q + c: rows 4 j + q, columns COLS c .. of dy, word c of the codes
     const auto multiply = [&] {
-        __builtin_amdgcn_wave_barrier();
+        wave_exchange();
         uint32_t code[8];
         float scale[8];
         struct alignas(COLS * sizeof(T)) Cols { uint32_t w[COLS * sizeof(T) / 4]; };
@@ -833,7 +841,7 @@ __global__ void __launch_bounds__(64 * kFewWaves, 2) k_mx4_grad_few(const T* __r
             code[j] = ((const uint32_t*)mine.code[4 * j + q])[c];
             scale[j] = mine.scale[4 * j + q][c >> 2];
         }
-        __builtin_amdgcn_wave_barrier();
+        wave_exchange();
         Frag a[P][COLS];
 #pragma unroll
         for (int t = 0; t < COLS; ++t) {

@@ -11,7 +11,6 @@ template <int N> struct RgPack<float, N> { typedef float type __attribute__((ext
 template <int N> struct RgPack<__bf16, N> { typedef __bf16 type __attribute__((ext_vector_type(N), aligned(2))); };
 template <int N> struct RgPack<_Float16, N> { typedef _Float16 type __attribute__((ext_vector_type(N), aligned(2))); };
 typedef uint32_t rg_u32x4 __attribute__((ext_vector_type(4), aligned(4)));
-typedef uint32_t rg_u32x2 __attribute__((ext_vector_type(2), aligned(4)));
 
 // The first `live` numbers of N from p as they are, the others 0.  (Where not all are there, loads of the last one stand in for those that are
 // not, so that none waits for another.)

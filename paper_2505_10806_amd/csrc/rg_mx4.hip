@@ -15,6 +15,8 @@ typedef uint32_t rg_u32x4a __attribute__((ext_vector_type(4)));
 constexpr int kGroup = 32;
 constexpr uint32_t kScaleNan = 255;
 
+constexpr int kLdsBytes = 160 * 1024;                       // that a workgroup may have
+
 // Between a wavefront's stores to LDS and its other lanes' loads of them (and the other way round): the memory's order is that of the instructions, so that
 // nothing is waited for, but only the fences keep the compiler to it.
 __device__ __forceinline__ void wave_exchange() {
@@ -437,6 +439,7 @@ template <typename T, int TF_> struct GradShape {
     static constexpr int kSums = 4 * 4 * FRAGS * 64;       // what four wavefronts hand to the others at the end
     static constexpr int kLds = 2 * kPieces > kSums ? 2 * kPieces : kSums;
     static_assert(GROUPS * 16 * TH <= 256 && GROUPS * 16 * TF <= 256, "a thread loads one item of a step");
+    static_assert(kLds * 16 <= kLdsBytes, "a workgroup's LDS");
 };
 
 // Bound by everything at once: 794 k rows, 256 x 256, bf16: 122 us; on copies of an earlier form (137 us) without the loads 99, without the products 106, without the turning
@@ -739,6 +742,7 @@ __global__ void __launch_bounds__(64 * kFewWaves, 2) k_mx4_grad_few(const T* __r
         FewLds<T> rows[kFewWaves];
         v4f sums[kFewWaves / 2][COLS * 8][64];
     } lds;
+    static_assert(sizeof(lds) <= kLdsBytes, "a workgroup's LDS");
     const int64_t n_act = rg_rows(n, n_dev);
     const int lane = rg_lane(), c = lane & 15, q = lane >> 4;
     const int wave = threadIdx.x >> 6;

@@ -455,6 +455,8 @@ typedef enum { RG_F32 = 0, RG_BF16 = 1, RG_F16 = 2 } rg_dtype;
  * Quantisation: s = max(0, floor(log2 max|x|) - 2 + 127) over the group, each x / 2^(s - 127) goes to the
  * nearest magnitude (halves to the even code, above 6 to 6, the sign of what becomes 0 is kept).  A group
  * that holds a NaN or an infinity gets s = 255 and codes 0: all of it reads as NaN.
+ * Quantisation makes no s of 253 or 254.  In rows that have them from elsewhere a number may leave the 32-bit range: it unpacks to an
+ * infinity, and the gradients it adds to are not finite; the product takes codes and scales as they are.
  * 1 <= dim <= RG_MX4_MAX_DIM; packed strides are in words of 32 bits. */
 #define RG_MX4_MAX_DIM 65536
 RG_API int64_t rg_mx4_row_words(int32_t dim);      /* 0 if dim is out of range */
@@ -471,9 +473,10 @@ RG_API rg_status rg_mx4_matmul(rg_ctx* ctx, const void* rows, int64_t rows_strid
                                const void* weight, int64_t weight_stride, int32_t out_dim, int32_t dim, void* y,
                                rg_dtype y_type, int64_t y_stride, void* stream);
 /* grad[j][k] = sum_i dy[i][j] rows[i][k]: the gradient of that product to its weight (taken as the numbers it
- * was rounded from: the rounding passes the gradient on).  dy keeps all its bits: a 32-bit number goes through
- * the matrix unit in three parts, one of 16 bits in one or two.  grad: device float[out_dim * grad_stride], overwritten
- * (zeros where there are no rows). */
+ * was rounded from: the rounding passes the gradient on).  dy keeps its bits: a 32-bit number goes through
+ * the matrix unit in three parts of bf16, one of 16 bits in one or two.  Only what a 32-bit number has below 2^-133, the
+ * smallest bf16 number, is cut off (numbers of 2^-110 and more have nothing there).
+ * grad: device float[out_dim * grad_stride], overwritten (zeros where there are no rows). */
 RG_API rg_status rg_mx4_matmul_grad(rg_ctx* ctx, const void* dy, rg_dtype dy_type, int64_t dy_stride, const void* rows,
                                     int64_t rows_stride, int64_t n, const int32_t* n_dev, int32_t out_dim, int32_t dim,
                                     float* grad, int64_t grad_stride, void* stream);
@@ -482,7 +485,8 @@ RG_API rg_status rg_mx4_matmul_grad(rg_ctx* ctx, const void* dy, rg_dtype dy_typ
  * mean_i = sum_k x[i][k] / dim, rstd_i = 1 / sqrt(sum_k (x[i][k] - mean_i)^2 / dim + eps),
  * y[i][k] = (x[i][k] - mean_i) rstd_i gamma[k] + beta[k].
  * x and y: device, of type `type`, and y may be x itself (same stride); gamma, beta: device float[dim], or NULL for 1 and
- * 0; mean, rstd: device float[n], or NULL where no backward pass follows.  eps >= 0. */
+ * 0; mean, rstd: device float[n], or NULL where no backward pass follows.  eps >= 0.  Both sums are taken in 32 bits: a row whose
+ * numbers add up beyond that range has no finite mean, one whose squares do has rstd 0. */
 #define RG_NORM_MAX_DIM 65536
 RG_API rg_status rg_layer_norm(rg_ctx* ctx, const void* x, rg_dtype type, int64_t x_stride, int64_t n, const int32_t* n_dev,
                                int32_t dim, const float* gamma, const float* beta, float eps, void* y, int64_t y_stride,

@@ -354,8 +354,9 @@ __global__ void __launch_bounds__(kKeptThreads, STEPS > 5 ? 2 : 1) k_mx4_matmul_
 // ---------------------------------------------------------------- grad = dy^T . rows
 // The contraction runs over the rows, so the matrix unit wants both operands column by column, eight rows of one column side by side.
 // Threads turn them on their way into LDS: one loads four neighbouring columns of eight rows of dy, or one word of codes (eight
-// columns) of eight rows, and puts pairs of rows together by byte permutations.  4-bit numbers times their scale are bf16 numbers
-// exactly; numbers of dy are cut into bf16 numbers that sum to them exactly (one for bf16, two for f16, three for f32).
+// columns) of eight rows, and puts pairs of rows together by byte permutations.  4-bit numbers times a scale of up to 2^125 (byte 252, the largest that
+// quantisation makes) are bf16 numbers exactly; numbers of dy are cut into bf16 numbers that sum to them exactly (one for bf16, two for f16, three for f32,
+// but for what f32 has below 2^-133, the smallest bf16 number; the matrix unit takes subnormal bf16 numbers as they are).
 
 constexpr uint32_t kLowHalves = 0x05040100u, kHighHalves = 0x07060302u;   // of (later, earlier) as {earlier, later}
 

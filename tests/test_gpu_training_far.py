@@ -53,3 +53,60 @@ def test_clip_of_norms_far_beyond_the_largest_wanted(ctx, dtype, largest, most):
     ctx.clip_grad_norm(B.TensorList([g.to(DEV) for g in grads], out), most, norm)
     for o, w in zip(out, want):
         check(o, w, 2.0 ** -22 * np.abs(w) + 2.0 ** -149 + ref.stored(w, dtype), "clipped")
+
+
+@pytest.mark.parametrize("dtype", ref.TYPES)
+@pytest.mark.parametrize("dim,out", [(64, 40), (64, 70), (256, 70)])
+@pytest.mark.parametrize("scale,size", [(0, 0), (1, 60), (2, 125), (20, 100), (60, 60), (127, 0), (200, -60), (245, -115), (252, -120), (252, -24), (60, -60), (127, -126), (127, -130)])
+def test_gradient_of_far_scales(ctx, dtype, dim, out, scale, size):
+    """Scale bytes from the first to the largest that quantisation makes, times dy of 2^size.  A 32-bit number of dy counts as the next multiple of 2^-133
+    towards 0; results below 2^-126 have roundings of 2^-149 each."""
+    if dtype == torch.float16 and not -24 <= size <= 15:
+        size = max(-24, min(15, size))
+    if scale - 127 + size > 110:
+        size = 0
+    n = 200
+    rng = np.random.default_rng(scale + 300 + size)
+    groups = -(-dim // 32)
+    packed = np.zeros((n, 4 * ref.words(dim)), dtype=np.uint8)
+    packed[:, :16 * groups] = rng.integers(0, 256, size=(n, 16 * groups))
+    packed[:, 16 * groups:17 * groups] = scale
+    values = ref.dequantize(packed, dim)
+    dy = torch.from_numpy(rng.uniform(-1.0, 1.0, (n, out)) * 2.0 ** size).to(dtype)
+    grad = torch.empty(out, dim, device=DEV)
+    ctx.mx4_matmul_grad(dy.to(DEV), torch.from_numpy(packed).view(F32).to(DEV), n, out, dim, grad)
+    d = f64(dy)
+    lost = 2.0 ** -133 * np.abs(values).sum(0)[None, :] if dtype == F32 else 0.0
+    want = d.T @ values
+    assert np.abs(want).max() < 2.0 ** 127
+    check(grad, want, ref.sum_error(n, np.abs(d).T @ np.abs(values)) + lost + (4 * np.sqrt(n) + 8) * 2.0 ** -149, "grad")
+
+
+def test_numbers_of_packed_rows_beyond_the_32_bit_range(ctx):
+    """Scale bytes 253 and 254, which quantisation never makes: what leaves the 32-bit range reads as an infinity, and what that adds to a gradient is not finite;
+    the product takes codes and scales as they are."""
+    n, dim, out = 16, 32, 70
+    packed = np.zeros((n, 20), dtype=np.uint8)
+    packed[:, 0] = np.arange(n)                              # one number of each code to a row, the others 0
+    packed[:, 16] = 252 + np.arange(n) % 3
+    rows = torch.from_numpy(packed).view(F32).to(DEV)
+    exact = ref.dequantize(packed, dim)
+    with np.errstate(over="ignore"):
+        read = exact.astype(np.float32)
+    assert np.isposinf(read).any() and np.isneginf(read).any()
+    back = torch.empty(n, dim, device=DEV)
+    ctx.mx4_dequantize(rows, n, dim, back)
+    assert np.array_equal(back.cpu().numpy(), read)
+    weight = np.zeros((out, 20), dtype=np.uint8)
+    weight[:, 0], weight[:, 16] = 2, 27                      # 2^-100
+    y = torch.empty(n, out, device=DEV)
+    ctx.mx4_matmul(rows, n, torch.from_numpy(weight).view(F32).to(DEV), out, dim, y)
+    assert np.array_equal(f64(y), exact @ ref.dequantize(weight, dim).T)
+    for outs in (out, 40):
+        for i in range(n):
+            grad = torch.empty(outs, dim, device=DEV)
+            dy = torch.full((1, outs), 2.0 ** -100, device=DEV)
+            ctx.mx4_matmul_grad(dy, rows[i:i + 1], 1, outs, dim, grad)
+            finite = np.isfinite(read[i])
+            assert np.array_equal(f64(grad)[:, finite], np.broadcast_to(exact[i, finite] * 2.0 ** -100, (outs, int(finite.sum()))))
+            assert not np.isfinite(f64(grad)[:, ~finite]).any()

@@ -536,7 +536,10 @@ def mx4_rows(n, dim, device, pin_memory=False):
 
 
 class TensorList:
-    """rg_tensor[] over contiguous cuda tensors (kept alive by this object); out: as many, or None to work in place."""
+    """rg_tensor[] over contiguous cuda tensors (kept alive by this object); out: as many, or None to work in place.
+
+    Addresses, sizes and types are taken here, once: a list serves as long as its tensors are the gradients.  A program whose gradients
+    are allocated anew each step makes a list each step, as one kept from an earlier step stands for that step's arrays."""
 
     def __init__(self, tensors, out=None):
         self.tensors = list(tensors)

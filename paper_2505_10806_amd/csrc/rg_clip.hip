@@ -187,6 +187,7 @@ extern "C" rg_status rg_clip_grad_norm(rg_ctx* ctx, const rg_tensor* tensors, in
     if (!single) next = 0;
     do {
         if (!single) fill(list, next);
+        // (where there are more than 16 Mi numbers in all; where each of them lies is not asked: an array has few ends that share 16 bytes with others)
         const auto kernel = rg_store_once(nullptr, 16, 16, numbers / 8) ? k_clip<true> : k_clip<false>;
         kernel<<<grid_of(list), kThreads, 0, s>>>(list, parts, num_parts, max_norm, next == count ? norm : nullptr);
         RG_LAUNCH_CHECK(ctx, "k_clip");

@@ -73,7 +73,9 @@ __device__ __forceinline__ void rg_store(T* p, const float (&v)[N]) {
 }
 
 // Whether results are stored past the caches: more of them than the L2s hold, in rows of whole 16 bytes (246 M clipped numbers 516 -> 490 us, 270 k
-// normalised rows of 256 floats 96 -> 92; rows of 602 numbers of 16 bits, which share 16 bytes with their neighbours, 135 -> 137).
+// normalised rows of 256 floats 96 -> 92; rows of 602 numbers of 16 bits, which share 16 bytes with their neighbours, 135 -> 137).  That the next call reads
+// them does not turn it (a product of 256 outputs and the layer norm of its result, through the caches -> past them: 41 MB 30.1 -> 29.6 us of f32 and 35.1 ->
+// 33.0 of bf16, 61 MB 48.5 -> 44.6, 82 MB 51.3 -> 50.6, 102 MB 68.2 -> 69.7, 123 MB 74.6 -> 75.5, 205 MB 127.9 -> 119.0, 276 MB 169 -> 157, 813 MB 509 -> 482).
 static inline bool rg_store_once(const void* p, int64_t row_bytes, int64_t stride_bytes, int64_t rows) {
     return ((uintptr_t)p | (uintptr_t)row_bytes | (uintptr_t)stride_bytes) % 16 == 0 && row_bytes * rows > (32ll << 20);
 }

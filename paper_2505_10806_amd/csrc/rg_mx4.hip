@@ -31,9 +31,9 @@ __device__ __forceinline__ float scale_bits(uint32_t s) { return __uint_as_float
 
 // ---------------------------------------------------------------- numbers to packed rows
 // s = max(0, E - 2) with E the exponent byte of a group's largest magnitude, codes the numbers times 2^(127 - s), rounded to the nearest of the eight
-// magnitudes (halves to the even code, what is beyond 6 to 6).  Bound by memory: 2.4 M rows of 100 floats, 980 MB in and 167 MB out, take 257 us
-// (4.5 TB/s).  What is stored leaves holes behind rows of less than whole words of 16 bytes, which costs more than the bytes: rows 17 words apart 244 us,
-// 20 apart 272.
+// magnitudes (halves to the even code, what is beyond 6 to 6).  Bound by memory: 2.4 M rows of 100 floats, 980 MB in and 167 MB out, packed into rows 20
+// words apart and unpacked again in turn, take 257 us (4.5 TB/s).  What is stored leaves holes behind rows of less than whole words of 16 bytes, which costs
+// more than the bytes: packed again and again 278 us, 213 into rows 17 words apart (of bf16 182 and 171).
 // A lane takes 16 bytes of a row (4 numbers of 32 bits, 8 of 16), so that a wavefront's loads and stores are one run of bytes; U pieces a thread
 // are on their way together (with one 537 instead of 464 us for these rows and back).  The largest magnitude of a group, as an integer
 // (so that NaN and infinities are the largest of all), goes round its 8 or 4 lanes; the numbers times 2^(127 - s), which is exact or far below the smallest magnitude, are rounded by the conversion instruction.
@@ -443,9 +443,12 @@ template <typename T, int TF_> struct GradShape {
     static_assert(kLds * 16 <= kLdsBytes, "a workgroup's LDS");
 };
 
-// Bound by everything at once: 794 k rows, 256 x 256, bf16: 122 us; on copies of an earlier form (137 us) without the loads 99, without the products 106, without the turning
-// 120 (62 at the rate of a large library product, 84 for the bytes).  100 k rows, 256 x 602, f32 (three parts of dy): 100 us, 69 without the products
-// (which are 55 at that rate), 89 without the cutting and turning, 93 without the loads.  Smaller tiles of 128 x 128 took 165 and 114 us (with the join).
+// Bound by everything at once.  One pass behind the other, with the join: 794 k rows, 256 x 256, bf16 133 to 137 us; on copies of an earlier form (137) without the
+// loads 99, without the products 106, without the turning 120 (62 at the rate of a large library product, 84 for the bytes).  100 k rows, 256 x 602, f32
+// (three parts of dy) 100 to 107 us; of 100, 69 without the products (which are 55 at that rate), 89 without the cutting and turning, 93 without the loads.  Smaller
+// tiles of 128 x 128 took 165 and 114 us.  (Under a tracer, which runs them one by one: 122 to 125 us and 8.4 for the join, 105 and 6.7.)
+// Rows counted on the device: ranges are cut from the room for them, so that workgroups whose range lies behind the count have nothing to do (794 k rows
+// counted in room for 4.3 M: 512 us).
 // Four wavefronts load dy, the others codes; all of them multiply.  While step s is multiplied from one half of LDS the other half
 // is free for step s + 1, whose rows, and those of s + 2, are on their way: one barrier a step.  The WK sums of a piece of the tile are added up in LDS
 // at the end, the ranges' of the rows by a second launch in their order.
@@ -635,7 +638,7 @@ __global__ void __launch_bounds__(kGradThreads, 2) k_mx4_grad(const T* __restric
                 if (s < steps) step(odd, s, 0);
             } else {
                 // dy's parts take longer to make: of the two wavefronts of a SIMD one does it while the other one multiplies; registers for one step's
-                // rows are left.  (In the shadow of the own products: 300 k rows, 256 x 256 of f16 80 us instead of 77, 128 x 64 32 and 30, f32 the same.)
+                // rows are left.  (In the shadow of the own products, on one set of rows: 300 k rows, 256 x 256 of f16 80 us instead of 77, 128 x 64 32 and 30, f32 the same.)
                 Raw raw;
                 load(raw, 0);
                 turn_all(raw, 0, 8);
@@ -712,7 +715,7 @@ __global__ void __launch_bounds__(kGradThreads, 2) k_mx4_grad(const T* __restric
 // neighbouring rows, and adds theirs up in LDS; so the parts that a second launch joins are few.  A row of the tile is 128 bytes of dy,
 // 64 of codes and 4 of scales each: a wavefront loads them 16 bytes a lane and turns them round by way of LDS of its own (without a barrier), and
 // the next 32 rows are on their way meanwhile.  Bound by the latency of these steps where rows are few, else by memory: 100 k rows, 41 x 602, f32:
-// 34 us; 1.5 M rows, 41 x 100, bf16: 59 us (3.8 TB/s).  (Loaded as the lanes need them, 24 accesses of 4 and 8 bytes to a step instead of 7, a step
+// 33 us with the join; 1.5 M rows, 41 x 100, bf16: 59 to 61 us (3.7 TB/s).  (Loaded as the lanes need them, 24 accesses of 4 and 8 bytes to a step instead of 7, a step
 // took a compute unit 400 to 540 cycles.)
 // Workgroups of one range of rows follow each other on one XCD, whose L2 serves all but the first.
 // NARROW: rows of dy are shorter than 16 bytes.
@@ -1072,7 +1075,7 @@ rg_status rg_mx4_matmul(rg_ctx* ctx, const void* rows, int64_t rows_stride, int6
                                                  (T*)y, y_stride, slices, slice_groups, run_on, rg_inverse((uint32_t)rg_div_up(last_bytes, 16)));
         } else {
             // Longer rows, whose weight registers do not hold: read again (from L2) for every 32 rows.  (100 k rows of 1024 numbers times 256 outputs of bf16
-            // this way 131 us, kept 45; of 2048 numbers 267.)  Few rows: workgroups side by side on their outputs (2000 rows of 2048 times 256: 20 us).
+            // this way 131 us, kept 45; of 2048 numbers 280.)  Few rows: workgroups side by side on their outputs (2000 rows of 2048 times 256: 20 us).
             const int64_t across = rg_min64(rg_div_up(n, 128), 1 << 20);
             const dim3 grid((unsigned)across, (unsigned)rg_min64(rg_div_up(out_dim, 64), rg_div_up((int64_t)ctx->num_cus * 4, across)));
             k_mx4_matmul<T, 2, 4><<<grid, 256, 0, s>>>((const uint32_t*)rows, rows_stride, n, n_dev, (const uint32_t*)weight, weight_stride, out_dim,
@@ -1096,8 +1099,9 @@ rg_status rg_mx4_matmul_grad(rg_ctx* ctx, const void* dy, rg_dtype dy_type, int6
     RG_HIP(ctx, hipSetDevice(ctx->device));
     hipStream_t s = (hipStream_t)stream;
     // Few outputs: tiles of 64 (32) outputs, which read each row of dy once and need no turning by the whole workgroup.  (With the join, 100 k rows, 41 x 602,
-    // f32 34 us, 56 by tiles of 128; 1.5 M rows, 41 x 100, bf16 59 and 92, 64 x 100 66 and 78; 128 x 100 97 and 95, 794 k rows, 256 x 256 156 and 137.)
-    // Columns of codes: 256 to a tile, so that dy is turned less often, but 128 where there are no more (1.5 M rows, 256 x 100, bf16 164 us, 217 by 256).
+    // f32 33 us, 57 by tiles of 128; 1.5 M rows, 41 x 100, bf16 61 and 92, 64 x 100 67 and 78, 128 x 100 98 and 95; 300 k rows, 128 x 64, f16 33 and 34.)
+    // Columns of codes: 256 to a tile, so that dy is turned less often, but 128 where there are no more (1.5 M rows of bf16, 256 x 100 163 us, 213 by 256;
+    // 128 x 100 96 and 113; 300 k of f16, 128 x 64 34 and 42).
     const bool few = out_dim <= 64;
     const int tile_h = few ? (dy_type == RG_F32 ? 32 : 64) : 128, tile_f = few || dim <= 128 ? 128 : 256;
     const int waves = few ? kFewWaves : 1, step = few ? 32 : 64;                  // ranges of rows to a workgroup, rows of a step

@@ -6,7 +6,7 @@ namespace {
 // A row lies in the registers of L = 2^log2L lanes: lane l holds chunks l, l + L, ... (NC of them) of V numbers, 16 bytes each.
 template <typename T> struct Chunk { static constexpr int V = 16 / (int)sizeof(T); };
 // Numbers of each of its rows that a lane holds at most: rows of up to 64 times as many stay in registers, longer ones are read again.  (50 k rows of
-// 2048 floats 155 us, 198 if read again, of bf16 85 and 126; the gradient's of 1024 floats 117 and 209, of 1000 bf16 56 and 132.)
+// 2048 floats 154 us, 198 if read again, of bf16 84 and 126; the gradient's of 1024 floats 116 and 209, of 1000 bf16 59 and 132.)
 constexpr int kHeld = 32, kHeldGrad = 16;
 
 // What another lane of the row of 16 holds.
@@ -139,7 +139,7 @@ __global__ void __launch_bounds__(256) k_layer_norm(const T* x, int64_t x_stride
 }
 
 // Rows too long for a wavefront's registers (and those of less than 16 bytes): a workgroup each, read three times, twice of them from the caches (50 k
-// rows of 2056 bf16 171 us).
+// rows of 2056 bf16 165 us).
 template <typename T>
 __global__ void __launch_bounds__(256) k_layer_norm_long(const T* x, int64_t x_stride, int64_t n, const int32_t* __restrict__ n_dev, int dim,
                                                          const float* __restrict__ gamma, const float* __restrict__ beta, float eps, T* y,
@@ -341,7 +341,8 @@ __global__ void __launch_bounds__(256) k_layer_norm_grad_long(const T* dy, int64
     }
 }
 
-// ... and, before dx takes their place, a workgroup to 64 chunks of columns and a range of the rows for the sums.
+// ... and, before dx takes their place, a workgroup to 64 chunks of columns and a range of the rows for the sums.  (Both and the join, 50 k rows of 1032 numbers
+// of bf16: 144 us; of 1000 numbers, which lanes hold, 59.)
 template <typename T>
 __global__ void __launch_bounds__(256) k_layer_norm_sums_long(const T* __restrict__ dy, int64_t dy_stride, const T* __restrict__ x, int64_t x_stride,
                                                               int64_t n, const int32_t* __restrict__ n_dev, int dim, const float* __restrict__ mean,
@@ -473,8 +474,9 @@ rg_status rg_layer_norm_grad(rg_ctx* ctx, const void* dy, int64_t dy_stride, con
         const Shape shape = row_shape(dim, V, kHeldGrad);
         const int64_t stripes = rg_div_up(dim, 64 * V);
         if (shape.chunks == 0) blocks = rg_max64(1, rg_min64(rg_div_up(n, 16), rg_div_up((int64_t)ctx->num_cus * 8, stripes)));
-        // Two workgroups to a compute unit (794 k rows of 256 numbers of bf16 229 / 215 / 239 / 231 us with 1 / 2 / 3 / 4), one where lanes hold several
-        // chunks of a row, whose sums take longer to join (200 k rows of 602 numbers: of bf16 170 / 175 / 180 / 184, of f32 260 / 272 / 271 / 271).
+        // Two workgroups to a compute unit (1.5 M rows of 100 numbers of bf16 197 / 182 / 217 / 188 us with 1 / 2 / 3 / 4, 794 k of 256 215 / 217 / 240 /
+        // 222), one where lanes hold several chunks of a row, whose sums take longer to join (200 k rows of 602 numbers: of bf16 156 / 160 / 166 / 172, of f32
+        // 269 / 278 / 282 / 282).
         else blocks = rg_max64(1, rg_min64(rg_div_up(n, kGradWaves * (RG_WAVE >> shape.log2L)), (int64_t)ctx->num_cus * (shape.chunks > 1 ? 1 : 2)));
         if (sums) {
             const rg_status st = rg_scratch(ctx, ctx->norm_parts, (size_t)blocks * 2 * dim * 4, s, "rg_layer_norm_grad");

@@ -518,6 +518,29 @@ typedef struct {
 RG_API rg_status rg_clip_grad_norm(rg_ctx* ctx, const rg_tensor* tensors, int32_t count, float max_norm, float* norm,
                                    void* stream);
 
+/* ---- learned vectors: lookup and its gradient -----------------------------------------------------
+ * y[i][k] = scale table[ids[i]][k].  An id outside [0, num_rows) is padding: its row of y is zeros, and its row of dy adds to no
+ * gradient (whatever it holds).
+ * table: device, num_rows rows of type table_type; ids: device int32[n], in any order, any of them any number of times; y: device,
+ * of type y_type; products are formed in 32 bits.  1 <= dim <= RG_EMBED_MAX_DIM; 1 <= num_rows < 2^31; scale is not a NaN. */
+#define RG_EMBED_MAX_DIM 65536
+RG_API rg_status rg_embedding(rg_ctx* ctx, const void* table, rg_dtype table_type, int64_t table_stride, int64_t num_rows,
+                              const int32_t* ids, int64_t n, const int32_t* n_dev, int32_t dim, float scale, void* y,
+                              rg_dtype y_type, int64_t y_stride, void* stream);
+/* grad[r][k] = scale sum_{i: ids[i] = r} dy[i][k], a whole table: rows that no id names become zeros.  With add != 0 the sums are added to
+ * what grad holds (a weight's gradient, where the table is that weight too), and rows that no id names are left alone.
+ * The entries are sorted by id, so that every row is written once and its sum has one order.
+ * dy: device, n rows of type dy_type; grad: device, num_rows rows of type grad_type; num_rows >= 0. */
+RG_API rg_status rg_embedding_grad(rg_ctx* ctx, const void* dy, rg_dtype dy_type, int64_t dy_stride, const int32_t* ids, int64_t n,
+                                   const int32_t* n_dev, int32_t dim, int64_t num_rows, float scale, int add, void* grad,
+                                   rg_dtype grad_type, int64_t grad_stride, void* stream);
+/* The same sums for the rows that are named only, for tables much larger than a batch: touched[0 .. *num_touched) = the ids met, ascending,
+ * grad[j] = the sum of touched[j]'s rows.  What lies behind them is left as it was.
+ * touched: device int32[min(n, num_rows)]; num_touched: device int32, written; grad: device float[min(n, num_rows) * grad_stride]. */
+RG_API rg_status rg_embedding_grad_rows(rg_ctx* ctx, const void* dy, rg_dtype dy_type, int64_t dy_stride, const int32_t* ids, int64_t n,
+                                        const int32_t* n_dev, int32_t dim, int64_t num_rows, float scale, float* grad,
+                                        int64_t grad_stride, int32_t* touched, int32_t* num_touched, void* stream);
+
 /* ---- kernel timing for the benchmark ------------------------------------------------------
  * With profiling on, every launch of the listed kernels is bracketed by hipEvents on its own
  * stream.  rg_profile_read synchronises the recorded events and returns the summed duration

@@ -23,7 +23,7 @@ RG_ORDER_ASCENDING, RG_ORDER_FIRST_SEEN = 0, 1
 RG_STATIC_GATHER_MAX_ROWS = 1 << 20
 RG_GATHER_PART_HBM, RG_GATHER_PART_MISS = 1, 2
 RG_F32, RG_BF16, RG_F16 = range(3)
-RG_MX4_MAX_DIM = RG_NORM_MAX_DIM = 65536
+RG_MX4_MAX_DIM = RG_NORM_MAX_DIM = RG_EMBED_MAX_DIM = 65536
 RG_K_GATHER_HBM, RG_K_GATHER_MISS, RG_K_SAMPLE, RG_K_HISTOGRAM, RG_K_CACHE_FILL, RG_K_AGGREGATE = range(6)
 
 _TYPES = {torch.float32: RG_F32, torch.bfloat16: RG_BF16, torch.float16: RG_F16}
@@ -115,6 +115,9 @@ def _load():
     L.rg_layer_norm.argtypes = [c_p, c_p, c_i32, c_i64, c_i64, c_p, c_i32, c_p, c_p, ctypes.c_float, c_p, c_i64, c_p, c_p, c_p]
     L.rg_layer_norm_grad.argtypes = [c_p, c_p, c_i64, c_p, c_i64, c_i32, c_i64, c_p, c_i32, c_p, c_p, c_p, c_p, c_i64, c_p, c_p, c_p]
     L.rg_clip_grad_norm.argtypes = [c_p, ctypes.POINTER(rg_tensor), c_i32, ctypes.c_float, c_p, c_p]
+    L.rg_embedding.argtypes = [c_p, c_p, c_i32, c_i64, c_i64, c_p, c_i64, c_p, c_i32, ctypes.c_float, c_p, c_i32, c_i64, c_p]
+    L.rg_embedding_grad.argtypes = [c_p, c_p, c_i32, c_i64, c_p, c_i64, c_p, c_i32, c_i64, ctypes.c_float, ctypes.c_int, c_p, c_i32, c_i64, c_p]
+    L.rg_embedding_grad_rows.argtypes = [c_p, c_p, c_i32, c_i64, c_p, c_i64, c_p, c_i32, c_i64, ctypes.c_float, c_p, c_i64, c_p, c_p, c_p]
     L.rg_profile_enable.argtypes = [c_p, ctypes.c_int]
     L.rg_profile_reset.argtypes = [c_p]
     L.rg_profile_select.argtypes = [c_p, ctypes.c_uint32]
@@ -125,7 +128,7 @@ def _load():
                  "rg_gather_features_static", "rg_gather_prepare", "rg_gather_run", "rg_mean_aggregate", "rg_profile_enable",
                  "rg_profile_reset", "rg_profile_read", "rg_profile_select", "rg_stream_create", "rg_stream_destroy", "rg_gather_run_part",
                  "rg_mx4_quantize", "rg_mx4_dequantize", "rg_mx4_matmul", "rg_mx4_matmul_grad", "rg_layer_norm", "rg_layer_norm_grad",
-                 "rg_clip_grad_norm"):
+                 "rg_clip_grad_norm", "rg_embedding", "rg_embedding_grad", "rg_embedding_grad_rows"):
         getattr(L, name).restype = ctypes.c_int
     return L
 
@@ -140,6 +143,7 @@ EXPORTED_SYMBOLS = ["rg_create", "rg_destroy", "rg_last_error", "rg_version", "r
                     "rg_stream_create", "rg_stream_destroy", "rg_gather_prepare", "rg_gather_run_part",
                     "rg_gather_run", "rg_mean_aggregate", "rg_mx4_row_words", "rg_mx4_quantize", "rg_mx4_dequantize",
                     "rg_mx4_matmul", "rg_mx4_matmul_grad", "rg_layer_norm", "rg_layer_norm_grad", "rg_clip_grad_norm",
+                    "rg_embedding", "rg_embedding_grad", "rg_embedding_grad_rows",
                     "rg_profile_enable", "rg_profile_select", "rg_profile_reset", "rg_profile_read"]
 
 
@@ -490,6 +494,34 @@ class Context:
         self._check(_lib.rg_clip_grad_norm(self._h, tensors.c_array, tensors.count, float(max_norm),
                                            _numbers(norm, 1, torch.float32, "norm"), _stream_handle(stream)))
         return norm
+
+    # -- rg_embedding / rg_embedding_grad / rg_embedding_grad_rows
+    def embedding(self, table, num_rows, ids, n, dim, y, scale=1.0, n_dev=None, stream=None):
+        """y[:n, :dim] = scale * table[ids[:n]]; ids outside [0, num_rows) give zeros."""
+        pt, st = _rows(table, num_rows, dim, None, "cuda", "table")
+        py, sy = _rows(y, n, dim, None, "cuda", "y")
+        self._check(_lib.rg_embedding(self._h, pt, _type(table, "table"), st, int(num_rows), _numbers(ids, n, torch.int32, "ids"), int(n),
+                                      _count(n_dev), int(dim), float(scale), py, _type(y, "y"), sy, _stream_handle(stream)))
+        return y
+
+    def embedding_grad(self, dy, ids, n, dim, num_rows, grad, scale=1.0, add=False, n_dev=None, stream=None):
+        """grad[:num_rows, :dim] = scale * (sums of dy by id), or that added to what grad holds."""
+        pd, sd = _rows(dy, n, dim, None, "cuda", "dy")
+        pg, sg = _rows(grad, num_rows, dim, None, "cuda", "grad")
+        self._check(_lib.rg_embedding_grad(self._h, pd, _type(dy, "dy"), sd, _numbers(ids, n, torch.int32, "ids"), int(n), _count(n_dev),
+                                           int(dim), int(num_rows), float(scale), 1 if add else 0, pg, _type(grad, "grad"), sg,
+                                           _stream_handle(stream)))
+        return grad
+
+    def embedding_grad_rows(self, dy, ids, n, dim, num_rows, grad, touched, num_touched, scale=1.0, n_dev=None, stream=None):
+        """touched[:num_touched] = the ids met, ascending; grad[j] (float32) = scale * (sum of the rows of dy of touched[j])."""
+        most = min(int(n), int(num_rows))
+        pd, sd = _rows(dy, n, dim, None, "cuda", "dy")
+        pg, sg = _rows(grad, most, dim, torch.float32, "cuda", "grad")
+        self._check(_lib.rg_embedding_grad_rows(self._h, pd, _type(dy, "dy"), sd, _numbers(ids, n, torch.int32, "ids"), int(n), _count(n_dev),
+                                                int(dim), int(num_rows), float(scale), pg, sg, _numbers(touched, most, torch.int32, "touched"),
+                                                _numbers(num_touched, 1, torch.int32, "num_touched"), _stream_handle(stream)))
+        return grad
 
     # -- rg_profile_*
     def profile_enable(self, on=True):

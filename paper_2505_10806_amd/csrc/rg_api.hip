@@ -204,7 +204,7 @@ void rg_destroy(rg_ctx* ctx) {
     (void)hipDeviceSynchronize();
     RgBuf* bufs[] = {&ctx->visited, &ctx->marked, &ctx->slice_marks, &ctx->pos, &ctx->chunk_sum, &ctx->row_start, &ctx->row_deg, &ctx->first_key, &ctx->seen, &ctx->sched_pairs, &ctx->sched_late, &ctx->sched_buckets,
                      &ctx->hist_bounds, &ctx->topk_ctl, &ctx->topk_blk, &ctx->topk_caps, &ctx->pf_list, &ctx->pf_ctl, &ctx->plan_cursor, &ctx->claim_bits, &ctx->claim_blk, &ctx->gather_src, &ctx->miss_list,
-                     &ctx->gather_ctl, &ctx->mx4_parts, &ctx->norm_parts, &ctx->clip_parts};
+                     &ctx->gather_ctl, &ctx->mx4_parts, &ctx->norm_parts, &ctx->clip_parts, &ctx->embed_parts, &ctx->loss_parts};
     for (RgBuf* b : bufs)
         if (b->p) (void)hipFree(b->p);
     for (RgBuf& b : ctx->rank)

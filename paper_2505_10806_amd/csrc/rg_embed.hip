@@ -1,0 +1,517 @@
+// Rows of a table by id, and the gradient of the rows that were looked up, summed by id.
+#include "rg_elements.h"
+
+namespace {
+
+constexpr int kThreads = 256;
+
+// What lanes of a wavefront exchange through LDS stands between these: they execute together.
+__device__ __forceinline__ void wave_exchange() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+}
+
+// V numbers of a row from column `col`, in 32 bits (SHORT: of rows shorter than V).
+template <int V, bool SHORT, typename T>
+__device__ __forceinline__ typename RgPack<T, V>::type load_chunk(const T* row, int col, int dim) {
+    if constexpr (SHORT) return rg_load_raw<V>(row + col, dim - col);
+    else return rg_load_row<V>(row, col, dim);
+}
+template <int V, bool SHORT, typename P>
+__device__ __forceinline__ void chunk_numbers(const P& a, int col, int dim, float (&v)[V]) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = (float)a[i];
+    if (!SHORT) rg_row_end<V>(v, col, dim);
+}
+
+// ---------------------------------------------------------------- lookup
+// y[i] = scale table[ids[i]].  A workgroup takes `group` rows and deals their chunks of V numbers to its threads, kAhead of them on their way at a time: rows
+// of any length fill the lanes.  Bound by memory.
+constexpr int kAhead = 4;
+
+template <typename T, typename U, int V, bool SHORT, bool ONCE>
+__global__ void __launch_bounds__(kThreads) k_embedding(const T* __restrict__ table, int64_t table_stride, int num_rows, const int32_t* __restrict__ ids,
+                                                        int64_t n, const int32_t* __restrict__ n_dev, int dim, int chunks, uint32_t inverse, int group,
+                                                        float scale, U* __restrict__ y, int64_t y_stride) {
+    const int64_t n_act = rg_rows(n, n_dev);
+    for (int64_t first = (int64_t)blockIdx.x * group; first < n_act; first += (int64_t)gridDim.x * group) {
+        const int total = (int)rg_least(group, n_act - first) * chunks;
+        for (int i0 = threadIdx.x; i0 < total; i0 += kThreads * kAhead) {
+            int row[kAhead], col[kAhead], id[kAhead];
+            typename RgPack<T, V>::type a[kAhead];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                const int i = min(i0 + u * kThreads, total - 1);
+                row[u] = (int)rg_divide((uint32_t)i, inverse);
+                col[u] = (i - row[u] * chunks) * V;
+                id[u] = ids[first + row[u]];
+            }
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {             // (padding reads row 0, and is cleared below)
+                const int from = (uint32_t)id[u] < (uint32_t)num_rows ? id[u] : 0;
+                a[u] = load_chunk<V, SHORT>(table + from * table_stride, col[u], dim);
+            }
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                if (i0 + u * kThreads >= total) break;
+                float v[V];
+                chunk_numbers<V, SHORT>(a[u], col[u], dim, v);
+                const bool there = (uint32_t)id[u] < (uint32_t)num_rows;
+#pragma unroll
+                for (int j = 0; j < V; ++j) v[j] = there ? v[j] * scale : 0.0f;
+                rg_store_live<V, ONCE>(y + (first + row[u]) * y_stride + col[u], dim - col[u], v);
+            }
+        }
+    }
+}
+
+// ---------------------------------------------------------------- ids in order
+// The gradient's sums run over the entries sorted by id, entries of an id in their own order, so that the same call adds in the same order each time.  Least
+// digit first, eight bits a pass; padding gets the id behind the last row and comes to lie behind all others.
+struct Entry {
+    uint32_t id, at;
+};
+
+constexpr int kDigits = 256, kRounds = 4, kTile = kThreads * kRounds, kSortWaves = kThreads / RG_WAVE;
+
+__device__ __forceinline__ Entry entry_of(const Entry* from, const int32_t* ids, int64_t i, uint32_t num_rows) {
+    if (from) return from[i];
+    const uint32_t id = (uint32_t)ids[i];
+    return {id < num_rows ? id : num_rows, (uint32_t)i};
+}
+
+// Lanes that hold the same digit as this one.
+__device__ __forceinline__ uint64_t same_digit(uint32_t digit, bool live) {
+    uint64_t mask = __ballot(live);
+#pragma unroll
+    for (int b = 0; b < 8; ++b) {
+        const uint64_t set = __ballot(digit >> b & 1);
+        mask &= digit >> b & 1 ? set : ~set;
+    }
+    return mask;
+}
+
+__global__ void __launch_bounds__(kThreads) k_sort_count(const Entry* __restrict__ from, const int32_t* __restrict__ ids, int64_t n,
+                                                         const int32_t* __restrict__ n_dev, uint32_t num_rows, int shift, int64_t per_block,
+                                                         int32_t* __restrict__ counts) {
+    __shared__ int32_t bins[kDigits];
+    bins[threadIdx.x] = 0;
+    __syncthreads();
+    const int64_t first = (int64_t)blockIdx.x * per_block, last = rg_least(first + per_block, rg_rows(n, n_dev));
+    for (int64_t i = first + threadIdx.x; i < last; i += kThreads) atomicAdd(&bins[entry_of(from, ids, i, num_rows).id >> shift & 255], 1);
+    __syncthreads();
+    counts[(int64_t)threadIdx.x * gridDim.x + blockIdx.x] = bins[threadIdx.x];
+}
+
+// Each digit's counts become its entries in front of every block; totals[digit] = all of them.
+__global__ void __launch_bounds__(kThreads) k_sort_scan(int32_t* __restrict__ counts, int blocks, int32_t* __restrict__ totals) {
+    __shared__ int smem[kSortWaves + 1];
+    int32_t* row = counts + (int64_t)blockIdx.x * blocks;
+    int before = 0;
+    for (int b0 = 0; b0 < blocks; b0 += kThreads) {
+        const int b = b0 + threadIdx.x;
+        const int x = b < blocks ? row[b] : 0;
+        int total;
+        const int excl = rg_block_excl_scan<kSortWaves>(x, smem, &total);
+        if (b < blocks) row[b] = before + excl;
+        before += total;
+    }
+    if (threadIdx.x == 0) totals[blockIdx.x] = before;
+}
+
+__global__ void __launch_bounds__(kThreads) k_sort_scatter(const Entry* __restrict__ from, const int32_t* __restrict__ ids, int64_t n,
+                                                           const int32_t* __restrict__ n_dev, uint32_t num_rows, int shift, int64_t per_block,
+                                                           const int32_t* __restrict__ counts, const int32_t* __restrict__ totals, Entry* __restrict__ to) {
+    __shared__ int smem[kSortWaves + 1];
+    __shared__ int32_t next[kDigits], met[kSortWaves][kDigits];
+    const int wave = threadIdx.x >> 6, lane = rg_lane();
+    int all;
+    const int base = rg_block_excl_scan<kSortWaves>(totals[threadIdx.x], smem, &all);
+    next[threadIdx.x] = base + counts[(int64_t)threadIdx.x * gridDim.x + blockIdx.x];
+    const int64_t first = (int64_t)blockIdx.x * per_block, last = rg_least(first + per_block, rg_rows(n, n_dev));
+    for (int64_t tile = first; tile < last; tile += kTile) {
+#pragma unroll
+        for (int w = 0; w < kSortWaves; ++w) met[w][threadIdx.x] = 0;
+        __syncthreads();
+        Entry e[kRounds];
+        int rank[kRounds];
+#pragma unroll
+        for (int r = 0; r < kRounds; ++r) {
+            const int64_t i = tile + wave * (kRounds * RG_WAVE) + r * RG_WAVE + lane;
+            e[r] = i < last ? entry_of(from, ids, i, num_rows) : Entry{0, 0};
+        }
+#pragma unroll
+        for (int r = 0; r < kRounds; ++r) {
+            const int64_t i = tile + wave * (kRounds * RG_WAVE) + r * RG_WAVE + lane;
+            const uint32_t digit = e[r].id >> shift & 255;
+            const uint64_t same = same_digit(digit, i < last);
+            const int below = __popcll(same & ((1ull << lane) - 1));
+            const int so_far = met[wave][digit];
+            wave_exchange();
+            if (i < last && below == 0) met[wave][digit] = so_far + __popcll(same);
+            wave_exchange();
+            rank[r] = so_far + below;
+        }
+        __syncthreads();
+        int at = next[threadIdx.x];
+#pragma unroll
+        for (int w = 0; w < kSortWaves; ++w) {
+            const int here = met[w][threadIdx.x];
+            met[w][threadIdx.x] = at;
+            at += here;
+        }
+        next[threadIdx.x] = at;
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < kRounds; ++r) {
+            const int64_t i = tile + wave * (kRounds * RG_WAVE) + r * RG_WAVE + lane;
+            if (i < last) to[met[wave][e[r].id >> shift & 255] + rank[r]] = e[r];
+        }
+        __syncthreads();
+    }
+}
+
+// ---------------------------------------------------------------- sums by id
+// The sorted entries are cut into pieces of `size`.  An id is met for the first time in a piece where its first entry lies.
+__device__ __forceinline__ bool opens(const Entry* sorted, int64_t i) { return i == 0 || sorted[i - 1].id != sorted[i].id; }
+
+__global__ void __launch_bounds__(kThreads) k_count_ids(const Entry* __restrict__ sorted, int64_t n, const int32_t* __restrict__ n_dev, uint32_t num_rows,
+                                                        int64_t size, int pieces, int32_t* __restrict__ before) {
+    const int64_t n_act = rg_rows(n, n_dev);
+    const int piece = blockIdx.x * (kThreads / RG_WAVE) + (threadIdx.x >> 6);
+    if (piece >= pieces) return;
+    const int64_t first = piece * size, last = rg_least(first + size, n_act);
+    int count = 0;
+    for (int64_t i0 = first; i0 < last; i0 += RG_WAVE) {
+        const int64_t i = i0 + rg_lane();
+        count += __popcll(__ballot(i < last && sorted[i].id < num_rows && opens(sorted, i)));
+    }
+    if (rg_lane() == 0) before[piece] = count;
+}
+
+// before[piece] = ids met in front of it, before[pieces] and *num_touched = all.
+__global__ void __launch_bounds__(1024) k_scan_ids(int32_t* __restrict__ before, int pieces, int32_t* __restrict__ num_touched) {
+    __shared__ int smem[17];
+    int so_far = 0;
+    for (int p0 = 0; p0 < pieces; p0 += 1024) {
+        const int p = p0 + threadIdx.x;
+        const int x = p < pieces ? before[p] : 0;
+        int total;
+        const int excl = rg_block_excl_scan<16>(x, smem, &total);
+        if (p < pieces) before[p] = so_far + excl;
+        so_far += total;
+    }
+    if (threadIdx.x == 0) {
+        before[pieces] = so_far;
+        *num_touched = so_far;
+    }
+}
+
+// Where sums go: the table's rows (LIST false), or a row for each id met.
+template <typename U>
+struct Target {
+    U* grad;
+    int64_t stride;
+    int32_t* touched;          // or NULL
+    const int32_t* before;
+    float scale;
+    int add;
+};
+
+template <int V, typename U>
+__device__ __forceinline__ void put_sum(const Target<U>& t, int64_t row, int col, int dim, float (&v)[V]) {
+    U* to = t.grad + row * t.stride + col;
+#pragma unroll
+    for (int j = 0; j < V; ++j) v[j] *= t.scale;
+    if (t.add) {
+        float old[V];
+        rg_load_head<V>(to, dim - col, old);
+#pragma unroll
+        for (int j = 0; j < V; ++j) v[j] += old[j];
+    }
+    rg_store_live<V>(to, dim - col, v);
+}
+
+// A group of 2^log2L lanes walks a piece, a chunk of V columns to a lane (blockIdx.y: which 2^log2L chunks), kWalk rows on their way at a time, and adds up in 32 bits.
+// The sums of an id that opens and ends in the piece are final; what belongs to an id that opened before goes to parts[piece][0], to one that goes on
+// behind to parts[piece][1], for k_join_pieces.  Bound by memory.
+constexpr int kWalk = 4;
+
+template <typename T, typename U, int V, bool SHORT>
+__global__ void __launch_bounds__(kThreads) k_sum_pieces(const T* __restrict__ dy, int64_t dy_stride, const Entry* __restrict__ sorted, int64_t n,
+                                                         const int32_t* __restrict__ n_dev, uint32_t num_rows, int dim, int64_t size, int pieces, int log2L,
+                                                         Target<U> t, float* __restrict__ parts) {
+    const int64_t n_act = rg_rows(n, n_dev);
+    const int piece = (int)(((int64_t)blockIdx.x * kThreads + threadIdx.x) >> log2L), l = threadIdx.x & ((1 << log2L) - 1);
+    const int col = ((blockIdx.y << log2L) + l) * V;
+    const int64_t first = piece * size, last = rg_least(first + size, n_act);
+    if (piece >= pieces || first >= last || col >= dim) return;
+    uint32_t id = sorted[first].id;
+    bool open = first > 0 && sorted[first - 1].id == id;   // the first id's sums are not whole
+    int64_t row = t.touched ? (int64_t)t.before[piece] - (open ? 1 : 0) : id;
+    float sum[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) sum[j] = 0.0f;
+    float* part = parts + (int64_t)piece * 2 * dim + col;
+    if (t.touched && !open && id < num_rows && col == 0) t.touched[row] = (int32_t)id;
+    for (int64_t i = first; i < last && id < num_rows; i += kWalk) {
+        Entry e[kWalk];
+        typename RgPack<T, V>::type a[kWalk];
+#pragma unroll
+        for (int u = 0; u < kWalk; ++u) e[u] = sorted[rg_least(i + u, last - 1)];
+#pragma unroll
+        for (int u = 0; u < kWalk; ++u) a[u] = load_chunk<V, SHORT>(dy + (int64_t)e[u].at * dy_stride, col, dim);
+#pragma unroll
+        for (int u = 0; u < kWalk; ++u) {
+            if (i + u >= last || id >= num_rows) break;
+            if (e[u].id != id) {
+                if (open) rg_store_live<V>(part, dim - col, sum);
+                else put_sum<V>(t, row, col, dim, sum);
+                open = false;
+                id = e[u].id;
+                if (id >= num_rows) break;
+                row = t.touched ? row + 1 : id;
+                if (t.touched && col == 0) t.touched[row] = (int32_t)id;
+#pragma unroll
+                for (int j = 0; j < V; ++j) sum[j] = 0.0f;
+            }
+            float v[V];
+            chunk_numbers<V, SHORT>(a[u], col, dim, v);
+#pragma unroll
+            for (int j = 0; j < V; ++j) sum[j] += v[j];
+        }
+    }
+    if (id >= num_rows) return;
+    if (open) rg_store_live<V>(part, dim - col, sum);
+    else if (last < n_act && sorted[last].id == id) rg_store_live<V>(part + dim, dim - col, sum);
+    else put_sum<V>(t, row, col, dim, sum);
+}
+
+// The sums of ids whose entries lie in several pieces: a workgroup for the piece in which one of them opens (nothing to do for most), 64 chunks of 4 columns
+// (blockIdx.y: which), four runs of pieces side by side.
+template <typename U>
+__global__ void __launch_bounds__(kThreads) k_join_pieces(const Entry* __restrict__ sorted, int64_t n, const int32_t* __restrict__ n_dev, uint32_t num_rows, int dim,
+                                                          int64_t size, int pieces, Target<U> t, const float* __restrict__ parts) {
+    constexpr int V = 4, RUNS = kThreads / RG_WAVE;
+    __shared__ float runs[RUNS][RG_WAVE * V];
+    const int64_t n_act = rg_rows(n, n_dev);
+    const int lane = rg_lane(), run = threadIdx.x >> 6, col = (blockIdx.y * RG_WAVE + lane) * V;
+    for (int piece = blockIdx.x; piece + 1 < pieces; piece += gridDim.x) {
+        const int64_t first = piece * size, next = first + size;
+        if (next >= n_act) return;
+        const uint32_t id = sorted[next].id;
+        if (id >= num_rows || sorted[next - 1].id != id || (sorted[first].id == id && !opens(sorted, first))) continue;
+        // pieces behind this one that begin with the id: those in front of the first entry of a larger one
+        int64_t lo = next, hi = n_act;                     // (sorted[lo].id == id; larger from hi on)
+        while (hi - lo > 1) {
+            const int64_t mid = (lo + hi) >> 1;
+            if (sorted[mid].id == id) lo = mid; else hi = mid;
+        }
+        const int from = piece + 1, to = (int)(lo / size) + 1, per = (to - from + RUNS - 1) / RUNS;
+        const int start = from + run * per, stop = min(start + per, to);
+        float sum[V] = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (col < dim) {
+#pragma unroll 4
+            for (int p = start; p < stop; ++p) {
+                float v[V];
+                rg_load_head<V>(parts + (int64_t)p * 2 * dim + col, dim - col, v);
+#pragma unroll
+                for (int j = 0; j < V; ++j) sum[j] += v[j];
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < V; ++j) runs[run][lane * V + j] = sum[j];
+        __syncthreads();
+        if (run == 0 && col < dim) {
+            rg_load_head<V>(parts + ((int64_t)piece * 2 + 1) * dim + col, dim - col, sum);
+#pragma unroll
+            for (int r = 0; r < RUNS; ++r)
+#pragma unroll
+                for (int j = 0; j < V; ++j) sum[j] += runs[r][lane * V + j];
+            put_sum<V>(t, t.touched ? (int64_t)t.before[piece + 1] - 1 : id, col, dim, sum);
+        }
+        __syncthreads();
+    }
+}
+
+// Rows of zeros.
+template <typename U, bool ONCE>
+__global__ void __launch_bounds__(kThreads) k_clear_rows(U* __restrict__ grad, int64_t stride, int64_t num_rows, int dim, int chunks) {
+    constexpr int V = 16 / (int)sizeof(U);
+    const float zero[V] = {};
+    const int64_t total = num_rows * chunks;
+    for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < total; i += (int64_t)gridDim.x * kThreads) {
+        const int64_t row = i / chunks;
+        const int col = (int)(i - row * chunks) * V;
+        rg_store_live<V, ONCE>(grad + row * stride + col, dim - col, zero);
+    }
+}
+
+bool aligned(const void* p, int bytes) { return (uintptr_t)p % (uintptr_t)bytes == 0; }
+
+constexpr int64_t kMostRows = (1ll << 31) - 1;
+
+template <typename U>
+void clear_rows(rg_ctx* ctx, U* grad, int64_t stride, int64_t num_rows, int dim, hipStream_t s) {
+    const int chunks = (int)rg_div_up(dim, 16 / (int)sizeof(U));
+    const unsigned grid = (unsigned)rg_min64(rg_div_up(num_rows * chunks, kThreads), (int64_t)ctx->num_cus * 32);
+    const auto kernel = rg_store_once(grad, (int64_t)dim * sizeof(U), stride * (int64_t)sizeof(U), num_rows) ? k_clear_rows<U, true> : k_clear_rows<U, false>;
+    kernel<<<grid, kThreads, 0, s>>>(grad, stride, num_rows, dim, chunks);
+}
+
+// The gradient's two forms: a whole table (touched NULL), or the rows met.
+template <typename U>
+rg_status sum_by_id(rg_ctx* ctx, const char* who, const void* dy, rg_dtype dy_type, int64_t dy_stride, const int32_t* ids, int64_t n, const int32_t* n_dev,
+                    int dim, int64_t num_rows, float scale, U* grad, int64_t grad_stride, int add, int32_t* touched, int32_t* num_touched, hipStream_t s) {
+    if (!touched && !add && n == 0) { clear_rows(ctx, grad, grad_stride, num_rows, dim, s); return RG_OK; }
+    // pieces of 16 entries or more, and as many of them as fill the device
+    const int most = (int)rg_max64(1024, rg_min64(16384, (1ll << 23) / dim));
+    const int64_t size = rg_max64(16, rg_div_up(n, most));
+    const int pieces = (int)rg_div_up(n, size);
+    int bits = 1;
+    while (bits < 31 && num_rows >> bits) ++bits;          // ids 0 .. num_rows, padding the last
+    const int passes = (bits + 7) / 8;
+    const int64_t per_block = kTile * rg_max64(1, rg_div_up(n, (int64_t)kTile * 4096));
+    const int blocks = (int)rg_div_up(n, per_block);
+    // scratch: two lists of entries, counts, totals, ids in front of the pieces, sums of parts
+    const size_t list = (size_t)rg_div_up(n * (int64_t)sizeof(Entry), 256) * 256;
+    const size_t counts_bytes = (size_t)rg_div_up((int64_t)kDigits * (blocks + 1) * 4, 256) * 256, before_bytes = (size_t)rg_div_up((pieces + 1) * 4ll, 256) * 256;
+    const rg_status st = rg_scratch(ctx, ctx->embed_parts, 2 * list + counts_bytes + before_bytes + (size_t)pieces * 2 * dim * 4, s, who);
+    if (st != RG_OK) return st;
+    char* at = (char*)ctx->embed_parts.p;
+    Entry* lists[2] = {(Entry*)at, (Entry*)(at + list)};
+    int32_t* counts = (int32_t*)(at + 2 * list);
+    int32_t* totals = counts + (int64_t)kDigits * blocks;
+    int32_t* before = (int32_t*)(at + 2 * list + counts_bytes);
+    float* parts = (float*)(at + 2 * list + counts_bytes + before_bytes);
+    if (!touched && !add) clear_rows(ctx, grad, grad_stride, num_rows, dim, s);
+    const Entry* from = nullptr;
+    for (int pass = 0; pass < passes; ++pass) {
+        Entry* to = lists[pass & 1];
+        k_sort_count<<<blocks, kThreads, 0, s>>>(from, ids, n, n_dev, (uint32_t)num_rows, pass * 8, per_block, counts);
+        k_sort_scan<<<kDigits, kThreads, 0, s>>>(counts, blocks, totals);
+        k_sort_scatter<<<blocks, kThreads, 0, s>>>(from, ids, n, n_dev, (uint32_t)num_rows, pass * 8, per_block, counts, totals, to);
+        from = to;
+    }
+    RG_LAUNCH_CHECK(ctx, "k_sort_scatter");
+    if (touched) {
+        k_count_ids<<<(unsigned)rg_div_up(pieces, kThreads / RG_WAVE), kThreads, 0, s>>>(from, n, n_dev, (uint32_t)num_rows, size, pieces, before);
+        k_scan_ids<<<1, 1024, 0, s>>>(before, pieces, num_touched);
+        RG_LAUNCH_CHECK(ctx, "k_scan_ids");
+    }
+    const Target<U> t = {grad, grad_stride, touched, before, scale, add};
+    RG_FOR_TYPE(dy_type, {
+        constexpr int V = 16 / (int)sizeof(T);
+        const int chunks = (int)rg_div_up(dim, V);
+        int log2L = 0;
+        while (log2L < 6 && 1 << log2L < chunks) ++log2L;
+        const dim3 grid((unsigned)rg_div_up((int64_t)pieces << log2L, kThreads), (unsigned)rg_div_up(chunks, 1 << log2L));
+        const auto kernel = dim < V ? k_sum_pieces<T, U, V, true> : k_sum_pieces<T, U, V, false>;
+        kernel<<<grid, kThreads, 0, s>>>((const T*)dy, dy_stride, from, n, n_dev, (uint32_t)num_rows, dim, size, pieces, log2L, t, parts);
+    });
+    RG_LAUNCH_CHECK(ctx, "k_sum_pieces");
+    if (pieces > 1) {
+        k_join_pieces<U><<<dim3((unsigned)rg_min64(pieces, 4096), (unsigned)rg_div_up(dim, RG_WAVE * 4)), kThreads, 0, s>>>(
+            from, n, n_dev, (uint32_t)num_rows, dim, size, pieces, t, parts);
+        RG_LAUNCH_CHECK(ctx, "k_join_pieces");
+    }
+    return RG_OK;
+}
+
+rg_status check_grad(rg_ctx* ctx, const char* who, const void* dy, rg_dtype dy_type, int64_t dy_stride, const int32_t* ids, int64_t n, int32_t dim,
+                     int64_t num_rows, float scale) {
+    RG_REQUIRE(ctx, n >= 0 && n <= kMostRows, "%s: n = %lld out of range", who, (long long)n);
+    RG_REQUIRE(ctx, dim >= 1 && dim <= RG_EMBED_MAX_DIM, "%s: dim = %d not in [1,%d]", who, dim, RG_EMBED_MAX_DIM);
+    RG_REQUIRE(ctx, num_rows >= 0 && num_rows <= kMostRows, "%s: num_rows = %lld out of range", who, (long long)num_rows);
+    RG_REQUIRE(ctx, rg_type_known(dy_type), "%s: unknown type %d", who, (int)dy_type);
+    RG_REQUIRE(ctx, dy_stride >= dim, "%s: bad stride", who);
+    RG_REQUIRE(ctx, scale == scale, "%s: scale is not a number", who);
+    RG_REQUIRE(ctx, n == 0 || (dy && ids), "%s: null pointer", who);
+    RG_REQUIRE(ctx, aligned(dy, rg_type_bytes(dy_type)) && aligned(ids, 4), "%s: pointer not aligned to its numbers", who);
+    return RG_OK;
+}
+
+__global__ void k_no_ids(int32_t* num_touched) { *num_touched = 0; }
+
+}  // namespace
+
+extern "C" {
+
+rg_status rg_embedding(rg_ctx* ctx, const void* table, rg_dtype table_type, int64_t table_stride, int64_t num_rows, const int32_t* ids, int64_t n,
+                       const int32_t* n_dev, int32_t dim, float scale, void* y, rg_dtype y_type, int64_t y_stride, void* stream) {
+    if (!ctx) return RG_ERR_INVALID_ARG;
+    RG_REQUIRE(ctx, n >= 0 && n <= kMostRows, "rg_embedding: n = %lld out of range", (long long)n);
+    RG_REQUIRE(ctx, dim >= 1 && dim <= RG_EMBED_MAX_DIM, "rg_embedding: dim = %d not in [1,%d]", dim, RG_EMBED_MAX_DIM);
+    RG_REQUIRE(ctx, num_rows >= 1 && num_rows <= kMostRows, "rg_embedding: num_rows = %lld out of range", (long long)num_rows);
+    RG_REQUIRE(ctx, rg_type_known(table_type) && rg_type_known(y_type), "rg_embedding: unknown type");
+    RG_REQUIRE(ctx, table_stride >= dim && y_stride >= dim, "rg_embedding: bad stride");
+    RG_REQUIRE(ctx, scale == scale, "rg_embedding: scale is not a number");
+    if (n == 0) return RG_OK;
+    RG_REQUIRE(ctx, table && ids && y, "rg_embedding: null pointer");
+    RG_REQUIRE(ctx, aligned(table, rg_type_bytes(table_type)) && aligned(ids, 4) && aligned(y, rg_type_bytes(y_type)),
+               "rg_embedding: pointer not aligned to its numbers");
+    RG_HIP(ctx, hipSetDevice(ctx->device));
+    hipStream_t s = (hipStream_t)stream;
+    const bool once = rg_store_once(y, (int64_t)dim * rg_type_bytes(y_type), y_stride * rg_type_bytes(y_type), n);
+    const auto launch = [&](auto t, auto u) {
+        typedef decltype(t) T;
+        typedef decltype(u) U;
+        constexpr int V = 16 / (int)(sizeof(T) < sizeof(U) ? sizeof(T) : sizeof(U));
+        const int chunks = (int)rg_div_up(dim, V), group = (int)rg_max64(1, kThreads * kAhead / chunks);
+        const auto kernel = dim < V ? k_embedding<T, U, V, true, false> : once ? k_embedding<T, U, V, false, true> : k_embedding<T, U, V, false, false>;
+        kernel<<<(unsigned)rg_min64(rg_div_up(n, group), 1 << 22), kThreads, 0, s>>>((const T*)table, table_stride, (int)num_rows, ids, n, n_dev, dim, chunks,
+                                                                                     rg_inverse((uint32_t)chunks), group, scale, (U*)y, y_stride);
+    };
+    RG_FOR_TYPE(table_type, {
+        const T t = {};
+        if (y_type == RG_F32) launch(t, float());
+        else if (y_type == RG_BF16) launch(t, __bf16());
+        else launch(t, _Float16());
+    });
+    RG_LAUNCH_CHECK(ctx, "k_embedding");
+    return RG_OK;
+}
+
+rg_status rg_embedding_grad(rg_ctx* ctx, const void* dy, rg_dtype dy_type, int64_t dy_stride, const int32_t* ids, int64_t n, const int32_t* n_dev,
+                            int32_t dim, int64_t num_rows, float scale, int add, void* grad, rg_dtype grad_type, int64_t grad_stride, void* stream) {
+    if (!ctx) return RG_ERR_INVALID_ARG;
+    const rg_status bad = check_grad(ctx, "rg_embedding_grad", dy, dy_type, dy_stride, ids, n, dim, num_rows, scale);
+    if (bad != RG_OK) return bad;
+    RG_REQUIRE(ctx, rg_type_known(grad_type), "rg_embedding_grad: unknown type %d", (int)grad_type);
+    RG_REQUIRE(ctx, grad_stride >= dim, "rg_embedding_grad: bad stride");
+    if (num_rows == 0 || (add && n == 0)) return RG_OK;
+    RG_REQUIRE(ctx, grad, "rg_embedding_grad: null pointer");
+    RG_REQUIRE(ctx, aligned(grad, rg_type_bytes(grad_type)), "rg_embedding_grad: pointer not aligned to its numbers");
+    RG_HIP(ctx, hipSetDevice(ctx->device));
+    hipStream_t s = (hipStream_t)stream;
+    const auto sums = [&](auto u) {
+        typedef decltype(u) U;
+        return sum_by_id<U>(ctx, "rg_embedding_grad", dy, dy_type, dy_stride, ids, n, n_dev, dim, num_rows, scale, (U*)grad, grad_stride, add, nullptr, nullptr, s);
+    };
+    const rg_status st = grad_type == RG_F32 ? sums(float()) : grad_type == RG_BF16 ? sums(__bf16()) : sums(_Float16());
+    if (st != RG_OK) return st;
+    RG_LAUNCH_CHECK(ctx, "k_clear_rows");
+    return RG_OK;
+}
+
+rg_status rg_embedding_grad_rows(rg_ctx* ctx, const void* dy, rg_dtype dy_type, int64_t dy_stride, const int32_t* ids, int64_t n, const int32_t* n_dev,
+                                 int32_t dim, int64_t num_rows, float scale, float* grad, int64_t grad_stride, int32_t* touched, int32_t* num_touched,
+                                 void* stream) {
+    if (!ctx) return RG_ERR_INVALID_ARG;
+    const rg_status bad = check_grad(ctx, "rg_embedding_grad_rows", dy, dy_type, dy_stride, ids, n, dim, num_rows, scale);
+    if (bad != RG_OK) return bad;
+    RG_REQUIRE(ctx, grad_stride >= dim, "rg_embedding_grad_rows: bad stride");
+    RG_REQUIRE(ctx, num_touched && (n == 0 || num_rows == 0 || (grad && touched)), "rg_embedding_grad_rows: null pointer");
+    RG_REQUIRE(ctx, aligned(grad, 4) && aligned(touched, 4) && aligned(num_touched, 4), "rg_embedding_grad_rows: pointer not aligned to its numbers");
+    RG_HIP(ctx, hipSetDevice(ctx->device));
+    hipStream_t s = (hipStream_t)stream;
+    if (n == 0 || num_rows == 0) {
+        k_no_ids<<<1, 1, 0, s>>>(num_touched);
+        RG_LAUNCH_CHECK(ctx, "k_no_ids");
+        return RG_OK;
+    }
+    return sum_by_id<float>(ctx, "rg_embedding_grad_rows", dy, dy_type, dy_stride, ids, n, n_dev, dim, num_rows, scale, grad, grad_stride, 0, touched, num_touched, s);
+}
+
+}  // extern "C"

@@ -94,8 +94,9 @@ struct rg_ctx {
     void* static_scratch = nullptr;   // device address of the library's file-scope gather scratch on ctx->device
     std::vector<hipStream_t> streams;   // streams made by rg_stream_create and not yet destroyed (rg_destroy takes the rest)
 
-    // training-step scratch: sums of parts of the rows, or of the tensors, that a second launch joins
-    RgBuf mx4_parts, norm_parts, clip_parts;
+    // training-step scratch: sums of parts of the rows, or of the tensors, that a second launch joins; with them the lookup gradient's ids in order
+    // and the loss's packed operands
+    RgBuf mx4_parts, norm_parts, clip_parts, embed_parts, loss_parts;
 
     // profiling
     bool profiling = false;

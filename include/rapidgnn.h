@@ -439,8 +439,9 @@ RG_API rg_status rg_mean_aggregate(rg_ctx* ctx, const int32_t* indptr, const int
  * rg_access_histogram (rows beyond min(n, *n_dev) are neither read nor written and add to no sum).  Every
  * sum is kept in 32 bits or more; a 16-bit result is rounded once, to the nearest.  Results do not
  * depend on timing: the same call gives the same bits.  Inputs and outputs do not overlap unless a
- * call says that they may.  rg_mx4_matmul_grad, rg_layer_norm_grad and rg_clip_grad_norm keep partial sums in
- * scratch of the ctx that grows on demand: calls of one of them are ordered by the caller (one stream does),
+ * call says that they may.  rg_mx4_matmul_grad, rg_layer_norm_grad, rg_clip_grad_norm, the gradients of rg_embedding and both
+ * calls of rg_cross_entropy keep partial sums in scratch of the ctx that grows on demand: calls of one of them (both gradients of rg_embedding
+ * together, rg_cross_entropy and its gradient together) are ordered by the caller (one stream does),
  * and a call that needs more than there is while its stream records a graph returns RG_ERR_STATE and
  * launches nothing: the same call once before the recording makes room. */
 typedef enum { RG_F32 = 0, RG_BF16 = 1, RG_F16 = 2 } rg_dtype;
@@ -540,6 +541,29 @@ RG_API rg_status rg_embedding_grad(rg_ctx* ctx, const void* dy, rg_dtype dy_type
 RG_API rg_status rg_embedding_grad_rows(rg_ctx* ctx, const void* dy, rg_dtype dy_type, int64_t dy_stride, const int32_t* ids, int64_t n,
                                         const int32_t* n_dev, int32_t dim, int64_t num_rows, float scale, float* grad,
                                         int64_t grad_stride, int32_t* touched, int32_t* num_touched, void* stream);
+
+/* ---- softmax cross entropy over the rows of a weight -----------------------------------------------
+ * With z[i][c] = sum_k x[i][k] weight[c][k]:  lse_i = log sum_c exp z[i][c],  loss_i = lse_i - z[i][labels[i]].
+ * A classifier's last product and its loss in one, for a data set's classes or for all nodes as classes: nothing of size n by classes is
+ * stored.  A row whose label lies outside [0, classes) does not count: its loss and lse are 0, whatever it holds.
+ * x: device, n rows of type `type`; weight: device, `classes` rows of the same type; labels: device int32[n]; loss, lse: device float[n],
+ * either may be NULL (not wanted).  1 <= dim <= RG_LOSS_MAX_DIM; classes >= 1.
+ * Products and sums are the matrix unit's, in 32 bits; 32-bit numbers go through it in three parts of bf16, and what they have below 2^-133
+ * is cut off.  A row whose z are not all finite, or -infinity, has no finite lse; an infinity among 32-bit numbers gives NaN. */
+#define RG_LOSS_MAX_DIM 65536
+RG_API rg_status rg_cross_entropy(rg_ctx* ctx, const void* x, rg_dtype type, int64_t x_stride, int64_t n, const int32_t* n_dev,
+                                  int32_t dim, const void* weight, int64_t weight_stride, int32_t classes, const int32_t* labels,
+                                  float* loss, float* lse, void* stream);
+/* Its gradients.  With share_i = scale dloss[i] (dloss NULL: scale) and g[i][c] = exp(z[i][c] - lse_i) - [c = labels[i]]:
+ * dx[i][k] = share_i sum_c g[i][c] weight[c][k],  dweight[c][k] = sum_i share_i g[i][c] x[i][k].
+ * lse: the forward pass's.  Rows that do not count get a dx of zeros and add nothing to dweight; their lse, dloss and x may hold anything.
+ * z is formed anew.  For 16-bit types g is rounded to `type` for its products, whose sums are in 32 bits.
+ * dx, dweight: device, of type `type`, overwritten (dweight: zeros where there are no rows); each may be NULL (not wanted).  Neither
+ * overlaps an input.  scale is not a NaN. */
+RG_API rg_status rg_cross_entropy_grad(rg_ctx* ctx, const void* x, rg_dtype type, int64_t x_stride, int64_t n, const int32_t* n_dev,
+                                       int32_t dim, const void* weight, int64_t weight_stride, int32_t classes, const int32_t* labels,
+                                       const float* lse, const float* dloss, float scale, void* dx, int64_t dx_stride,
+                                       void* dweight, int64_t dweight_stride, void* stream);
 
 /* ---- kernel timing for the benchmark ------------------------------------------------------
  * With profiling on, every launch of the listed kernels is bracketed by hipEvents on its own

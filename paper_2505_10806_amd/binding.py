@@ -23,7 +23,7 @@ RG_ORDER_ASCENDING, RG_ORDER_FIRST_SEEN = 0, 1
 RG_STATIC_GATHER_MAX_ROWS = 1 << 20
 RG_GATHER_PART_HBM, RG_GATHER_PART_MISS = 1, 2
 RG_F32, RG_BF16, RG_F16 = range(3)
-RG_MX4_MAX_DIM = RG_NORM_MAX_DIM = RG_EMBED_MAX_DIM = 65536
+RG_MX4_MAX_DIM = RG_NORM_MAX_DIM = RG_EMBED_MAX_DIM = RG_LOSS_MAX_DIM = 65536
 RG_K_GATHER_HBM, RG_K_GATHER_MISS, RG_K_SAMPLE, RG_K_HISTOGRAM, RG_K_CACHE_FILL, RG_K_AGGREGATE = range(6)
 
 _TYPES = {torch.float32: RG_F32, torch.bfloat16: RG_BF16, torch.float16: RG_F16}
@@ -118,6 +118,9 @@ def _load():
     L.rg_embedding.argtypes = [c_p, c_p, c_i32, c_i64, c_i64, c_p, c_i64, c_p, c_i32, ctypes.c_float, c_p, c_i32, c_i64, c_p]
     L.rg_embedding_grad.argtypes = [c_p, c_p, c_i32, c_i64, c_p, c_i64, c_p, c_i32, c_i64, ctypes.c_float, ctypes.c_int, c_p, c_i32, c_i64, c_p]
     L.rg_embedding_grad_rows.argtypes = [c_p, c_p, c_i32, c_i64, c_p, c_i64, c_p, c_i32, c_i64, ctypes.c_float, c_p, c_i64, c_p, c_p, c_p]
+    L.rg_cross_entropy.argtypes = [c_p, c_p, c_i32, c_i64, c_i64, c_p, c_i32, c_p, c_i64, c_i32, c_p, c_p, c_p, c_p]
+    L.rg_cross_entropy_grad.argtypes = [c_p, c_p, c_i32, c_i64, c_i64, c_p, c_i32, c_p, c_i64, c_i32, c_p, c_p, c_p, ctypes.c_float, c_p, c_i64,
+                                        c_p, c_i64, c_p]
     L.rg_profile_enable.argtypes = [c_p, ctypes.c_int]
     L.rg_profile_reset.argtypes = [c_p]
     L.rg_profile_select.argtypes = [c_p, ctypes.c_uint32]
@@ -128,7 +131,8 @@ def _load():
                  "rg_gather_features_static", "rg_gather_prepare", "rg_gather_run", "rg_mean_aggregate", "rg_profile_enable",
                  "rg_profile_reset", "rg_profile_read", "rg_profile_select", "rg_stream_create", "rg_stream_destroy", "rg_gather_run_part",
                  "rg_mx4_quantize", "rg_mx4_dequantize", "rg_mx4_matmul", "rg_mx4_matmul_grad", "rg_layer_norm", "rg_layer_norm_grad",
-                 "rg_clip_grad_norm", "rg_embedding", "rg_embedding_grad", "rg_embedding_grad_rows"):
+                 "rg_clip_grad_norm", "rg_embedding", "rg_embedding_grad", "rg_embedding_grad_rows",
+                 "rg_cross_entropy", "rg_cross_entropy_grad"):
         getattr(L, name).restype = ctypes.c_int
     return L
 
@@ -143,7 +147,7 @@ EXPORTED_SYMBOLS = ["rg_create", "rg_destroy", "rg_last_error", "rg_version", "r
                     "rg_stream_create", "rg_stream_destroy", "rg_gather_prepare", "rg_gather_run_part",
                     "rg_gather_run", "rg_mean_aggregate", "rg_mx4_row_words", "rg_mx4_quantize", "rg_mx4_dequantize",
                     "rg_mx4_matmul", "rg_mx4_matmul_grad", "rg_layer_norm", "rg_layer_norm_grad", "rg_clip_grad_norm",
-                    "rg_embedding", "rg_embedding_grad", "rg_embedding_grad_rows",
+                    "rg_embedding", "rg_embedding_grad", "rg_embedding_grad_rows", "rg_cross_entropy", "rg_cross_entropy_grad",
                     "rg_profile_enable", "rg_profile_select", "rg_profile_reset", "rg_profile_read"]
 
 
@@ -522,6 +526,28 @@ class Context:
                                                 int(dim), int(num_rows), float(scale), pg, sg, _numbers(touched, most, torch.int32, "touched"),
                                                 _numbers(num_touched, 1, torch.int32, "num_touched"), _stream_handle(stream)))
         return grad
+
+    # -- rg_cross_entropy / rg_cross_entropy_grad
+    def cross_entropy(self, x, n, dim, weight, classes, labels, loss, lse, n_dev=None, stream=None):
+        """loss[:n] and lse[:n] (float32, either None) of softmax cross entropy of x . weight^T against int32 labels."""
+        px, sx = _rows(x, n, dim, None, "cuda", "x")
+        pw, sw = _rows(weight, classes, dim, x.dtype, "cuda", "weight")
+        f32 = torch.float32
+        self._check(_lib.rg_cross_entropy(self._h, px, _type(x, "x"), sx, int(n), _count(n_dev), int(dim), pw, sw, int(classes),
+                                          _numbers(labels, n, torch.int32, "labels"), _numbers(loss, n, f32, "loss"), _numbers(lse, n, f32, "lse"),
+                                          _stream_handle(stream)))
+        return loss
+
+    def cross_entropy_grad(self, x, n, dim, weight, classes, labels, lse, dx, dweight, dloss=None, scale=1.0, n_dev=None, stream=None):
+        """dx[:n, :dim] and dweight[:classes, :dim] (of x's type, either None) of sum(scale * dloss * loss); dloss None: ones."""
+        px, sx = _rows(x, n, dim, None, "cuda", "x")
+        pw, sw = _rows(weight, classes, dim, x.dtype, "cuda", "weight")
+        pd, sd = _rows(dx, n, dim, x.dtype, "cuda", "dx")
+        pg, sg = _rows(dweight, classes, dim, x.dtype, "cuda", "dweight")
+        f32 = torch.float32
+        self._check(_lib.rg_cross_entropy_grad(self._h, px, _type(x, "x"), sx, int(n), _count(n_dev), int(dim), pw, sw, int(classes),
+                                               _numbers(labels, n, torch.int32, "labels"), _numbers(lse, n, f32, "lse"),
+                                               _numbers(dloss, n, f32, "dloss"), float(scale), pd, sd, pg, sg, _stream_handle(stream)))
 
     # -- rg_profile_*
     def profile_enable(self, on=True):

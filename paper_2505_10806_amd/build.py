@@ -12,7 +12,7 @@ BUILD_DIR = os.path.join(HERE, "_build")
 LIB_PATH = os.path.join(HERE, "librapidgnn.so")
 
 SOURCES = ["rg_api.hip", "rg_sampler.hip", "rg_cache.hip", "rg_gather.hip", "rg_aggregate.hip", "rg_mx4.hip", "rg_norm.hip",
-           "rg_clip.hip", "rg_embed.hip"]
+           "rg_clip.hip", "rg_embed.hip", "rg_loss.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden",

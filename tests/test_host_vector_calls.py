@@ -19,6 +19,13 @@ def grad(dy=None, type=F32, stride=100, ids=None, n=10, n_dev=0, dim=100, rows=5
 def grad_rows(dy=None, type=F32, stride=100, ids=None, n=10, n_dev=0, dim=100, rows=50, scale=1.0, grad=None, grad_stride=100, touched=None, met=None, stream=0):
     return lib.rg_embedding_grad_rows(c, a(dy), i32(type), i64(stride), a(ids), i64(n), p(n_dev), i32(dim), i64(rows), f32(scale), a(grad), i64(grad_stride),
                                       a(touched), a(met), p(stream))
+def loss(x=None, type=F32, stride=100, n=10, n_dev=0, dim=100, weight=None, weight_stride=100, classes=30, labels=None, loss=None, lse=None, stream=0):
+    return lib.rg_cross_entropy(c, a(x), i32(type), i64(stride), i64(n), p(n_dev), i32(dim), a(weight), i64(weight_stride), i32(classes), a(labels), a(loss),
+                                a(lse), p(stream))
+def loss_grad(x=None, type=F32, stride=100, n=10, n_dev=0, dim=100, weight=None, weight_stride=100, classes=30, labels=None, lse=None, dloss=0, scale=1.0,
+              dx=None, dx_stride=100, dweight=None, dweight_stride=100, stream=0):
+    return lib.rg_cross_entropy_grad(c, a(x), i32(type), i64(stride), i64(n), p(n_dev), i32(dim), a(weight), i64(weight_stride), i32(classes), a(labels),
+                                     a(lse), p(dloss), f32(scale), a(dx), i64(dx_stride), a(dweight), i64(dweight_stride), p(stream))
 def refuses(status, text):
     assert status == INVALID and text in message(), (status, message())
     assert not kernels()
@@ -69,7 +76,42 @@ assert lookup(table=0x7002, type=F16, y=0x7006, y_type=BF16) == OK
 ''')
 
 
-@pytest.mark.parametrize("call,small,large", [("grad", "n=3000", "n=2_000_000"), ("grad_rows", "n=3000", "n=2_000_000, rows=1 << 30")])
+def test_loss_and_its_gradient_refuse():
+    run(r'''
+for call in (loss, loss_grad):
+    refuses(call(n=-1), "out of range")
+    refuses(call(n=1 << 31), "out of range")
+    refuses(call(dim=0), "dim")
+    refuses(call(dim=65537, stride=70000, weight_stride=70000), "dim")
+    refuses(call(classes=0), "classes")
+    refuses(call(classes=-5), "classes")
+    refuses(call(type=3), "type")
+    refuses(call(stride=99), "stride")
+    refuses(call(weight_stride=99), "stride")
+    refuses(call(x=0), "null")
+    refuses(call(weight=0), "null")
+    refuses(call(labels=0), "null")
+    refuses(call(x=0x7002), "aligned")
+    refuses(call(weight=0x7001, type=BF16), "aligned")
+    refuses(call(labels=0x7002), "aligned")
+    refuses(call(lse=0x7002), "aligned")
+refuses(loss(loss=0x7002), "aligned")
+refuses(loss_grad(lse=0), "null")
+refuses(loss_grad(dloss=0x7002), "aligned")
+refuses(loss_grad(dx_stride=99), "stride")
+refuses(loss_grad(dweight_stride=99), "stride")
+refuses(loss_grad(dx=0x7002), "aligned")
+refuses(loss_grad(dweight=0x7001, type=F16), "aligned")
+refuses(loss_grad(scale=math.nan), "scale")
+assert loss(n=0, x=0, weight=0, labels=0) == OK and loss(loss=0, lse=0) == OK and loss_grad(dx=0, dweight=0) == OK and not kernels()
+assert loss_grad(n=0, x=0, weight=0, labels=0, lse=0, dweight=0) == OK and not kernels()
+assert loss_grad(n=0, x=0, weight=0, labels=0, lse=0) == OK and len(kernels()) == 1       # zeros
+assert loss(x=0x7002, weight=0x7006, type=F16) == OK and loss_grad(dx=0, dx_stride=0) == OK and loss_grad(dweight=0, dweight_stride=0) == OK
+''')
+
+
+@pytest.mark.parametrize("call,small,large", [("grad", "n=3000", "n=2_000_000"), ("grad_rows", "n=3000", "n=2_000_000, rows=1 << 30"),
+                                              ("loss", "n=300", "n=20_000, classes=100_000"), ("loss_grad", "n=300", "n=20_000, classes=100_000")])
 def test_scratch_outlives_graphs_and_is_refused_inside_them(call, small, large):
     """Growing keeps what a graph may hold; inside a recording a call that wants more is refused before it launches anything."""
     run(rf'''
@@ -97,16 +139,16 @@ assert rt.memory_held() == 0 and held > 0
 def test_calls_without_memory_fail_and_work_again():
     run(r'''
 rt.limit_memory(rt.memory_held())
-for call in (grad, grad_rows):
+for call in (grad, grad_rows, loss, loss_grad):
     assert call() == OOM and not kernels(), message()
 rt.limit_memory((1 << 64) - 1)
-for call in (grad, grad_rows):
+for call in (grad, grad_rows, loss, loss_grad):
     assert call() == OK
 ''')
 
 
 def test_launches_stay_within_the_device_limits():
-    """Largest sizes: less than 2^32 threads to a launch, LDS within 64 KiB."""
+    """Largest sizes: less than 2^32 threads to a launch, LDS that is asked for at a launch within 64 KiB."""
     run(r'''
 N = (1 << 31) - 1
 for dim in (1, 100, 65536):
@@ -114,6 +156,11 @@ for dim in (1, 100, 65536):
         assert lookup(n=N, rows=N, dim=dim, stride=dim, y_stride=dim, type=t) == OK
         assert grad(n=N, rows=N, dim=dim, stride=dim, grad_stride=dim, type=t) == OK and grad_rows(n=N, rows=N, dim=dim, stride=dim, grad_stride=dim, type=t) == OK
         assert grad(n=1, rows=N, dim=dim, stride=dim, grad_stride=dim, type=t) == OK and grad(n=0, rows=N, dim=dim, grad_stride=dim, stride=dim) == OK
+for dim, most in ((1, N), (100, 1 << 27), (300, 1 << 25), (65536, 100_000)):
+    for t in (F32, BF16):
+        for n, classes in ((most, 1), (1, most), (1 << 20, 1 << 20) if dim < 65536 else (3000, 3000), (1, 1)):
+            assert loss(n=n, classes=classes, dim=dim, stride=dim, weight_stride=dim, type=t) == OK
+            assert loss_grad(n=n, classes=classes, dim=dim, stride=dim, weight_stride=dim, dx_stride=dim, dweight_stride=dim, type=t) == OK
 for line in log("launch"):
     at = line.rsplit(" ", 5)
     x, y, block, lds = (int(v) for v in at[1:5])

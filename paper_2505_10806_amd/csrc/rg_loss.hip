@@ -27,7 +27,7 @@ template <> struct Part<_Float16> { typedef _Float16 type; static constexpr int 
 
 constexpr int kCols = 128, kRowBytes = kCols * 2;           // of a staged tile
 constexpr int kSteps = kCols / 16;                          // matrix products to its columns
-constexpr int kWaves = 4, kThreads = 64 * kWaves;
+constexpr int kWaves = 8, kThreads = 64 * kWaves, kOwners = 32 * kWaves;      // rows that a workgroup owns
 constexpr float kLog2e = 1.44269504088896340736f;
 enum { LOSS = 0, DX = 1, DW = 2 };
 
@@ -82,29 +82,40 @@ __device__ __forceinline__ typename RgPack<T, 8>::type load_eight(const T* row, 
     if (!SHORT || dim >= 8) return rg_load_row<8>(row, col, dim);
     return rg_load_raw<8>(row + col, dim - col);
 }
-// Them as parts (zeros if the row does not count).
-template <bool SHORT, typename T>
-__device__ __forceinline__ void row_parts(const typename RgPack<T, 8>::type& raw, int col, int dim, bool counts, Words4 (&w)[Part<T>::P]) {
+// Them as parts.  TAIL: they may reach over the row's end.
+template <bool TAIL, bool SHORT, typename T>
+__device__ __forceinline__ void row_parts(const typename RgPack<T, 8>::type& raw, int col, int dim, Words4 (&w)[Part<T>::P]) {
     if constexpr (Part<T>::P == 1) {
-        T v[8];
+        uint32_t x[4];
+        __builtin_memcpy(x, &raw, 16);
+        if (TAIL && (!SHORT || dim >= 8)) {                // what was loaded from `over` numbers further left moves down by as many, zeros after it
+            const int over = col - min(col, dim - 8);
+            if (dim % 8 != 0) {
+                const bool four = over & 4, two = over & 2;
+                x[0] = four ? x[2] : x[0];
+                x[1] = four ? x[3] : x[1];
+                x[2] = four ? 0 : x[2];
+                x[3] = four ? 0 : x[3];
+                x[0] = two ? x[1] : x[0];
+                x[1] = two ? x[2] : x[1];
+                x[2] = two ? x[3] : x[2];
+                x[3] = two ? 0 : x[3];
+                const uint32_t odd = 2 * (over & 1);
+                x[0] = __builtin_amdgcn_alignbyte(x[1], x[0], odd);
+                x[1] = __builtin_amdgcn_alignbyte(x[2], x[1], odd);
+                x[2] = __builtin_amdgcn_alignbyte(x[3], x[2], odd);
+                x[3] = __builtin_amdgcn_alignbyte(0, x[3], odd);
+            }
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = raw[j];
-        if (!SHORT || dim >= 8) rg_row_end<8>(v, col, dim);
-        typedef T Eight __attribute__((ext_vector_type(8)));
-        Eight e;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) e[j] = v[j];
-        w[0] = __builtin_bit_cast(Words4, e);
+            for (int j = 0; j < 4; ++j) x[j] = over < 8 ? x[j] : 0;
+        }
+        w[0] = Words4{x[0], x[1], x[2], x[3]};
     } else {
         float v[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = raw[j];
-        if (!SHORT || dim >= 8) rg_row_end<8>(v, col, dim);
+        if (TAIL && (!SHORT || dim >= 8)) rg_row_end<8>(v, col, dim);
         cut<T>(v, w);
-    }
-    if (!counts) {
-#pragma unroll
-        for (int p = 0; p < Part<T>::P; ++p) w[p] = Words4{0, 0, 0, 0};
     }
 }
 
@@ -157,28 +168,34 @@ struct Job {
     float* parts;              // else [split][owned row][dim]
 };
 
-// STEPS: 16 columns each, of rows of up to 256 numbers; 0: any, in chunks.  HOLD: the owned rows stay in registers.
-template <typename T, int MODE, int OB, int NB, int STEPS, bool HOLD>
+// STEPS: 16 columns each, of rows of up to 256 numbers; 0: any, in chunks of 128 columns.
+template <typename T, int MODE, int NB, int STEPS>
 __global__ void __launch_bounds__(kThreads, 2) k_softmax_rows(const Job job) {
     typedef Part<T> S;
     typedef typename S::type E;
-    constexpr int P = S::P, ROWS = S::ROWS, OWNERS = kWaves * 32 * OB, ITEMS = ROWS * 16 / kThreads, SB = ROWS / 32;
-    __shared__ __attribute__((aligned(16))) char staged[2][P][ROWS * kRowBytes];
-    __shared__ __attribute__((aligned(16))) float row_lse[2][ROWS], row_share[2][ROWS];
-    __shared__ __attribute__((aligned(16))) int row_label[2][ROWS];
+    constexpr int P = S::P, ROWS = S::ROWS, SB = ROWS / 32, GROUPS = ROWS / 16;
+    // HOLD: the owned rows stay in registers.  PIPE: the exponentials of a tile are formed between the products of the next one's z, so that the vector and the
+    // matrix units work side by side; for that the tile stays in LDS for its second product while two more arrive.
+    constexpr bool HOLD = P == 1 && STEPS > 0 && (STEPS <= kSteps || MODE == LOSS), PIPE = STEPS > 0 && (STEPS <= kSteps || HOLD);
+    constexpr int CHUNKS = PIPE && STEPS > kSteps ? 2 : 1, BUFFERS = PIPE && MODE != LOSS ? 3 : 2;
+    constexpr int ITEMS = (STEPS > 0 && STEPS < kSteps ? STEPS / 2 * GROUPS + kWaves - 1 : 4 * GROUPS) / kWaves;
+    __shared__ __attribute__((aligned(16))) char staged[BUFFERS][CHUNKS][P][ROWS * kRowBytes];
+    __shared__ __attribute__((aligned(16))) float row_lse[3][ROWS], row_share[3][ROWS], row_both[3][ROWS];
+    __shared__ __attribute__((aligned(16))) int row_label[3][ROWS];
     __shared__ float largest[kWaves];
     const int lane = rg_lane(), wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), half = lane >> 5;
     const int order = rg_xcd_block(blockIdx.x, gridDim.x), split = order / job.tiles, tile = order - split * job.tiles;
     const int64_t n_act = rg_rows(job.n, job.n_dev);
     const int64_t rows = MODE == DW ? n_act : job.rows, owners = MODE == DW ? job.owners : rg_least(job.owners, n_act - job.first);
-    const int64_t first_owner = (int64_t)tile * OWNERS;
+    const int64_t first_owner = (int64_t)tile * kOwners;
     if (first_owner >= owners) return;
     const T* walked = (const T*)job.walked;
     const int dim = job.dim, steps = job.steps, chunks = job.chunks;
 
-    // the walked tiles of this split, and the stages of a tile: its chunks of 128 columns for z, the last of them one of this workgroup's output columns, which it
-    // serves at once; then the other output columns' chunk
-    const int64_t all = (rows + ROWS - 1) / ROWS, per = (all + job.splits - 1) / job.splits, t0 = rg_least(split * per, all), t1 = rg_least(t0 + per, all);
+    // The walked tiles of this split, and (not PIPE) the stages of a tile: its chunks of 128 columns for z, the last of them one of this workgroup's output columns,
+    // which it serves at once; then the other output columns' chunk.
+    const int64_t all = (rows + ROWS - 1) / ROWS, per = (all + job.splits - 1) / job.splits, t0 = rg_least(split * per, all);
+    const int tiles = (int)rg_least(per, all - t0), here = (int)(rows - t0 * ROWS);        // tiles, and rows from the first of them on
     constexpr int SLICE = NB / 4;
     const int slice = blockIdx.y * SLICE;
     const int more = MODE == LOSS ? 0 : min(SLICE, chunks - slice) - 1;
@@ -193,7 +210,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_softmax_rows(const Job job) {
     int power = 0;
     if (MODE == DW && job.dloss) {
         float top = 0.0f;
-        for (int64_t r = t0 * ROWS + threadIdx.x; r < rg_least(t1 * ROWS, rows); r += kThreads)
+        for (int64_t r = t0 * ROWS + threadIdx.x; r < rg_least((t0 + tiles) * ROWS, rows); r += kThreads)
             if (has_label(job.labels[r], job.classes)) top = fmaxf(top, fabsf(job.dloss[r]));
         for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, RG_WAVE));
         if (lane == 0) largest[wave] = top;
@@ -203,106 +220,134 @@ __global__ void __launch_bounds__(kThreads, 2) k_softmax_rows(const Job job) {
         if (top > 0.0f && top < __builtin_inff()) (void)frexpf(top, &power);
     }
 
-    // what a lane's owned rows bring
-    int64_t owner[OB];
-    int label[OB];
-    float lse2[OB], m[OB], s[OB];
-#pragma unroll
-    for (int b = 0; b < OB; ++b) {
-        owner[b] = first_owner + (wave * OB + b) * 32 + (lane & 31);
-        label[b] = -1;
-        lse2[b] = 0.0f;
-        m[b] = -__builtin_inff();
-        s[b] = 0.0f;
-        if (MODE != DW && owner[b] < owners) {
-            label[b] = job.labels[owner[b]];
-            if (!has_label(label[b], job.classes)) label[b] = -1;
-            if (MODE == DX && label[b] >= 0) lse2[b] = job.lse[owner[b]] * kLog2e - (float)S::BIAS;
-        }
+    // what a lane's owned row brings
+    const int64_t owner = first_owner + wave * 32 + (lane & 31);
+    int label = -1;
+    float lse2 = 0.0f, m = -__builtin_inff(), s = 0.0f, base = 0.0f;
+    if (MODE != DW && owner < owners) {
+        label = job.labels[owner];
+        if (!has_label(label, job.classes)) label = -1;
+        if (MODE == DX && label >= 0) lse2 = job.lse[owner] * kLog2e - (float)S::BIAS;
     }
-    const Words4* owned[OB];
-#pragma unroll
-    for (int b = 0; b < OB; ++b) owned[b] = job.owned + ((first_owner / 32 + wave * OB + b) * steps) * (P * 64) + lane;
-    Words4 held[OB][HOLD ? STEPS : 1][P];
+    const int told = label - (int)(t0 * ROWS);              // (the label among this split's rows; less than 0 if there is none)
+    const Words4* owned = job.owned + (first_owner / 32 + wave) * steps * (P * 64) + lane;
+    Words4 held[HOLD ? STEPS : 1][P];
     if constexpr (HOLD) {
 #pragma unroll
-        for (int b = 0; b < OB; ++b)
+        for (int k = 0; k < STEPS; ++k)
 #pragma unroll
-            for (int k = 0; k < STEPS; ++k)
+            for (int p = 0; p < P; ++p) held[k][p] = owned[(k * P + p) * 64];
+    }
+    // dweight: whether one of the owned numbers is not finite (which times the zeros of a row that does not count is a NaN)
+    bool odd = false;
+    if constexpr (MODE == DW) {
+        const uint32_t top = std::is_same<E, _Float16>::value ? 0x7C00u : 0x7F80u;
+        const auto look = [&](const Words4& w) __attribute__((always_inline)) {
 #pragma unroll
-                for (int p = 0; p < P; ++p) held[b][k][p] = owned[b][(k * P + p) * 64];
+            for (int j = 0; j < 4; ++j) odd |= (w[j] & top) == top || (w[j] >> 16 & top) == top;
+        };
+        if constexpr (HOLD) {
+#pragma unroll
+            for (int k = 0; k < STEPS; ++k) look(held[k][0]);
+        } else {
+#pragma unroll 8
+            for (int k = 0; k < steps * P; ++k) look(owned[k * 64]);
+        }
+        odd = __any(odd);
     }
 
-    // staging: a thread's pieces of eight columns
-    typename RgPack<T, 8>::type raw[ITEMS];
-    bool counts[ITEMS];
+    // Staging: a wavefront's pieces of 16 rows by 32 columns (four lanes to a row), so that only the last columns' ones look for the rows' end.  Within a row's 16
+    // pieces of 16 bytes the place is the column's exclusive or with four bits of the row: both ways of reading the tile (16 rows of one piece, 4 rows of
+    // 4) then meet all 64 banks once a cycle, where three bits for 128 bytes took twice as long.
+    // (Loads are made without a branch, of the last row where there is no other: registers that are written in some paths only are waited for where paths meet.)
+    typename RgPack<T, 8>::type raw[CHUNKS][ITEMS];
     float next_lse = 0.0f, next_share = 0.0f;
-    int next_label = -1;
-    const auto load = [&](int64_t t, int stage) __attribute__((always_inline)) {
-        const int chunk = chunk_of(stage);
+    int next_label = -1, to_label = -1;
+    const int to_row = wave % GROUPS * 16 + (lane >> 2), group0 = wave / GROUPS;          // (of 32 columns; item u: group0 + u * kWaves / GROUPS)
+    const int to_at = to_row * kRowBytes + (((group0 * 4 + (lane & 3)) ^ ((to_row & 3) << 2 | (to_row >> 2 & 3))) << 4);
+    const T *ahead = walked + (t0 * ROWS + to_row) * job.stride, *const last = walked + (rows - 1) * job.stride;
+    const auto load = [&](int t, int first_chunk, bool first) __attribute__((always_inline)) {
+        const T* src = ahead < last ? ahead : last;
+        if (MODE == DW) to_label = job.labels[t0 * ROWS + min(t * ROWS + to_row, here - 1)];
 #pragma unroll
-        for (int u = 0; u < ITEMS; ++u) {
-            const int i = threadIdx.x + u * kThreads;
-            const int64_t r = t * ROWS + (i >> 4), from = rg_least(r, rows - 1);
-            counts[u] = r < rows && (MODE != DW || has_label(job.labels[from], job.classes));
-            raw[u] = load_eight<STEPS == 2>(walked + from * job.stride, chunk * kCols + (i & 15) * 8, dim);
-        }
-        if (MODE == DW && stage == 0 && threadIdx.x < ROWS) {
-            const int64_t r = t * ROWS + threadIdx.x, from = rg_least(r, rows - 1);
+        for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+            for (int u = 0; u < ITEMS; ++u) {
+                if (STEPS > 0 && c * kSteps + u * (kWaves / GROUPS) * 2 >= STEPS) continue;
+                raw[c][u] = load_eight<STEPS == 2>(src, (first_chunk + c) * kCols + (group0 + u * (kWaves / GROUPS)) * 32 + (lane & 3) * 8, dim);
+            }
+        if (MODE == DW && first) {
+            const int r = t * ROWS + (threadIdx.x & (ROWS - 1));
+            const int64_t from = t0 * ROWS + min(r, here - 1);
             next_label = job.labels[from];
-            const bool live = r < rows && has_label(next_label, job.classes);
-            next_lse = live ? job.lse[from] * kLog2e : 0.0f;
-            next_share = live ? ldexpf(job.dloss ? job.dloss[from] : 1.0f, S::BIAS - power) : 0.0f;
-            if (!live) next_label = -1;
+            next_lse = job.lse[from];
+            next_share = job.dloss ? job.dloss[from] : 1.0f;
+            if (r >= here) next_label = -1;
         }
     };
-    const auto store = [&](int64_t t, int stage, int buffer) __attribute__((always_inline)) {
-        const int chunk = chunk_of(stage);
+    const auto next_tile = [&]() __attribute__((always_inline)) { ahead += ROWS * job.stride; };
+    const auto store = [&](int t, int first_chunk, int buffer, bool first, int place) __attribute__((always_inline)) {
         int dim = job.dim;
         asm volatile("" : "+s"(dim));                      // (else what depends on it is formed before the loop and takes registers through all of it)
+        const bool counts = t * ROWS + to_row < here && (MODE != DW || has_label(to_label, job.classes)), whole = __all(counts);
 #pragma unroll
-        for (int u = 0; u < ITEMS; ++u) {
-            const int i = threadIdx.x + u * kThreads, row = i >> 4, piece = (i & 15) ^ ((row & 3) << 1 | (row >> 2 & 1));
-            Words4 w[P];
-            row_parts<STEPS == 2, T>(raw[u], chunk * kCols + (i & 15) * 8, dim, counts[u], w);
+        for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
-            for (int p = 0; p < P; ++p) *(Words4*)(staged[buffer][p] + row * kRowBytes + piece * 16) = w[p];
+            for (int u = 0; u < ITEMS; ++u) {
+                if (STEPS > 0 && c * kSteps + u * (kWaves / GROUPS) * 2 >= STEPS) continue;
+                const int chunk = first_chunk + c, group = group0 + u * (kWaves / GROUPS), col = chunk * kCols + group * 32 + (lane & 3) * 8;
+                // (rows of STEPS steps end in the last two: in the last item's columns, if that)
+                const bool may_end = STEPS == 0 || STEPS == 12 || STEPS == 16 || c * kSteps + (u + 1) * (kWaves / GROUPS) * 2 >= STEPS;
+                Words4 w[P];
+                if (may_end && chunk * kCols + group * 32 + 32 > dim) row_parts<true, STEPS == 2, T>(raw[c][u], col, dim, w);
+                else row_parts<false, false, T>(raw[c][u], col, dim, w);
+#pragma unroll
+                for (int p = 0; p < P; ++p) *(Words4*)(staged[buffer][c][p] + (to_at ^ u * (kWaves / GROUPS) << 6)) = w[p];
+            }
+        if (!whole && !counts) {                           // (rows that do not count are zeros)
+#pragma unroll
+            for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+                for (int u = 0; u < ITEMS; ++u)
+#pragma unroll
+                    for (int p = 0; p < P; ++p) *(Words4*)(staged[buffer][c][p] + (to_at ^ u * (kWaves / GROUPS) << 6)) = Words4{0, 0, 0, 0};
         }
-        if (MODE == DW && stage == 0 && threadIdx.x < ROWS) {
-            row_lse[t & 1][threadIdx.x] = next_lse;
-            row_share[t & 1][threadIdx.x] = next_share;
-            row_label[t & 1][threadIdx.x] = next_label;
+        if (MODE == DW && first && threadIdx.x < ROWS) {
+            const bool live = has_label(next_label, job.classes);
+            const float lse = live ? next_lse * kLog2e : 0.0f, share = live ? ldexpf(next_share, S::BIAS - power) : 0.0f;
+            row_lse[place][threadIdx.x] = lse;
+            row_share[place][threadIdx.x] = share;
+            row_label[place][threadIdx.x] = live ? next_label : -1;
+            // share exp2(z - lse) = exp2(z - row_both); 0 where the share is
+            row_both[place][threadIdx.x] = share > 0.0f ? lse - __builtin_amdgcn_logf(share) : __builtin_inff();
         }
     };
 
-    Acc z[SB][OB], out[MODE == LOSS ? 1 : OB][MODE == LOSS ? 1 : NB];
-    Words4 g[MODE == LOSS ? 1 : SB][2][MODE == LOSS ? 1 : OB][P];
+    Acc out[MODE == LOSS ? 1 : NB];
+    Words4 g[MODE == LOSS ? 1 : SB][2][P];
     if (MODE != LOSS) {
 #pragma unroll
-        for (int b = 0; b < OB; ++b)
+        for (int d = 0; d < NB; ++d)
 #pragma unroll
-            for (int d = 0; d < NB; ++d)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) out[b][d][i] = 0.0f;
+            for (int i = 0; i < 16; ++i) out[d][i] = 0.0f;
     }
 
-    const int walk_row = lane & 31, twist = (walk_row & 3) << 1 | (walk_row >> 2 & 1);
-    // z += the products of K steps of 16 columns, FROM the chunk's first step on.  Fragments of the walked rows are read RING - 1 products ahead, those of the owned
-    // rows, where they are not held, two steps; the barriers keep the compiler from reading all of them at once, for which there are no registers.
-    constexpr int RING = P == 1 ? 4 : 2;
-    const auto products = [&](auto count, auto from, int chunk, int buffer) __attribute__((always_inline)) {
-        constexpr int K = decltype(count)::value, FROM = decltype(from)::value, UNITS = K * SB, AHEAD = P == 1 ? 3 : 2;
-        Words4 left[RING][P], right[AHEAD][OB][P];
+    // z += the products of K steps of 16 columns.  Fragments of the walked rows are read RING - 1 products ahead, those of the owned rows, where they are not held,
+    // a step or two; the barriers keep the compiler from reading all of them at once, for which there are no registers.  `between` has work for the vector units.
+    constexpr int RING = P > 1 ? 2 : 4;
+    const int walk_row = lane & 31, walk_at = walk_row * kRowBytes + ((half ^ ((walk_row & 3) << 2 | (walk_row >> 2 & 3))) << 4);
+    const auto products = [&](auto count, int chunk, int buffer, Acc (&z)[SB], auto between) __attribute__((always_inline)) {
+        constexpr int K = decltype(count)::value, UNITS = K * SB, AHEAD = P == 1 ? 3 : 2;
+        Words4 left[RING][P], right[AHEAD][P];
         const auto read = [&](int u) __attribute__((always_inline)) {
             const int k = u / SB, q = u % SB;
 #pragma unroll
-            for (int p = 0; p < P; ++p) left[u % RING][p] = *(const Words4*)(staged[buffer][p] + (q * 32 + walk_row) * kRowBytes + (((2 * k + half) ^ twist) << 4));
+            for (int p = 0; p < P; ++p)
+                left[u % RING][p] = *(const Words4*)(staged[buffer][CHUNKS > 1 ? k / kSteps : 0][p] + q * 32 * kRowBytes + (walk_at ^ k % kSteps << 5));
         };
         const auto fetch = [&](int k) __attribute__((always_inline)) {
 #pragma unroll
-            for (int b = 0; b < OB; ++b)
-#pragma unroll
-                for (int p = 0; p < P; ++p) right[k % AHEAD][b][p] = owned[b][((int64_t)(chunk * kSteps + k) * P + p) * 64];
+            for (int p = 0; p < P; ++p) right[k % AHEAD][p] = owned[((int64_t)(chunk * kSteps + k) * P + p) * 64];
         };
         if constexpr (!HOLD) {
 #pragma unroll
@@ -319,29 +364,34 @@ __global__ void __launch_bounds__(kThreads, 2) k_softmax_rows(const Job job) {
             if constexpr (!HOLD) {
                 if (q == 0 && k + AHEAD - 1 < K) fetch(k + AHEAD - 1);
             }
-#pragma unroll
-            for (int b = 0; b < OB; ++b) {
-                if constexpr (HOLD) z[q][b] = mma_parts<E, P>(left[u % RING], held[b][FROM + k], z[q][b]);
-                else z[q][b] = mma_parts<E, P>(left[u % RING], right[k % AHEAD][b], z[q][b]);
-            }
+            if constexpr (HOLD) z[q] = mma_parts<E, P>(left[u % RING], held[HOLD ? k : 0], z[q]);
+            else z[q] = mma_parts<E, P>(left[u % RING], right[k % AHEAD], z[q]);
+            between(u, UNITS);
             __builtin_amdgcn_sched_barrier(0);
         }
     };
+    const auto nothing = [](int, int) __attribute__((always_inline)) {};
+    const auto clear = [&](Acc (&z)[SB]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int q = 0; q < SB; ++q)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) z[q][i] = 0.0f;
+    };
+
     // out += g . the staged rows, for D blocks of 32 columns
-    const auto second = [&](auto base, auto count, int buffer) __attribute__((always_inline)) {
+    const int i16 = lane & 15, low_at = (4 * half + (i16 >> 2)) * kRowBytes + ((((lane >> 4 & 1) * 2 + (i16 >> 1 & 1)) ^ ((i16 >> 2) << 2 | half)) << 4) + (i16 & 1) * 8;
+    const auto second = [&](auto base, auto count, int buffer, auto between) __attribute__((always_inline)) {
         constexpr int D0 = decltype(base)::value, D = decltype(count)::value, UNITS = SB * 2 * D;
-        const int i = lane & 15, row0 = 4 * half + (i >> 2), turn = (i >> 2) << 1 | half;
-        Words4 left[RING][P];
+        Words4 turned[RING][P];
         const auto read = [&](int u) __attribute__((always_inline)) {
             const int q = u / (2 * D), f = u / D % 2, d = u % D;
-            const int piece = ((d * 4 + (lane >> 4 & 1) * 2 + (i >> 1 & 1)) ^ turn) * 16 + (i & 1) * 8;
 #pragma unroll
             for (int p = 0; p < P; ++p) {
-                const char* at = staged[buffer][p] + (q * 32 + f * 16 + row0) * kRowBytes + piece;
+                const char* at = staged[buffer][0][p] + (q * 32 + f * 16) * kRowBytes;
                 typedef __attribute__((address_space(3))) Short4 Lds;
-                const Words2 low = __builtin_bit_cast(Words2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds*)at));
-                const Words2 high = __builtin_bit_cast(Words2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds*)(at + 8 * kRowBytes)));
-                left[u % RING][p] = Words4{low[0], low[1], high[0], high[1]};
+                const Words2 low = __builtin_bit_cast(Words2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds*)(at + (low_at ^ d << 6))));
+                const Words2 high = __builtin_bit_cast(Words2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds*)(at + 8 * kRowBytes + (low_at ^ d << 6 ^ 2 << 4))));
+                turned[u % RING][p] = Words4{low[0], low[1], high[0], high[1]};
             }
         };
 #pragma unroll
@@ -351,225 +401,248 @@ __global__ void __launch_bounds__(kThreads, 2) k_softmax_rows(const Job job) {
         for (int u = 0; u < UNITS; ++u) {
             const int q = u / (2 * D), f = u / D % 2, d = u % D;
             if (u + RING - 1 < UNITS) read(u + RING - 1);
-#pragma unroll
-            for (int b = 0; b < OB; ++b) out[b][D0 + d] = mma_parts<E, P>(left[u % RING], g[q][f][b], out[b][D0 + d]);
+            out[D0 + d] = mma_parts<E, P>(turned[u % RING], g[q][f], out[D0 + d]);
+            between(u, UNITS);
             __builtin_amdgcn_sched_barrier(0);
         }
     };
 
-    // z of a whole tile is there.  (What few tiles need, labels and the ends, stands in loops of its own behind barriers: mixed into the others it took 70 registers.)
-    const auto finish = [&](int64_t t) __attribute__((always_inline)) {
-        const int64_t first = t * ROWS;
-        __builtin_amdgcn_sched_barrier(0);
+    // z of a whole tile is there, register i of z[q] the walked row q * 32 + row_at(i) + 4 half.  What few tiles need (labels, the ends, a new maximum) stands in blocks
+    // of its own that most pass by; side by side with the other path, each with its registers, it made the compiler spill.
+    const auto row_at = [](int i) __attribute__((always_inline)) { return 8 * (i >> 2) + (i & 3); };
+    const auto open_tile = [&](int t, int place, Acc (&z)[SB]) __attribute__((always_inline)) {
         if (MODE == DW) {
-            const int seen = row_label[t & 1][lane & (ROWS - 1)];
-            const int64_t mine = job.first + first_owner + wave * OB * 32;
-            const bool hits = __any(seen >= mine && seen < mine + OB * 32), idle = __any(row_share[t & 1][lane & (ROWS - 1)] == 0.0f);
+            const int seen = row_label[place][lane & (ROWS - 1)], mine = (int)(job.first + first_owner) + wave * 32;
+            const float share = row_share[place][lane & (ROWS - 1)];
+            return (bool)__any((seen >= mine && seen - mine < 32) || !(share > 0.0f || (share == 0.0f && !odd)));
+        }
+        if ((t + 1) * ROWS > here) {                       // (behind the last class)
+            int end = here - t * ROWS - 4 * half;
+            asm volatile("" : "+v"(end));                  // (else the 32 rows that it is compared to are formed before the loop, and kept)
 #pragma unroll
             for (int q = 0; q < SB; ++q)
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
-#pragma unroll
-                    for (int b = 0; b < OB; ++b)
-                        z[q][b][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[q][b][i], kLog2e, -row_lse[t & 1][q * 32 + 8 * (i >> 2) + 4 * half + (i & 3)]));
+                for (int i = 0; i < 16; ++i) z[q][i] = q * 32 + row_at(i) >= end ? -__builtin_inff() : z[q][i];
             __builtin_amdgcn_sched_barrier(0);
+        }
+        const bool met = told >= t * ROWS && told < (t + 1) * ROWS, hits = __any(met);
+        if (MODE == LOSS) {
             if (hits) {
+                int at = told - t * ROWS - 4 * half;       // (of this half's, if it equals one of them)
+                asm volatile("" : "+v"(at));
+                float there = 0.0f;
+                bool mine = false;
 #pragma unroll
                 for (int q = 0; q < SB; ++q)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i)
-#pragma unroll
-                        for (int b = 0; b < OB; ++b)
-                            z[q][b][i] -= row_label[t & 1][q * 32 + 8 * (i >> 2) + 4 * half + (i & 3)] == (int)(job.first + owner[b]) ? 1.0f : 0.0f;
+                    for (int i = 0; i < 16; ++i) {
+                        const bool is = at == q * 32 + row_at(i);
+                        there = is ? z[q][i] : there;
+                        mine |= is;
+                    }
+                if (met && mine) job.target[owner] = there;
                 __builtin_amdgcn_sched_barrier(0);
             }
-            if (idle) {                                    // (nothing of a row that does not count, whatever its p is)
-#pragma unroll
-                for (int q = 0; q < SB; ++q)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-#pragma unroll
-                        for (int b = 0; b < OB; ++b) z[q][b][i] = row_share[t & 1][q * 32 + 8 * (i >> 2) + 4 * half + (i & 3)] == 0.0f ? 0.0f : z[q][b][i];
-                __builtin_amdgcn_sched_barrier(0);
-            }
+            // s is the sum of exp(z - m) with an m that need not be the maximum, but is within e^22 of it
+            float top = z[0][0];
 #pragma unroll
             for (int q = 0; q < SB; ++q)
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
-#pragma unroll
-                    for (int b = 0; b < OB; ++b) z[q][b][i] *= row_share[t & 1][q * 32 + 8 * (i >> 2) + 4 * half + (i & 3)];
-        } else {
-            if (first + ROWS > rows) {                    // (behind the last class)
-                const int end = (int)(rows - first) - 4 * half;
-#pragma unroll
-                for (int q = 0; q < SB; ++q)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-#pragma unroll
-                        for (int b = 0; b < OB; ++b) z[q][b][i] = q * 32 + 8 * (i >> 2) + (i & 3) >= end ? -__builtin_inff() : z[q][b][i];
+                for (int i = 0; i < 16; ++i) top = fmaxf(top, z[q][i]);
+            if (__any(!(top - m < 22.0f))) {
+                const float higher = fmaxf(m, top);
+                if (m != -__builtin_inff()) s *= __builtin_amdgcn_exp2f((m - higher) * kLog2e);
+                m = higher;
                 __builtin_amdgcn_sched_barrier(0);
-            }
-#pragma unroll
-            for (int b = 0; b < OB; ++b) {
-                const bool here = label[b] >= first && label[b] < first + ROWS;
-                const int at = (int)(label[b] - first) - 4 * half;           // (of this half's, if it equals one of them)
-                const bool hits = __any(here);
-                if (MODE == LOSS) {
-                    if (hits) {
-                        float told = 0.0f;
-                        bool mine = false;
-#pragma unroll
-                        for (int q = 0; q < SB; ++q)
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) {
-                                const bool is = at == q * 32 + 8 * (i >> 2) + (i & 3);
-                                told = is ? z[q][b][i] : told;
-                                mine |= is;
-                            }
-                        if (here && mine) job.target[owner[b]] = told;
-                        __builtin_amdgcn_sched_barrier(0);
-                    }
-                    float top = m[b];
-#pragma unroll
-                    for (int q = 0; q < SB; ++q)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) top = fmaxf(top, z[q][b][i]);
-                    const float base = top == -__builtin_inff() ? 0.0f : top * kLog2e;
-                    float sum[4] = {s[b] * __builtin_amdgcn_exp2f(__builtin_fmaf(m[b], kLog2e, -base)), 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                    for (int q = 0; q < SB; ++q)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) sum[i & 3] += __builtin_amdgcn_exp2f(__builtin_fmaf(z[q][b][i], kLog2e, -base));
-                    m[b] = top;
-                    s[b] = (sum[0] + sum[1]) + (sum[2] + sum[3]);
-                } else {
-#pragma unroll
-                    for (int q = 0; q < SB; ++q)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) z[q][b][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[q][b][i], kLog2e, -lse2[b]));
-                    if (hits) {
-                        __builtin_amdgcn_sched_barrier(0);
-                        const int there = here ? at : -1000;
-#pragma unroll
-                        for (int q = 0; q < SB; ++q)
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) z[q][b][i] -= there == q * 32 + 8 * (i >> 2) + (i & 3) ? (float)(1 << S::BIAS) : 0.0f;
-                        __builtin_amdgcn_sched_barrier(0);
-                    }
-                }
             }
         }
-        if constexpr (MODE != LOSS) {
+        return hits;
+    };
+    // exp(z - m), or share g, of row i of z[q] ...
+    const auto power_of = [&](float z, float both) __attribute__((always_inline)) {
+        return __builtin_amdgcn_exp2f(__builtin_fmaf(z, kLog2e, MODE == LOSS ? -base : MODE == DX ? -lse2 : -both));
+    };
+    // ... and of the eight rows of z[q]'s half f in a tile that has labels here, or rows that do not count
+    const auto mend = [&](int t, int place, const Acc (&z)[SB], int q, int f, float (&v)[8]) __attribute__((always_inline)) {
+        if (MODE == DX) {
+            int at = told - t * ROWS - 4 * half - q * 32 - f * 16;
+            asm volatile("" : "+v"(at));
 #pragma unroll
-            for (int q = 0; q < SB; ++q)
+            for (int j = 0; j < 8; ++j) v[j] -= at == row_at(j) && told >= 0 ? (float)(1 << S::BIAS) : 0.0f;
+        } else {
+            const int mine = (int)(job.first + owner);
 #pragma unroll
-                for (int b = 0; b < OB; ++b)
-#pragma unroll
-                    for (int f = 0; f < 2; ++f) {
-                        float v[8];
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) v[j] = z[q][b][f * 8 + j];
-                        cut<T>(v, g[q][f][b]);
-                    }
+            for (int j = 0; j < 8; ++j) {
+                const int row = q * 32 + f * 16 + row_at(j) + 4 * half;
+                const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(z[q][f * 8 + j], kLog2e, -row_lse[place][row])), share = row_share[place][row];
+                v[j] = share == 0.0f ? 0.0f : share * (p - (row_label[place][row] == mine ? 1.0f : 0.0f));       // (nothing of a row that does not count, whatever its p is)
+            }
         }
         __builtin_amdgcn_sched_barrier(0);
     };
 
 #define RG_INT(N) std::integral_constant<int, N>()
     constexpr int FIRST = STEPS == 0 || STEPS > kSteps ? 4 : STEPS / 2, SECOND = STEPS > kSteps ? (STEPS - kSteps) / 2 : 4;      // blocks of output columns
-    const auto add_products = [&](int chunk, int buffer) __attribute__((always_inline)) {
-        if constexpr (STEPS > kSteps) {
-            if (chunk == 0) products(RG_INT(kSteps), RG_INT(0), chunk, buffer);
-            else products(RG_INT(STEPS - kSteps), RG_INT(kSteps), chunk, buffer);
-        } else if constexpr (STEPS > 0) {
-            products(RG_INT(STEPS), RG_INT(0), chunk, buffer);
-        } else {
-            const int here = steps - chunk * kSteps;
-            if (here > 6) products(RG_INT(8), RG_INT(0), chunk, buffer);
-            else if (here > 4) products(RG_INT(6), RG_INT(0), chunk, buffer);
-            else if (here > 2) products(RG_INT(4), RG_INT(0), chunk, buffer);
-            else products(RG_INT(2), RG_INT(0), chunk, buffer);
+    if constexpr (PIPE) {
+        // A tile: its exponentials beside the next one's products, its second product, the tile after the next one to LDS.  (Behind the last tile the products are of
+        // what lies there, and are not used.)
+        const auto turn = [&](int t, int now, Acc (&z)[SB], Acc (&next)[SB]) __attribute__((always_inline)) {
+            const int then = now + 1 == BUFFERS ? 0 : now + 1, free = BUFFERS == 2 ? now : then + 1 == BUFFERS ? 0 : then + 1;
+            load(t + 2, 0, true);
+            next_tile();
+            const bool rare = open_tile(t, now, z);
+            base = m == -__builtin_inff() ? 0.0f : m * kLog2e;
+            clear(next);
+            float sum[4] = {s, 0.0f, 0.0f, 0.0f}, both[2][4], v[8];
+            const auto read_both = [&](int e) __attribute__((always_inline)) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) both[e / 4 % 2][j] = row_both[now][e / 16 * 32 + row_at(e % 16) + 4 * half + j];
+            };
+            if (MODE == DW) read_both(0);
+            const auto exponentials = [&](int from, int to) __attribute__((always_inline)) {
+#pragma unroll
+                for (int e = from; e < to; ++e) {
+                    const int q = e / 16, i = e % 16;
+                    if (MODE == DW && e % 4 == 0 && e + 4 < SB * 16) read_both(e + 4);
+                    v[e % 8] = power_of(z[q][i], both[e / 4 % 2][e % 4]);
+                    if (MODE == LOSS) sum[i & 3] += v[e % 8];
+                    // (held here: the compiler would move them behind all products, where they are used)
+                    if (MODE == LOSS) asm volatile("" : "+v"(sum[i & 3]));
+                    else asm volatile("" : "+v"(v[e % 8]));
+                    if (MODE != LOSS && e % 8 == 7) {
+                        if (rare) mend(t, now, z, q, i / 8, v);
+                        cut<T>(v, g[MODE == LOSS ? 0 : q][i / 8]);
+                    }
+                }
+            };
+            // half of them beside the products of the next z, half beside those of the first half
+            constexpr int ALL = SB * 16, BEFORE = MODE == LOSS ? ALL : ALL / 2;
+            products(RG_INT(STEPS), 0, then, next, [&](int u, int units) __attribute__((always_inline)) { exponentials(u * BEFORE / units, (u + 1) * BEFORE / units); });
+            if (MODE == LOSS) s = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            if constexpr (MODE != LOSS)
+                second(RG_INT(0), RG_INT(FIRST), now, [&](int u, int units) __attribute__((always_inline)) {
+                    if (u < units / 2) exponentials(BEFORE + u * BEFORE / (units / 2), BEFORE + (u + 1) * BEFORE / (units / 2));
+                });
+            if (t + 2 < tiles) store(t + 2, 0, free, true, free);
+            __syncthreads();
+            return then;
+        };
+        Acc z[2][SB];
+        int now = 0;
+        if (tiles > 0) {
+            load(0, 0, true);
+            next_tile();
+            store(0, 0, 0, true, 0);
+            if (tiles > 1) {
+                load(1, 0, true);
+                store(1, 0, 1, true, 1);
+            }
+            next_tile();
+            __syncthreads();
+            clear(z[0]);
+            products(RG_INT(STEPS), 0, 0, z[0], nothing);
+            if (BUFFERS == 2) __syncthreads();             // (the first turn's store takes the first tile's place)
         }
-    };
-    if (t0 < t1) {
-        load(t0, 0);
-        store(t0, 0, 0);
-        __syncthreads();
-    }
-    int buffer = 0;
 #pragma unroll 1
-    for (int64_t t = t0; t < t1; ++t) {
-#pragma unroll
-        for (int q = 0; q < SB; ++q)
-#pragma unroll
-            for (int b = 0; b < OB; ++b)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) z[q][b][i] = 0.0f;
-        if (STEPS == 0 || STEPS > kSteps) {
+        for (int t = 0; t < tiles; t += 2) {
+            now = turn(t, now, z[0], z[1]);
+            if (t + 1 < tiles) now = turn(t + 1, now, z[1], z[0]);
+        }
+    } else {
+        Acc z[SB];
+        const auto add_products = [&](int chunk, int buffer) __attribute__((always_inline)) {
+            const int here = steps - chunk * kSteps;
+            if (here > 6) products(RG_INT(8), chunk, buffer, z, nothing);
+            else if (here > 4) products(RG_INT(6), chunk, buffer, z, nothing);
+            else if (here > 2) products(RG_INT(4), chunk, buffer, z, nothing);
+            else products(RG_INT(2), chunk, buffer, z, nothing);
+        };
+        if (tiles > 0) {
+            load(0, chunk_of(0), true);
+            store(0, chunk_of(0), 0, true, 0);
+            __syncthreads();
+        }
+        int buffer = 0;
 #pragma unroll 1
-            for (int stage = 0; stage < (STEPS > kSteps ? 1 : chunks - 1); ++stage) {
-                load(t, stage + 1);
-                add_products(MODE != LOSS && STEPS > kSteps ? 1 : chunk_of(stage), buffer);
-                store(t, stage + 1, buffer ^ 1);
+        for (int t = 0; t < tiles; ++t) {
+            const int place = t & 1;
+            clear(z);
+#pragma unroll 1
+            for (int stage = 0; stage < chunks - 1; ++stage) {
+                load(t, chunk_of(stage + 1), false);
+                add_products(chunk_of(stage), buffer);
+                store(t, chunk_of(stage + 1), buffer ^ 1, false, 0);
                 __syncthreads();
                 buffer ^= 1;
             }
-        }
-        // (the next rows are asked for behind the products of z, which leave no registers for them)
-        add_products(STEPS > 0 && (MODE != LOSS || STEPS <= kSteps) ? 0 : STEPS > 0 ? 1 : chunk_of(chunks - 1), buffer);
-        finish(t);
-        const bool rest = NB > 4 && more > 0, go_on = t + 1 < t1;
-        if (rest) load(t, chunks);
-        else if (go_on) load(t + 1, 0);
-        if constexpr (MODE != LOSS) second(RG_INT(0), RG_INT(FIRST), buffer);
-        if (rest) store(t, chunks, buffer ^ 1);
-        else if (go_on) store(t + 1, 0, buffer ^ 1);
-        __syncthreads();
-        buffer ^= 1;
-        if constexpr (MODE != LOSS && NB > 4) {
-            if (rest) {
-                if (go_on) load(t + 1, 0);
-                second(RG_INT(4), RG_INT(SECOND), buffer);
-                if (go_on) store(t + 1, 0, buffer ^ 1);
-                __syncthreads();
-                buffer ^= 1;
+            // (the next rows are asked for behind the products of z, which leave no registers for them)
+            const bool rest = NB > 4 && more > 0, go_on = t + 1 < tiles;
+            add_products(chunk_of(chunks - 1), buffer);
+            const bool rare = open_tile(t, place, z);
+            base = m == -__builtin_inff() ? 0.0f : m * kLog2e;
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int q = 0; q < SB; ++q)
+#pragma unroll
+                for (int f = 0; f < 2; ++f) {
+                    float v[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        v[j] = power_of(z[q][f * 8 + j], MODE == DW ? row_both[place][q * 32 + f * 16 + row_at(j) + 4 * half] : 0.0f);
+                        if (MODE == LOSS) s += v[j];
+                    }
+                    if (MODE != LOSS) {
+                        if (rare) mend(t, place, z, q, f, v);
+                        cut<T>(v, g[MODE == LOSS ? 0 : q][f]);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            if (!rest) next_tile();
+            load(rest ? t : t + 1, rest ? chunk_of(chunks) : chunk_of(0), !rest);
+            if constexpr (MODE != LOSS) second(RG_INT(0), RG_INT(4), buffer, nothing);
+            if (rest || go_on) store(rest ? t : t + 1, rest ? chunk_of(chunks) : chunk_of(0), buffer ^ 1, !rest, place ^ 1);
+            __syncthreads();
+            buffer ^= 1;
+            if constexpr (MODE != LOSS && NB > 4) {
+                if (rest) {
+                    next_tile();
+                    load(t + 1, chunk_of(0), true);
+                    second(RG_INT(4), RG_INT(SECOND), buffer, nothing);
+                    if (go_on) store(t + 1, chunk_of(0), buffer ^ 1, true, place ^ 1);
+                    __syncthreads();
+                    buffer ^= 1;
+                }
             }
         }
     }
 #undef RG_INT
 
     if constexpr (MODE == LOSS) {
-#pragma unroll
-        for (int b = 0; b < OB; ++b) {
-            const float other_m = __shfl_xor(m[b], 32, RG_WAVE), other_s = __shfl_xor(s[b], 32, RG_WAVE);
-            const float top = fmaxf(m[b], other_m), base = top == -__builtin_inff() ? 0.0f : top * kLog2e;
-            const float sum = s[b] * __builtin_amdgcn_exp2f(__builtin_fmaf(m[b], kLog2e, -base)) + other_s * __builtin_amdgcn_exp2f(__builtin_fmaf(other_m, kLog2e, -base));
-            if (half == 0 && owner[b] < owners) job.stats[split * job.owners + owner[b]] = make_float2(top, sum);
-        }
+        const float other_m = __shfl_xor(m, 32, RG_WAVE), other_s = __shfl_xor(s, 32, RG_WAVE);
+        const float top = fmaxf(m, other_m), base = top == -__builtin_inff() ? 0.0f : top * kLog2e;
+        const float sum = s * __builtin_amdgcn_exp2f(__builtin_fmaf(m, kLog2e, -base)) + other_s * __builtin_amdgcn_exp2f(__builtin_fmaf(other_m, kLog2e, -base));
+        if (half == 0 && owner < owners) job.stats[split * job.owners + owner] = make_float2(top, sum);
     } else {
+        if (owner >= owners) return;
+        float factor = job.scale;
+        const bool none = MODE == DX && label < 0;
+        if (MODE == DX && !none && job.dloss) factor *= job.dloss[owner];
 #pragma unroll
-        for (int b = 0; b < OB; ++b) {
-            if (owner[b] >= owners) continue;
-            float factor = job.scale;
-            const bool none = MODE == DX && label[b] < 0;
-            if (MODE == DX && !none && job.dloss) factor *= job.dloss[owner[b]];
+        for (int d = 0; d < NB; ++d)
 #pragma unroll
-            for (int d = 0; d < NB; ++d)
+            for (int i = 0; i < 4; ++i) {
+                const int col = (slice * 4 + d) * 32 + i * 8 + half * 4;
+                if (col >= dim) continue;
+                float v[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int col = (slice * 4 + d) * 32 + i * 8 + half * 4;
-                    if (col >= dim) continue;
-                    float v[4];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        v[j] = out[b][d][i * 4 + j] * factor;
-                        if (MODE == DW || S::BIAS) v[j] = ldexpf(v[j], power - S::BIAS);
-                        if (none) v[j] = 0.0f;
-                    }
-                    if (job.splits == 1) rg_store_live<4>((T*)job.out + owner[b] * job.out_stride + col, dim - col, v);
-                    else rg_store_live<4>(job.parts + (split * job.owners + owner[b]) * dim + col, dim - col, v);
+                for (int j = 0; j < 4; ++j) {
+                    v[j] = out[d][i * 4 + j] * factor;
+                    if (MODE == DW || S::BIAS) v[j] = ldexpf(v[j], power - S::BIAS);
+                    if (none) v[j] = 0.0f;
                 }
-        }
+                if (job.splits == 1) rg_store_live<4>((T*)job.out + owner * job.out_stride + col, dim - col, v);
+                else rg_store_live<4>(job.parts + (split * job.owners + owner) * dim + col, dim - col, v);
+            }
     }
 }
 
@@ -645,12 +718,10 @@ int steps_of(int dim) {
 
 int64_t packed_row(int steps, int parts) { return (int64_t)steps * parts * 32; }
 
-constexpr int kOwners = 256;                                // packed rows come in so many
-
 // Rows that are owned at a time: their packed form stays in the last level of cache.
 int64_t piece_rows(int64_t rows, int steps, int parts) {
-    const int64_t most = rg_max64(1, (128ll << 20) / packed_row(steps, parts) / kOwners) * kOwners;
-    return rg_min64(most, rg_div_up(rows, kOwners) * kOwners);
+    const int64_t most = rg_max64(1, (128ll << 20) / packed_row(steps, parts) / kOwners) * kOwners, pieces = rg_div_up(rows, most);
+    return rg_div_up(rg_div_up(rows, pieces), kOwners) * kOwners;
 }
 
 template <typename T>
@@ -679,23 +750,18 @@ rg_status check_loss(rg_ctx* ctx, const char* who, const void* x, rg_dtype type,
     return RG_OK;
 }
 
-// The kernel for a job, and the rows that a workgroup of it owns.
-template <typename T, int MODE>
-constexpr int owned_blocks() { return Part<T>::P == 1 && MODE == LOSS ? 2 : 1; }
-
+// The kernel for a job.
 template <typename T, int MODE>
 void launch(const Job& job, int64_t slices, hipStream_t s) {
-    constexpr bool ONE = Part<T>::P == 1;
-    constexpr int OB = owned_blocks<T, MODE>();
     const dim3 grid((unsigned)((int64_t)job.tiles * job.splits), (unsigned)slices);
     switch (job.steps) {
-        case 2: k_softmax_rows<T, MODE, OB, 4, 2, ONE><<<grid, kThreads, 0, s>>>(job); break;
-        case 4: k_softmax_rows<T, MODE, OB, 4, 4, ONE><<<grid, kThreads, 0, s>>>(job); break;
-        case 6: k_softmax_rows<T, MODE, OB, 4, 6, ONE><<<grid, kThreads, 0, s>>>(job); break;
-        case 8: k_softmax_rows<T, MODE, OB, 4, 8, ONE><<<grid, kThreads, 0, s>>>(job); break;
-        case 12: k_softmax_rows<T, MODE, OB, 8, 12, ONE && MODE == LOSS><<<grid, kThreads, 0, s>>>(job); break;
-        case 16: k_softmax_rows<T, MODE, OB, 8, 16, ONE && MODE == LOSS><<<grid, kThreads, 0, s>>>(job); break;
-        default: k_softmax_rows<T, MODE, OB, 8, 0, false><<<grid, kThreads, 0, s>>>(job);
+        case 2: k_softmax_rows<T, MODE, 4, 2><<<grid, kThreads, 0, s>>>(job); break;
+        case 4: k_softmax_rows<T, MODE, 4, 4><<<grid, kThreads, 0, s>>>(job); break;
+        case 6: k_softmax_rows<T, MODE, 4, 6><<<grid, kThreads, 0, s>>>(job); break;
+        case 8: k_softmax_rows<T, MODE, 4, 8><<<grid, kThreads, 0, s>>>(job); break;
+        case 12: k_softmax_rows<T, MODE, 8, 12><<<grid, kThreads, 0, s>>>(job); break;
+        case 16: k_softmax_rows<T, MODE, 8, 16><<<grid, kThreads, 0, s>>>(job); break;
+        default: k_softmax_rows<T, MODE, 8, 0><<<grid, kThreads, 0, s>>>(job);
     }
 }
 
@@ -715,9 +781,9 @@ rg_status rg_cross_entropy(rg_ctx* ctx, const void* x, rg_dtype type, int64_t x_
     RG_FOR_TYPE(type, {
         constexpr int P = Part<T>::P;
         const int steps = steps_of(dim);
-        const int64_t piece = piece_rows(n, steps, P), most = rg_min64(piece, n), tiles = rg_div_up(most, (int64_t)kWaves * 32 * owned_blocks<T, LOSS>());
+        const int64_t piece = piece_rows(n, steps, P), most = rg_min64(piece, n), tiles = rg_div_up(most, kOwners);
         const int splits = splits_for(ctx, tiles, classes);
-        const size_t packed = (size_t)(rg_div_up(most, kOwners) * kOwners * packed_row(steps, P)), stats = (size_t)splits * most * sizeof(float2);
+        const size_t packed = (size_t)(tiles * kOwners * packed_row(steps, P)), stats = (size_t)splits * most * sizeof(float2);
         const rg_status st = rg_scratch(ctx, ctx->loss_parts, packed + stats + (size_t)most * 4, s, "rg_cross_entropy");
         if (st != RG_OK) return st;
         char* at = (char*)ctx->loss_parts.p;
@@ -740,7 +806,7 @@ rg_status rg_cross_entropy(rg_ctx* ctx, const void* x, rg_dtype type, int64_t x_
             pack<T>(ctx, x, x_stride, first, count, n, n_dev, dim, steps, nullptr, classes, at, s);
             job.owners = count;
             job.first = first;
-            job.tiles = (int)rg_div_up(count, (int64_t)kWaves * 32 * owned_blocks<T, LOSS>());
+            job.tiles = (int)rg_div_up(count, kOwners);
             job.labels = labels + first;
             launch<T, LOSS>(job, 1, s);
             RG_LAUNCH_CHECK(ctx, "k_softmax_rows");
@@ -788,9 +854,9 @@ rg_status rg_cross_entropy_grad(rg_ctx* ctx, const void* x, rg_dtype type, int64
             v.rows = rows;
             v.piece = piece_rows(rows, steps, P);
             v.most = rg_min64(v.piece, rows);
-            v.tiles = rg_div_up(v.most, kWaves * 32);
+            v.tiles = rg_div_up(v.most, kOwners);
             v.splits = splits_for(ctx, v.tiles * slices, walked);
-            v.packed = (size_t)(rg_div_up(v.most, kOwners) * kOwners * packed_row(steps, P));
+            v.packed = (size_t)(v.tiles * kOwners * packed_row(steps, P));
             v.parts = v.splits > 1 ? (size_t)v.splits * v.most * dim * 4 : 0;
             return v;
         };
@@ -811,7 +877,7 @@ rg_status rg_cross_entropy_grad(rg_ctx* ctx, const void* x, rg_dtype type, int64
         const auto take = [&](const Side& v, int64_t first, void* out, int64_t stride) {
             job.owners = rg_min64(v.piece, v.rows - first);
             job.first = first;
-            job.tiles = (int)rg_div_up(job.owners, kWaves * 32);
+            job.tiles = (int)rg_div_up(job.owners, kOwners);
             job.splits = v.splits;
             job.parts = (float*)(at + v.packed);
             job.out = (T*)out + first * stride;

@@ -1,4 +1,6 @@
 // Rows of a table by id, and the gradient of the rows that were looked up, summed by id.
+#include <type_traits>
+
 #include "rg_elements.h"
 
 namespace {
@@ -68,12 +70,12 @@ __global__ void __launch_bounds__(kThreads) k_embedding(const T* __restrict__ ta
 
 // ---------------------------------------------------------------- ids in order
 // The gradient's sums run over the entries sorted by id, entries of an id in their own order, so that the same call adds in the same order each time.  Least
-// digit first, eight bits a pass; padding gets the id behind the last row and comes to lie behind all others.
+// digit first, up to ten bits a pass (three launches); padding gets the id behind the last row and comes to lie behind all others.
 struct Entry {
     uint32_t id, at;
 };
 
-constexpr int kDigits = 256, kRounds = 4, kTile = kThreads * kRounds, kSortWaves = kThreads / RG_WAVE;
+constexpr int kRounds = 4, kTile = kThreads * kRounds, kSortWaves = kThreads / RG_WAVE;
 
 __device__ __forceinline__ Entry entry_of(const Entry* from, const int32_t* ids, int64_t i, uint32_t num_rows) {
     if (from) return from[i];
@@ -82,57 +84,84 @@ __device__ __forceinline__ Entry entry_of(const Entry* from, const int32_t* ids,
 }
 
 // Lanes that hold the same digit as this one.
+template <int BITS>
 __device__ __forceinline__ uint64_t same_digit(uint32_t digit, bool live) {
     uint64_t mask = __ballot(live);
 #pragma unroll
-    for (int b = 0; b < 8; ++b) {
+    for (int b = 0; b < BITS; ++b) {
         const uint64_t set = __ballot(digit >> b & 1);
         mask &= digit >> b & 1 ? set : ~set;
     }
     return mask;
 }
 
+template <int BITS>
 __global__ void __launch_bounds__(kThreads) k_sort_count(const Entry* __restrict__ from, const int32_t* __restrict__ ids, int64_t n,
                                                          const int32_t* __restrict__ n_dev, uint32_t num_rows, int shift, int64_t per_block,
                                                          int32_t* __restrict__ counts) {
-    __shared__ int32_t bins[kDigits];
-    bins[threadIdx.x] = 0;
+    constexpr int DIGITS = 1 << BITS;
+    __shared__ int32_t bins[DIGITS];
+#pragma unroll
+    for (int d = threadIdx.x; d < DIGITS; d += kThreads) bins[d] = 0;
     __syncthreads();
     const int64_t first = (int64_t)blockIdx.x * per_block, last = rg_least(first + per_block, rg_rows(n, n_dev));
-    for (int64_t i = first + threadIdx.x; i < last; i += kThreads) atomicAdd(&bins[entry_of(from, ids, i, num_rows).id >> shift & 255], 1);
+    for (int64_t i = first + threadIdx.x; i < last; i += kThreads) atomicAdd(&bins[entry_of(from, ids, i, num_rows).id >> shift & (DIGITS - 1)], 1);
     __syncthreads();
-    counts[(int64_t)threadIdx.x * gridDim.x + blockIdx.x] = bins[threadIdx.x];
+#pragma unroll
+    for (int d = threadIdx.x; d < DIGITS; d += kThreads) counts[(int64_t)d * gridDim.x + blockIdx.x] = bins[d];
 }
 
 // Each digit's counts become its entries in front of every block; totals[digit] = all of them.
 __global__ void __launch_bounds__(kThreads) k_sort_scan(int32_t* __restrict__ counts, int blocks, int32_t* __restrict__ totals) {
     __shared__ int smem[kSortWaves + 1];
+    constexpr int EACH = 4;
     int32_t* row = counts + (int64_t)blockIdx.x * blocks;
     int before = 0;
-    for (int b0 = 0; b0 < blocks; b0 += kThreads) {
-        const int b = b0 + threadIdx.x;
-        const int x = b < blocks ? row[b] : 0;
-        int total;
-        const int excl = rg_block_excl_scan<kSortWaves>(x, smem, &total);
-        if (b < blocks) row[b] = before + excl;
+    for (int b0 = 0; b0 < blocks; b0 += kThreads * EACH) {
+        const int b = b0 + threadIdx.x * EACH;
+        int x[EACH], sum = 0, total;
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) x[i] = row[min(b + i, blocks - 1)];
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            x[i] = b + i < blocks ? x[i] : 0;
+            sum += x[i];
+        }
+        int at = before + rg_block_excl_scan<kSortWaves>(sum, smem, &total);
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            if (b + i < blocks) row[b + i] = at;
+            at += x[i];
+        }
         before += total;
     }
     if (threadIdx.x == 0) totals[blockIdx.x] = before;
 }
 
+template <int BITS>
 __global__ void __launch_bounds__(kThreads) k_sort_scatter(const Entry* __restrict__ from, const int32_t* __restrict__ ids, int64_t n,
                                                            const int32_t* __restrict__ n_dev, uint32_t num_rows, int shift, int64_t per_block,
                                                            const int32_t* __restrict__ counts, const int32_t* __restrict__ totals, Entry* __restrict__ to) {
+    constexpr int DIGITS = 1 << BITS, EACH = DIGITS / kThreads;          // (a thread: EACH neighbouring digits)
     __shared__ int smem[kSortWaves + 1];
-    __shared__ int32_t next[kDigits], met[kSortWaves][kDigits];
+    __shared__ int32_t next[DIGITS], met[kSortWaves][DIGITS];
     const int wave = threadIdx.x >> 6, lane = rg_lane();
-    int all;
-    const int base = rg_block_excl_scan<kSortWaves>(totals[threadIdx.x], smem, &all);
-    next[threadIdx.x] = base + counts[(int64_t)threadIdx.x * gridDim.x + blockIdx.x];
+    int mine[EACH], sum = 0, all;
+#pragma unroll
+    for (int d = 0; d < EACH; ++d) {
+        mine[d] = sum;
+        sum += totals[threadIdx.x * EACH + d];
+    }
+    const int base = rg_block_excl_scan<kSortWaves>(sum, smem, &all);
+#pragma unroll
+    for (int d = 0; d < EACH; ++d)
+        next[threadIdx.x * EACH + d] = base + mine[d] + counts[(int64_t)(threadIdx.x * EACH + d) * gridDim.x + blockIdx.x];
     const int64_t first = (int64_t)blockIdx.x * per_block, last = rg_least(first + per_block, rg_rows(n, n_dev));
     for (int64_t tile = first; tile < last; tile += kTile) {
 #pragma unroll
-        for (int w = 0; w < kSortWaves; ++w) met[w][threadIdx.x] = 0;
+        for (int w = 0; w < kSortWaves; ++w)
+#pragma unroll
+            for (int d = 0; d < EACH; ++d) met[w][threadIdx.x + d * kThreads] = 0;
         __syncthreads();
         Entry e[kRounds];
         int rank[kRounds];
@@ -144,8 +173,8 @@ __global__ void __launch_bounds__(kThreads) k_sort_scatter(const Entry* __restri
 #pragma unroll
         for (int r = 0; r < kRounds; ++r) {
             const int64_t i = tile + wave * (kRounds * RG_WAVE) + r * RG_WAVE + lane;
-            const uint32_t digit = e[r].id >> shift & 255;
-            const uint64_t same = same_digit(digit, i < last);
+            const uint32_t digit = e[r].id >> shift & (DIGITS - 1);
+            const uint64_t same = same_digit<BITS>(digit, i < last);
             const int below = __popcll(same & ((1ull << lane) - 1));
             const int so_far = met[wave][digit];
             wave_exchange();
@@ -154,19 +183,22 @@ __global__ void __launch_bounds__(kThreads) k_sort_scatter(const Entry* __restri
             rank[r] = so_far + below;
         }
         __syncthreads();
-        int at = next[threadIdx.x];
 #pragma unroll
-        for (int w = 0; w < kSortWaves; ++w) {
-            const int here = met[w][threadIdx.x];
-            met[w][threadIdx.x] = at;
-            at += here;
+        for (int d = 0; d < EACH; ++d) {
+            int at = next[threadIdx.x + d * kThreads];
+#pragma unroll
+            for (int w = 0; w < kSortWaves; ++w) {
+                const int here = met[w][threadIdx.x + d * kThreads];
+                met[w][threadIdx.x + d * kThreads] = at;
+                at += here;
+            }
+            next[threadIdx.x + d * kThreads] = at;
         }
-        next[threadIdx.x] = at;
         __syncthreads();
 #pragma unroll
         for (int r = 0; r < kRounds; ++r) {
             const int64_t i = tile + wave * (kRounds * RG_WAVE) + r * RG_WAVE + lane;
-            if (i < last) to[met[wave][e[r].id >> shift & 255] + rank[r]] = e[r];
+            if (i < last) to[met[wave][e[r].id >> shift & (DIGITS - 1)] + rank[r]] = e[r];
         }
         __syncthreads();
     }
@@ -193,13 +225,24 @@ __global__ void __launch_bounds__(kThreads) k_count_ids(const Entry* __restrict_
 // before[piece] = ids met in front of it, before[pieces] and *num_touched = all.
 __global__ void __launch_bounds__(1024) k_scan_ids(int32_t* __restrict__ before, int pieces, int32_t* __restrict__ num_touched) {
     __shared__ int smem[17];
+    constexpr int EACH = 4;
     int so_far = 0;
-    for (int p0 = 0; p0 < pieces; p0 += 1024) {
-        const int p = p0 + threadIdx.x;
-        const int x = p < pieces ? before[p] : 0;
-        int total;
-        const int excl = rg_block_excl_scan<16>(x, smem, &total);
-        if (p < pieces) before[p] = so_far + excl;
+    for (int p0 = 0; p0 < pieces; p0 += 1024 * EACH) {
+        const int p = p0 + threadIdx.x * EACH;
+        int x[EACH], sum = 0, total;
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) x[i] = before[min(p + i, pieces)];        // (without branches, which the loads would wait for one by one)
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            x[i] = p + i < pieces ? x[i] : 0;
+            sum += x[i];
+        }
+        int at = so_far + rg_block_excl_scan<16>(sum, smem, &total);
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            if (p + i < pieces) before[p + i] = at;
+            at += x[i];
+        }
         so_far += total;
     }
     if (threadIdx.x == 0) {
@@ -236,7 +279,7 @@ __device__ __forceinline__ void put_sum(const Target<U>& t, int64_t row, int col
 // A group of 2^log2L lanes walks a piece, a chunk of V columns to a lane (blockIdx.y: which 2^log2L chunks), kWalk rows on their way at a time, and adds up in 32 bits.
 // The sums of an id that opens and ends in the piece are final; what belongs to an id that opened before goes to parts[piece][0], to one that goes on
 // behind to parts[piece][1], for k_join_pieces.  Bound by memory.
-constexpr int kWalk = 4;
+constexpr int kWalk = 8;
 
 template <typename T, typename U, int V, bool SHORT>
 __global__ void __launch_bounds__(kThreads) k_sum_pieces(const T* __restrict__ dy, int64_t dy_stride, const Entry* __restrict__ sorted, int64_t n,
@@ -255,11 +298,16 @@ __global__ void __launch_bounds__(kThreads) k_sum_pieces(const T* __restrict__ d
     for (int j = 0; j < V; ++j) sum[j] = 0.0f;
     float* part = parts + (int64_t)piece * 2 * dim + col;
     if (t.touched && !open && id < num_rows && col == 0) t.touched[row] = (int32_t)id;
+    Entry e[kWalk], ahead[kWalk];
+#pragma unroll
+    for (int u = 0; u < kWalk; ++u) ahead[u] = sorted[rg_least(first + u, last - 1)];
     for (int64_t i = first; i < last && id < num_rows; i += kWalk) {
-        Entry e[kWalk];
         typename RgPack<T, V>::type a[kWalk];
 #pragma unroll
-        for (int u = 0; u < kWalk; ++u) e[u] = sorted[rg_least(i + u, last - 1)];
+        for (int u = 0; u < kWalk; ++u) {
+            e[u] = ahead[u];
+            ahead[u] = sorted[rg_least(i + kWalk + u, last - 1)];
+        }
 #pragma unroll
         for (int u = 0; u < kWalk; ++u) a[u] = load_chunk<V, SHORT>(dy + (int64_t)e[u].at * dy_stride, col, dim);
 #pragma unroll
@@ -288,51 +336,187 @@ __global__ void __launch_bounds__(kThreads) k_sum_pieces(const T* __restrict__ d
     else put_sum<V>(t, row, col, dim, sum);
 }
 
-// The sums of ids whose entries lie in several pieces: a workgroup for the piece in which one of them opens (nothing to do for most), 64 chunks of 4 columns
-// (blockIdx.y: which), four runs of pieces side by side.
-template <typename U>
-__global__ void __launch_bounds__(kThreads) k_join_pieces(const Entry* __restrict__ sorted, int64_t n, const int32_t* __restrict__ n_dev, uint32_t num_rows, int dim,
-                                                          int64_t size, int pieces, Target<U> t, const float* __restrict__ parts) {
-    constexpr int V = 4, RUNS = kThreads / RG_WAVE;
-    __shared__ float runs[RUNS][RG_WAVE * V];
+// The sums of ids whose entries lie in several pieces: a workgroup for the piece in which one of them opens (nothing to do for most), groups of 2^log2L lanes
+// with 4 columns each (blockIdx.y: which 2^log2L) side by side on runs of its pieces.
+constexpr int kJoinThreads = 256, kJoinPieces = 2;
+
+template <typename U, bool SHORT>
+__global__ void __launch_bounds__(kJoinThreads) k_join_pieces(const Entry* __restrict__ sorted, int64_t n, const int32_t* __restrict__ n_dev, uint32_t num_rows, int dim,
+                                                              int64_t size, int pieces, int log2L, Target<U> t, const float* __restrict__ parts) {
+    constexpr int V = 4;
+    __shared__ float sums[kJoinThreads][V];
     const int64_t n_act = rg_rows(n, n_dev);
-    const int lane = rg_lane(), run = threadIdx.x >> 6, col = (blockIdx.y * RG_WAVE + lane) * V;
-    for (int piece = blockIdx.x; piece + 1 < pieces; piece += gridDim.x) {
-        const int64_t first = piece * size, next = first + size;
-        if (next >= n_act) return;
+    const int l = threadIdx.x & ((1 << log2L) - 1), run = threadIdx.x >> log2L, runs = kJoinThreads >> log2L, col = ((blockIdx.y << log2L) + l) * V;
+    // (every wavefront looks at the workgroup's kJoinPieces pieces, a lane each)
+    const int looked = blockIdx.x * kJoinPieces + (rg_lane() & (kJoinPieces - 1));
+    const int64_t begins = looked * size, ends = begins + size;
+    bool open = looked + 1 < pieces && ends < n_act;
+    if (open) {
+        const uint32_t id = sorted[ends].id;
+        open = id < num_rows && sorted[ends - 1].id == id && !(sorted[begins].id == id && !opens(sorted, begins));
+    }
+    for (uint32_t left = (uint32_t)__ballot(open) & ((1u << kJoinPieces) - 1); left; left &= left - 1) {
+        const int piece = blockIdx.x * kJoinPieces + __builtin_ctz(left);
+        const int64_t next = (piece + 1) * size;
         const uint32_t id = sorted[next].id;
-        if (id >= num_rows || sorted[next - 1].id != id || (sorted[first].id == id && !opens(sorted, first))) continue;
         // pieces behind this one that begin with the id: those in front of the first entry of a larger one
         int64_t lo = next, hi = n_act;                     // (sorted[lo].id == id; larger from hi on)
         while (hi - lo > 1) {
             const int64_t mid = (lo + hi) >> 1;
             if (sorted[mid].id == id) lo = mid; else hi = mid;
         }
-        const int from = piece + 1, to = (int)(lo / size) + 1, per = (to - from + RUNS - 1) / RUNS;
+        const int from = piece + 1, to = (int)(lo / size) + 1, per = (to - from + runs - 1) / runs;
         const int start = from + run * per, stop = min(start + per, to);
         float sum[V] = {0.0f, 0.0f, 0.0f, 0.0f};
         if (col < dim) {
-#pragma unroll 4
-            for (int p = start; p < stop; ++p) {
-                float v[V];
-                rg_load_head<V>(parts + (int64_t)p * 2 * dim + col, dim - col, v);
+            constexpr int AHEAD = 8;
+            for (int p0 = start; p0 < stop; p0 += AHEAD) {
+                typename RgPack<float, V>::type a[AHEAD];
 #pragma unroll
-                for (int j = 0; j < V; ++j) sum[j] += v[j];
+                for (int u = 0; u < AHEAD; ++u) a[u] = load_chunk<V, SHORT>(parts + (int64_t)min(p0 + u, stop - 1) * 2 * dim, col, dim);
+#pragma unroll
+                for (int u = 0; u < AHEAD; ++u) {
+                    if (p0 + u >= stop) break;
+                    float v[V];
+                    chunk_numbers<V, SHORT>(a[u], col, dim, v);
+#pragma unroll
+                    for (int j = 0; j < V; ++j) sum[j] += v[j];
+                }
             }
         }
 #pragma unroll
-        for (int j = 0; j < V; ++j) runs[run][lane * V + j] = sum[j];
+        for (int j = 0; j < V; ++j) sums[threadIdx.x][j] = sum[j];
         __syncthreads();
         if (run == 0 && col < dim) {
             rg_load_head<V>(parts + ((int64_t)piece * 2 + 1) * dim + col, dim - col, sum);
+            for (int r = 0; r < min(runs, to - from); ++r)
 #pragma unroll
-            for (int r = 0; r < RUNS; ++r)
-#pragma unroll
-                for (int j = 0; j < V; ++j) sum[j] += runs[r][lane * V + j];
+                for (int j = 0; j < V; ++j) sum[j] += sums[(r << log2L) + l][j];
             put_sum<V>(t, t.touched ? (int64_t)t.before[piece + 1] - 1 : id, col, dim, sum);
         }
         __syncthreads();
     }
+}
+
+// ---------------------------------------------------------------- few entries
+// One workgroup sorts them in LDS and lists the ids met: order[] the entries' rows of dy, run r the entries starts[r] .. starts[r + 1] - 1, of id touched[r].
+constexpr int kFew = 2048, kFewThreads = 1024, kFewWaves = kFewThreads / RG_WAVE, kFewRounds = kFew / kFewThreads;
+
+__global__ void __launch_bounds__(kFewThreads) k_sort_few(const int32_t* __restrict__ ids, int n, const int32_t* __restrict__ n_dev, uint32_t num_rows, int bits,
+                                                          int32_t* __restrict__ order, int32_t* __restrict__ starts, int32_t* __restrict__ touched,
+                                                          int32_t* __restrict__ num_touched, int32_t* __restrict__ count) {
+    constexpr int BITS = 8, DIGITS = 1 << BITS;
+    __shared__ int smem[kFewWaves + 1];
+    __shared__ int32_t met[kFewWaves][DIGITS];
+    __shared__ Entry list[kFew];
+    const int n_act = (int)rg_rows(n, n_dev), wave = threadIdx.x >> 6, lane = rg_lane();
+    Entry e[kFewRounds];
+#pragma unroll
+    for (int r = 0; r < kFewRounds; ++r) {
+        const int i = (wave * kFewRounds + r) * RG_WAVE + lane;
+        const uint32_t id = i < n_act ? (uint32_t)ids[i] : num_rows;
+        e[r] = {id < num_rows ? id : num_rows, (uint32_t)i};
+    }
+    for (int shift = 0; shift < bits; shift += BITS) {
+        int rank[kFewRounds];
+        for (int i = threadIdx.x; i < kFewWaves * DIGITS; i += kFewThreads) met[i / DIGITS][i % DIGITS] = 0;
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < kFewRounds; ++r) {             // (places behind the last entry sort as padding and stay behind all others)
+            const uint32_t digit = e[r].id >> shift & (DIGITS - 1);
+            const uint64_t same = same_digit<BITS>(digit, true);
+            const int below = __popcll(same & ((1ull << lane) - 1));
+            const int so_far = met[wave][digit];
+            wave_exchange();
+            if (below == 0) met[wave][digit] = so_far + __popcll(same);
+            wave_exchange();
+            rank[r] = so_far + below;
+        }
+        __syncthreads();
+        int here[kFewWaves], sum = 0, all;
+        if (threadIdx.x < DIGITS) {
+#pragma unroll
+            for (int w = 0; w < kFewWaves; ++w) {
+                here[w] = sum;
+                sum += met[w][threadIdx.x];
+            }
+        }
+        const int base = rg_block_excl_scan<kFewWaves>(sum, smem, &all);
+        if (threadIdx.x < DIGITS) {
+#pragma unroll
+            for (int w = 0; w < kFewWaves; ++w) met[w][threadIdx.x] = base + here[w];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < kFewRounds; ++r) list[met[wave][e[r].id >> shift & (DIGITS - 1)] + rank[r]] = e[r];
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < kFewRounds; ++r) e[r] = list[(wave * kFewRounds + r) * RG_WAVE + lane];
+    }
+    int heads = 0, total;
+    bool head[kFewRounds];
+#pragma unroll
+    for (int r = 0; r < kFewRounds; ++r) {
+        const int i = threadIdx.x * kFewRounds + r;
+        head[r] = list[i].id < num_rows && (i == 0 || list[i - 1].id != list[i].id);
+        heads += head[r];
+    }
+    int run = rg_block_excl_scan<kFewWaves>(heads, smem, &total);
+#pragma unroll
+    for (int r = 0; r < kFewRounds; ++r) {
+        const int i = threadIdx.x * kFewRounds + r;
+        if (list[i].id < num_rows) order[i] = (int32_t)list[i].at;
+        else if (i > 0 && list[i - 1].id < num_rows) starts[total] = i;         // the entries' end
+        if (head[r]) {
+            starts[run] = i;
+            touched[run++] = (int32_t)list[i].id;
+        }
+    }
+    if (threadIdx.x == 0) {
+        if (list[kFew - 1].id < num_rows) starts[total] = kFew;
+        *count = total;
+        if (num_touched) *num_touched = total;
+    }
+}
+
+// A workgroup to a run and 2^log2L chunks of V columns (blockIdx.y), its groups of lanes side by side on the run's entries.
+template <typename T, typename U, int V, bool SHORT>
+__global__ void __launch_bounds__(kThreads) k_sum_runs(const T* __restrict__ dy, int64_t dy_stride, const int32_t* __restrict__ order, const int32_t* __restrict__ starts,
+                                                       const int32_t* __restrict__ touched, const int32_t* __restrict__ count, int dim, int log2L, int rows,
+                                                       Target<U> t) {
+    __shared__ float sums[kThreads][V];
+    const int run = blockIdx.x;
+    if (run >= *count) return;
+    const int l = threadIdx.x & ((1 << log2L) - 1), group = threadIdx.x >> log2L, groups = kThreads >> log2L, col = ((blockIdx.y << log2L) + l) * V;
+    const int first = starts[run], last = starts[run + 1];
+    float sum[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) sum[j] = 0.0f;
+    if (col < dim) {
+        for (int i = first + group; i < last; i += groups * kWalk) {
+            typename RgPack<T, V>::type a[kWalk];
+#pragma unroll
+            for (int u = 0; u < kWalk; ++u) a[u] = load_chunk<V, SHORT>(dy + (int64_t)order[min(i + u * groups, last - 1)] * dy_stride, col, dim);
+#pragma unroll
+            for (int u = 0; u < kWalk; ++u) {
+                if (i + u * groups >= last) break;
+                float v[V];
+                chunk_numbers<V, SHORT>(a[u], col, dim, v);
+#pragma unroll
+                for (int j = 0; j < V; ++j) sum[j] += v[j];
+            }
+        }
+    }
+    if (last - first > 1) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) sums[threadIdx.x][j] = sum[j];
+        __syncthreads();
+        if (group == 0)
+            for (int r = 1; r < min(groups, last - first); ++r)
+#pragma unroll
+                for (int j = 0; j < V; ++j) sum[j] += sums[(r << log2L) + l][j];
+    }
+    if (group == 0 && col < dim) put_sum<V>(t, rows ? touched[run] : run, col, dim, sum);
 }
 
 // Rows of zeros.
@@ -365,35 +549,62 @@ template <typename U>
 rg_status sum_by_id(rg_ctx* ctx, const char* who, const void* dy, rg_dtype dy_type, int64_t dy_stride, const int32_t* ids, int64_t n, const int32_t* n_dev,
                     int dim, int64_t num_rows, float scale, U* grad, int64_t grad_stride, int add, int32_t* touched, int32_t* num_touched, hipStream_t s) {
     if (!touched && !add && n == 0) { clear_rows(ctx, grad, grad_stride, num_rows, dim, s); return RG_OK; }
-    // pieces of 16 entries or more, and as many of them as fill the device
-    const int most = (int)rg_max64(1024, rg_min64(16384, (1ll << 23) / dim));
-    const int64_t size = rg_max64(16, rg_div_up(n, most));
-    const int pieces = (int)rg_div_up(n, size);
     int bits = 1;
     while (bits < 31 && num_rows >> bits) ++bits;          // ids 0 .. num_rows, padding the last
-    const int passes = (bits + 7) / 8;
+    if (n <= kFew) {
+        const rg_status st = rg_scratch(ctx, ctx->embed_parts, (3 * kFew + 64) * 4, s, who);
+        if (st != RG_OK) return st;
+        int32_t* order = (int32_t*)ctx->embed_parts.p;
+        int32_t *starts = order + kFew, *named = starts + kFew + 32, *count = named + kFew;
+        if (!touched && !add) clear_rows(ctx, grad, grad_stride, num_rows, dim, s);
+        k_sort_few<<<1, kFewThreads, 0, s>>>(ids, (int)n, n_dev, (uint32_t)num_rows, bits, order, starts, touched ? touched : named, num_touched, count);
+        RG_LAUNCH_CHECK(ctx, "k_sort_few");
+        const Target<U> t = {grad, grad_stride, nullptr, nullptr, scale, add};
+        RG_FOR_TYPE(dy_type, {
+            constexpr int V = 16 / (int)(sizeof(T) > sizeof(U) ? sizeof(T) : sizeof(U));
+            const int chunks = (int)rg_div_up(dim, V);
+            int log2L = 0;
+            while (log2L < 6 && 1 << log2L < chunks) ++log2L;
+            const dim3 grid((unsigned)rg_min64(n, num_rows), (unsigned)rg_div_up(chunks, 1 << log2L));
+            const auto kernel = dim < V ? k_sum_runs<T, U, V, true> : k_sum_runs<T, U, V, false>;
+            kernel<<<grid, kThreads, 0, s>>>((const T*)dy, dy_stride, order, starts, touched ? touched : named, count, dim, log2L, touched ? 0 : 1, t);
+        });
+        RG_LAUNCH_CHECK(ctx, "k_sum_runs");
+        return RG_OK;
+    }
+    // pieces of 16 entries or more, and as many of them as fill the device
+    const int most = (int)rg_max64(1024, rg_min64(n / rg_max64(num_rows, 1) >= 64 ? 4096 : 16384, (1ll << 23) / dim));
+    const int64_t size = rg_max64(16, rg_div_up(n, most));
+    const int pieces = (int)rg_div_up(n, size);
+    const int passes = (bits + 9) / 10, digit = (int)rg_max64(8, rg_div_up(bits, passes));
     const int64_t per_block = kTile * rg_max64(1, rg_div_up(n, (int64_t)kTile * 4096));
     const int blocks = (int)rg_div_up(n, per_block);
     // scratch: two lists of entries, counts, totals, ids in front of the pieces, sums of parts
     const size_t list = (size_t)rg_div_up(n * (int64_t)sizeof(Entry), 256) * 256;
-    const size_t counts_bytes = (size_t)rg_div_up((int64_t)kDigits * (blocks + 1) * 4, 256) * 256, before_bytes = (size_t)rg_div_up((pieces + 1) * 4ll, 256) * 256;
+    const size_t counts_bytes = (size_t)rg_div_up(((int64_t)(blocks + 1) << digit) * 4, 256) * 256, before_bytes = (size_t)rg_div_up((pieces + 1) * 4ll, 256) * 256;
     const rg_status st = rg_scratch(ctx, ctx->embed_parts, 2 * list + counts_bytes + before_bytes + (size_t)pieces * 2 * dim * 4, s, who);
     if (st != RG_OK) return st;
     char* at = (char*)ctx->embed_parts.p;
     Entry* lists[2] = {(Entry*)at, (Entry*)(at + list)};
     int32_t* counts = (int32_t*)(at + 2 * list);
-    int32_t* totals = counts + (int64_t)kDigits * blocks;
+    int32_t* totals = counts + ((int64_t)blocks << digit);
     int32_t* before = (int32_t*)(at + 2 * list + counts_bytes);
     float* parts = (float*)(at + 2 * list + counts_bytes + before_bytes);
     if (!touched && !add) clear_rows(ctx, grad, grad_stride, num_rows, dim, s);
     const Entry* from = nullptr;
-    for (int pass = 0; pass < passes; ++pass) {
-        Entry* to = lists[pass & 1];
-        k_sort_count<<<blocks, kThreads, 0, s>>>(from, ids, n, n_dev, (uint32_t)num_rows, pass * 8, per_block, counts);
-        k_sort_scan<<<kDigits, kThreads, 0, s>>>(counts, blocks, totals);
-        k_sort_scatter<<<blocks, kThreads, 0, s>>>(from, ids, n, n_dev, (uint32_t)num_rows, pass * 8, per_block, counts, totals, to);
-        from = to;
-    }
+    const auto sort = [&](auto width) {
+        constexpr int BITS = decltype(width)::value;
+        for (int pass = 0; pass < passes; ++pass) {
+            Entry* to = lists[pass & 1];
+            k_sort_count<BITS><<<blocks, kThreads, 0, s>>>(from, ids, n, n_dev, (uint32_t)num_rows, pass * BITS, per_block, counts);
+            k_sort_scan<<<1 << BITS, kThreads, 0, s>>>(counts, blocks, totals);
+            k_sort_scatter<BITS><<<blocks, kThreads, 0, s>>>(from, ids, n, n_dev, (uint32_t)num_rows, pass * BITS, per_block, counts, totals, to);
+            from = to;
+        }
+    };
+    if (digit == 8) sort(std::integral_constant<int, 8>());
+    else if (digit == 9) sort(std::integral_constant<int, 9>());
+    else sort(std::integral_constant<int, 10>());
     RG_LAUNCH_CHECK(ctx, "k_sort_scatter");
     if (touched) {
         k_count_ids<<<(unsigned)rg_div_up(pieces, kThreads / RG_WAVE), kThreads, 0, s>>>(from, n, n_dev, (uint32_t)num_rows, size, pieces, before);
@@ -402,7 +613,7 @@ rg_status sum_by_id(rg_ctx* ctx, const char* who, const void* dy, rg_dtype dy_ty
     }
     const Target<U> t = {grad, grad_stride, touched, before, scale, add};
     RG_FOR_TYPE(dy_type, {
-        constexpr int V = 16 / (int)sizeof(T);
+        constexpr int V = 16 / (int)(sizeof(T) > sizeof(U) ? sizeof(T) : sizeof(U));
         const int chunks = (int)rg_div_up(dim, V);
         int log2L = 0;
         while (log2L < 6 && 1 << log2L < chunks) ++log2L;
@@ -412,8 +623,12 @@ rg_status sum_by_id(rg_ctx* ctx, const char* who, const void* dy, rg_dtype dy_ty
     });
     RG_LAUNCH_CHECK(ctx, "k_sum_pieces");
     if (pieces > 1) {
-        k_join_pieces<U><<<dim3((unsigned)rg_min64(pieces, 4096), (unsigned)rg_div_up(dim, RG_WAVE * 4)), kThreads, 0, s>>>(
-            from, n, n_dev, (uint32_t)num_rows, dim, size, pieces, t, parts);
+        const int fours = (int)rg_div_up(dim, 4);
+        int log2L = 0;
+        while (log2L < 6 && 1 << log2L < fours) ++log2L;
+        const auto kernel = dim < 4 ? k_join_pieces<U, true> : k_join_pieces<U, false>;
+        kernel<<<dim3((unsigned)rg_div_up(pieces, kJoinPieces), (unsigned)rg_div_up(fours, 1 << log2L)), kJoinThreads, 0, s>>>(
+            from, n, n_dev, (uint32_t)num_rows, dim, size, pieces, log2L, t, parts);
         RG_LAUNCH_CHECK(ctx, "k_join_pieces");
     }
     return RG_OK;

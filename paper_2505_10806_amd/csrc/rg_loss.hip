@@ -672,24 +672,45 @@ __global__ void __launch_bounds__(256) k_loss_join(const float2* __restrict__ st
     if (loss) loss[row] = counts ? sum - target[row] : 0.0f;
 }
 
-// Sums of the splits' parts, in the order of the splits.
-template <typename T>
-__global__ void __launch_bounds__(256) k_grad_join(const float* __restrict__ parts, int splits, int64_t rows, int64_t first, int64_t n,
-                                                   const int32_t* __restrict__ n_dev, int dim, int chunks, T* __restrict__ out, int64_t stride) {
+// Sums of the splits' parts, in one order: RUNS runs of them side by side, 64 chunks of four columns to a workgroup.
+template <typename T, int RUNS, bool SHORT>
+__global__ void __launch_bounds__(64 * RUNS) k_grad_join(const float* __restrict__ parts, int splits, int64_t rows, int64_t first, int64_t n,
+                                                         const int32_t* __restrict__ n_dev, int dim, int chunks, T* __restrict__ out, int64_t stride) {
     constexpr int V = 4;
+    __shared__ float sums[RUNS][64][V];
     const int64_t total = rg_least(rows, rg_rows(n, n_dev) - first) * chunks, one = rows * dim;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-        const int64_t row = i / chunks;
-        const int col = (int)(i - row * chunks) * V;
+    const int lane = threadIdx.x & 63, run = threadIdx.x >> 6, each = (splits + RUNS - 1) / RUNS, from = run * each, to = min(from + each, splits);
+    for (int64_t i0 = (int64_t)blockIdx.x * 64; i0 < total; i0 += (int64_t)gridDim.x * 64) {
+        const int64_t i = i0 + lane, row = rg_least(i, total - 1) / chunks;
+        const int col = (int)(rg_least(i, total - 1) - row * chunks) * V;
+        const float* part = parts + row * dim;
         float sum[V] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 8
-        for (int k = 0; k < splits; ++k) {
-            float v[V];
-            rg_load_head<V>(parts + k * one + row * dim + col, dim - col, v);
+        constexpr int AHEAD = 8;
+        for (int k0 = from; k0 < to; k0 += AHEAD) {
+            typename RgPack<float, V>::type v[AHEAD];
 #pragma unroll
-            for (int j = 0; j < V; ++j) sum[j] += v[j];
+            for (int u = 0; u < AHEAD; ++u) v[u] = SHORT ? rg_load_raw<V>(part + min(k0 + u, to - 1) * one, dim) : rg_load_row<V>(part + min(k0 + u, to - 1) * one, col, dim);
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                if (k0 + u >= to) break;
+#pragma unroll
+                for (int j = 0; j < V; ++j) sum[j] += v[u][j];
+            }
         }
-        rg_store_live<V>(out + row * stride + col, dim - col, sum);
+        if (!SHORT) rg_row_end<V>(sum, col, dim);
+        if constexpr (RUNS > 1) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) sums[run][lane][j] = sum[j];
+            __syncthreads();
+            if (run == 0) {
+#pragma unroll
+                for (int r = 1; r < RUNS; ++r)
+#pragma unroll
+                    for (int j = 0; j < V; ++j) sum[j] += sums[r][lane][j];
+            }
+        }
+        if (run == 0 && i < total) rg_store_live<V>(out + row * stride + col, dim - col, sum);
+        if constexpr (RUNS > 1) __syncthreads();
     }
 }
 
@@ -703,6 +724,324 @@ __global__ void __launch_bounds__(256) k_zero_rows(T* __restrict__ out, int64_t 
         const int64_t row = i / chunks;
         const int col = (int)(i - row * chunks) * V;
         rg_store_live<V>(out + row * stride + col, dim - col, zero);
+    }
+}
+
+// ---------------------------------------------------------------- few classes
+// Up to 64 classes, whose weight rows fit LDS beside a tile of R rows of x: a workgroup walks its rows once, each tile z, g, dx and its share of dweight, so that x is
+// read and dx written once and z is formed once.  z is [class][row] (rows along the lanes); g goes through LDS, from where dx's product reads it by rows and
+// dweight's transposed.  A wavefront's output columns are every fourth 32; dweight's sums stay in registers until the end, then a second launch joins the workgroups'.
+template <int P, int R, int CHUNKS>
+struct FewLds {
+    static constexpr int ROW = CHUNKS * kRowBytes, G_ROW = 128;
+    char weight[P][64 * ROW], x[P][R * ROW], g[P][R * G_ROW];
+    float top[2][R], sum[2][R], target[R];
+    float largest[4];
+};
+static_assert(sizeof(FewLds<3, 32, 2>) <= 160 * 1024 && sizeof(FewLds<3, 64, 1>) <= 160 * 1024 && sizeof(FewLds<1, 32, 4>) <= 160 * 1024, "LDS of a compute unit");
+
+struct FewJob {
+    const void *x, *weight;
+    int64_t x_stride, weight_stride, n;
+    const int32_t *n_dev, *labels;
+    const float *lse, *dloss;
+    int dim, classes;
+    float scale;
+    float *loss, *log_sum;     // LOSS
+    void* dx;                  // else; may be NULL
+    int64_t dx_stride;
+    float* parts;              // [workgroup][class][dim], or NULL
+};
+
+template <typename T, bool GRAD, int R, int CHUNKS>
+__global__ void __launch_bounds__(256, 1) k_few_classes(const FewJob job) {
+    typedef Part<T> S;
+    typedef typename S::type E;
+    typedef FewLds<S::P, R, CHUNKS> Lds;
+    constexpr int P = S::P, ROW = Lds::ROW, RB = R / 32, ROWGROUPS = R / 16, ITEMS = ROWGROUPS * CHUNKS * 4 / 4;
+    __shared__ __attribute__((aligned(16))) Lds lds;
+    const int lane = rg_lane(), wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), half = lane >> 5, i16 = lane & 15;
+    const int64_t n_act = rg_rows(job.n, job.n_dev);
+    const int64_t all = (n_act + R - 1) / R, per = (all + gridDim.x - 1) / gridDim.x, t0 = rg_least(blockIdx.x * per, all);
+    const int tiles = (int)rg_least(per, all - t0), here = (int)(n_act - t0 * R), dim = job.dim, classes = job.classes;
+    const int steps = 2 * ((dim + 31) / 32), blocks = (dim + 31) / 32;
+    if (!GRAD && tiles == 0) return;
+
+    const auto twist = [](int row) __attribute__((always_inline)) { return (row & 3) << 2 | (row >> 2 & 3); };
+    const auto g_twist = [](int row) __attribute__((always_inline)) { return (row >> 1 & 1) << 2 | (row >> 2 & 3); };
+    // 16 rows by 32 columns of a staged matrix: four lanes to a row
+    const auto put = [&](char* const (&plane)[P], const typename RgPack<T, 8>::type& raw, int row, int group, bool counts) __attribute__((always_inline)) {
+        Words4 w[P];
+        const int col = group * 32 + (lane & 3) * 8;
+        if (group * 32 + 32 > dim) row_parts<true, false, T>(raw, col, dim, w);
+        else row_parts<false, false, T>(raw, col, dim, w);
+        const int piece = group * 4 + (lane & 3);
+#pragma unroll
+        for (int p = 0; p < P; ++p) *(Words4*)(plane[p] + row * ROW + ((piece ^ twist(row)) << 4)) = counts ? w[p] : Words4{0, 0, 0, 0};
+    };
+    char *weight_planes[P], *x_planes[P];
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+        weight_planes[p] = lds.weight[p];
+        x_planes[p] = lds.x[p];
+    }
+    // the next tile's rows, on their way while one is worked on
+    typename RgPack<T, 8>::type raw[ITEMS];
+    int raw_label = -1;
+    const T* x = (const T*)job.x;
+    const int to_row = wave % ROWGROUPS * 16 + (lane >> 2), group0 = wave / ROWGROUPS;   // (of 32 columns; item u: group0 + u * 4 / ROWGROUPS)
+    const auto load = [&](int t) __attribute__((always_inline)) {
+        const int64_t from = t0 * R + min(t * R + to_row, here - 1);
+        raw_label = job.labels[from];
+        const T* src = x + from * job.x_stride;
+#pragma unroll
+        for (int u = 0; u < ITEMS; ++u) raw[u] = load_eight<false>(src, (group0 + u * (4 / ROWGROUPS)) * 32 + (lane & 3) * 8, dim);
+    };
+    if (tiles > 0) load(0);
+    int power = 0;
+    if (GRAD && job.dloss) {                               // (shares to at most 1, as above)
+        float top = 0.0f;
+        for (int64_t r = t0 * R + threadIdx.x; r < rg_least((t0 + tiles) * R, n_act); r += 256)
+            if (has_label(job.labels[r], classes)) top = fmaxf(top, fabsf(job.dloss[r]));
+        for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, RG_WAVE));
+        if (lane == 0) lds.largest[wave] = top;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < 4; ++w) top = fmaxf(top, lds.largest[w]);
+        if (top > 0.0f && top < __builtin_inff()) (void)frexpf(top, &power);
+    }
+    for (int group = 0; group < blocks; ++group) {
+        const int row = wave * 16 + (lane >> 2);
+        const T* src = (const T*)job.weight + (int64_t)min(row, classes - 1) * job.weight_stride;
+        put(weight_planes, load_eight<false>(src, group * 32 + (lane & 3) * 8, dim), row, group, row < classes);
+    }
+
+    Acc dw[GRAD ? CHUNKS : 1][2];                          // columns (wave + 4 j) * 32 .., classes 32 c ..
+    if (GRAD) {
+#pragma unroll
+        for (int j = 0; j < CHUNKS; ++j)
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) dw[j][c][i] = 0.0f;
+    }
+    // fragments: rows l % 32 of a block, 16 columns of step k; and, transposed, 16 rows from `first` on of 32 columns
+    const int row_at = (lane & 31) * ROW + ((half ^ twist(lane & 31)) << 4);
+    const int turned_at = (8 * half + (i16 >> 2)) * ROW + ((((lane >> 4 & 1) * 2 + (i16 >> 1 & 1)) ^ ((i16 >> 2) << 2 | 2 * half)) << 4) + (i16 & 1) * 8;
+    typedef __attribute__((address_space(3))) Short4 Lds4;
+    const auto turned = [&](const char* plane, int first, int d) __attribute__((always_inline)) {
+        const char* at = plane + first * ROW + (d >> 2) * kRowBytes;
+        const Words2 low = __builtin_bit_cast(Words2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds4*)(at + (turned_at ^ (d & 3) << 6))));
+        const Words2 high = __builtin_bit_cast(Words2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds4*)(at + 4 * ROW + (turned_at ^ (d & 3) << 6 ^ 1 << 4))));
+        return Words4{low[0], low[1], high[0], high[1]};
+    };
+
+    for (int t = 0; t < tiles; ++t) {
+        __syncthreads();                                   // (the tile before is done with)
+        int label[RB];
+#pragma unroll
+        for (int b = 0; b < RB; ++b) {
+            const int r = t * R + b * 32 + (lane & 31);
+            label[b] = job.labels[t0 * R + min(r, here - 1)];
+            if (r >= here || !has_label(label[b], classes)) label[b] = -1;
+        }
+        const bool counts = t * R + to_row < here && has_label(raw_label, classes);
+#pragma unroll
+        for (int u = 0; u < ITEMS; ++u) {
+            const int group = group0 + u * (4 / ROWGROUPS);
+            if (group < blocks) put(x_planes, raw[u], to_row, group, counts);
+        }
+        load(t + 1);                                       // (of the last row, behind the last tile)
+        __syncthreads();
+
+        // z: a wavefront's block of 32 classes by 32 rows
+        const int cb = wave & 1, rb = wave >> 1;
+        if (rb < RB) {
+            Acc z;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) z[i] = 0.0f;
+            for (int k0 = 0; k0 < steps; k0 += 2) {        // (an even number of them)
+                Words4 a[2][P], b[2][P];
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int p = 0; p < P; ++p) {
+                        const int at = (k0 >> 3) * kRowBytes + (row_at ^ ((k0 & 7) + i) << 5);
+                        a[i][p] = *(const Words4*)(lds.weight[p] + cb * 32 * ROW + at);
+                        b[i][p] = *(const Words4*)(lds.x[p] + rb * 32 * ROW + at);
+                    }
+#pragma unroll
+                for (int i = 0; i < 2; ++i) z = mma_parts<E, P>(a[i], b[i], z);
+            }
+            const int mine = RB == 1 ? label[0] : rb ? label[RB - 1] : label[0], first = cb * 32 + 4 * half;     // register i: class first + 8 (i >> 2) + (i & 3)
+            const int64_t row = t0 * R + min(t * R + rb * 32 + (lane & 31), here - 1);
+            if constexpr (!GRAD) {
+                float top = -__builtin_inff(), there = 0.0f;
+                bool met = false;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int c = first + 8 * (i >> 2) + (i & 3);
+                    z[i] = c < classes ? z[i] : -__builtin_inff();
+                    top = fmaxf(top, z[i]);
+                    there = c == mine ? z[i] : there;
+                    met |= c == mine;
+                }
+                top = fmaxf(top, __shfl_xor(top, 32, RG_WAVE));
+                const float base = top == -__builtin_inff() ? 0.0f : top;
+                float sum = 0.0f;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) sum += __builtin_amdgcn_exp2f((z[i] - base) * kLog2e);
+                sum += __shfl_xor(sum, 32, RG_WAVE);
+                const int at = rb * 32 + (lane & 31);
+                if (half == 0) {
+                    lds.top[cb][at] = top;
+                    lds.sum[cb][at] = sum;
+                }
+                if (met) lds.target[at] = there;
+            } else {
+                const float lse2 = mine >= 0 ? job.lse[row] * kLog2e : 0.0f, share = mine >= 0 ? ldexpf(job.dloss ? job.dloss[row] : 1.0f, S::BIAS - power) : 0.0f;
+                const bool idle = mine < 0 || share == 0.0f;
+                float v[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int c = first + 8 * (i >> 2) + (i & 3);
+                    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(z[i], kLog2e, -lse2));
+                    v[i] = idle || c >= classes ? 0.0f : share * (p - (c == mine ? 1.0f : 0.0f));
+                }
+                const int at = rb * 32 + (lane & 31);
+#pragma unroll
+                for (int i = 0; i < 16; i += 8) {
+                    float eight[8];
+                    Words4 w[P];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) eight[j] = v[i + j];
+                    cut<T>(eight, w);
+#pragma unroll
+                    for (int p = 0; p < P; ++p)
+#pragma unroll
+                        for (int j = 0; j < 2; ++j)
+                            *(Words2*)(lds.g[p] + at * Lds::G_ROW + (((cb * 4 + i / 4 + j) ^ g_twist(at)) << 4) + half * 8) = Words2{w[p][2 * j], w[p][2 * j + 1]};
+                }
+            }
+        }
+        __syncthreads();
+        if constexpr (!GRAD) {
+            if (threadIdx.x < R && t * R + (int)threadIdx.x < here) {
+                const float m0 = lds.top[0][threadIdx.x], m1 = lds.top[1][threadIdx.x], top = fmaxf(m0, m1), base = top == -__builtin_inff() ? 0.0f : top;
+                const float sum = lds.sum[0][threadIdx.x] * __builtin_amdgcn_exp2f((m0 - base) * kLog2e) +
+                                  (m1 == -__builtin_inff() ? 0.0f : lds.sum[1][threadIdx.x] * __builtin_amdgcn_exp2f((m1 - base) * kLog2e));
+                const int64_t row = t0 * R + t * R + threadIdx.x;
+                const bool counts = has_label(job.labels[row], classes);
+                const float lse = top + logf(sum);
+                if (job.log_sum) job.log_sum[row] = counts ? lse : 0.0f;
+                if (job.loss) job.loss[row] = counts ? lse - lds.target[threadIdx.x] : 0.0f;
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < CHUNKS; ++j) {
+                const int d = wave + 4 * j;
+                if (d >= blocks) continue;
+                if (job.dx) {
+                    Acc out[RB];
+#pragma unroll
+                    for (int b = 0; b < RB; ++b)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) out[b][i] = 0.0f;
+#pragma unroll
+                    for (int f = 0; f < 4; ++f) {
+                        Words4 a[P];
+#pragma unroll
+                        for (int p = 0; p < P; ++p) a[p] = turned(lds.weight[p], f * 16, d);
+#pragma unroll
+                        for (int b = 0; b < RB; ++b) {
+                            const int at = b * 32 + (lane & 31);
+                            Words4 g[P];
+#pragma unroll
+                            for (int p = 0; p < P; ++p) g[p] = *(const Words4*)(lds.g[p] + at * Lds::G_ROW + (((2 * f + half) ^ g_twist(at)) << 4));
+                            out[b] = mma_parts<E, P>(a, g, out[b]);
+                        }
+                    }
+#pragma unroll
+                    for (int b = 0; b < RB; ++b) {
+                        const int r = t * R + b * 32 + (lane & 31);
+                        if (r >= here) continue;
+                        T* to = (T*)job.dx + (t0 * R + r) * job.dx_stride;
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            const int col = d * 32 + q * 8 + half * 4;
+                            if (col >= dim) continue;
+                            float v[4];
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) v[i] = label[b] < 0 ? 0.0f : ldexpf(out[b][q * 4 + i] * job.scale, power - S::BIAS);
+                            rg_store_live<4>(to + col, dim - col, v);
+                        }
+                    }
+                }
+                if (job.parts) {
+#pragma unroll
+                    for (int f = 0; f < R / 16; ++f) {
+                        Words4 a[P];
+#pragma unroll
+                        for (int p = 0; p < P; ++p) a[p] = turned(lds.x[p], f * 16, d);
+#pragma unroll
+                        for (int c = 0; c < 2; ++c) {
+                            const int row = f * 16 + 8 * half + (i16 >> 2), piece = c * 4 + (lane >> 4 & 1) * 2 + (i16 >> 1 & 1);
+                            Words4 g[P];
+#pragma unroll
+                            for (int p = 0; p < P; ++p) {
+                                const Words2 low = __builtin_bit_cast(Words2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                    (Lds4*)(lds.g[p] + row * Lds::G_ROW + ((piece ^ g_twist(row)) << 4) + (i16 & 1) * 8)));
+                                const Words2 high = __builtin_bit_cast(Words2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                    (Lds4*)(lds.g[p] + (row + 4) * Lds::G_ROW + ((piece ^ g_twist(row + 4)) << 4) + (i16 & 1) * 8)));
+                                g[p] = Words4{low[0], low[1], high[0], high[1]};
+                            }
+                            dw[j][c] = mma_parts<E, P>(a, g, dw[j][c]);
+                        }
+                    }
+                }
+            }
+        }
+    }
+    if constexpr (GRAD) {
+        if (!job.parts) return;
+#pragma unroll
+        for (int j = 0; j < CHUNKS; ++j)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                const int own = c * 32 + (lane & 31);
+                if (own >= classes) continue;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int col = (wave + 4 * j) * 32 + q * 8 + half * 4;
+                    if (col >= dim) continue;
+                    float v[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) v[i] = ldexpf(dw[j][c][q * 4 + i] * job.scale, power - S::BIAS);
+                    rg_store_live<4>(job.parts + ((int64_t)blockIdx.x * classes + own) * dim + col, dim - col, v);
+                }
+            }
+    }
+}
+
+// Whether the kernel above takes rows of `dim` numbers, and its launch.
+constexpr int kFewClasses = 64;
+template <typename T>
+bool few_classes(int classes, int dim) { return classes <= kFewClasses && dim >= 8 && dim <= (Part<T>::P > 1 ? 256 : 512); }
+// Rows of a tile: 64, or 32 where LDS or registers do not suffice.
+template <typename T>
+int few_rows(int dim) { return dim > (Part<T>::P > 1 ? kCols : 2 * kCols) ? 32 : 64; }
+
+template <typename T, bool GRAD>
+void launch_few(const FewJob& job, unsigned grid, hipStream_t s) {
+    const int chunks = (int)rg_div_up(job.dim, kCols);
+    if constexpr (Part<T>::P > 1) {
+        if (chunks == 1) k_few_classes<T, GRAD, 64, 1><<<grid, 256, 0, s>>>(job);
+        else k_few_classes<T, GRAD, 32, 2><<<grid, 256, 0, s>>>(job);
+    } else {
+        if (chunks == 1) k_few_classes<T, GRAD, 64, 1><<<grid, 256, 0, s>>>(job);
+        else if (chunks == 2) k_few_classes<T, GRAD, 64, 2><<<grid, 256, 0, s>>>(job);
+        else if (chunks == 3) k_few_classes<T, GRAD, 32, 3><<<grid, 256, 0, s>>>(job);
+        else k_few_classes<T, GRAD, 32, 4><<<grid, 256, 0, s>>>(job);
     }
 }
 
@@ -730,6 +1069,15 @@ void pack(rg_ctx* ctx, const void* x, int64_t stride, int64_t first, int64_t cou
     const int64_t units = rg_div_up(count, kOwners) * (kOwners / 32) * steps;
     k_pack_rows<T><<<(unsigned)rg_min64(rg_div_up(units, 4), (int64_t)ctx->num_cus * 32), 256, 0, s>>>((const T*)x, stride, first, n, n_dev, dim, steps, labels, classes,
                                                                                                  units, (Words4*)packed);
+}
+
+template <typename T>
+void join_parts(rg_ctx* ctx, const float* parts, int splits, int64_t rows, int64_t first, int64_t n, const int32_t* n_dev, int dim, T* out, int64_t stride, hipStream_t s) {
+    const int quads = (int)rg_div_up(dim, 4);
+    const unsigned grid = (unsigned)rg_min64(rg_div_up(rows * quads, 64), (int64_t)ctx->num_cus * 32);
+    const int runs = splits >= 32 ? 16 : 4;
+    const auto kernel = dim < 4 ? k_grad_join<T, 4, true> : runs == 4 ? k_grad_join<T, 4, false> : k_grad_join<T, 16, false>;
+    kernel<<<grid, dim < 4 ? 256 : 64 * runs, 0, s>>>(parts, splits, rows, first, n, n_dev, dim, quads, out, stride);
 }
 
 // Splits of the walked rows: as many workgroups as fill the device twice.
@@ -780,6 +1128,23 @@ rg_status rg_cross_entropy(rg_ctx* ctx, const void* x, rg_dtype type, int64_t x_
     hipStream_t s = (hipStream_t)stream;
     RG_FOR_TYPE(type, {
         constexpr int P = Part<T>::P;
+        if (few_classes<T>(classes, dim)) {
+            FewJob job = {};
+            job.x = x;
+            job.weight = weight;
+            job.x_stride = x_stride;
+            job.weight_stride = weight_stride;
+            job.n = n;
+            job.n_dev = n_dev;
+            job.labels = labels;
+            job.dim = dim;
+            job.classes = classes;
+            job.loss = loss;
+            job.log_sum = lse;
+            launch_few<T, false>(job, (unsigned)rg_min64(rg_div_up(n, few_rows<T>(dim)), (int64_t)ctx->num_cus * 2), s);
+            RG_LAUNCH_CHECK(ctx, "k_few_classes");
+            return RG_OK;
+        }
         const int steps = steps_of(dim);
         const int64_t piece = piece_rows(n, steps, P), most = rg_min64(piece, n), tiles = rg_div_up(most, kOwners);
         const int splits = splits_for(ctx, tiles, classes);
@@ -834,12 +1199,41 @@ rg_status rg_cross_entropy_grad(rg_ctx* ctx, const void* x, rg_dtype type, int64
     hipStream_t s = (hipStream_t)stream;
     RG_FOR_TYPE(type, {
         constexpr int P = Part<T>::P;
-        const int quads = (int)rg_div_up(dim, 4);
         if (n == 0) {
             const int pieces = (int)rg_div_up(dim, 16 / (int)sizeof(T));
             k_zero_rows<T><<<(unsigned)rg_min64(rg_div_up((int64_t)classes * pieces, 256), (int64_t)ctx->num_cus * 32), 256, 0, s>>>((T*)dweight, dweight_stride, classes,
                                                                                                                      dim, pieces);
             RG_LAUNCH_CHECK(ctx, "k_zero_rows");
+            return RG_OK;
+        }
+        if (few_classes<T>(classes, dim)) {
+            const int64_t tiles = rg_div_up(n, few_rows<T>(dim)), grid = rg_min64(tiles, ctx->num_cus);
+            if (dweight) {
+                const rg_status st = rg_scratch(ctx, ctx->loss_parts, (size_t)grid * classes * dim * 4, s, "rg_cross_entropy_grad");
+                if (st != RG_OK) return st;
+            }
+            FewJob job = {};
+            job.x = x;
+            job.weight = weight;
+            job.x_stride = x_stride;
+            job.weight_stride = weight_stride;
+            job.n = n;
+            job.n_dev = n_dev;
+            job.labels = labels;
+            job.lse = lse;
+            job.dloss = dloss;
+            job.dim = dim;
+            job.classes = classes;
+            job.scale = scale;
+            job.dx = dx;
+            job.dx_stride = dx_stride;
+            job.parts = dweight ? (float*)ctx->loss_parts.p : nullptr;
+            launch_few<T, true>(job, (unsigned)grid, s);
+            RG_LAUNCH_CHECK(ctx, "k_few_classes");
+            if (dweight) {
+                join_parts<T>(ctx, job.parts, (int)grid, classes, 0, classes, nullptr, dim, (T*)dweight, dweight_stride, s);
+                RG_LAUNCH_CHECK(ctx, "k_grad_join");
+            }
             return RG_OK;
         }
         const int steps = steps_of(dim), chunks = (int)rg_div_up(dim, kCols);
@@ -884,9 +1278,7 @@ rg_status rg_cross_entropy_grad(rg_ctx* ctx, const void* x, rg_dtype type, int64
             job.out_stride = stride;
         };
         const auto join = [&](int64_t rows, const int32_t* count) {
-            if (job.splits > 1)
-                k_grad_join<T><<<(unsigned)rg_min64(rg_div_up(job.owners * quads, 256), (int64_t)ctx->num_cus * 32), 256, 0, s>>>(
-                    job.parts, job.splits, job.owners, job.first, rows, count, dim, quads, (T*)job.out, job.out_stride);
+            if (job.splits > 1) join_parts<T>(ctx, job.parts, job.splits, job.owners, job.first, rows, count, dim, (T*)job.out, job.out_stride, s);
         };
         for (int64_t first = 0; dx && first < n; first += for_dx.piece) {
             take(for_dx, first, dx, dx_stride);

@@ -177,7 +177,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_softmax_rows(const Job job) {
     // HOLD: the owned rows stay in registers.  PIPE: the exponentials of a tile are formed between the products of the next one's z, so that the vector and the
     // matrix units work side by side; for that the tile stays in LDS for its second product while two more arrive.
     constexpr bool HOLD = P == 1 && STEPS > 0 && (STEPS <= kSteps || MODE == LOSS), PIPE = STEPS > 0 && (STEPS <= kSteps || HOLD);
-    constexpr int CHUNKS = PIPE && STEPS > kSteps ? 2 : 1, BUFFERS = PIPE && MODE != LOSS ? 3 : 2;
+    constexpr int CHUNKS = STEPS > kSteps ? 2 : 1, BUFFERS = PIPE && MODE != LOSS ? 3 : 2;
     constexpr int ITEMS = (STEPS > 0 && STEPS < kSteps ? STEPS / 2 * GROUPS + kWaves - 1 : 4 * GROUPS) / kWaves;
     __shared__ __attribute__((aligned(16))) char staged[BUFFERS][CHUNKS][P][ROWS * kRowBytes];
     __shared__ __attribute__((aligned(16))) float row_lse[3][ROWS], row_share[3][ROWS], row_both[3][ROWS];
@@ -387,10 +387,10 @@ __global__ void __launch_bounds__(kThreads, 2) k_softmax_rows(const Job job) {
             const int q = u / (2 * D), f = u / D % 2, d = u % D;
 #pragma unroll
             for (int p = 0; p < P; ++p) {
-                const char* at = staged[buffer][0][p] + (q * 32 + f * 16) * kRowBytes;
+                const char* at = staged[buffer][d / 4][p] + (q * 32 + f * 16) * kRowBytes;
                 typedef __attribute__((address_space(3))) Short4 Lds;
-                const Words2 low = __builtin_bit_cast(Words2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds*)(at + (low_at ^ d << 6))));
-                const Words2 high = __builtin_bit_cast(Words2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds*)(at + 8 * kRowBytes + (low_at ^ d << 6 ^ 2 << 4))));
+                const Words2 low = __builtin_bit_cast(Words2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds*)(at + (low_at ^ d % 4 << 6))));
+                const Words2 high = __builtin_bit_cast(Words2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds*)(at + 8 * kRowBytes + (low_at ^ d % 4 << 6 ^ 2 << 4))));
                 turned[u % RING][p] = Words4{low[0], low[1], high[0], high[1]};
             }
         };
@@ -481,8 +481,31 @@ __global__ void __launch_bounds__(kThreads, 2) k_softmax_rows(const Job job) {
         __builtin_amdgcn_sched_barrier(0);
     };
 
+    // the powers of a whole tile
+    const auto powers = [&](int t, int place, Acc (&z)[SB]) __attribute__((always_inline)) {
+        const bool rare = open_tile(t, place, z);
+        base = m == -__builtin_inff() ? 0.0f : m * kLog2e;
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int q = 0; q < SB; ++q)
+#pragma unroll
+            for (int f = 0; f < 2; ++f) {
+                float v[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    v[j] = power_of(z[q][f * 8 + j], MODE == DW ? row_both[place][q * 32 + f * 16 + row_at(j) + 4 * half] : 0.0f);
+                    if (MODE == LOSS) s += v[j];
+                }
+                if (MODE != LOSS) {
+                    if (rare) mend(t, place, z, q, f, v);
+                    cut<T>(v, g[MODE == LOSS ? 0 : q][f]);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+    };
+
 #define RG_INT(N) std::integral_constant<int, N>()
-    constexpr int FIRST = STEPS == 0 || STEPS > kSteps ? 4 : STEPS / 2, SECOND = STEPS > kSteps ? (STEPS - kSteps) / 2 : 4;      // blocks of output columns
+    constexpr int FIRST = STEPS == 0 ? 4 : STEPS / 2;      // blocks of output columns
     if constexpr (PIPE) {
         // A tile: its exponentials beside the next one's products, its second product, the tile after the next one to LDS.  (Behind the last tile the products are of
         // what lies there, and are not used.)
@@ -548,6 +571,27 @@ __global__ void __launch_bounds__(kThreads, 2) k_softmax_rows(const Job job) {
             now = turn(t, now, z[0], z[1]);
             if (t + 1 < tiles) now = turn(t + 1, now, z[1], z[0]);
         }
+    } else if constexpr (STEPS > 0) {
+        // A tile after the other, the next one's rows on their way: z, powers, second product.  (Sums for 256 output columns leave no registers for a second z.)
+        Acc z[SB];
+        if (tiles > 0) {
+            load(0, 0, true);
+            next_tile();
+            store(0, 0, 0, true, 0);
+            __syncthreads();
+        }
+#pragma unroll 1
+        for (int t = 0; t < tiles; ++t) {
+            const int buffer = t & 1;
+            clear(z);
+            products(RG_INT(STEPS), 0, buffer, z, nothing);
+            load(t + 1, 0, true);                          // (behind the products of z, which leave no registers for them)
+            next_tile();
+            powers(t, buffer, z);
+            if constexpr (MODE != LOSS) second(RG_INT(0), RG_INT(FIRST), buffer, nothing);
+            if (t + 1 < tiles) store(t + 1, 0, buffer ^ 1, true, buffer ^ 1);
+            __syncthreads();
+        }
     } else {
         Acc z[SB];
         const auto add_products = [&](int chunk, int buffer) __attribute__((always_inline)) {
@@ -578,25 +622,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_softmax_rows(const Job job) {
             // (the next rows are asked for behind the products of z, which leave no registers for them)
             const bool rest = NB > 4 && more > 0, go_on = t + 1 < tiles;
             add_products(chunk_of(chunks - 1), buffer);
-            const bool rare = open_tile(t, place, z);
-            base = m == -__builtin_inff() ? 0.0f : m * kLog2e;
-            __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int q = 0; q < SB; ++q)
-#pragma unroll
-                for (int f = 0; f < 2; ++f) {
-                    float v[8];
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        v[j] = power_of(z[q][f * 8 + j], MODE == DW ? row_both[place][q * 32 + f * 16 + row_at(j) + 4 * half] : 0.0f);
-                        if (MODE == LOSS) s += v[j];
-                    }
-                    if (MODE != LOSS) {
-                        if (rare) mend(t, place, z, q, f, v);
-                        cut<T>(v, g[MODE == LOSS ? 0 : q][f]);
-                    }
-                    __builtin_amdgcn_sched_barrier(0);
-                }
+            powers(t, place, z);
             if (!rest) next_tile();
             load(rest ? t : t + 1, rest ? chunk_of(chunks) : chunk_of(0), !rest);
             if constexpr (MODE != LOSS) second(RG_INT(0), RG_INT(4), buffer, nothing);
@@ -607,7 +633,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_softmax_rows(const Job job) {
                 if (rest) {
                     next_tile();
                     load(t + 1, chunk_of(0), true);
-                    second(RG_INT(4), RG_INT(SECOND), buffer, nothing);
+                    second(RG_INT(4), RG_INT(4), buffer, nothing);
                     if (go_on) store(t + 1, chunk_of(0), buffer ^ 1, true, place ^ 1);
                     __syncthreads();
                     buffer ^= 1;

@@ -173,7 +173,7 @@ template <typename T, int MODE, int NB, int STEPS>
 __global__ void __launch_bounds__(kThreads, 2) k_softmax_rows(const Job job) {
     typedef Part<T> S;
     typedef typename S::type E;
-    constexpr int P = S::P, ROWS = S::ROWS, SB = ROWS / 32, GROUPS = ROWS / 16;
+    constexpr int P = S::P, ROWS = MODE == LOSS && STEPS == 0 ? 2 * S::ROWS : S::ROWS, SB = ROWS / 32, GROUPS = ROWS / 16;     // (owned rows are read again for every tile)
     // HOLD: the owned rows stay in registers.  PIPE: the exponentials of a tile are formed between the products of the next one's z, so that the vector and the
     // matrix units work side by side; for that the tile stays in LDS for its second product while two more arrive.
     constexpr bool HOLD = P == 1 && STEPS > 0 && (STEPS <= kSteps || MODE == LOSS), PIPE = STEPS > 0 && (STEPS <= kSteps || HOLD);
@@ -672,13 +672,11 @@ __global__ void __launch_bounds__(kThreads, 2) k_softmax_rows(const Job job) {
     }
 }
 
-// Each row's log-sum and loss from its splits.
-__global__ void __launch_bounds__(256) k_loss_join(const float2* __restrict__ stats, int splits, int64_t first, int64_t count, int64_t n,
-                                                   const int32_t* __restrict__ n_dev, const int32_t* __restrict__ labels, int classes, const float* __restrict__ target, float* __restrict__ loss,
-                                                   float* __restrict__ lse) {
-    // 16 lanes to a row
-    const int64_t row = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 4;
-    const int l = threadIdx.x & 15;
+// Each row's log-sum and loss from its splits, a wavefront to a row.
+__global__ void __launch_bounds__(64) k_loss_join(const float2* __restrict__ stats, int splits, int64_t first, int64_t count, int64_t n,
+                                                  const int32_t* __restrict__ n_dev, const int32_t* __restrict__ labels, int classes,
+                                                  const float* __restrict__ target, float* __restrict__ loss, float* __restrict__ lse) {
+    const int64_t row = blockIdx.x;
     if (row >= rg_least(count, rg_rows(n, n_dev) - first)) return;
     float m = -__builtin_inff(), s = 0.0f;
     const auto merge = [&](float other_m, float other_s) {
@@ -686,12 +684,17 @@ __global__ void __launch_bounds__(256) k_loss_join(const float2* __restrict__ st
         s = s * __builtin_amdgcn_exp2f((m - base) * kLog2e) + other_s * __builtin_amdgcn_exp2f((other_m - base) * kLog2e);
         m = top;
     };
-    for (int k = l; k < splits; k += 16) {
-        const float2 part = stats[(int64_t)k * count + row];
-        merge(part.x, part.y);
+    constexpr int AHEAD = 4;
+    for (int k0 = rg_lane(); k0 < splits; k0 += 64 * AHEAD) {
+        float2 part[AHEAD];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) part[u] = stats[(int64_t)min(k0 + 64 * u, splits - 1) * count + row];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u)
+            if (k0 + 64 * u < splits) merge(part[u].x, part[u].y);
     }
-    for (int off = 8; off > 0; off >>= 1) merge(__shfl_xor(m, off, 16), __shfl_xor(s, off, 16));
-    if (l != 0) return;
+    for (int off = 32; off > 0; off >>= 1) merge(__shfl_xor(m, off, RG_WAVE), __shfl_xor(s, off, RG_WAVE));
+    if (rg_lane() != 0) return;
     const bool counts = has_label(labels[row], classes);
     const float sum = m + logf(s);
     if (lse) lse[row] = counts ? sum : 0.0f;
@@ -1071,6 +1074,107 @@ void launch_few(const FewJob& job, unsigned grid, hipStream_t s) {
     }
 }
 
+// ---------------------------------------------------------------- few rows
+// The loss of up to 32 rows against many classes: the weight is read once, by every wavefront for itself, 32 classes at a time straight into the matrix units' registers
+// (x's rows, 16-bit parts of them, stay in LDS).  A lane takes 16 neighbouring columns at a time, two steps' worth: the order of the columns is free as
+// long as both operands have the same.  Bound by memory.
+constexpr int kFewWaves = 8;
+
+template <typename T>
+__global__ void __launch_bounds__(64 * kFewWaves, 2) k_few_rows(const T* __restrict__ x, int64_t x_stride, int n, const int32_t* __restrict__ n_dev, int dim, int pairs,
+                                                                const T* __restrict__ weight, int64_t weight_stride, int classes, const int32_t* __restrict__ labels,
+                                                                float2* __restrict__ stats, float* __restrict__ target) {
+    typedef typename Part<T>::type E;
+    constexpr int P = Part<T>::P, AHEAD = P == 1 ? 4 : 2;
+    extern __shared__ __attribute__((aligned(16))) Words4 rows[];          // [pair of steps][step][part][lane]
+    __shared__ float tops[kFewWaves][32], sums[kFewWaves][32];
+    const int n_act = (int)rg_rows(n, n_dev), lane = rg_lane(), wave = threadIdx.x >> 6, half = lane >> 5, row = lane & 31;
+    const auto parts_of = [&](const T* src, int col, bool counts, Words4 (&w)[P]) __attribute__((always_inline)) {
+        const typename RgPack<T, 8>::type raw = load_eight<false>(src, col, dim);
+        if (col + 8 > dim) row_parts<true, false, T>(raw, col, dim, w);
+        else row_parts<false, false, T>(raw, col, dim, w);
+        if (!counts) {
+#pragma unroll
+            for (int p = 0; p < P; ++p) w[p] = Words4{0, 0, 0, 0};
+        }
+    };
+    for (int k = wave; k < 2 * pairs; k += kFewWaves) {
+        Words4 w[P];
+        parts_of(x + (int64_t)min(row, max(n_act - 1, 0)) * x_stride, (k >> 1) * 32 + half * 16 + (k & 1) * 8, row < n_act, w);
+#pragma unroll
+        for (int p = 0; p < P; ++p) rows[(k * P + p) * 64 + lane] = w[p];
+    }
+    const int label = row < n_act && has_label(labels[row], classes) ? labels[row] : -1;
+    __syncthreads();
+    float m = -__builtin_inff(), s = 0.0f;
+    const int blocks = (classes + 31) / 32, step = gridDim.x * kFewWaves;
+    for (int block = blockIdx.x * kFewWaves + wave; block < blocks; block += step) {
+        const T* src = weight + (int64_t)min(block * 32 + row, classes - 1) * weight_stride;
+        Acc z;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) z[i] = 0.0f;
+        for (int k0 = 0; k0 < pairs; k0 += AHEAD) {
+            typename RgPack<T, 8>::type raw[AHEAD][2];
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) raw[u][j] = load_eight<false>(src, min(k0 + u, pairs - 1) * 32 + half * 16 + j * 8, dim);
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                if (k0 + u >= pairs) break;
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    Words4 a[P], b[P];
+                    const int col = (k0 + u) * 32 + half * 16 + j * 8;
+                    if (k0 + u + 1 == pairs) row_parts<true, false, T>(raw[u][j], col, dim, a);
+                    else row_parts<false, false, T>(raw[u][j], col, dim, a);
+#pragma unroll
+                    for (int p = 0; p < P; ++p) b[p] = rows[(((k0 + u) * 2 + j) * P + p) * 64 + lane];
+                    z = mma_parts<E, P>(a, b, z);
+                }
+            }
+        }
+        const int first = block * 32 + 4 * half;           // register i: class first + 8 (i >> 2) + (i & 3)
+        if (block * 32 + 32 > classes) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) z[i] = first + 8 * (i >> 2) + (i & 3) < classes ? z[i] : -__builtin_inff();
+        }
+        if (__any(label >= block * 32 && label < block * 32 + 32)) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (label == first + 8 * (i >> 2) + (i & 3)) target[row] = z[i];
+        }
+        float top = m;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top = fmaxf(top, z[i]);
+        const float base = top == -__builtin_inff() ? 0.0f : top;
+        s *= __builtin_amdgcn_exp2f((m - base) * kLog2e);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s += __builtin_amdgcn_exp2f((z[i] - base) * kLog2e);
+        m = top;
+    }
+    const auto merge = [&](float other_m, float other_s) __attribute__((always_inline)) {
+        const float top = fmaxf(m, other_m), base = top == -__builtin_inff() ? 0.0f : top;
+        s = s * __builtin_amdgcn_exp2f((m - base) * kLog2e) + other_s * __builtin_amdgcn_exp2f((other_m - base) * kLog2e);
+        m = top;
+    };
+    merge(__shfl_xor(m, 32, RG_WAVE), __shfl_xor(s, 32, RG_WAVE));
+    if (half == 0) {
+        tops[wave][row] = m;
+        sums[wave][row] = s;
+    }
+    __syncthreads();
+    if (threadIdx.x >= 32) return;
+#pragma unroll
+    for (int w = 1; w < kFewWaves; ++w) merge(tops[w][row], sums[w][row]);
+    if (row < n_act) stats[(int64_t)blockIdx.x * n + row] = make_float2(m, s);
+}
+
+// Whether the kernel above takes the call: its rows as parts lie in LDS (16 KB at 256 numbers of 16 bits).
+constexpr int kFewRows = 32;
+template <typename T>
+bool few_rows_many_classes(int64_t n, int dim) { return n <= kFewRows && dim >= 8 && rg_div_up(dim, 32) * 2 * Part<T>::P * 1024 <= 60 * 1024; }
+
 bool aligned(const void* p, int bytes) { return (uintptr_t)p % (uintptr_t)bytes == 0; }
 
 constexpr int64_t kMostRows = (1ll << 31) - 1;
@@ -1171,6 +1275,19 @@ rg_status rg_cross_entropy(rg_ctx* ctx, const void* x, rg_dtype type, int64_t x_
             RG_LAUNCH_CHECK(ctx, "k_few_classes");
             return RG_OK;
         }
+        if (few_rows_many_classes<T>(n, dim)) {
+            const int pairs = (int)rg_div_up(dim, 32), grid = (int)rg_min64(rg_div_up(classes, 32 * kFewWaves), (int64_t)ctx->num_cus * 2);
+            const rg_status st = rg_scratch(ctx, ctx->loss_parts, (size_t)grid * n * sizeof(float2) + kFewRows * 4, s, "rg_cross_entropy");
+            if (st != RG_OK) return st;
+            float2* stats = (float2*)ctx->loss_parts.p;
+            float* target = (float*)(stats + (int64_t)grid * n);
+            k_few_rows<T><<<grid, 64 * kFewWaves, pairs * 2 * P * 1024, s>>>((const T*)x, x_stride, (int)n, n_dev, dim, pairs, (const T*)weight, weight_stride, classes,
+                                                                             labels, stats, target);
+            RG_LAUNCH_CHECK(ctx, "k_few_rows");
+            k_loss_join<<<(unsigned)n, 64, 0, s>>>(stats, grid, 0, n, n, n_dev, labels, classes, target, loss, lse);
+            RG_LAUNCH_CHECK(ctx, "k_loss_join");
+            return RG_OK;
+        }
         const int steps = steps_of(dim);
         const int64_t piece = piece_rows(n, steps, P), most = rg_min64(piece, n), tiles = rg_div_up(most, kOwners);
         const int splits = splits_for(ctx, tiles, classes);
@@ -1201,7 +1318,7 @@ rg_status rg_cross_entropy(rg_ctx* ctx, const void* x, rg_dtype type, int64_t x_
             job.labels = labels + first;
             launch<T, LOSS>(job, 1, s);
             RG_LAUNCH_CHECK(ctx, "k_softmax_rows");
-            k_loss_join<<<(unsigned)rg_div_up(count, 16), 256, 0, s>>>(job.stats, splits, first, count, n, n_dev, job.labels, classes, job.target,
+            k_loss_join<<<(unsigned)count, 64, 0, s>>>(job.stats, splits, first, count, n, n_dev, job.labels, classes, job.target,
                                                                        loss ? loss + first : nullptr, lse ? lse + first : nullptr);
             RG_LAUNCH_CHECK(ctx, "k_loss_join");
         }

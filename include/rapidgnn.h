@@ -547,10 +547,11 @@ RG_API rg_status rg_embedding_grad_rows(rg_ctx* ctx, const void* dy, rg_dtype dy
  * A classifier's last product and its loss in one, for a data set's classes or for all nodes as classes: nothing of size n by classes is
  * stored.  A row whose label lies outside [0, classes) does not count: its loss and lse are 0, whatever it holds.
  * x: device, n rows of type `type`; weight: device, `classes` rows of the same type; labels: device int32[n]; loss, lse: device float[n],
- * either may be NULL (not wanted).  1 <= dim <= RG_LOSS_MAX_DIM; classes >= 1.
+ * either may be NULL (not wanted).  1 <= dim <= RG_LOSS_MAX_DIM, 1 <= classes <= RG_LOSS_MAX_CLASSES.
  * Products and sums are the matrix unit's, in 32 bits; 32-bit numbers go through it in three parts of bf16, and what they have below 2^-133
  * is cut off.  A row whose z are not all finite, or -infinity, has no finite lse; an infinity among 32-bit numbers gives NaN. */
 #define RG_LOSS_MAX_DIM 65536
+#define RG_LOSS_MAX_CLASSES (1 << 30)
 RG_API rg_status rg_cross_entropy(rg_ctx* ctx, const void* x, rg_dtype type, int64_t x_stride, int64_t n, const int32_t* n_dev,
                                   int32_t dim, const void* weight, int64_t weight_stride, int32_t classes, const int32_t* labels,
                                   float* loss, float* lse, void* stream);

@@ -24,6 +24,7 @@ RG_STATIC_GATHER_MAX_ROWS = 1 << 20
 RG_GATHER_PART_HBM, RG_GATHER_PART_MISS = 1, 2
 RG_F32, RG_BF16, RG_F16 = range(3)
 RG_MX4_MAX_DIM = RG_NORM_MAX_DIM = RG_EMBED_MAX_DIM = RG_LOSS_MAX_DIM = 65536
+RG_LOSS_MAX_CLASSES = 1 << 30
 RG_K_GATHER_HBM, RG_K_GATHER_MISS, RG_K_SAMPLE, RG_K_HISTOGRAM, RG_K_CACHE_FILL, RG_K_AGGREGATE = range(6)
 
 _TYPES = {torch.float32: RG_F32, torch.bfloat16: RG_BF16, torch.float16: RG_F16}

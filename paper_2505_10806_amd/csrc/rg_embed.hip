@@ -664,6 +664,7 @@ rg_status rg_embedding(rg_ctx* ctx, const void* table, rg_dtype table_type, int6
     RG_REQUIRE(ctx, scale == scale, "rg_embedding: scale is not a number");
     if (n == 0) return RG_OK;
     RG_REQUIRE(ctx, table && ids && y, "rg_embedding: null pointer");
+    RG_REQUIRE(ctx, y != table && y != (const void*)ids, "rg_embedding: y is an input");
     RG_REQUIRE(ctx, aligned(table, rg_type_bytes(table_type)) && aligned(ids, 4) && aligned(y, rg_type_bytes(y_type)),
                "rg_embedding: pointer not aligned to its numbers");
     RG_HIP(ctx, hipSetDevice(ctx->device));
@@ -697,6 +698,7 @@ rg_status rg_embedding_grad(rg_ctx* ctx, const void* dy, rg_dtype dy_type, int64
     RG_REQUIRE(ctx, grad_stride >= dim, "rg_embedding_grad: bad stride");
     if (num_rows == 0 || (add && n == 0)) return RG_OK;
     RG_REQUIRE(ctx, grad, "rg_embedding_grad: null pointer");
+    RG_REQUIRE(ctx, n == 0 || (grad != dy && grad != (const void*)ids), "rg_embedding_grad: grad is an input");
     RG_REQUIRE(ctx, aligned(grad, rg_type_bytes(grad_type)), "rg_embedding_grad: pointer not aligned to its numbers");
     RG_HIP(ctx, hipSetDevice(ctx->device));
     hipStream_t s = (hipStream_t)stream;
@@ -719,6 +721,8 @@ rg_status rg_embedding_grad_rows(rg_ctx* ctx, const void* dy, rg_dtype dy_type, 
     RG_REQUIRE(ctx, grad_stride >= dim, "rg_embedding_grad_rows: bad stride");
     RG_REQUIRE(ctx, num_touched && (n == 0 || num_rows == 0 || (grad && touched)), "rg_embedding_grad_rows: null pointer");
     RG_REQUIRE(ctx, aligned(grad, 4) && aligned(touched, 4) && aligned(num_touched, 4), "rg_embedding_grad_rows: pointer not aligned to its numbers");
+    RG_REQUIRE(ctx, n == 0 || num_rows == 0 || ((const void*)grad != dy && touched != ids && num_touched != touched && num_touched != ids),
+               "rg_embedding_grad_rows: an output is an input, or another output");
     RG_HIP(ctx, hipSetDevice(ctx->device));
     hipStream_t s = (hipStream_t)stream;
     if (n == 0 || num_rows == 0) {

@@ -15,7 +15,8 @@ from test_gpu_training_ops import DEV, F32, PAD, check, ctx, f64, padded, untouc
 
 pytestmark = pytest.mark.gpu
 CUT = 2.0 ** -20
-SIZES = [(1, 1, 1), (1, 2, 3), (2, 31, 7), (3, 64, 8), (31, 33, 9), (33, 41, 16), (64, 47, 17), (65, 65, 64), (63, 63, 100), (100, 257, 100), (129, 1000, 127),
+# (and where one kernel hands over to the next: 8 numbers, 128, 256, 512; 32 rows; 64 classes)
+SIZES = [(32, 65, 8), (33, 64, 512), (32, 300, 7), (64, 64, 256), (65, 66, 257), (2000, 64, 513), (31, 9000, 130), (32, 700, 640), (500, 33, 384), (257, 65, 8), (400, 2, 513), (1, 1, 1), (1, 2, 3), (2, 31, 7), (3, 64, 8), (31, 33, 9), (33, 41, 16), (64, 47, 17), (65, 65, 64), (63, 63, 100), (100, 257, 100), (129, 1000, 127),
          (256, 128, 128), (257, 300, 129), (300, 70, 256), (5, 4097, 300), (200, 41, 602), (70, 130, 1025), (1000, 47, 33), (3000, 10, 40), (1, 20_000, 100), (40, 3, 3000)]
 
 
@@ -113,9 +114,9 @@ def test_strides_and_alignment(ctx, dtype, n, classes, dim, extra, offset):  # n
 
 
 @pytest.mark.parametrize("dtype", ref.TYPES)
-def test_rows_that_do_not_count_may_hold_anything(ctx, dtype):  # noqa: F811
+@pytest.mark.parametrize("n,classes,dim", [(200, 60, 70), (200, 100, 70), (30, 100, 70), (200, 100, 200), (200, 100, 300), (200, 64, 300)])
+def test_rows_that_do_not_count_may_hold_anything(ctx, dtype, n, classes, dim):  # noqa: F811
     rng = np.random.default_rng(4)
-    n, classes, dim = 200, 60, 70
     x, w, labels = inputs(rng, n, classes, dim, dtype)
     gone = ~((labels >= 0) & (labels < classes))
     at = torch.from_numpy(np.flatnonzero(gone)).to(DEV)
@@ -142,10 +143,10 @@ def test_rows_that_do_not_count_may_hold_anything(ctx, dtype):  # noqa: F811
     assert bool((dx == 0).all()) and bool((dw == 0).all())
 
 
+@pytest.mark.parametrize("n,classes,dim", [(100, 70, 90), (100, 41, 90), (100, 64, 300), (20, 700, 90), (100, 70, 300), (100, 90, 200)])
 @pytest.mark.parametrize("live", [0, 1, 64, 100, 101, -2])
-def test_counts_on_the_device(ctx, live):  # noqa: F811
+def test_counts_on_the_device(ctx, live, n, classes, dim):  # noqa: F811
     rng = np.random.default_rng(live + 20)
-    n, classes, dim = 100, 70, 90
     real = max(0, min(n, live))
     n_dev = torch.tensor([live], dtype=torch.int32, device=DEV)
     for dtype in ref.TYPES:
@@ -188,10 +189,10 @@ def test_outputs_that_are_not_wanted(ctx):  # noqa: F811
 
 
 @pytest.mark.parametrize("dtype", ref.TYPES)
-def test_large_and_small_logits(ctx, dtype):  # noqa: F811
+@pytest.mark.parametrize("n,classes,dim", [(64, 100, 40), (64, 60, 40), (64, 2000, 40), (64, 400, 200), (64, 400, 300)])
+def test_large_and_small_logits(ctx, dtype, n, classes, dim):  # noqa: F811
     """Rows far from zero, a class that takes everything, all classes alike, and lse far below zero."""
     rng = np.random.default_rng(6)
-    n, classes, dim = 64, 100, 40
     x, w, labels = inputs(rng, n, classes, dim, dtype)
     x[:16] *= 60.0
     x[16:20] = 0.0
@@ -245,9 +246,9 @@ def test_not_a_number_stays_in_its_row(ctx):  # noqa: F811
 
 
 @pytest.mark.parametrize("dtype", ref.TYPES)
-def test_the_same_call_gives_the_same_bits(ctx, dtype):  # noqa: F811
+@pytest.mark.parametrize("n,classes,dim", [(700, 3000, 100), (5000, 47, 100), (20, 30_000, 100), (300, 3000, 600)])
+def test_the_same_call_gives_the_same_bits(ctx, dtype, n, classes, dim):  # noqa: F811
     rng = np.random.default_rng(10)
-    n, classes, dim = 700, 3000, 100
     x, w, labels = inputs(rng, n, classes, dim, dtype)
     runs = []
     for _ in range(2):
@@ -334,3 +335,49 @@ def test_weight_in_several_pieces_and_many_splits(ctx, dtype):  # noqa: F811
     g[torch.arange(n, device=DEV), told] -= 1.0
     for got, want, size in ((dx, g @ w.double(), 64.0), (dw, g.t().contiguous() @ x.double(), 16.0 * n)):
         assert float((got.double() - want).abs().max()) <= (2.0 ** -7 if dtype != F32 else 2.0 ** -12) * size
+
+
+@pytest.mark.parametrize("n,classes,dim", [(40, 200, 60), (40, 50, 60), (3, 200, 60)])
+def test_shares_of_any_sign_and_size(ctx, n, classes, dim):  # noqa: F811
+    """Negative shares, zeros, and shares of very different size; a share that is not a number shows in its row and in all of dweight."""
+    rng = np.random.default_rng(14)
+    for dtype in ref.TYPES:
+        x, w, labels = inputs(rng, n, classes, dim, dtype)
+        labels = np.clip(labels, 0, classes - 1)
+        _, lse64 = vec.cross_entropy(vec.logits(f64(x), f64(w)), labels)
+        lse = torch.from_numpy(lse64).float().to(DEV)
+        dloss = torch.from_numpy(rng.normal(size=n)).float().to(DEV)
+        dloss[0] = 0.0
+        dloss[1] *= 2.0 ** -6
+        dx, dw = torch.empty(n, dim, dtype=dtype, device=DEV), torch.empty(classes, dim, dtype=dtype, device=DEV)
+        ctx.cross_entropy_grad(x, n, dim, w, classes, on_gpu(labels), lse, dx, dw, dloss=dloss, scale=-0.5)
+        check_grads(dx, dw, f64(x), f64(w), labels, f64(lse), f64(dloss) * -0.5, dtype)
+        dloss[2] = float("nan")
+        ctx.cross_entropy_grad(x, n, dim, w, classes, on_gpu(labels), lse, dx, dw, dloss=dloss)
+        bad = torch.isnan(dx).any(1)
+        assert bool(bad[2]) and int(bad.sum()) == 1 and bool(torch.isnan(dw).all())
+
+
+def test_two_contexts_on_two_streams(ctx):  # noqa: F811
+    """Scratch belongs to a context: calls of two of them run side by side."""
+    from paper_2505_10806_amd import binding as B
+    rng = np.random.default_rng(15)
+    other = B.Context(0)
+    n, classes, dim = 600, 5000, 100
+    x, w, labels = inputs(rng, n, classes, dim, torch.bfloat16)
+    at = on_gpu(labels)
+    lse = torch.empty(n, device=DEV)
+    ctx.cross_entropy(x, n, dim, w, classes, at, None, lse)
+    want = [torch.empty_like(x), torch.empty_like(w)]
+    ctx.cross_entropy_grad(x, n, dim, w, classes, at, lse, *want)
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream(), torch.cuda.Stream()], []
+    for _ in range(3):
+        for c, s in zip((ctx, other), streams):
+            out = [torch.empty_like(x), torch.empty_like(w)]
+            torch.cuda.synchronize() if len(got) < 2 else None
+            c.cross_entropy_grad(x, n, dim, w, classes, at, lse, *out, stream=s)
+            got.append(out)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for out in got for a, b in zip(out, want))
+    other.close()

@@ -83,7 +83,7 @@ def check_rows(grad, touched, met, want, size, count):
 
 
 @pytest.mark.parametrize("dtype", ref.TYPES)
-@pytest.mark.parametrize("n,rows,dim,extra", [(1, 1, 1, 0), (2, 100_000, 3, 1), (17, 1, 8, 0), (300, 7, 100, 0), (1000, 47, 64, 0), (1024, 900, 33, 2), (1025, 255, 602, 0),
+@pytest.mark.parametrize("n,rows,dim,extra", [(1, 1, 1, 0), (2, 100_000, 3, 1), (17, 1, 8, 0), (300, 7, 100, 0), (1000, 47, 64, 0), (1024, 900, 33, 2), (1025, 255, 602, 0), (2048, 3, 12, 0), (2049, 700, 12, 1), (2047, 1_000_000, 24, 0),
                                               (4096, 256, 40, 0), (5000, 70_000, 128, 0), (20_011, 3, 20, 0), (70_000, 65_537, 16, 0), (40_000, 20_000_000, 4, 0),
                                               (50, 30, 5000, 0), (9, 4, 65_535, 1)])
 def test_gradient_sums_by_id(ctx, dtype, n, rows, dim, extra):  # noqa: F811

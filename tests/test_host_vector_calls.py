@@ -64,6 +64,11 @@ for call in (grad, grad_rows):
     refuses(call(grad_stride=99), "stride")
     refuses(call(dy=0x7001, type=F16), "aligned")
 refuses(grad(grad_type=7), "type")
+refuses(lookup(table=0x8000, y=0x8000), "input")
+refuses(grad(dy=0x8000, grad=0x8000), "input")
+refuses(grad_rows(dy=0x8000, grad=0x8000), "input")
+refuses(grad_rows(ids=0x8000, touched=0x8000), "input")
+refuses(grad_rows(touched=0x8000, met=0x8000), "output")
 refuses(grad_rows(touched=0), "null")
 refuses(grad_rows(met=0), "null")
 refuses(grad_rows(met=0x7001), "aligned")
@@ -103,6 +108,11 @@ refuses(loss_grad(dweight_stride=99), "stride")
 refuses(loss_grad(dx=0x7002), "aligned")
 refuses(loss_grad(dweight=0x7001, type=F16), "aligned")
 refuses(loss_grad(scale=math.nan), "scale")
+refuses(loss(classes=(1 << 30) + 1), "classes")
+refuses(loss_grad(classes=(1 << 30) + 1), "classes")
+refuses(loss_grad(x=0x8000, dx=0x8000), "input")
+refuses(loss_grad(weight=0x8000, dweight=0x8000), "input")
+refuses(loss_grad(dx=0x8000, dweight=0x8000), "output")
 assert loss(n=0, x=0, weight=0, labels=0) == OK and loss(loss=0, lse=0) == OK and loss_grad(dx=0, dweight=0) == OK and not kernels()
 assert loss_grad(n=0, x=0, weight=0, labels=0, lse=0, dweight=0) == OK and not kernels()
 assert loss_grad(n=0, x=0, weight=0, labels=0, lse=0) == OK and len(kernels()) == 1       # zeros
@@ -156,10 +166,12 @@ for dim in (1, 100, 65536):
         assert lookup(n=N, rows=N, dim=dim, stride=dim, y_stride=dim, type=t) == OK
         assert grad(n=N, rows=N, dim=dim, stride=dim, grad_stride=dim, type=t) == OK and grad_rows(n=N, rows=N, dim=dim, stride=dim, grad_stride=dim, type=t) == OK
         assert grad(n=1, rows=N, dim=dim, stride=dim, grad_stride=dim, type=t) == OK and grad(n=0, rows=N, dim=dim, grad_stride=dim, stride=dim) == OK
-for dim, most in ((1, N), (100, 1 << 27), (300, 1 << 25), (65536, 100_000)):
+for dim, most in ((1, 1 << 30), (100, 1 << 27), (300, 1 << 25), (65536, 100_000)):
     for t in (F32, BF16):
         for n, classes in ((most, 1), (1, most), (1 << 20, 1 << 20) if dim < 65536 else (3000, 3000), (1, 1)):
-            assert loss(n=n, classes=classes, dim=dim, stride=dim, weight_stride=dim, type=t) == OK
+            assert loss(n=n, classes=classes, dim=dim, stride=dim, weight_stride=dim, type=t) == OK and loss(n=30, classes=most, dim=dim, stride=dim, weight_stride=dim, type=t) == OK
+            assert loss(n=most, classes=50, dim=dim, stride=dim, weight_stride=dim, type=t) == OK
+            assert loss_grad(n=most, classes=50, dim=dim, stride=dim, weight_stride=dim, dx_stride=dim, dweight_stride=dim, type=t) == OK
             assert loss_grad(n=n, classes=classes, dim=dim, stride=dim, weight_stride=dim, dx_stride=dim, dweight_stride=dim, type=t) == OK
 for line in log("launch"):
     at = line.rsplit(" ", 5)

@@ -177,11 +177,12 @@ __global__ void __launch_bounds__(kThreads, 2) k_softmax_rows(const Job job) {
     // HOLD: the owned rows stay in registers.  PIPE: the exponentials of a tile are formed between the products of the next one's z, so that the vector and the
     // matrix units work side by side; for that the tile stays in LDS for its second product while two more arrive.
     constexpr bool HOLD = P == 1 && STEPS > 0 && (STEPS <= kSteps || MODE == LOSS), PIPE = STEPS > 0 && (STEPS <= kSteps || HOLD);
-    constexpr int CHUNKS = STEPS > kSteps ? 2 : 1, BUFFERS = PIPE && MODE != LOSS ? 3 : 2;
+    // PERIOD: tiles between barriers; LOOK: how far ahead of its second product a tile is staged.
+    constexpr int CHUNKS = STEPS > kSteps ? 2 : 1, PERIOD = PIPE && CHUNKS == 1 ? 2 : 1, LOOK = 2 * PERIOD, BUFFERS = PERIOD == 2 ? 6 : PIPE && MODE != LOSS ? 3 : 2;
     constexpr int ITEMS = (STEPS > 0 && STEPS < kSteps ? STEPS / 2 * GROUPS + kWaves - 1 : 4 * GROUPS) / kWaves;
     __shared__ __attribute__((aligned(16))) char staged[BUFFERS][CHUNKS][P][ROWS * kRowBytes];
-    __shared__ __attribute__((aligned(16))) float row_lse[3][ROWS], row_share[3][ROWS], row_both[3][ROWS];
-    __shared__ __attribute__((aligned(16))) int row_label[3][ROWS];
+    __shared__ __attribute__((aligned(16))) float row_lse[BUFFERS][ROWS], row_share[BUFFERS][ROWS], row_both[BUFFERS][ROWS];
+    __shared__ __attribute__((aligned(16))) int row_label[BUFFERS][ROWS];
     __shared__ float largest[kWaves];
     const int lane = rg_lane(), wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), half = lane >> 5;
     const int order = rg_xcd_block(blockIdx.x, gridDim.x), split = order / job.tiles, tile = order - split * job.tiles;
@@ -336,6 +337,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_softmax_rows(const Job job) {
     // a step or two; the barriers keep the compiler from reading all of them at once, for which there are no registers.  `between` has work for the vector units.
     constexpr int RING = P > 1 ? 2 : 4;
     const int walk_row = lane & 31, walk_at = walk_row * kRowBytes + ((half ^ ((walk_row & 3) << 2 | (walk_row >> 2 & 3))) << 4);
+    const bool trim = dim <= (STEPS - 1) * 16;              // the last step has no numbers
     const auto products = [&](auto count, int chunk, int buffer, Acc (&z)[SB], auto between) __attribute__((always_inline)) {
         constexpr int K = decltype(count)::value, UNITS = K * SB, AHEAD = P == 1 ? 3 : 2;
         Words4 left[RING][P], right[AHEAD][P];
@@ -364,8 +366,10 @@ __global__ void __launch_bounds__(kThreads, 2) k_softmax_rows(const Job job) {
             if constexpr (!HOLD) {
                 if (q == 0 && k + AHEAD - 1 < K) fetch(k + AHEAD - 1);
             }
-            if constexpr (HOLD) z[q] = mma_parts<E, P>(left[u % RING], held[HOLD ? k : 0], z[q]);
-            else z[q] = mma_parts<E, P>(left[u % RING], right[k % AHEAD], z[q]);
+            if (STEPS == 0 || k + 1 < K || !trim) {
+                if constexpr (HOLD) z[q] = mma_parts<E, P>(left[u % RING], held[HOLD ? k : 0], z[q]);
+                else z[q] = mma_parts<E, P>(left[u % RING], right[k % AHEAD], z[q]);
+            }
             between(u, UNITS);
             __builtin_amdgcn_sched_barrier(0);
         }
@@ -510,8 +514,9 @@ __global__ void __launch_bounds__(kThreads, 2) k_softmax_rows(const Job job) {
         // A tile: its exponentials beside the next one's products, its second product, the tile after the next one to LDS.  (Behind the last tile the products are of
         // what lies there, and are not used.)
         const auto turn = [&](int t, int now, Acc (&z)[SB], Acc (&next)[SB]) __attribute__((always_inline)) {
-            const int then = now + 1 == BUFFERS ? 0 : now + 1, free = BUFFERS == 2 ? now : then + 1 == BUFFERS ? 0 : then + 1;
-            load(t + 2, 0, true);
+            const auto behind = [&](int k) __attribute__((always_inline)) { return now + k >= BUFFERS ? now + k - BUFFERS : now + k; };
+            const int then = behind(1), free = behind(LOOK % BUFFERS);
+            load(t + LOOK, 0, true);
             next_tile();
             const bool rare = open_tile(t, now, z);
             base = m == -__builtin_inff() ? 0.0f : m * kLog2e;
@@ -546,21 +551,18 @@ __global__ void __launch_bounds__(kThreads, 2) k_softmax_rows(const Job job) {
                 second(RG_INT(0), RG_INT(FIRST), now, [&](int u, int units) __attribute__((always_inline)) {
                     if (u < units / 2) exponentials(BEFORE + u * BEFORE / (units / 2), BEFORE + (u + 1) * BEFORE / (units / 2));
                 });
-            if (t + 2 < tiles) store(t + 2, 0, free, true, free);
-            __syncthreads();
+            if (t + LOOK < tiles) store(t + LOOK, 0, free, true, free);
             return then;
         };
         Acc z[2][SB];
         int now = 0;
         if (tiles > 0) {
-            load(0, 0, true);
-            next_tile();
-            store(0, 0, 0, true, 0);
-            if (tiles > 1) {
-                load(1, 0, true);
-                store(1, 0, 1, true, 1);
+#pragma unroll 1
+            for (int t = 0; t < LOOK; ++t) {
+                load(t, 0, true);
+                if (t < tiles) store(t, 0, t, true, t);
+                next_tile();
             }
-            next_tile();
             __syncthreads();
             clear(z[0]);
             products(RG_INT(STEPS), 0, 0, z[0], nothing);
@@ -569,7 +571,9 @@ __global__ void __launch_bounds__(kThreads, 2) k_softmax_rows(const Job job) {
 #pragma unroll 1
         for (int t = 0; t < tiles; t += 2) {
             now = turn(t, now, z[0], z[1]);
+            if (PERIOD == 1) __syncthreads();
             if (t + 1 < tiles) now = turn(t + 1, now, z[1], z[0]);
+            __syncthreads();
         }
     } else if constexpr (STEPS > 0) {
         // A tile after the other, the next one's rows on their way: z, powers, second product.  (Sums for 256 output columns leave no registers for a second z.)

@@ -763,13 +763,13 @@ __global__ void __launch_bounds__(256) k_zero_rows(T* __restrict__ out, int64_t 
 // ---------------------------------------------------------------- few classes
 // Up to 64 classes, whose weight rows fit LDS beside a tile of R rows of x: a workgroup walks its rows once, each tile z, g, dx and its share of dweight, so that x is
 // read and dx written once and z is formed once.  z is [class][row] (rows along the lanes); g goes through LDS, from where dx's product reads it by rows and
-// dweight's transposed.  A wavefront's output columns are every fourth 32; dweight's sums stay in registers until the end, then a second launch joins the workgroups'.
+// dweight's transposed.  Outputs go to the wavefronts by blocks of 32 columns; dweight's sums stay in registers until the end, then a second launch joins the workgroups'.
 template <int P, int R, int CHUNKS>
 struct FewLds {
     static constexpr int ROW = CHUNKS * kRowBytes, G_ROW = 128;
     char weight[P][64 * ROW], x[P][R * ROW], g[P][R * G_ROW];
     float top[2][R], sum[2][R], target[R];
-    float largest[4];
+    float largest[8];
 };
 static_assert(sizeof(FewLds<3, 32, 2>) <= 160 * 1024 && sizeof(FewLds<3, 64, 1>) <= 160 * 1024 && sizeof(FewLds<1, 32, 4>) <= 160 * 1024, "LDS of a compute unit");
 
@@ -786,12 +786,14 @@ struct FewJob {
     float* parts;              // [workgroup][class][dim], or NULL
 };
 
+constexpr int kClassWaves = 8, kClassThreads = 64 * kClassWaves;
+
 template <typename T, bool GRAD, int R, int CHUNKS>
-__global__ void __launch_bounds__(256, 1) k_few_classes(const FewJob job) {
+__global__ void __launch_bounds__(kClassThreads, 2) k_few_classes(const FewJob job) {
     typedef Part<T> S;
     typedef typename S::type E;
     typedef FewLds<S::P, R, CHUNKS> Lds;
-    constexpr int P = S::P, ROW = Lds::ROW, RB = R / 32, ROWGROUPS = R / 16, ITEMS = ROWGROUPS * CHUNKS * 4 / 4;
+    constexpr int P = S::P, ROW = Lds::ROW, RB = R / 32, ROWGROUPS = R / 16, ITEMS = ROWGROUPS * CHUNKS * 4 / kClassWaves;
     __shared__ __attribute__((aligned(16))) Lds lds;
     const int lane = rg_lane(), wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), half = lane >> 5, i16 = lane & 15;
     const int64_t n_act = rg_rows(job.n, job.n_dev);
@@ -822,41 +824,39 @@ __global__ void __launch_bounds__(256, 1) k_few_classes(const FewJob job) {
     typename RgPack<T, 8>::type raw[ITEMS];
     int raw_label = -1;
     const T* x = (const T*)job.x;
-    const int to_row = wave % ROWGROUPS * 16 + (lane >> 2), group0 = wave / ROWGROUPS;   // (of 32 columns; item u: group0 + u * 4 / ROWGROUPS)
+    const int to_row = wave % ROWGROUPS * 16 + (lane >> 2), group0 = wave / ROWGROUPS;   // (of 32 columns; item u: group0 + u * kClassWaves / ROWGROUPS)
     const auto load = [&](int t) __attribute__((always_inline)) {
         const int64_t from = t0 * R + min(t * R + to_row, here - 1);
         raw_label = job.labels[from];
         const T* src = x + from * job.x_stride;
 #pragma unroll
-        for (int u = 0; u < ITEMS; ++u) raw[u] = load_eight<false>(src, (group0 + u * (4 / ROWGROUPS)) * 32 + (lane & 3) * 8, dim);
+        for (int u = 0; u < ITEMS; ++u) raw[u] = load_eight<false>(src, (group0 + u * (kClassWaves / ROWGROUPS)) * 32 + (lane & 3) * 8, dim);
     };
     if (tiles > 0) load(0);
     int power = 0;
     if (GRAD && job.dloss) {                               // (shares to at most 1, as above)
         float top = 0.0f;
-        for (int64_t r = t0 * R + threadIdx.x; r < rg_least((t0 + tiles) * R, n_act); r += 256)
+        for (int64_t r = t0 * R + threadIdx.x; r < rg_least((t0 + tiles) * R, n_act); r += kClassThreads)
             if (has_label(job.labels[r], classes)) top = fmaxf(top, fabsf(job.dloss[r]));
         for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, RG_WAVE));
         if (lane == 0) lds.largest[wave] = top;
         __syncthreads();
 #pragma unroll
-        for (int w = 0; w < 4; ++w) top = fmaxf(top, lds.largest[w]);
+        for (int w = 0; w < kClassWaves; ++w) top = fmaxf(top, lds.largest[w]);
         if (top > 0.0f && top < __builtin_inff()) (void)frexpf(top, &power);
     }
-    for (int group = 0; group < blocks; ++group) {
-        const int row = wave * 16 + (lane >> 2);
+    for (int group = wave / 4; group < blocks; group += kClassWaves / 4) {
+        const int row = wave % 4 * 16 + (lane >> 2);
         const T* src = (const T*)job.weight + (int64_t)min(row, classes - 1) * job.weight_stride;
         put(weight_planes, load_eight<false>(src, group * 32 + (lane & 3) * 8, dim), row, group, row < classes);
     }
 
-    Acc dw[GRAD ? CHUNKS : 1][2];                          // columns (wave + 4 j) * 32 .., classes 32 c ..
+    Acc dw[GRAD ? CHUNKS : 1];                             // unit u = wave + 8 j: columns u / 2 * 32 .., classes u % 2 * 32 ..
     if (GRAD) {
 #pragma unroll
         for (int j = 0; j < CHUNKS; ++j)
 #pragma unroll
-            for (int c = 0; c < 2; ++c)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) dw[j][c][i] = 0.0f;
+            for (int i = 0; i < 16; ++i) dw[j][i] = 0.0f;
     }
     // fragments: rows l % 32 of a block, 16 columns of step k; and, transposed, 16 rows from `first` on of 32 columns
     const int row_at = (lane & 31) * ROW + ((half ^ twist(lane & 31)) << 4);
@@ -881,19 +881,21 @@ __global__ void __launch_bounds__(256, 1) k_few_classes(const FewJob job) {
         const bool counts = t * R + to_row < here && has_label(raw_label, classes);
 #pragma unroll
         for (int u = 0; u < ITEMS; ++u) {
-            const int group = group0 + u * (4 / ROWGROUPS);
+            const int group = group0 + u * (kClassWaves / ROWGROUPS);
             if (group < blocks) put(x_planes, raw[u], to_row, group, counts);
         }
         load(t + 1);                                       // (of the last row, behind the last tile)
         __syncthreads();
 
-        // z: a wavefront's block of 32 classes by 32 rows
-        const int cb = wave & 1, rb = wave >> 1;
-        if (rb < RB) {
-            Acc z;
+        // z: a wavefront's block of 32 classes by 32 rows, of numbers in three parts half of its steps, which the other half's wavefront adds
+        const int cb = wave & 1, rb = RB == 2 ? wave >> 1 & 1 : 0, part = wave >> RB;
+        constexpr int HALVES = P > 1 ? 2 : 1;
+        Acc z;
+        if (part < HALVES) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) z[i] = 0.0f;
-            for (int k0 = 0; k0 < steps; k0 += 2) {        // (an even number of them)
+            const int middle = HALVES == 2 ? steps / 4 * 2 : steps, from = part * middle, to = part == 0 ? middle : steps;
+            for (int k0 = from; k0 < to; k0 += 2) {        // (an even number of them)
                 Words4 a[2][P], b[2][P];
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
@@ -906,6 +908,21 @@ __global__ void __launch_bounds__(256, 1) k_few_classes(const FewJob job) {
 #pragma unroll
                 for (int i = 0; i < 2; ++i) z = mma_parts<E, P>(a[i], b[i], z);
             }
+        }
+        if constexpr (HALVES == 2) {                       // by way of the place of g, which the tile before is done with
+            float* const place = (float*)lds.g + (rb * 2 + cb) * 16 * 64 + lane;
+            if (part == 1) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) place[i * 64] = z[i];
+            }
+            __syncthreads();
+            if (part == 0) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) z[i] += place[i * 64];
+            }
+            __syncthreads();
+        }
+        if (part == 0) {
             const int mine = RB == 1 ? label[0] : rb ? label[RB - 1] : label[0], first = cb * 32 + 4 * half;     // register i: class first + 8 (i >> 2) + (i & 3)
             const int64_t row = t0 * R + min(t * R + rb * 32 + (lane & 31), here - 1);
             if constexpr (!GRAD) {
@@ -970,66 +987,59 @@ __global__ void __launch_bounds__(256, 1) k_few_classes(const FewJob job) {
                 if (job.loss) job.loss[row] = counts ? lse - lds.target[threadIdx.x] : 0.0f;
             }
         } else {
+            if (job.dx) {
+                constexpr int UNITS = RB == 2 ? CHUNKS : (CHUNKS + 1) / 2;
 #pragma unroll
-            for (int j = 0; j < CHUNKS; ++j) {
-                const int d = wave + 4 * j;
-                if (d >= blocks) continue;
-                if (job.dx) {
-                    Acc out[RB];
+                for (int j = 0; j < UNITS; ++j) {
+                    const int unit = wave + kClassWaves * j, d = RB == 2 ? unit >> 1 : unit, b = RB == 2 ? unit & 1 : 0, at = b * 32 + (lane & 31);
+                    if (d >= blocks) continue;
+                    Acc out;
 #pragma unroll
-                    for (int b = 0; b < RB; ++b)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) out[b][i] = 0.0f;
+                    for (int i = 0; i < 16; ++i) out[i] = 0.0f;
 #pragma unroll
                     for (int f = 0; f < 4; ++f) {
-                        Words4 a[P];
+                        Words4 a[P], g[P];
 #pragma unroll
-                        for (int p = 0; p < P; ++p) a[p] = turned(lds.weight[p], f * 16, d);
-#pragma unroll
-                        for (int b = 0; b < RB; ++b) {
-                            const int at = b * 32 + (lane & 31);
-                            Words4 g[P];
-#pragma unroll
-                            for (int p = 0; p < P; ++p) g[p] = *(const Words4*)(lds.g[p] + at * Lds::G_ROW + (((2 * f + half) ^ g_twist(at)) << 4));
-                            out[b] = mma_parts<E, P>(a, g, out[b]);
+                        for (int p = 0; p < P; ++p) {
+                            a[p] = turned(lds.weight[p], f * 16, d);
+                            g[p] = *(const Words4*)(lds.g[p] + at * Lds::G_ROW + (((2 * f + half) ^ g_twist(at)) << 4));
                         }
+                        out = mma_parts<E, P>(a, g, out);
                     }
+                    const int r = t * R + at, mine = RB == 2 ? (b ? label[RB - 1] : label[0]) : label[0];
+                    if (r >= here) continue;
+                    T* to = (T*)job.dx + (t0 * R + r) * job.dx_stride;
+                    const float factor = mine < 0 ? 0.0f : job.scale;
 #pragma unroll
-                    for (int b = 0; b < RB; ++b) {
-                        const int r = t * R + b * 32 + (lane & 31);
-                        if (r >= here) continue;
-                        T* to = (T*)job.dx + (t0 * R + r) * job.dx_stride;
+                    for (int q = 0; q < 4; ++q) {
+                        const int col = d * 32 + q * 8 + half * 4;
+                        if (col >= dim) continue;
+                        float v[4];
 #pragma unroll
-                        for (int q = 0; q < 4; ++q) {
-                            const int col = d * 32 + q * 8 + half * 4;
-                            if (col >= dim) continue;
-                            float v[4];
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) v[i] = label[b] < 0 ? 0.0f : ldexpf(out[b][q * 4 + i] * job.scale, power - S::BIAS);
-                            rg_store_live<4>(to + col, dim - col, v);
-                        }
+                        for (int i = 0; i < 4; ++i) v[i] = mine < 0 ? 0.0f : ldexpf(out[q * 4 + i] * factor, power - S::BIAS);
+                        rg_store_live<4>(to + col, dim - col, v);
                     }
                 }
-                if (job.parts) {
+            }
+            if (job.parts) {
+#pragma unroll
+                for (int j = 0; j < CHUNKS; ++j) {
+                    const int unit = wave + kClassWaves * j, d = unit >> 1, c = unit & 1;
+                    if (d >= blocks) continue;
 #pragma unroll
                     for (int f = 0; f < R / 16; ++f) {
-                        Words4 a[P];
+                        const int row = f * 16 + 8 * half + (i16 >> 2), piece = c * 4 + (lane >> 4 & 1) * 2 + (i16 >> 1 & 1);
+                        Words4 a[P], g[P];
 #pragma unroll
-                        for (int p = 0; p < P; ++p) a[p] = turned(lds.x[p], f * 16, d);
-#pragma unroll
-                        for (int c = 0; c < 2; ++c) {
-                            const int row = f * 16 + 8 * half + (i16 >> 2), piece = c * 4 + (lane >> 4 & 1) * 2 + (i16 >> 1 & 1);
-                            Words4 g[P];
-#pragma unroll
-                            for (int p = 0; p < P; ++p) {
-                                const Words2 low = __builtin_bit_cast(Words2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                                    (Lds4*)(lds.g[p] + row * Lds::G_ROW + ((piece ^ g_twist(row)) << 4) + (i16 & 1) * 8)));
-                                const Words2 high = __builtin_bit_cast(Words2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                                    (Lds4*)(lds.g[p] + (row + 4) * Lds::G_ROW + ((piece ^ g_twist(row + 4)) << 4) + (i16 & 1) * 8)));
-                                g[p] = Words4{low[0], low[1], high[0], high[1]};
-                            }
-                            dw[j][c] = mma_parts<E, P>(a, g, dw[j][c]);
+                        for (int p = 0; p < P; ++p) {
+                            a[p] = turned(lds.x[p], f * 16, d);
+                            const Words2 low = __builtin_bit_cast(Words2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                (Lds4*)(lds.g[p] + row * Lds::G_ROW + ((piece ^ g_twist(row)) << 4) + (i16 & 1) * 8)));
+                            const Words2 high = __builtin_bit_cast(Words2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                (Lds4*)(lds.g[p] + (row + 4) * Lds::G_ROW + ((piece ^ g_twist(row + 4)) << 4) + (i16 & 1) * 8)));
+                            g[p] = Words4{low[0], low[1], high[0], high[1]};
                         }
+                        dw[j] = mma_parts<E, P>(a, g, dw[j]);
                     }
                 }
             }
@@ -1038,21 +1048,19 @@ __global__ void __launch_bounds__(256, 1) k_few_classes(const FewJob job) {
     if constexpr (GRAD) {
         if (!job.parts) return;
 #pragma unroll
-        for (int j = 0; j < CHUNKS; ++j)
+        for (int j = 0; j < CHUNKS; ++j) {
+            const int unit = wave + kClassWaves * j, own = (unit & 1) * 32 + (lane & 31);
+            if (own >= classes) continue;
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                const int own = c * 32 + (lane & 31);
-                if (own >= classes) continue;
+            for (int q = 0; q < 4; ++q) {
+                const int col = (unit >> 1) * 32 + q * 8 + half * 4;
+                if (col >= dim) continue;
+                float v[4];
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int col = (wave + 4 * j) * 32 + q * 8 + half * 4;
-                    if (col >= dim) continue;
-                    float v[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) v[i] = ldexpf(dw[j][c][q * 4 + i] * job.scale, power - S::BIAS);
-                    rg_store_live<4>(job.parts + ((int64_t)blockIdx.x * classes + own) * dim + col, dim - col, v);
-                }
+                for (int i = 0; i < 4; ++i) v[i] = ldexpf(dw[j][q * 4 + i] * job.scale, power - S::BIAS);
+                rg_store_live<4>(job.parts + ((int64_t)blockIdx.x * classes + own) * dim + col, dim - col, v);
             }
+        }
     }
 }
 
@@ -1068,13 +1076,13 @@ template <typename T, bool GRAD>
 void launch_few(const FewJob& job, unsigned grid, hipStream_t s) {
     const int chunks = (int)rg_div_up(job.dim, kCols);
     if constexpr (Part<T>::P > 1) {
-        if (chunks == 1) k_few_classes<T, GRAD, 64, 1><<<grid, 256, 0, s>>>(job);
-        else k_few_classes<T, GRAD, 32, 2><<<grid, 256, 0, s>>>(job);
+        if (chunks == 1) k_few_classes<T, GRAD, 64, 1><<<grid, kClassThreads, 0, s>>>(job);
+        else k_few_classes<T, GRAD, 32, 2><<<grid, kClassThreads, 0, s>>>(job);
     } else {
-        if (chunks == 1) k_few_classes<T, GRAD, 64, 1><<<grid, 256, 0, s>>>(job);
-        else if (chunks == 2) k_few_classes<T, GRAD, 64, 2><<<grid, 256, 0, s>>>(job);
-        else if (chunks == 3) k_few_classes<T, GRAD, 32, 3><<<grid, 256, 0, s>>>(job);
-        else k_few_classes<T, GRAD, 32, 4><<<grid, 256, 0, s>>>(job);
+        if (chunks == 1) k_few_classes<T, GRAD, 64, 1><<<grid, kClassThreads, 0, s>>>(job);
+        else if (chunks == 2) k_few_classes<T, GRAD, 64, 2><<<grid, kClassThreads, 0, s>>>(job);
+        else if (chunks == 3) k_few_classes<T, GRAD, 32, 3><<<grid, kClassThreads, 0, s>>>(job);
+        else k_few_classes<T, GRAD, 32, 4><<<grid, kClassThreads, 0, s>>>(job);
     }
 }
 

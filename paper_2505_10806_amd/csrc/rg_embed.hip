@@ -68,6 +68,33 @@ __global__ void __launch_bounds__(kThreads) k_embedding(const T* __restrict__ ta
     }
 }
 
+// ---------------------------------------------------------------- zeros
+// Rows of a whole table that no id meets are zeros: all of it is cleared first, by workgroups of their own beside those of the launches that sort the ids (which
+// wait for each other more than they work: 65536 ids take 25 us in six launches).  pieces `from` .. `to` - 1 of 16 bytes, `chunks` to a row.
+struct Zeros {
+    void* grad;
+    int64_t stride, from, to;
+    int dim, chunks, bytes, once;
+};
+
+template <typename U, bool ONCE>
+__device__ __forceinline__ void clear_as(const Zeros& z, int block, int blocks) {
+    constexpr int V = 16 / (int)sizeof(U);
+    const float zero[V] = {};
+    for (int64_t i = z.from + (int64_t)block * blockDim.x + threadIdx.x; i < z.to; i += (int64_t)blocks * blockDim.x) {
+        const int64_t row = i / z.chunks;
+        const int col = (int)(i - row * z.chunks) * V;
+        rg_store_live<V, ONCE>((U*)z.grad + row * z.stride + col, z.dim - col, zero);
+    }
+}
+
+__device__ __forceinline__ void clear(const Zeros& z, int block, int blocks) {
+    if (z.bytes == 4) z.once ? clear_as<float, true>(z, block, blocks) : clear_as<float, false>(z, block, blocks);
+    else z.once ? clear_as<_Float16, true>(z, block, blocks) : clear_as<_Float16, false>(z, block, blocks);
+}
+
+__global__ void __launch_bounds__(kThreads) k_clear_rows(const Zeros z) { clear(z, blockIdx.x, gridDim.x); }
+
 // ---------------------------------------------------------------- ids in order
 // The gradient's sums run over the entries sorted by id, entries of an id in their own order, so that the same call adds in the same order each time.  Least
 // digit first, up to ten bits a pass (three launches); padding gets the id behind the last row and comes to lie behind all others.
@@ -96,11 +123,12 @@ __device__ __forceinline__ uint64_t same_digit(uint32_t digit, bool live) {
 }
 
 template <int BITS>
-__global__ void __launch_bounds__(kThreads) k_sort_count(const Entry* __restrict__ from, const int32_t* __restrict__ ids, int64_t n,
+__global__ void __launch_bounds__(kThreads) k_sort_count(const Zeros zeros, int blocks, const Entry* __restrict__ from, const int32_t* __restrict__ ids, int64_t n,
                                                          const int32_t* __restrict__ n_dev, uint32_t num_rows, int shift, int64_t per_block,
                                                          int32_t* __restrict__ counts) {
     constexpr int DIGITS = 1 << BITS;
     __shared__ int32_t bins[DIGITS];
+    if ((int)blockIdx.x >= blocks) return clear(zeros, blockIdx.x - blocks, gridDim.x - blocks);
 #pragma unroll
     for (int d = threadIdx.x; d < DIGITS; d += kThreads) bins[d] = 0;
     __syncthreads();
@@ -108,12 +136,13 @@ __global__ void __launch_bounds__(kThreads) k_sort_count(const Entry* __restrict
     for (int64_t i = first + threadIdx.x; i < last; i += kThreads) atomicAdd(&bins[entry_of(from, ids, i, num_rows).id >> shift & (DIGITS - 1)], 1);
     __syncthreads();
 #pragma unroll
-    for (int d = threadIdx.x; d < DIGITS; d += kThreads) counts[(int64_t)d * gridDim.x + blockIdx.x] = bins[d];
+    for (int d = threadIdx.x; d < DIGITS; d += kThreads) counts[(int64_t)d * blocks + blockIdx.x] = bins[d];
 }
 
 // Each digit's counts become its entries in front of every block; totals[digit] = all of them.
-__global__ void __launch_bounds__(kThreads) k_sort_scan(int32_t* __restrict__ counts, int blocks, int32_t* __restrict__ totals) {
+__global__ void __launch_bounds__(kThreads) k_sort_scan(const Zeros zeros, int digits, int32_t* __restrict__ counts, int blocks, int32_t* __restrict__ totals) {
     __shared__ int smem[kSortWaves + 1];
+    if ((int)blockIdx.x >= digits) return clear(zeros, blockIdx.x - digits, gridDim.x - digits);
     constexpr int EACH = 4;
     int32_t* row = counts + (int64_t)blockIdx.x * blocks;
     int before = 0;
@@ -139,12 +168,13 @@ __global__ void __launch_bounds__(kThreads) k_sort_scan(int32_t* __restrict__ co
 }
 
 template <int BITS>
-__global__ void __launch_bounds__(kThreads) k_sort_scatter(const Entry* __restrict__ from, const int32_t* __restrict__ ids, int64_t n,
+__global__ void __launch_bounds__(kThreads) k_sort_scatter(const Zeros zeros, int blocks, const Entry* __restrict__ from, const int32_t* __restrict__ ids, int64_t n,
                                                            const int32_t* __restrict__ n_dev, uint32_t num_rows, int shift, int64_t per_block,
                                                            const int32_t* __restrict__ counts, const int32_t* __restrict__ totals, Entry* __restrict__ to) {
     constexpr int DIGITS = 1 << BITS, EACH = DIGITS / kThreads;          // (a thread: EACH neighbouring digits)
     __shared__ int smem[kSortWaves + 1];
     __shared__ int32_t next[DIGITS], met[kSortWaves][DIGITS];
+    if ((int)blockIdx.x >= blocks) return clear(zeros, blockIdx.x - blocks, gridDim.x - blocks);
     const int wave = threadIdx.x >> 6, lane = rg_lane();
     int mine[EACH], sum = 0, all;
 #pragma unroll
@@ -155,7 +185,7 @@ __global__ void __launch_bounds__(kThreads) k_sort_scatter(const Entry* __restri
     const int base = rg_block_excl_scan<kSortWaves>(sum, smem, &all);
 #pragma unroll
     for (int d = 0; d < EACH; ++d)
-        next[threadIdx.x * EACH + d] = base + mine[d] + counts[(int64_t)(threadIdx.x * EACH + d) * gridDim.x + blockIdx.x];
+        next[threadIdx.x * EACH + d] = base + mine[d] + counts[(int64_t)(threadIdx.x * EACH + d) * blocks + blockIdx.x];
     const int64_t first = (int64_t)blockIdx.x * per_block, last = rg_least(first + per_block, rg_rows(n, n_dev));
     for (int64_t tile = first; tile < last; tile += kTile) {
 #pragma unroll
@@ -402,13 +432,14 @@ __global__ void __launch_bounds__(kJoinThreads) k_join_pieces(const Entry* __res
 // One workgroup sorts them in LDS and lists the ids met: order[] the entries' rows of dy, run r the entries starts[r] .. starts[r + 1] - 1, of id touched[r].
 constexpr int kFew = 2048, kFewThreads = 1024, kFewWaves = kFewThreads / RG_WAVE, kFewRounds = kFew / kFewThreads;
 
-__global__ void __launch_bounds__(kFewThreads) k_sort_few(const int32_t* __restrict__ ids, int n, const int32_t* __restrict__ n_dev, uint32_t num_rows, int bits,
+__global__ void __launch_bounds__(kFewThreads) k_sort_few(const Zeros zeros, const int32_t* __restrict__ ids, int n, const int32_t* __restrict__ n_dev, uint32_t num_rows, int bits,
                                                           int32_t* __restrict__ order, int32_t* __restrict__ starts, int32_t* __restrict__ touched,
                                                           int32_t* __restrict__ num_touched, int32_t* __restrict__ count) {
     constexpr int BITS = 8, DIGITS = 1 << BITS;
     __shared__ int smem[kFewWaves + 1];
     __shared__ int32_t met[kFewWaves][DIGITS];
     __shared__ Entry list[kFew];
+    if (blockIdx.x) return clear(zeros, blockIdx.x - 1, gridDim.x - 1);
     const int n_act = (int)rg_rows(n, n_dev), wave = threadIdx.x >> 6, lane = rg_lane();
     Entry e[kFewRounds];
 #pragma unroll
@@ -519,36 +550,30 @@ __global__ void __launch_bounds__(kThreads) k_sum_runs(const T* __restrict__ dy,
     if (group == 0 && col < dim) put_sum<V>(t, rows ? touched[run] : run, col, dim, sum);
 }
 
-// Rows of zeros.
-template <typename U, bool ONCE>
-__global__ void __launch_bounds__(kThreads) k_clear_rows(U* __restrict__ grad, int64_t stride, int64_t num_rows, int dim, int chunks) {
-    constexpr int V = 16 / (int)sizeof(U);
-    const float zero[V] = {};
-    const int64_t total = num_rows * chunks;
-    for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < total; i += (int64_t)gridDim.x * kThreads) {
-        const int64_t row = i / chunks;
-        const int col = (int)(i - row * chunks) * V;
-        rg_store_live<V, ONCE>(grad + row * stride + col, dim - col, zero);
-    }
-}
-
 bool aligned(const void* p, int bytes) { return (uintptr_t)p % (uintptr_t)bytes == 0; }
 
 constexpr int64_t kMostRows = (1ll << 31) - 1;
 
 template <typename U>
-void clear_rows(rg_ctx* ctx, U* grad, int64_t stride, int64_t num_rows, int dim, hipStream_t s) {
+Zeros zeros_of(U* grad, int64_t stride, int64_t num_rows, int dim) {
     const int chunks = (int)rg_div_up(dim, 16 / (int)sizeof(U));
-    const unsigned grid = (unsigned)rg_min64(rg_div_up(num_rows * chunks, kThreads), (int64_t)ctx->num_cus * 32);
-    const auto kernel = rg_store_once(grad, (int64_t)dim * sizeof(U), stride * (int64_t)sizeof(U), num_rows) ? k_clear_rows<U, true> : k_clear_rows<U, false>;
-    kernel<<<grid, kThreads, 0, s>>>(grad, stride, num_rows, dim, chunks);
+    return {grad, stride, 0, num_rows * chunks, dim, chunks, (int)sizeof(U), rg_store_once(grad, (int64_t)dim * sizeof(U), stride * (int64_t)sizeof(U), num_rows)};
 }
+
+// Workgroups of `threads` for pieces of zeros.
+int clear_blocks(rg_ctx* ctx, int64_t pieces, int threads) { return (int)rg_min64(rg_div_up(pieces, threads * 4), (int64_t)ctx->num_cus * (8192 / threads)); }
 
 // The gradient's two forms: a whole table (touched NULL), or the rows met.
 template <typename U>
 rg_status sum_by_id(rg_ctx* ctx, const char* who, const void* dy, rg_dtype dy_type, int64_t dy_stride, const int32_t* ids, int64_t n, const int32_t* n_dev,
                     int dim, int64_t num_rows, float scale, U* grad, int64_t grad_stride, int add, int32_t* touched, int32_t* num_touched, hipStream_t s) {
-    if (!touched && !add && n == 0) { clear_rows(ctx, grad, grad_stride, num_rows, dim, s); return RG_OK; }
+    Zeros zeros = {};
+    if (!touched && !add) zeros = zeros_of(grad, grad_stride, num_rows, dim);
+    if (!touched && n == 0) {
+        k_clear_rows<<<(unsigned)clear_blocks(ctx, zeros.to, kThreads), kThreads, 0, s>>>(zeros);
+        RG_LAUNCH_CHECK(ctx, "k_clear_rows");
+        return RG_OK;
+    }
     int bits = 1;
     while (bits < 31 && num_rows >> bits) ++bits;          // ids 0 .. num_rows, padding the last
     if (n <= kFew) {
@@ -556,8 +581,7 @@ rg_status sum_by_id(rg_ctx* ctx, const char* who, const void* dy, rg_dtype dy_ty
         if (st != RG_OK) return st;
         int32_t* order = (int32_t*)ctx->embed_parts.p;
         int32_t *starts = order + kFew, *named = starts + kFew + 32, *count = named + kFew;
-        if (!touched && !add) clear_rows(ctx, grad, grad_stride, num_rows, dim, s);
-        k_sort_few<<<1, kFewThreads, 0, s>>>(ids, (int)n, n_dev, (uint32_t)num_rows, bits, order, starts, touched ? touched : named, num_touched, count);
+        k_sort_few<<<1 + clear_blocks(ctx, zeros.to, kFewThreads), kFewThreads, 0, s>>>(zeros, ids, (int)n, n_dev, (uint32_t)num_rows, bits, order, starts, touched ? touched : named, num_touched, count);
         RG_LAUNCH_CHECK(ctx, "k_sort_few");
         const Target<U> t = {grad, grad_stride, nullptr, nullptr, scale, add};
         RG_FOR_TYPE(dy_type, {
@@ -590,15 +614,24 @@ rg_status sum_by_id(rg_ctx* ctx, const char* who, const void* dy, rg_dtype dy_ty
     int32_t* totals = counts + ((int64_t)blocks << digit);
     int32_t* before = (int32_t*)(at + 2 * list + counts_bytes);
     float* parts = (float*)(at + 2 * list + counts_bytes + before_bytes);
-    if (!touched && !add) clear_rows(ctx, grad, grad_stride, num_rows, dim, s);
+    const int64_t all_zeros = zeros.to;
+    int launches = 0;
+    const auto part_of_zeros = [&] {                       // a launch's share of the pieces
+        zeros.from = all_zeros * launches / (3 * passes);
+        zeros.to = all_zeros * ++launches / (3 * passes);
+        return clear_blocks(ctx, zeros.to - zeros.from, kThreads);
+    };
     const Entry* from = nullptr;
     const auto sort = [&](auto width) {
         constexpr int BITS = decltype(width)::value;
         for (int pass = 0; pass < passes; ++pass) {
             Entry* to = lists[pass & 1];
-            k_sort_count<BITS><<<blocks, kThreads, 0, s>>>(from, ids, n, n_dev, (uint32_t)num_rows, pass * BITS, per_block, counts);
-            k_sort_scan<<<1 << BITS, kThreads, 0, s>>>(counts, blocks, totals);
-            k_sort_scatter<BITS><<<blocks, kThreads, 0, s>>>(from, ids, n, n_dev, (uint32_t)num_rows, pass * BITS, per_block, counts, totals, to);
+            int more = part_of_zeros();
+            k_sort_count<BITS><<<blocks + more, kThreads, 0, s>>>(zeros, blocks, from, ids, n, n_dev, (uint32_t)num_rows, pass * BITS, per_block, counts);
+            more = part_of_zeros();
+            k_sort_scan<<<(1 << BITS) + more, kThreads, 0, s>>>(zeros, 1 << BITS, counts, blocks, totals);
+            more = part_of_zeros();
+            k_sort_scatter<BITS><<<blocks + more, kThreads, 0, s>>>(zeros, blocks, from, ids, n, n_dev, (uint32_t)num_rows, pass * BITS, per_block, counts, totals, to);
             from = to;
         }
     };
@@ -707,9 +740,7 @@ rg_status rg_embedding_grad(rg_ctx* ctx, const void* dy, rg_dtype dy_type, int64
         return sum_by_id<U>(ctx, "rg_embedding_grad", dy, dy_type, dy_stride, ids, n, n_dev, dim, num_rows, scale, (U*)grad, grad_stride, add, nullptr, nullptr, s);
     };
     const rg_status st = grad_type == RG_F32 ? sums(float()) : grad_type == RG_BF16 ? sums(__bf16()) : sums(_Float16());
-    if (st != RG_OK) return st;
-    RG_LAUNCH_CHECK(ctx, "k_clear_rows");
-    return RG_OK;
+    return st;
 }
 
 rg_status rg_embedding_grad_rows(rg_ctx* ctx, const void* dy, rg_dtype dy_type, int64_t dy_stride, const int32_t* ids, int64_t n, const int32_t* n_dev,

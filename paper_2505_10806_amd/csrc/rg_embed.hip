@@ -379,21 +379,21 @@ __global__ void __launch_bounds__(kJoinThreads) k_join_pieces(const Entry* __res
     const int l = threadIdx.x & ((1 << log2L) - 1), run = threadIdx.x >> log2L, runs = kJoinThreads >> log2L, col = ((blockIdx.y << log2L) + l) * V;
     // (every wavefront looks at the workgroup's kJoinPieces pieces, a lane each)
     const int looked = blockIdx.x * kJoinPieces + (rg_lane() & (kJoinPieces - 1));
-    const int64_t begins = looked * size, ends = begins + size;
-    bool open = looked + 1 < pieces && ends < n_act;
-    if (open) {
-        const uint32_t id = sorted[ends].id;
-        open = id < num_rows && sorted[ends - 1].id == id && !(sorted[begins].id == id && !opens(sorted, begins));
-    }
+    const int64_t begins = looked * size, ends = begins + size, past = n_act > 0 ? n_act - 1 : 0;
+    const uint32_t id_behind = sorted[rg_least(ends, past)].id, id_last = sorted[rg_least(ends - 1, past)].id, id_first = sorted[rg_least(begins, past)].id,
+                   id_before = sorted[rg_least(begins > 0 ? begins - 1 : 0, past)].id;
+    const bool open = looked + 1 < pieces && ends < n_act && id_behind < num_rows && id_last == id_behind && (id_first != id_behind || begins == 0 || id_before != id_first);
     for (uint32_t left = (uint32_t)__ballot(open) & ((1u << kJoinPieces) - 1); left; left &= left - 1) {
         const int piece = blockIdx.x * kJoinPieces + __builtin_ctz(left);
         const int64_t next = (piece + 1) * size;
         const uint32_t id = sorted[next].id;
-        // pieces behind this one that begin with the id: those in front of the first entry of a larger one
+        // pieces behind this one that begin with the id: those in front of the first entry of a larger one, which is looked for at 64 places at a time
         int64_t lo = next, hi = n_act;                     // (sorted[lo].id == id; larger from hi on)
         while (hi - lo > 1) {
-            const int64_t mid = (lo + hi) >> 1;
-            if (sorted[mid].id == id) lo = mid; else hi = mid;
+            const int64_t step = (hi - lo + RG_WAVE) / (RG_WAVE + 1), probe = lo + (rg_lane() + 1) * step;
+            const int same = __popcll(__ballot(sorted[rg_least(probe, hi - 1)].id == id && probe < hi));
+            hi = rg_least(hi, lo + (same + 1) * step);
+            lo += same * step;
         }
         const int from = piece + 1, to = (int)(lo / size) + 1, per = (to - from + runs - 1) / runs;
         const int start = from + run * per, stop = min(start + per, to);
@@ -597,7 +597,8 @@ rg_status sum_by_id(rg_ctx* ctx, const char* who, const void* dy, rg_dtype dy_ty
         return RG_OK;
     }
     // pieces of 16 entries or more, and as many of them as fill the device
-    const int most = (int)rg_max64(1024, rg_min64(n / rg_max64(num_rows, 1) >= 64 ? 4096 : 16384, (1ll << 23) / dim));
+    const bool dense = n / rg_max64(num_rows, 1) >= 64;    // ids of many entries: pieces that are joined by the hundred
+    const int most = (int)rg_max64(1024, rg_min64(dense ? 4096 : 16384, (1ll << 23) / dim));
     const int64_t size = rg_max64(16, rg_div_up(n, most));
     const int pieces = (int)rg_div_up(n, size);
     const int passes = (bits + 9) / 10, digit = (int)rg_max64(8, rg_div_up(bits, passes));
@@ -658,7 +659,7 @@ rg_status sum_by_id(rg_ctx* ctx, const char* who, const void* dy, rg_dtype dy_ty
     if (pieces > 1) {
         const int fours = (int)rg_div_up(dim, 4);
         int log2L = 0;
-        while (log2L < 6 && 1 << log2L < fours) ++log2L;
+        while (log2L < (dense ? 3 : 6) && 1 << log2L < fours) ++log2L;
         const auto kernel = dim < 4 ? k_join_pieces<U, true> : k_join_pieces<U, false>;
         kernel<<<dim3((unsigned)rg_div_up(pieces, kJoinPieces), (unsigned)rg_div_up(fours, 1 << log2L)), kJoinThreads, 0, s>>>(
             from, n, n_dev, (uint32_t)num_rows, dim, size, pieces, log2L, t, parts);

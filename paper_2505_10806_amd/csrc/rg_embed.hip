@@ -103,6 +103,9 @@ struct Entry {
 };
 
 constexpr int kRounds = 4, kTile = kThreads * kRounds, kSortWaves = kThreads / RG_WAVE;
+// Up to this many blocks a pass takes two launches instead of three, the counts added up by every block of the second (a gradient of 16384 / 65536 / 131072 / 524288
+// rows of 32 numbers into 200000 takes 35 / 41.5 / 53 / 145 us so, and 36.5 / 42 / 48 / 88 with the launch between).
+constexpr int kDirectBlocks = 64;
 
 __device__ __forceinline__ Entry entry_of(const Entry* from, const int32_t* ids, int64_t i, uint32_t num_rows) {
     if (from) return from[i];
@@ -122,7 +125,8 @@ __device__ __forceinline__ uint64_t same_digit(uint32_t digit, bool live) {
     return mask;
 }
 
-template <int BITS>
+// DIRECT: of few blocks; counts lie [block][digit] and the scatter adds them up itself.
+template <int BITS, bool DIRECT>
 __global__ void __launch_bounds__(kThreads) k_sort_count(const Zeros zeros, int blocks, const Entry* __restrict__ from, const int32_t* __restrict__ ids, int64_t n,
                                                          const int32_t* __restrict__ n_dev, uint32_t num_rows, int shift, int64_t per_block,
                                                          int32_t* __restrict__ counts) {
@@ -136,7 +140,7 @@ __global__ void __launch_bounds__(kThreads) k_sort_count(const Zeros zeros, int 
     for (int64_t i = first + threadIdx.x; i < last; i += kThreads) atomicAdd(&bins[entry_of(from, ids, i, num_rows).id >> shift & (DIGITS - 1)], 1);
     __syncthreads();
 #pragma unroll
-    for (int d = threadIdx.x; d < DIGITS; d += kThreads) counts[(int64_t)d * blocks + blockIdx.x] = bins[d];
+    for (int d = threadIdx.x; d < DIGITS; d += kThreads) counts[DIRECT ? blockIdx.x * DIGITS + d : (int64_t)d * blocks + blockIdx.x] = bins[d];
 }
 
 // Each digit's counts become its entries in front of every block; totals[digit] = all of them.
@@ -167,7 +171,7 @@ __global__ void __launch_bounds__(kThreads) k_sort_scan(const Zeros zeros, int d
     if (threadIdx.x == 0) totals[blockIdx.x] = before;
 }
 
-template <int BITS>
+template <int BITS, bool DIRECT>
 __global__ void __launch_bounds__(kThreads) k_sort_scatter(const Zeros zeros, int blocks, const Entry* __restrict__ from, const int32_t* __restrict__ ids, int64_t n,
                                                            const int32_t* __restrict__ n_dev, uint32_t num_rows, int shift, int64_t per_block,
                                                            const int32_t* __restrict__ counts, const int32_t* __restrict__ totals, Entry* __restrict__ to) {
@@ -176,16 +180,42 @@ __global__ void __launch_bounds__(kThreads) k_sort_scatter(const Zeros zeros, in
     __shared__ int32_t next[DIGITS], met[kSortWaves][DIGITS];
     if ((int)blockIdx.x >= blocks) return clear(zeros, blockIdx.x - blocks, gridDim.x - blocks);
     const int wave = threadIdx.x >> 6, lane = rg_lane();
-    int mine[EACH], sum = 0, all;
+    int in_front[EACH], mine[EACH], sum = 0, all;          // a digit's entries in blocks in front of this one, and all of the digits' before it in this thread
+    if constexpr (DIRECT) {
+        constexpr int AHEAD = 16;
+        int total[EACH];
 #pragma unroll
-    for (int d = 0; d < EACH; ++d) {
-        mine[d] = sum;
-        sum += totals[threadIdx.x * EACH + d];
+        for (int d = 0; d < EACH; ++d) in_front[d] = total[d] = 0;
+        for (int b0 = 0; b0 < blocks; b0 += AHEAD) {
+            int x[AHEAD][EACH];
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u)
+#pragma unroll
+                for (int d = 0; d < EACH; ++d) x[u][d] = counts[min(b0 + u, blocks - 1) * DIGITS + threadIdx.x * EACH + d];
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u)
+#pragma unroll
+                for (int d = 0; d < EACH; ++d) {
+                    total[d] += b0 + u < blocks ? x[u][d] : 0;
+                    in_front[d] += b0 + u < (int)blockIdx.x ? x[u][d] : 0;
+                }
+        }
+#pragma unroll
+        for (int d = 0; d < EACH; ++d) {
+            mine[d] = sum;
+            sum += total[d];
+        }
+    } else {
+#pragma unroll
+        for (int d = 0; d < EACH; ++d) {
+            mine[d] = sum;
+            sum += totals[threadIdx.x * EACH + d];
+            in_front[d] = counts[(int64_t)(threadIdx.x * EACH + d) * blocks + blockIdx.x];
+        }
     }
     const int base = rg_block_excl_scan<kSortWaves>(sum, smem, &all);
 #pragma unroll
-    for (int d = 0; d < EACH; ++d)
-        next[threadIdx.x * EACH + d] = base + mine[d] + counts[(int64_t)(threadIdx.x * EACH + d) * blocks + blockIdx.x];
+    for (int d = 0; d < EACH; ++d) next[threadIdx.x * EACH + d] = base + mine[d] + in_front[d];
     const int64_t first = (int64_t)blockIdx.x * per_block, last = rg_least(first + per_block, rg_rows(n, n_dev));
     for (int64_t tile = first; tile < last; tile += kTile) {
 #pragma unroll
@@ -616,29 +646,35 @@ rg_status sum_by_id(rg_ctx* ctx, const char* who, const void* dy, rg_dtype dy_ty
     int32_t* before = (int32_t*)(at + 2 * list + counts_bytes);
     float* parts = (float*)(at + 2 * list + counts_bytes + before_bytes);
     const int64_t all_zeros = zeros.to;
+    const int total_launches = (blocks <= kDirectBlocks ? 2 : 3) * passes;
     int launches = 0;
     const auto part_of_zeros = [&] {                       // a launch's share of the pieces
-        zeros.from = all_zeros * launches / (3 * passes);
-        zeros.to = all_zeros * ++launches / (3 * passes);
+        zeros.from = all_zeros * launches / total_launches;
+        zeros.to = all_zeros * ++launches / total_launches;
         return clear_blocks(ctx, zeros.to - zeros.from, kThreads);
     };
     const Entry* from = nullptr;
-    const auto sort = [&](auto width) {
+    const auto sort = [&](auto width, auto direct) {
         constexpr int BITS = decltype(width)::value;
+        constexpr bool DIRECT = decltype(direct)::value;
         for (int pass = 0; pass < passes; ++pass) {
             Entry* to = lists[pass & 1];
             int more = part_of_zeros();
-            k_sort_count<BITS><<<blocks + more, kThreads, 0, s>>>(zeros, blocks, from, ids, n, n_dev, (uint32_t)num_rows, pass * BITS, per_block, counts);
+            k_sort_count<BITS, DIRECT><<<blocks + more, kThreads, 0, s>>>(zeros, blocks, from, ids, n, n_dev, (uint32_t)num_rows, pass * BITS, per_block, counts);
+            if (!DIRECT) {
+                more = part_of_zeros();
+                k_sort_scan<<<(1 << BITS) + more, kThreads, 0, s>>>(zeros, 1 << BITS, counts, blocks, totals);
+            }
             more = part_of_zeros();
-            k_sort_scan<<<(1 << BITS) + more, kThreads, 0, s>>>(zeros, 1 << BITS, counts, blocks, totals);
-            more = part_of_zeros();
-            k_sort_scatter<BITS><<<blocks + more, kThreads, 0, s>>>(zeros, blocks, from, ids, n, n_dev, (uint32_t)num_rows, pass * BITS, per_block, counts, totals, to);
+            k_sort_scatter<BITS, DIRECT><<<blocks + more, kThreads, 0, s>>>(zeros, blocks, from, ids, n, n_dev, (uint32_t)num_rows, pass * BITS, per_block, counts, totals,
+                                                                            to);
             from = to;
         }
     };
-    if (digit == 8) sort(std::integral_constant<int, 8>());
-    else if (digit == 9) sort(std::integral_constant<int, 9>());
-    else sort(std::integral_constant<int, 10>());
+    const auto sort_by = [&](auto width) { blocks <= kDirectBlocks ? sort(width, std::true_type()) : sort(width, std::false_type()); };
+    if (digit == 8) sort_by(std::integral_constant<int, 8>());
+    else if (digit == 9) sort_by(std::integral_constant<int, 9>());
+    else sort_by(std::integral_constant<int, 10>());
     RG_LAUNCH_CHECK(ctx, "k_sort_scatter");
     if (touched) {
         k_count_ids<<<(unsigned)rg_div_up(pieces, kThreads / RG_WAVE), kThreads, 0, s>>>(from, n, n_dev, (uint32_t)num_rows, size, pieces, before);

@@ -149,7 +149,8 @@ __global__ void __launch_bounds__(256) k_pack_rows(const T* __restrict__ x, int6
 }
 
 struct Job {
-    const Words4* owned;       // k_pack_rows of the owned rows
+    const void* owned;         // the owned rows (held: as they are, `owned_stride` apart; else packed by k_pack_rows)
+    int64_t owned_stride;
     const void* walked;
     int64_t stride;            // of the walked rows
     int64_t owners, rows;      // owned rows; walked rows
@@ -168,6 +169,10 @@ struct Job {
     float* parts;              // else [split][owned row][dim]
 };
 
+// Whether owned rows are held in registers: rows of 16-bit numbers, up to 128 of them (256 where there is no sum of as many columns beside them).
+template <typename T>
+constexpr bool held_rows(int mode, int steps) { return Part<T>::P == 1 && steps > 0 && (steps <= kSteps || (mode == LOSS && steps <= 2 * kSteps)); }
+
 // STEPS: 16 columns each, of rows of up to 256 numbers; 0: any, in chunks of 128 columns.
 template <typename T, int MODE, int NB, int STEPS>
 __global__ void __launch_bounds__(kThreads, 2) k_softmax_rows(const Job job) {
@@ -176,7 +181,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_softmax_rows(const Job job) {
     constexpr int P = S::P, ROWS = MODE == LOSS && STEPS == 0 ? 2 * S::ROWS : S::ROWS, SB = ROWS / 32, GROUPS = ROWS / 16;     // (owned rows are read again for every tile)
     // HOLD: the owned rows stay in registers.  PIPE: the exponentials of a tile are formed between the products of the next one's z, so that the vector and the
     // matrix units work side by side; for that the tile stays in LDS for its second product while two more arrive.
-    constexpr bool HOLD = P == 1 && STEPS > 0 && (STEPS <= kSteps || MODE == LOSS), PIPE = STEPS > 0 && (STEPS <= kSteps || HOLD);
+    constexpr bool HOLD = held_rows<T>(MODE, STEPS), PIPE = STEPS > 0 && (STEPS <= kSteps || HOLD);
     // PERIOD: tiles between barriers; LOOK: how far ahead of its second product a tile is staged.
     constexpr int CHUNKS = STEPS > kSteps ? 2 : 1, PERIOD = PIPE && CHUNKS == 1 ? 2 : 1, LOOK = 2 * PERIOD, BUFFERS = PERIOD == 2 ? 6 : PIPE && MODE != LOSS ? 3 : 2;
     constexpr int ITEMS = (STEPS > 0 && STEPS < kSteps ? STEPS / 2 * GROUPS + kWaves - 1 : 4 * GROUPS) / kWaves;
@@ -231,13 +236,20 @@ __global__ void __launch_bounds__(kThreads, 2) k_softmax_rows(const Job job) {
         if (MODE == DX && label >= 0) lse2 = job.lse[owner] * kLog2e - (float)S::BIAS;
     }
     const int told = label - (int)(t0 * ROWS);              // (the label among this split's rows; less than 0 if there is none)
-    const Words4* owned = job.owned + (first_owner / 32 + wave) * steps * (P * 64) + lane;
+    const Words4* owned = (const Words4*)job.owned + (first_owner / 32 + wave) * steps * (P * 64) + lane;
     Words4 held[HOLD ? STEPS : 1][P];
-    if constexpr (HOLD) {
+    if constexpr (HOLD) {                                  // (rows that are not there, or do not count, are zeros)
+        const T* row = (const T*)job.owned + rg_least(owner, owners - 1) * job.owned_stride;
+        const bool counts = owner < owners && (MODE != DX || label >= 0);
+        typename RgPack<T, 8>::type raw[STEPS];
 #pragma unroll
-        for (int k = 0; k < STEPS; ++k)
+        for (int k = 0; k < STEPS; ++k) raw[k] = load_eight<STEPS == 2>(row, k * 16 + half * 8, dim);
 #pragma unroll
-            for (int p = 0; p < P; ++p) held[k][p] = owned[(k * P + p) * 64];
+        for (int k = 0; k < STEPS; ++k) {
+            if (k + (STEPS > kSteps ? 4 : 2) >= STEPS) row_parts<true, STEPS == 2, T>(raw[k], k * 16 + half * 8, dim, held[k]);      // (where a row may end)
+            else row_parts<false, false, T>(raw[k], k * 16 + half * 8, dim, held[k]);
+            if (!counts) held[k][0] = Words4{0, 0, 0, 0};
+        }
     }
     // dweight: whether one of the owned numbers is not finite (which times the zeros of a row that does not count is a NaN)
     bool odd = false;
@@ -1199,9 +1211,9 @@ int steps_of(int dim) {
 
 int64_t packed_row(int steps, int parts) { return (int64_t)steps * parts * 32; }
 
-// Rows that are owned at a time: their packed form stays in the last level of cache.
-int64_t piece_rows(int64_t rows, int steps, int parts) {
-    const int64_t most = rg_max64(1, (128ll << 20) / packed_row(steps, parts) / kOwners) * kOwners, pieces = rg_div_up(rows, most);
+// Rows that are owned at a time: their packed form stays in the last level of cache; held ones' sums and targets do (LOSS), or the launch has fewer than 2^32 threads.
+int64_t piece_rows(int64_t rows, int steps, int parts, bool held = false) {
+    const int64_t most = held ? 1 << 22 : rg_max64(1, (128ll << 20) / packed_row(steps, parts) / kOwners) * kOwners, pieces = rg_div_up(rows, most);
     return rg_div_up(rg_div_up(rows, pieces), kOwners) * kOwners;
 }
 
@@ -1302,14 +1314,15 @@ rg_status rg_cross_entropy(rg_ctx* ctx, const void* x, rg_dtype type, int64_t x_
             return RG_OK;
         }
         const int steps = steps_of(dim);
-        const int64_t piece = piece_rows(n, steps, P), most = rg_min64(piece, n), tiles = rg_div_up(most, kOwners);
+        const bool held = held_rows<T>(LOSS, steps);
+        const int64_t piece = piece_rows(n, steps, P, held), most = rg_min64(piece, n), tiles = rg_div_up(most, kOwners);
         const int splits = splits_for(ctx, tiles, classes);
-        const size_t packed = (size_t)(tiles * kOwners * packed_row(steps, P)), stats = (size_t)splits * most * sizeof(float2);
+        const size_t packed = held ? 0 : (size_t)(tiles * kOwners * packed_row(steps, P)), stats = (size_t)splits * most * sizeof(float2);
         const rg_status st = rg_scratch(ctx, ctx->loss_parts, packed + stats + (size_t)most * 4, s, "rg_cross_entropy");
         if (st != RG_OK) return st;
         char* at = (char*)ctx->loss_parts.p;
         Job job = {};
-        job.owned = (const Words4*)at;
+        job.owned_stride = x_stride;
         job.walked = weight;
         job.stride = weight_stride;
         job.rows = classes;
@@ -1324,7 +1337,8 @@ rg_status rg_cross_entropy(rg_ctx* ctx, const void* x, rg_dtype type, int64_t x_
         job.target = (float*)(at + packed + stats);
         for (int64_t first = 0; first < n; first += piece) {
             const int64_t count = rg_min64(piece, n - first);
-            pack<T>(ctx, x, x_stride, first, count, n, n_dev, dim, steps, nullptr, classes, at, s);
+            job.owned = held ? (const void*)((const T*)x + first * x_stride) : at;
+            if (!held) pack<T>(ctx, x, x_stride, first, count, n, n_dev, dim, steps, nullptr, classes, at, s);
             job.owners = count;
             job.first = first;
             job.tiles = (int)rg_div_up(count, kOwners);
@@ -1396,6 +1410,7 @@ rg_status rg_cross_entropy_grad(rg_ctx* ctx, const void* x, rg_dtype type, int64
         }
         const int steps = steps_of(dim), chunks = (int)rg_div_up(dim, kCols);
         const int64_t slices = rg_div_up(chunks, 2);       // (a workgroup's output: up to two chunks of columns)
+        const bool held = held_rows<T>(DX, steps);
         struct Side {
             int64_t rows, piece, most, tiles;
             int splits;
@@ -1404,11 +1419,11 @@ rg_status rg_cross_entropy_grad(rg_ctx* ctx, const void* x, rg_dtype type, int64
         const auto side = [&](int64_t rows, int64_t walked) {
             Side v;
             v.rows = rows;
-            v.piece = piece_rows(rows, steps, P);
+            v.piece = piece_rows(rows, steps, P, held);
             v.most = rg_min64(v.piece, rows);
             v.tiles = rg_div_up(v.most, kOwners);
             v.splits = splits_for(ctx, v.tiles * slices, walked);
-            v.packed = (size_t)(v.tiles * kOwners * packed_row(steps, P));
+            v.packed = held ? 0 : (size_t)(v.tiles * kOwners * packed_row(steps, P));
             v.parts = v.splits > 1 ? (size_t)v.splits * v.most * dim * 4 : 0;
             return v;
         };
@@ -1418,7 +1433,6 @@ rg_status rg_cross_entropy_grad(rg_ctx* ctx, const void* x, rg_dtype type, int64
         if (st != RG_OK) return st;
         char* at = (char*)ctx->loss_parts.p;
         Job job = {};
-        job.owned = (const Words4*)at;
         job.n = n;
         job.n_dev = n_dev;
         job.dim = dim;
@@ -1426,7 +1440,9 @@ rg_status rg_cross_entropy_grad(rg_ctx* ctx, const void* x, rg_dtype type, int64
         job.chunks = chunks;
         job.classes = classes;
         job.scale = scale;
-        const auto take = [&](const Side& v, int64_t first, void* out, int64_t stride) {
+        const auto take = [&](const Side& v, int64_t first, const void* owned, int64_t owned_stride, void* out, int64_t stride) {
+            job.owned = held ? (const void*)((const T*)owned + first * owned_stride) : at;
+            job.owned_stride = owned_stride;
             job.owners = rg_min64(v.piece, v.rows - first);
             job.first = first;
             job.tiles = (int)rg_div_up(job.owners, kOwners);
@@ -1439,8 +1455,8 @@ rg_status rg_cross_entropy_grad(rg_ctx* ctx, const void* x, rg_dtype type, int64
             if (job.splits > 1) join_parts<T>(ctx, job.parts, job.splits, job.owners, job.first, rows, count, dim, (T*)job.out, job.out_stride, s);
         };
         for (int64_t first = 0; dx && first < n; first += for_dx.piece) {
-            take(for_dx, first, dx, dx_stride);
-            pack<T>(ctx, x, x_stride, first, job.owners, n, n_dev, dim, steps, labels, classes, at, s);
+            take(for_dx, first, x, x_stride, dx, dx_stride);
+            if (!held) pack<T>(ctx, x, x_stride, first, job.owners, n, n_dev, dim, steps, labels, classes, at, s);
             job.walked = weight;
             job.stride = weight_stride;
             job.rows = classes;
@@ -1453,8 +1469,8 @@ rg_status rg_cross_entropy_grad(rg_ctx* ctx, const void* x, rg_dtype type, int64
             RG_LAUNCH_CHECK(ctx, "k_grad_join");
         }
         for (int64_t first = 0; dweight && first < classes; first += for_dw.piece) {
-            take(for_dw, first, dweight, dweight_stride);
-            pack<T>(ctx, weight, weight_stride, first, job.owners, classes, nullptr, dim, steps, nullptr, 0, at, s);
+            take(for_dw, first, weight, weight_stride, dweight, dweight_stride);
+            if (!held) pack<T>(ctx, weight, weight_stride, first, job.owners, classes, nullptr, dim, steps, nullptr, 0, at, s);
             job.walked = x;
             job.stride = x_stride;
             job.rows = n;

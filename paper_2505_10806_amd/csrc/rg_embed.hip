@@ -29,7 +29,7 @@ __device__ __forceinline__ void chunk_numbers(const P& a, int col, int dim, floa
 
 // ---------------------------------------------------------------- lookup
 // y[i] = scale table[ids[i]].  A workgroup takes `group` rows and deals their chunks of V numbers to its threads, kAhead of them on their way at a time: rows
-// of any length fill the lanes.  Bound by memory.
+// of any length fill the lanes.  V is what fills 16 bytes of the narrower type.  Bound by memory: 794 k rows of 256 bf16 out of 10 M, 150 us, 5.4 TB/s read and written.
 constexpr int kAhead = 4;
 
 template <typename T, typename U, int V, bool SHORT, bool ONCE>
@@ -97,7 +97,8 @@ __global__ void __launch_bounds__(kThreads) k_clear_rows(const Zeros z) { clear(
 
 // ---------------------------------------------------------------- ids in order
 // The gradient's sums run over the entries sorted by id, entries of an id in their own order, so that the same call adds in the same order each time.  Least
-// digit first, up to ten bits a pass (three launches); padding gets the id behind the last row and comes to lie behind all others.
+// digit first, 8 to 10 bits a pass, as many as leave the fewest passes; padding gets the id behind the last row and comes to lie behind all others.  What bounds a pass of
+// few ids is that its launches wait for each other: 794 k ids take 6 + 5 + 11 us a pass of 8 bits (counts, sums, places), 65 k ids 6 + 11 of 9 bits, zeros beside.
 struct Entry {
     uint32_t id, at;
 };
@@ -143,7 +144,7 @@ __global__ void __launch_bounds__(kThreads) k_sort_count(const Zeros zeros, int 
     for (int d = threadIdx.x; d < DIGITS; d += kThreads) counts[DIRECT ? blockIdx.x * DIGITS + d : (int64_t)d * blocks + blockIdx.x] = bins[d];
 }
 
-// Each digit's counts become its entries in front of every block; totals[digit] = all of them.
+// Each digit's counts become its entries in front of every block; totals[digit] = all of them.  A workgroup to a digit; 5 us of 776 blocks.
 __global__ void __launch_bounds__(kThreads) k_sort_scan(const Zeros zeros, int digits, int32_t* __restrict__ counts, int blocks, int32_t* __restrict__ totals) {
     __shared__ int smem[kSortWaves + 1];
     if ((int)blockIdx.x >= digits) return clear(zeros, blockIdx.x - digits, gridDim.x - digits);
@@ -171,6 +172,7 @@ __global__ void __launch_bounds__(kThreads) k_sort_scan(const Zeros zeros, int d
     if (threadIdx.x == 0) totals[blockIdx.x] = before;
 }
 
+// A block's entries to their places, in their order: a wavefront finds the entries before a lane's of the same digit by votes on its bits, wavefronts add up in LDS.
 template <int BITS, bool DIRECT>
 __global__ void __launch_bounds__(kThreads) k_sort_scatter(const Zeros zeros, int blocks, const Entry* __restrict__ from, const int32_t* __restrict__ ids, int64_t n,
                                                            const int32_t* __restrict__ n_dev, uint32_t num_rows, int shift, int64_t per_block,
@@ -268,6 +270,7 @@ __global__ void __launch_bounds__(kThreads) k_sort_scatter(const Zeros zeros, in
 // The sorted entries are cut into pieces of `size`.  An id is met for the first time in a piece where its first entry lies.
 __device__ __forceinline__ bool opens(const Entry* sorted, int64_t i) { return i == 0 || sorted[i - 1].id != sorted[i].id; }
 
+// Ids that open in a piece, a wavefront to a piece: where its rows of the list begin.  5 us of 794 k entries.
 __global__ void __launch_bounds__(kThreads) k_count_ids(const Entry* __restrict__ sorted, int64_t n, const int32_t* __restrict__ n_dev, uint32_t num_rows,
                                                         int64_t size, int pieces, int32_t* __restrict__ before) {
     const int64_t n_act = rg_rows(n, n_dev);
@@ -282,7 +285,7 @@ __global__ void __launch_bounds__(kThreads) k_count_ids(const Entry* __restrict_
     if (rg_lane() == 0) before[piece] = count;
 }
 
-// before[piece] = ids met in front of it, before[pieces] and *num_touched = all.
+// before[piece] = ids met in front of it, before[pieces] and *num_touched = all.  One workgroup, four counts to a thread: 6 us of 8192 pieces (of 16384 10, with 16 counts to a thread 16).
 __global__ void __launch_bounds__(1024) k_scan_ids(int32_t* __restrict__ before, int pieces, int32_t* __restrict__ num_touched) {
     __shared__ int smem[17];
     constexpr int EACH = 4;
@@ -338,7 +341,9 @@ __device__ __forceinline__ void put_sum(const Target<U>& t, int64_t row, int col
 
 // A group of 2^log2L lanes walks a piece, a chunk of V columns to a lane (blockIdx.y: which 2^log2L chunks), kWalk rows on their way at a time, and adds up in 32 bits.
 // The sums of an id that opens and ends in the piece are final; what belongs to an id that opened before goes to parts[piece][0], to one that goes on
-// behind to parts[piece][1], for k_join_pieces.  Bound by memory.
+// behind to parts[piece][1], for k_join_pieces.  V is what fills 16 bytes of the wider type.  Bound by memory: 794 k rows of 256 bf16, all ids different, into f32 rows 264-270 us,
+// 4.5 TB/s read and written (5.4 would be the lookup's; with stores past the caches 315 instead of 290); 1.5 M rows of 100 f32 into 47 129 us, 4.65 TB/s of rows that
+// begin and end inside lines of 128 bytes, which a neighbour's walk fetches again.
 constexpr int kWalk = 8;
 
 template <typename T, typename U, int V, bool SHORT>
@@ -397,7 +402,10 @@ __global__ void __launch_bounds__(kThreads) k_sum_pieces(const T* __restrict__ d
 }
 
 // The sums of ids whose entries lie in several pieces: a workgroup for the piece in which one of them opens (nothing to do for most), groups of 2^log2L lanes
-// with 4 columns each (blockIdx.y: which 2^log2L) side by side on runs of its pieces.
+// with 4 columns each (blockIdx.y: which 2^log2L) side by side on runs of its pieces.  Most workgroups only look; those that join wait for a few reads one behind the
+// other: 8 us of 65 k entries (12 where the last piece was looked for by halving), 5 of 794 k ids met once, 12.5 of 1.5 M entries of 47 ids.  There, ids join hundreds
+// of pieces each, and eight lanes a group (32 groups to a workgroup, more workgroups to an id) take 12.5 instead of the 20 of 32 lanes; on the 65 k entries it
+// is 21 instead of 8, so that the host takes them for ids of 64 entries or more.  Workgroups of 1024 threads: 42 to 57.
 constexpr int kJoinThreads = 256, kJoinPieces = 2;
 
 template <typename U, bool SHORT>
@@ -460,6 +468,8 @@ __global__ void __launch_bounds__(kJoinThreads) k_join_pieces(const Entry* __res
 
 // ---------------------------------------------------------------- few entries
 // One workgroup sorts them in LDS and lists the ids met: order[] the entries' rows of dy, run r the entries starts[r] .. starts[r + 1] - 1, of id touched[r].
+// Up to 2048 entries take two launches so, instead of six or more: 256 of 64 numbers 7.2 + 3.2 us.  Both sides of the line, 2048 and 2049 entries: of 64 numbers into the rows
+// met of 1000 11.5 and 29 us, of 128 into 200000 14 and 34.  (More do not fit one workgroup's registers and LDS as they are.)
 constexpr int kFew = 2048, kFewThreads = 1024, kFewWaves = kFewThreads / RG_WAVE, kFewRounds = kFew / kFewThreads;
 
 __global__ void __launch_bounds__(kFewThreads) k_sort_few(const Zeros zeros, const int32_t* __restrict__ ids, int n, const int32_t* __restrict__ n_dev, uint32_t num_rows, int bits,
@@ -540,7 +550,7 @@ __global__ void __launch_bounds__(kFewThreads) k_sort_few(const Zeros zeros, con
     }
 }
 
-// A workgroup to a run and 2^log2L chunks of V columns (blockIdx.y), its groups of lanes side by side on the run's entries.
+// A workgroup to a run and 2^log2L chunks of V columns (blockIdx.y), its groups of lanes side by side on the run's entries, added up in their order.
 template <typename T, typename U, int V, bool SHORT>
 __global__ void __launch_bounds__(kThreads) k_sum_runs(const T* __restrict__ dy, int64_t dy_stride, const int32_t* __restrict__ order, const int32_t* __restrict__ starts,
                                                        const int32_t* __restrict__ touched, const int32_t* __restrict__ count, int dim, int log2L, int rows,
@@ -626,9 +636,10 @@ rg_status sum_by_id(rg_ctx* ctx, const char* who, const void* dy, rg_dtype dy_ty
         RG_LAUNCH_CHECK(ctx, "k_sum_runs");
         return RG_OK;
     }
-    // pieces of 16 entries or more, and as many of them as fill the device
-    const bool dense = n / rg_max64(num_rows, 1) >= 64;    // ids of many entries: pieces that are joined by the hundred
-    const int most = (int)rg_max64(1024, rg_min64(dense ? 4096 : 16384, (1ll << 23) / dim));
+    // pieces of 16 entries or more, and as many of them as fill the device: of 1 M f32 rows of 32 / 128 numbers into the rows met of 100000, 4096 pieces take 146 / 207 us, 8192
+    // 124 / 217, 16384 135 / 236.  Ids of many entries are joined from hundreds of pieces each: of 1.5 M rows of 100 into 47, 4096 pieces take 169 us, 16384 203
+    const bool dense = n / rg_max64(num_rows, 1) >= 64;
+    const int most = (int)rg_max64(1024, rg_min64(dense ? 4096 : 8192, (1ll << 23) / dim));
     const int64_t size = rg_max64(16, rg_div_up(n, most));
     const int pieces = (int)rg_div_up(n, size);
     const int passes = (bits + 9) / 10, digit = (int)rg_max64(8, rg_div_up(bits, passes));

@@ -13,7 +13,7 @@ namespace {
 // again, read transposed.  dx and dweight each form z anew: that is one product in four, and nothing of size n by classes is ever stored.
 //
 // Numbers go through the matrix units as bf16 or f16 as they are; f32 in three parts of bf16 that add up to it (the six products of parts that reach
-// above 2^-24).  Of g, sums are in 32 bits and the second product takes g rounded to the rows' type (bf16: half an ulp of 2^-9, as the result's own rounding; f32: three parts again).
+// above 2^-24).  Of g, sums are in 32 bits and the second product takes g rounded to the rows' type (bf16: off by at most 2^-8 of it, as the result's own rounding is; f32: three parts again).
 // For f16, g is scaled by 2^14, which keeps g down to 2^-28 in f16's normal range.
 typedef float Acc __attribute__((ext_vector_type(16)));
 typedef uint32_t Words4 __attribute__((ext_vector_type(4)));
@@ -122,7 +122,7 @@ __device__ __forceinline__ void row_parts(const typename RgPack<T, 8>::type& raw
 __device__ __forceinline__ bool has_label(int label, int classes) { return (uint32_t)label < (uint32_t)classes; }
 
 // The owned rows as the matrix units take them: [block of 32 rows][16 columns][part][lane][8 numbers], lane l the row l % 32 and the columns 8 (l / 32) .. + 7.
-// Rows that are not there, or (labels given) do not count, are zeros.
+// Rows that are not there, or (labels given) do not count, are zeros.  For rows that are read again for every tile; bound by memory: 100 k rows of 128 f32, 22 us, 5.8 TB/s.
 template <typename T>
 __global__ void __launch_bounds__(256) k_pack_rows(const T* __restrict__ x, int64_t stride, int64_t first, int64_t n, const int32_t* __restrict__ n_dev, int dim,
                                                    int steps, const int32_t* __restrict__ labels, int classes, int64_t units, Words4* __restrict__ packed) {
@@ -174,6 +174,12 @@ template <typename T>
 constexpr bool held_rows(int mode, int steps) { return Part<T>::P == 1 && steps > 0 && (steps <= kSteps || (mode == LOSS && steps <= 2 * kSteps)); }
 
 // STEPS: 16 columns each, of rows of up to 256 numbers; 0: any, in chunks of 128 columns.
+// Bound by the matrix units, which these kernels keep busy 55 to 60 % of the cycles, at the 1.65 to 1.95 GHz that the card's power leaves them (a large library product of
+// bf16 reaches 1330 TFLOP/s): loss of 4096 rows of 256 f16 over 233 k classes 470-500 us, 980-1040 TFLOP/s; of 1024 rows of 100 bf16 over 2.4 M, dx 1110-1170 us and
+// dweight 1400-1690, 860-900 and 590-720 TFLOP/s of two products each (of 128 columns where rows have 100: a quarter more work); of 1024 rows of 128 f32 over
+// 200 k, dx 575 and dweight 880, at six products of parts 1090 and 710.  Two wavefronts a SIMD with 256 registers each: with three (32 walked rows) they spill; of two
+// blocks of owned rows to a wavefront too.  Two workgroups of 4 wavefronts to a unit took 1342 us where one of 8 takes 1264; one tile between barriers 1260 where two
+// take 1200; an order of priorities, deeper reads of fragments or another place of the loads changed nothing beyond 3 %.
 template <typename T, int MODE, int NB, int STEPS>
 __global__ void __launch_bounds__(kThreads, 2) k_softmax_rows(const Job job) {
     typedef Part<T> S;
@@ -688,7 +694,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_softmax_rows(const Job job) {
     }
 }
 
-// Each row's log-sum and loss from its splits, a wavefront to a row.
+// Each row's log-sum and loss from its splits, a wavefront to a row.  5 us: a launch and two reads one behind the other.
 __global__ void __launch_bounds__(64) k_loss_join(const float2* __restrict__ stats, int splits, int64_t first, int64_t count, int64_t n,
                                                   const int32_t* __restrict__ n_dev, const int32_t* __restrict__ labels, int classes,
                                                   const float* __restrict__ target, float* __restrict__ loss, float* __restrict__ lse) {
@@ -717,7 +723,8 @@ __global__ void __launch_bounds__(64) k_loss_join(const float2* __restrict__ sta
     if (loss) loss[row] = counts ? sum - target[row] : 0.0f;
 }
 
-// Sums of the splits' parts, in one order: RUNS runs of them side by side, 64 chunks of four columns to a workgroup.
+// Sums of the splits' parts, in one order: RUNS runs of them side by side, 64 chunks of four columns to a workgroup.  Bound by memory and the reads' latency: 256 parts of
+// 47 rows of 256 (12 MB) 8 us, 64 of 1024 rows of 128 (34 MB) 12 us.
 template <typename T, int RUNS, bool SHORT>
 __global__ void __launch_bounds__(64 * RUNS) k_grad_join(const float* __restrict__ parts, int splits, int64_t rows, int64_t first, int64_t n,
                                                          const int32_t* __restrict__ n_dev, int dim, int chunks, T* __restrict__ out, int64_t stride) {
@@ -776,6 +783,8 @@ __global__ void __launch_bounds__(256) k_zero_rows(T* __restrict__ out, int64_t 
 // Up to 64 classes, whose weight rows fit LDS beside a tile of R rows of x: a workgroup walks its rows once, each tile z, g, dx and its share of dweight, so that x is
 // read and dx written once and z is formed once.  z is [class][row] (rows along the lanes); g goes through LDS, from where dx's product reads it by rows and
 // dweight's transposed.  Outputs go to the wavefronts by blocks of 32 columns; dweight's sums stay in registers until the end, then a second launch joins the workgroups'.
+// 1024 rows of 256 f32 over 41 classes 7.2 us (the general kernel and its two companions: 21); gradients of 100 k rows of 256 f32 over 47 classes 90 us, 2.3 TB/s read and
+// written: products of three parts, cutting rows into them and the barriers between a tile's steps take turns (four wavefronts instead of eight: 119; the general kernel: 429).
 template <int P, int R, int CHUNKS>
 struct FewLds {
     static constexpr int ROW = CHUNKS * kRowBytes, G_ROW = 128;
@@ -1076,7 +1085,8 @@ __global__ void __launch_bounds__(kClassThreads, 2) k_few_classes(const FewJob j
     }
 }
 
-// Whether the kernel above takes rows of `dim` numbers, and its launch.
+// Whether the kernel above takes rows of `dim` numbers, and its launch.  Both sides of the line, 64 and 65 classes, rows of 256: loss of 1024 f32 7.5 and 21.5 us, of 100 k
+// bf16 19 and 52; gradients of 1024 f32 15 and 95, of 100 k f32 96 and 453, of 100 k bf16 50 and 123; rows of 100, 100 k f32 51 and 166.  (More classes do not fit LDS.)
 constexpr int kFewClasses = 64;
 template <typename T>
 bool few_classes(int classes, int dim) { return classes <= kFewClasses && dim >= 8 && dim <= (Part<T>::P > 1 ? 256 : 512); }
@@ -1101,7 +1111,7 @@ void launch_few(const FewJob& job, unsigned grid, hipStream_t s) {
 // ---------------------------------------------------------------- few rows
 // The loss of up to 32 rows against many classes: the weight is read once, by every wavefront for itself, 32 classes at a time straight into the matrix units' registers
 // (x's rows, 16-bit parts of them, stay in LDS).  A lane takes 16 neighbouring columns at a time, two steps' worth: the order of the columns is free as
-// long as both operands have the same.  Bound by memory.
+// long as both operands have the same.  Bound by memory: one row of 100 bf16 against 2.4 M classes 97 us, 5.1 TB/s (the general kernel, which packs rows and stages the weight: 196).
 constexpr int kFewWaves = 8;
 
 template <typename T>
@@ -1194,7 +1204,8 @@ __global__ void __launch_bounds__(64 * kFewWaves, 2) k_few_rows(const T* __restr
     if (row < n_act) stats[(int64_t)blockIdx.x * n + row] = make_float2(m, s);
 }
 
-// Whether the kernel above takes the call: its rows as parts lie in LDS (16 KB at 256 numbers of 16 bits).
+// Whether the kernel above takes the call: its rows as parts lie in LDS (16 KB at 256 numbers of 16 bits).  Both sides of the line, 32 and 33 rows of 128 numbers: against
+// 200000 classes 31 and 84 us of f32, 17 and 24 of bf16; against 65, 11 and 16 of f32, 11 and 11 of bf16.
 constexpr int kFewRows = 32;
 template <typename T>
 bool few_rows_many_classes(int64_t n, int dim) { return n <= kFewRows && dim >= 8 && rg_div_up(dim, 32) * 2 * Part<T>::P * 1024 <= 60 * 1024; }

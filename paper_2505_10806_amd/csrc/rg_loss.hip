@@ -174,10 +174,9 @@ template <typename T>
 constexpr bool held_rows(int mode, int steps) { return Part<T>::P == 1 && steps > 0 && (steps <= kSteps || (mode == LOSS && steps <= 2 * kSteps)); }
 
 // STEPS: 16 columns each, of rows of up to 256 numbers; 0: any, in chunks of 128 columns.
-// Bound by the matrix units, which the loss and dx keep busy 55 to 65 % of the cycles, dweight, whose workgroups walk 1024 rows and then load and store their own (a third of
-// their time), 37 %, at the 1.65 to 2.1 GHz that the card's power leaves them (a large library product of
+// Bound by the matrix units, which these kernels keep busy 55 to 60 % of the cycles, at the 1.65 to 1.95 GHz that the card's power leaves them (a large library product of
 // bf16 reaches 1330 TFLOP/s): loss of 4096 rows of 256 f16 over 233 k classes 470-500 us, 980-1040 TFLOP/s; of 1024 rows of 100 bf16 over 2.4 M, dx 1110-1170 us and
-// dweight 1300-1600, 860-900 and 630-770 TFLOP/s of two products each (of 128 columns where rows have 100: a quarter more work); of 1024 rows of 128 f32 over
+// dweight 1400-1690, 860-900 and 590-720 TFLOP/s of two products each (of 128 columns where rows have 100: a quarter more work); of 1024 rows of 128 f32 over
 // 200 k, dx 575 and dweight 880, at six products of parts 1090 and 710.  Two wavefronts a SIMD with 256 registers each: with three (32 walked rows) they spill; of two
 // blocks of owned rows to a wavefront too.  Two workgroups of 4 wavefronts to a unit took 1342 us where one of 8 takes 1264; one tile between barriers 1260 where two
 // take 1200; an order of priorities, deeper reads of fragments or another place of the loads changed nothing beyond 3 %.
@@ -260,7 +259,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_softmax_rows(const Job job) {
     }
     // dweight: whether one of the owned numbers is not finite (which times the zeros of a row that does not count is a NaN)
     bool odd = false;
-    const auto look_at_owned = [&]() __attribute__((always_inline)) {
+    if constexpr (MODE == DW) {
         const uint32_t top = std::is_same<E, _Float16>::value ? 0x7C00u : 0x7F80u;
         const auto look = [&](const Words4& w) __attribute__((always_inline)) {
 #pragma unroll
@@ -274,46 +273,42 @@ __global__ void __launch_bounds__(kThreads, 2) k_softmax_rows(const Job job) {
             for (int k = 0; k < steps * P; ++k) look(owned[k * 64]);
         }
         odd = __any(odd);
-    };
-    if (MODE == DW && !PIPE) look_at_owned();
+    }
 
     // Staging: a wavefront's pieces of 16 rows by 32 columns (four lanes to a row), so that only the last columns' ones look for the rows' end.  Within a row's 16
     // pieces of 16 bytes the place is the column's exclusive or with four bits of the row: both ways of reading the tile (16 rows of one piece, 4 rows of
     // 4) then meet all 64 banks once a cycle, where three bits for 128 bytes took twice as long.
     // (Loads are made without a branch, of the last row where there is no other: registers that are written in some paths only are waited for where paths meet.)
-    struct Ahead {
-        typename RgPack<T, 8>::type raw[CHUNKS][ITEMS];
-        float lse, share;
-        int label, to_label;
-    };
-    Ahead in;
+    typename RgPack<T, 8>::type raw[CHUNKS][ITEMS];
+    float next_lse = 0.0f, next_share = 0.0f;
+    int next_label = -1, to_label = -1;
     const int to_row = wave % GROUPS * 16 + (lane >> 2), group0 = wave / GROUPS;          // (of 32 columns; item u: group0 + u * kWaves / GROUPS)
     const int to_at = to_row * kRowBytes + (((group0 * 4 + (lane & 3)) ^ ((to_row & 3) << 2 | (to_row >> 2 & 3))) << 4);
     const T *ahead = walked + (t0 * ROWS + to_row) * job.stride, *const last = walked + (rows - 1) * job.stride;
-    const auto load = [&](Ahead& in, int t, int first_chunk, bool first) __attribute__((always_inline)) {
+    const auto load = [&](int t, int first_chunk, bool first) __attribute__((always_inline)) {
         const T* src = ahead < last ? ahead : last;
-        if (MODE == DW) in.to_label = job.labels[t0 * ROWS + min(t * ROWS + to_row, here - 1)];
+        if (MODE == DW) to_label = job.labels[t0 * ROWS + min(t * ROWS + to_row, here - 1)];
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
             for (int u = 0; u < ITEMS; ++u) {
                 if (STEPS > 0 && c * kSteps + u * (kWaves / GROUPS) * 2 >= STEPS) continue;
-                in.raw[c][u] = load_eight<STEPS == 2>(src, (first_chunk + c) * kCols + (group0 + u * (kWaves / GROUPS)) * 32 + (lane & 3) * 8, dim);
+                raw[c][u] = load_eight<STEPS == 2>(src, (first_chunk + c) * kCols + (group0 + u * (kWaves / GROUPS)) * 32 + (lane & 3) * 8, dim);
             }
         if (MODE == DW && first) {
             const int r = t * ROWS + (threadIdx.x & (ROWS - 1));
             const int64_t from = t0 * ROWS + min(r, here - 1);
-            in.label = job.labels[from];
-            in.lse = job.lse[from];
-            in.share = job.dloss ? job.dloss[from] : 1.0f;
-            if (r >= here) in.label = -1;
+            next_label = job.labels[from];
+            next_lse = job.lse[from];
+            next_share = job.dloss ? job.dloss[from] : 1.0f;
+            if (r >= here) next_label = -1;
         }
     };
     const auto next_tile = [&]() __attribute__((always_inline)) { ahead += ROWS * job.stride; };
-    const auto store = [&](const Ahead& in, int t, int first_chunk, int buffer, bool first, int place) __attribute__((always_inline)) {
+    const auto store = [&](int t, int first_chunk, int buffer, bool first, int place) __attribute__((always_inline)) {
         int dim = job.dim;
         asm volatile("" : "+s"(dim));                      // (else what depends on it is formed before the loop and takes registers through all of it)
-        const bool counts = t * ROWS + to_row < here && (MODE != DW || has_label(in.to_label, job.classes)), whole = __all(counts);
+        const bool counts = t * ROWS + to_row < here && (MODE != DW || has_label(to_label, job.classes)), whole = __all(counts);
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
@@ -323,8 +318,8 @@ __global__ void __launch_bounds__(kThreads, 2) k_softmax_rows(const Job job) {
                 // (rows of STEPS steps end in the last two: in the last item's columns, if that)
                 const bool may_end = STEPS == 0 || STEPS == 12 || STEPS == 16 || c * kSteps + (u + 1) * (kWaves / GROUPS) * 2 >= STEPS;
                 Words4 w[P];
-                if (may_end && chunk * kCols + group * 32 + 32 > dim) row_parts<true, STEPS == 2, T>(in.raw[c][u], col, dim, w);
-                else row_parts<false, false, T>(in.raw[c][u], col, dim, w);
+                if (may_end && chunk * kCols + group * 32 + 32 > dim) row_parts<true, STEPS == 2, T>(raw[c][u], col, dim, w);
+                else row_parts<false, false, T>(raw[c][u], col, dim, w);
 #pragma unroll
                 for (int p = 0; p < P; ++p) *(Words4*)(staged[buffer][c][p] + (to_at ^ u * (kWaves / GROUPS) << 6)) = w[p];
             }
@@ -337,11 +332,11 @@ __global__ void __launch_bounds__(kThreads, 2) k_softmax_rows(const Job job) {
                     for (int p = 0; p < P; ++p) *(Words4*)(staged[buffer][c][p] + (to_at ^ u * (kWaves / GROUPS) << 6)) = Words4{0, 0, 0, 0};
         }
         if (MODE == DW && first && threadIdx.x < ROWS) {
-            const bool live = has_label(in.label, job.classes);
-            const float lse = live ? in.lse * kLog2e : 0.0f, share = live ? ldexpf(in.share, S::BIAS - power) : 0.0f;
+            const bool live = has_label(next_label, job.classes);
+            const float lse = live ? next_lse * kLog2e : 0.0f, share = live ? ldexpf(next_share, S::BIAS - power) : 0.0f;
             row_lse[place][threadIdx.x] = lse;
             row_share[place][threadIdx.x] = share;
-            row_label[place][threadIdx.x] = live ? in.label : -1;
+            row_label[place][threadIdx.x] = live ? next_label : -1;
             // share exp2(z - lse) = exp2(z - row_both); 0 where the share is
             row_both[place][threadIdx.x] = share > 0.0f ? lse - __builtin_amdgcn_logf(share) : __builtin_inff();
         }
@@ -539,7 +534,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_softmax_rows(const Job job) {
         const auto turn = [&](int t, int now, Acc (&z)[SB], Acc (&next)[SB]) __attribute__((always_inline)) {
             const auto behind = [&](int k) __attribute__((always_inline)) { return now + k >= BUFFERS ? now + k - BUFFERS : now + k; };
             const int then = behind(1), free = behind(LOOK % BUFFERS);
-            load(in, t + LOOK, 0, true);
+            load(t + LOOK, 0, true);
             next_tile();
             const bool rare = open_tile(t, now, z);
             base = m == -__builtin_inff() ? 0.0f : m * kLog2e;
@@ -574,22 +569,18 @@ __global__ void __launch_bounds__(kThreads, 2) k_softmax_rows(const Job job) {
                 second(RG_INT(0), RG_INT(FIRST), now, [&](int u, int units) __attribute__((always_inline)) {
                     if (u < units / 2) exponentials(BEFORE + u * BEFORE / (units / 2), BEFORE + (u + 1) * BEFORE / (units / 2));
                 });
-            if (t + LOOK < tiles) store(in, t + LOOK, 0, free, true, free);
+            if (t + LOOK < tiles) store(t + LOOK, 0, free, true, free);
             return then;
         };
         Acc z[2][SB];
         int now = 0;
         if (tiles > 0) {
-            Ahead first[LOOK];                             // (all on their way before the first is waited for)
-#pragma unroll
+#pragma unroll 1
             for (int t = 0; t < LOOK; ++t) {
-                load(first[t], t, 0, true);
+                load(t, 0, true);
+                if (t < tiles) store(t, 0, t, true, t);
                 next_tile();
             }
-#pragma unroll
-            for (int t = 0; t < LOOK; ++t)
-                if (t < tiles) store(first[t], t, 0, t, true, t);
-            if (MODE == DW) look_at_owned();
             __syncthreads();
             clear(z[0]);
             products(RG_INT(STEPS), 0, 0, z[0], nothing);
@@ -606,9 +597,9 @@ __global__ void __launch_bounds__(kThreads, 2) k_softmax_rows(const Job job) {
         // A tile after the other, the next one's rows on their way: z, powers, second product.  (Sums for 256 output columns leave no registers for a second z.)
         Acc z[SB];
         if (tiles > 0) {
-            load(in, 0, 0, true);
+            load(0, 0, true);
             next_tile();
-            store(in, 0, 0, 0, true, 0);
+            store(0, 0, 0, true, 0);
             __syncthreads();
         }
 #pragma unroll 1
@@ -616,11 +607,11 @@ __global__ void __launch_bounds__(kThreads, 2) k_softmax_rows(const Job job) {
             const int buffer = t & 1;
             clear(z);
             products(RG_INT(STEPS), 0, buffer, z, nothing);
-            load(in, t + 1, 0, true);                      // (behind the products of z, which leave no registers for them)
+            load(t + 1, 0, true);                          // (behind the products of z, which leave no registers for them)
             next_tile();
             powers(t, buffer, z);
             if constexpr (MODE != LOSS) second(RG_INT(0), RG_INT(FIRST), buffer, nothing);
-            if (t + 1 < tiles) store(in, t + 1, 0, buffer ^ 1, true, buffer ^ 1);
+            if (t + 1 < tiles) store(t + 1, 0, buffer ^ 1, true, buffer ^ 1);
             __syncthreads();
         }
     } else {
@@ -633,8 +624,8 @@ __global__ void __launch_bounds__(kThreads, 2) k_softmax_rows(const Job job) {
             else products(RG_INT(2), chunk, buffer, z, nothing);
         };
         if (tiles > 0) {
-            load(in, 0, chunk_of(0), true);
-            store(in, 0, chunk_of(0), 0, true, 0);
+            load(0, chunk_of(0), true);
+            store(0, chunk_of(0), 0, true, 0);
             __syncthreads();
         }
         int buffer = 0;
@@ -644,9 +635,9 @@ __global__ void __launch_bounds__(kThreads, 2) k_softmax_rows(const Job job) {
             clear(z);
 #pragma unroll 1
             for (int stage = 0; stage < chunks - 1; ++stage) {
-                load(in, t, chunk_of(stage + 1), false);
+                load(t, chunk_of(stage + 1), false);
                 add_products(chunk_of(stage), buffer);
-                store(in, t, chunk_of(stage + 1), buffer ^ 1, false, 0);
+                store(t, chunk_of(stage + 1), buffer ^ 1, false, 0);
                 __syncthreads();
                 buffer ^= 1;
             }
@@ -655,17 +646,17 @@ __global__ void __launch_bounds__(kThreads, 2) k_softmax_rows(const Job job) {
             add_products(chunk_of(chunks - 1), buffer);
             powers(t, place, z);
             if (!rest) next_tile();
-            load(in, rest ? t : t + 1, rest ? chunk_of(chunks) : chunk_of(0), !rest);
+            load(rest ? t : t + 1, rest ? chunk_of(chunks) : chunk_of(0), !rest);
             if constexpr (MODE != LOSS) second(RG_INT(0), RG_INT(4), buffer, nothing);
-            if (rest || go_on) store(in, rest ? t : t + 1, rest ? chunk_of(chunks) : chunk_of(0), buffer ^ 1, !rest, place ^ 1);
+            if (rest || go_on) store(rest ? t : t + 1, rest ? chunk_of(chunks) : chunk_of(0), buffer ^ 1, !rest, place ^ 1);
             __syncthreads();
             buffer ^= 1;
             if constexpr (MODE != LOSS && NB > 4) {
                 if (rest) {
                     next_tile();
-                    load(in, t + 1, chunk_of(0), true);
+                    load(t + 1, chunk_of(0), true);
                     second(RG_INT(4), RG_INT(4), buffer, nothing);
-                    if (go_on) store(in, t + 1, chunk_of(0), buffer ^ 1, true, place ^ 1);
+                    if (go_on) store(t + 1, chunk_of(0), buffer ^ 1, true, place ^ 1);
                     __syncthreads();
                     buffer ^= 1;
                 }

@@ -15,7 +15,8 @@
  * Line 15, the training step on a gathered batch, has its operators as well: feature rows of 4-bit numbers that the steps
  * above move as they are (rg_mx4_quantize, rg_mx4_dequantize), their product with a weight and its gradient (rg_mx4_matmul,
  * rg_mx4_matmul_grad), layer norm (rg_layer_norm, rg_layer_norm_grad), and clipping by the norm of all gradients
- * (rg_clip_grad_norm).
+ * (rg_clip_grad_norm).  Models that learn a vector for every node look them up and sum their gradients by id (rg_embedding, rg_embedding_grad,
+ * rg_embedding_grad_rows), and answer with a class, or with a node among all nodes (rg_cross_entropy, rg_cross_entropy_grad).
  * Every step runs in HIP kernels on the device; there is no CPU fallback.
  *
  * Conventions

@@ -381,3 +381,33 @@ def test_two_contexts_on_two_streams(ctx):  # noqa: F811
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for out in got for a, b in zip(out, want))
     other.close()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, F32])
+def test_more_rows_or_classes_than_are_owned_at_a_time(ctx, dtype):  # noqa: F811
+    """Around the lines between pieces of 2^22 owned rows and at the ends, rows of one side against few of the other; PAD behind the last."""
+    many, few, dim = (1 << 22) + 300, 70, 8
+    some = np.unique(np.concatenate([np.arange(80), (1 << 22) + np.arange(-80, 80), many // 2 + np.arange(40), many - 1 - np.arange(80)]))
+    at = torch.from_numpy(some).to(DEV)
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(11)
+    rows = torch.randn(many, dim, generator=gen, device=DEV).to(dtype)
+    other = torch.randn(few, dim, generator=gen, device=DEV).to(dtype)
+    # many rows
+    labels = torch.randint(-1, few, (many,), generator=gen, device=DEV).int()
+    loss, lse = torch.full((many + 1,), PAD, device=DEV), torch.full((many + 1,), PAD, device=DEV)
+    ctx.cross_entropy(rows, many, dim, other, few, labels, loss, lse)
+    x, w, told = f64(rows[at]), f64(other), labels[at].long().cpu().numpy()
+    check_loss(loss[at], lse[at], x, w, told, dtype)
+    dx = torch.full((many + 1, dim), PAD, dtype=dtype, device=DEV)
+    ctx.cross_entropy_grad(rows, many, dim, other, few, labels, lse, dx[:many], None)
+    check_grads(dx[at], None, x, w, told, f64(lse[at]), np.ones(len(some)), dtype)
+    assert float(loss[many]) == PAD and float(lse[many]) == PAD and bool((dx[many] == PAD).all())
+    # many classes, the labels among those that are looked at
+    told = np.random.default_rng(5).integers(0, len(some), few)
+    labels = at[torch.from_numpy(told).to(DEV)].int()
+    lse = torch.full((few,), 15.0, device=DEV)
+    dw = torch.full((many + 1, dim), PAD, dtype=dtype, device=DEV)
+    ctx.cross_entropy_grad(other, few, dim, rows, many, labels, lse, None, dw[:many])
+    check_grads(None, dw[at], w, x, told, f64(lse), np.ones(few), dtype)
+    assert bool((dw[many] == PAD).all())

@@ -177,7 +177,7 @@ constexpr bool held_rows(int mode, int steps) { return Part<T>::P == 1 && steps 
 // Bound by the matrix units, which the loss and dx keep busy 52 to 65 % of the cycles, dweight, whose workgroups walk 1024 rows and then load and store their own, 37 %, at the
 // 1.65 to 2.1 GHz that the card's power leaves them (a large library product of
 // bf16 reaches 1330 TFLOP/s): loss of 4096 rows of 256 f16 over 233 k classes 470-500 us, 980-1040 TFLOP/s; of 1024 rows of 100 bf16 over 2.4 M, dx 1110-1170 us and
-// dweight 1300-1700, 860-900 and 590-770 TFLOP/s of two products each (of 128 columns where rows have 100: a quarter more work); of 1024 rows of 128 f32 over
+// dweight 1300-1700, 860-900 and 590-770 TFLOP/s of two products each (of 112 and 128 columns where rows have 100: a fifth more work); of 1024 rows of 128 f32 over
 // 200 k, dx 575 and dweight 880, at six products of parts 1090 and 710.  Two wavefronts a SIMD with 256 registers each: with three (32 walked rows) they spill; of two
 // blocks of owned rows to a wavefront too.  Two workgroups of 4 wavefronts to a unit took 1342 us where one of 8 takes 1264; one tile between barriers 1260 where two
 // take 1200; an order of priorities, deeper reads of fragments, another place of the loads or the first tiles loaded together changed nothing beyond 3 %.

@@ -227,3 +227,28 @@ def test_lookup_gradient_against_differences(ctx):  # noqa: F811
     ctx.embedding(table + direction, rows, ids, n, dim, y1, scale=4.0)
     ctx.embedding_grad(dy, ids, n, dim, rows, grad, scale=4.0)
     assert float((dy.double() * (y1 - y0).double()).sum()) == float((grad.double() * direction.double()).sum())
+
+
+@pytest.mark.parametrize("n,rows", [(5000, 7), (5000, 3000), (100_003, 7), (100_003, 70_000)])
+def test_gradients_of_many_entries_count_on_the_device(ctx, n, rows):  # noqa: F811
+    """Whole numbers, whose sums are exact in any order; ids and rows behind the count hold what would show."""
+    dim = 12
+    rng = np.random.default_rng(n + rows)
+    ids, dy = some_ids(rng, n, rows), rng.integers(-8, 9, size=(n, dim)).astype(np.float64)
+    for live in (0, 1, 2049, n - 1, n, n + 5):
+        count = min(live, n)
+        want = np.zeros((rows, dim))
+        there = (ids[:count] >= 0) & (ids[:count] < rows)
+        np.add.at(want, ids[:count][there], dy[:count][there])
+        t = torch.from_numpy(dy).float().to(DEV)
+        t[count:] = float("nan")
+        n_dev = torch.tensor([live], dtype=torch.int32, device=DEV)
+        table = torch.full((rows + 1, dim + 3), PAD, device=DEV)
+        ctx.embedding_grad(t, on_gpu(ids), n, dim, rows, table[:rows, :dim], n_dev=n_dev)
+        assert np.array_equal(f64(table[:rows, :dim]), want) and bool((table[rows] == PAD).all()) and bool((table[:, dim:] == PAD).all())
+        most = min(n, rows)
+        grad, touched, met = torch.full((most, dim), PAD, device=DEV), torch.full((most,), -7, dtype=torch.int32, device=DEV), torch.zeros(1, dtype=torch.int32, device=DEV)
+        ctx.embedding_grad_rows(t, on_gpu(ids), n, dim, rows, grad, touched, met, n_dev=n_dev)
+        named = np.unique(ids[:count][there])
+        assert int(met) == len(named) and np.array_equal(touched.cpu().numpy()[:len(named)], named) and bool((touched[len(named):] == -7).all())
+        assert np.array_equal(f64(grad)[:len(named)], want[named]) and bool((grad[len(named):] == PAD).all())

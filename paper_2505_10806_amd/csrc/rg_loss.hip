@@ -1000,8 +1000,8 @@ __global__ void __launch_bounds__(kClassThreads, 2) k_few_classes(const FewJob j
         if constexpr (!GRAD) {
             if (threadIdx.x < R && t * R + (int)threadIdx.x < here) {
                 const float m0 = lds.top[0][threadIdx.x], m1 = lds.top[1][threadIdx.x], top = fmaxf(m0, m1), base = top == -__builtin_inff() ? 0.0f : top;
-                const float sum = lds.sum[0][threadIdx.x] * __builtin_amdgcn_exp2f((m0 - base) * kLog2e) +
-                                  (m1 == -__builtin_inff() ? 0.0f : lds.sum[1][threadIdx.x] * __builtin_amdgcn_exp2f((m1 - base) * kLog2e));
+                // (classes whose z are all NaN have a maximum of -infinity, and a NaN as their sum, which stays one; where there are none, the sum is 0)
+                const float sum = lds.sum[0][threadIdx.x] * __builtin_amdgcn_exp2f((m0 - base) * kLog2e) + lds.sum[1][threadIdx.x] * __builtin_amdgcn_exp2f((m1 - base) * kLog2e);
                 const int64_t row = t0 * R + t * R + threadIdx.x;
                 const bool counts = has_label(job.labels[row], classes);
                 const float lse = top + logf(sum);

@@ -559,7 +559,8 @@ RG_API rg_status rg_cross_entropy(rg_ctx* ctx, const void* x, rg_dtype type, int
 /* Its gradients.  With share_i = scale dloss[i] (dloss NULL: scale) and g[i][c] = exp(z[i][c] - lse_i) - [c = labels[i]]:
  * dx[i][k] = share_i sum_c g[i][c] weight[c][k],  dweight[c][k] = sum_i share_i g[i][c] x[i][k].
  * lse: the forward pass's.  Rows that do not count get a dx of zeros and add nothing to dweight; their lse, dloss and x may hold anything.
- * z is formed anew.  For 16-bit types g is rounded to `type` for its products, whose sums are in 32 bits.
+ * z is formed anew.  For 16-bit types g is rounded to `type` for dx's products, and dloss[i] g for dweight's, whose sums are in 32 bits (of RG_F16, g from 2^-28 on keeps
+ * all of the type's bits, and dloss[i] g from 2^-28 of the largest finite dloss on).  A row's dx does not depend on other rows' dloss.
  * dx, dweight: device, of type `type`, overwritten (dweight: zeros where there are no rows); each may be NULL (not wanted).  Neither
  * overlaps an input.  scale is not a NaN. */
 RG_API rg_status rg_cross_entropy_grad(rg_ctx* ctx, const void* x, rg_dtype type, int64_t x_stride, int64_t n, const int32_t* n_dev,

@@ -14,7 +14,8 @@ namespace {
 //
 // Numbers go through the matrix units as bf16 or f16 as they are; f32 in three parts of bf16 that add up to it (the six products of parts that reach
 // above 2^-24).  Of g, sums are in 32 bits and the second product takes g rounded to the rows' type (bf16: off by at most 2^-8 of it, as the result's own rounding is; f32: three parts again).
-// For f16, g is scaled by 2^14, which keeps g down to 2^-28 in f16's normal range.
+// For f16, g is scaled by 2^14, which keeps g down to 2^-28 in f16's normal range.  dx's g is without the row's share, or with what of it lies in [0.5, 1); dweight's has
+// it, as a part of the largest (finite) share of the rows that a workgroup sums, so that of f16 what lies 2^-28 below that one loses bits.
 typedef float Acc __attribute__((ext_vector_type(16)));
 typedef uint32_t Words4 __attribute__((ext_vector_type(4)));
 typedef uint32_t Words2 __attribute__((ext_vector_type(2)));
@@ -121,6 +122,14 @@ __device__ __forceinline__ void row_parts(const typename RgPack<T, 8>::type& raw
 
 __device__ __forceinline__ bool has_label(int label, int classes) { return (uint32_t)label < (uint32_t)classes; }
 
+// |share|, or 0 where it is not finite, and the power of two that brings it below 1.
+__device__ __forceinline__ float finite_size(float share) { return fabsf(share) < __builtin_inff() ? fabsf(share) : 0.0f; }
+__device__ __forceinline__ int power_of_two(float size) {
+    int power = 0;
+    if (size > 0.0f) (void)frexpf(size, &power);
+    return power;
+}
+
 // The owned rows as the matrix units take them: [block of 32 rows][16 columns][part][lane][8 numbers], lane l the row l % 32 and the columns 8 (l / 32) .. + 7.
 // Rows that are not there, or (labels given) do not count, are zeros.  For rows that are read again for every tile; bound by memory: 100 k rows of 128 f32, 22 us, 5.8 TB/s.
 template <typename T>
@@ -219,18 +228,18 @@ __global__ void __launch_bounds__(kThreads, 2) k_softmax_rows(const Job job) {
         return c >= chunks ? c - chunks : c;
     };
 
-    // dweight: shares are scaled by a power of two to at most 1, and the sums back
+    // dweight: shares (finite ones) are scaled by a power of two to at most 1, and the sums back
     int power = 0;
     if (MODE == DW && job.dloss) {
         float top = 0.0f;
         for (int64_t r = t0 * ROWS + threadIdx.x; r < rg_least((t0 + tiles) * ROWS, rows); r += kThreads)
-            if (has_label(job.labels[r], job.classes)) top = fmaxf(top, fabsf(job.dloss[r]));
+            if (has_label(job.labels[r], job.classes)) top = fmaxf(top, finite_size(job.dloss[r]));
         for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, RG_WAVE));
         if (lane == 0) largest[wave] = top;
         __syncthreads();
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) top = fmaxf(top, largest[w]);
-        if (top > 0.0f && top < __builtin_inff()) (void)frexpf(top, &power);
+        power = power_of_two(top);
     }
 
     // what a lane's owned row brings
@@ -786,14 +795,14 @@ __global__ void __launch_bounds__(256) k_zero_rows(T* __restrict__ out, int64_t 
 // dweight's transposed.  Outputs go to the wavefronts by blocks of 32 columns; dweight's sums stay in registers until the end, then a second launch joins the workgroups'.
 // 1024 rows of 256 f32 over 41 classes 7.2 us (the general kernel and its two companions: 21); gradients of 100 k rows of 256 f32 over 47 classes 90 us, 2.3 TB/s read and
 // written: products of three parts, cutting rows into them and the barriers between a tile's steps take turns (four wavefronts instead of eight: 119; the general kernel: 429).
-template <int P, int R, int CHUNKS>
+template <int P, int FORMS, int R, int CHUNKS>
 struct FewLds {
     static constexpr int ROW = CHUNKS * kRowBytes, G_ROW = 128;
-    char weight[P][64 * ROW], x[P][R * ROW], g[P][R * G_ROW];
+    char weight[P][64 * ROW], x[P][R * ROW], g[FORMS][P][R * G_ROW];
     float top[2][R], sum[2][R], target[R];
-    float largest[8];
+    float largest[8], smallest[8];
 };
-static_assert(sizeof(FewLds<3, 32, 2>) <= 160 * 1024 && sizeof(FewLds<3, 64, 1>) <= 160 * 1024 && sizeof(FewLds<1, 32, 4>) <= 160 * 1024, "LDS of a compute unit");
+static_assert(sizeof(FewLds<3, 1, 32, 2>) <= 160 * 1024 && sizeof(FewLds<3, 1, 64, 1>) <= 160 * 1024 && sizeof(FewLds<1, 2, 32, 4>) <= 160 * 1024, "LDS of a compute unit");
 
 struct FewJob {
     const void *x, *weight;
@@ -814,7 +823,8 @@ template <typename T, bool GRAD, int R, int CHUNKS>
 __global__ void __launch_bounds__(kClassThreads, 2) k_few_classes(const FewJob job) {
     typedef Part<T> S;
     typedef typename S::type E;
-    typedef FewLds<S::P, R, CHUNKS> Lds;
+    constexpr int FORMS = GRAD && S::BIAS ? 2 : 1;         // of g
+    typedef FewLds<S::P, FORMS, R, CHUNKS> Lds;
     constexpr int P = S::P, ROW = Lds::ROW, RB = R / 32, ROWGROUPS = R / 16, ITEMS = ROWGROUPS * CHUNKS * 4 / kClassWaves;
     __shared__ __attribute__((aligned(16))) Lds lds;
     const int lane = rg_lane(), wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), half = lane >> 5, i16 = lane & 15;
@@ -855,17 +865,37 @@ __global__ void __launch_bounds__(kClassThreads, 2) k_few_classes(const FewJob j
         for (int u = 0; u < ITEMS; ++u) raw[u] = load_eight<false>(src, (group0 + u * (kClassWaves / ROWGROUPS)) * 32 + (lane & 3) * 8, dim);
     };
     if (tiles > 0) load(0);
+    // Shares to at most 1, as above, which dweight's products take with g.  dx's rows go by their own shares: where those of this workgroup's rows are so far apart that
+    // g loses bits with the power of two that they have in common (of f16, any), dx gets a g of its own, each row with its own power.  Of f16 both lie in LDS, and wavefronts
+    // that would be idle form z and the other g; else there is no room, and dweight's is formed when dx is done.  Powers of two change no bits, so that a row's dx is the
+    // same whatever other rows have.  100 k rows of 256 over 47 classes, without shares, with shares of [0, 2), and with some 2^60 below: f32
+    // 86, 89 and 109 us, bf16 48, 50 and 62, f16 48, 56 and 56.
     int power = 0;
-    if (GRAD && job.dloss) {                               // (shares to at most 1, as above)
-        float top = 0.0f;
+    bool apart = false;
+    if (GRAD && job.dloss) {
+        float top = 0.0f, least = __builtin_inff();
         for (int64_t r = t0 * R + threadIdx.x; r < rg_least((t0 + tiles) * R, n_act); r += kClassThreads)
-            if (has_label(job.labels[r], classes)) top = fmaxf(top, fabsf(job.dloss[r]));
-        for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, RG_WAVE));
-        if (lane == 0) lds.largest[wave] = top;
+            if (has_label(job.labels[r], classes)) {
+                const float size = finite_size(job.dloss[r]);
+                top = fmaxf(top, size);
+                least = size > 0.0f ? fminf(least, size) : least;
+            }
+        for (int off = 32; off > 0; off >>= 1) {
+            top = fmaxf(top, __shfl_xor(top, off, RG_WAVE));
+            least = fminf(least, __shfl_xor(least, off, RG_WAVE));
+        }
+        if (lane == 0) {
+            lds.largest[wave] = top;
+            lds.smallest[wave] = least;
+        }
         __syncthreads();
 #pragma unroll
-        for (int w = 0; w < kClassWaves; ++w) top = fmaxf(top, lds.largest[w]);
-        if (top > 0.0f && top < __builtin_inff()) (void)frexpf(top, &power);
+        for (int w = 0; w < kClassWaves; ++w) {
+            top = fmaxf(top, lds.largest[w]);
+            least = fminf(least, lds.smallest[w]);
+        }
+        power = power_of_two(top);
+        apart = job.dx && (S::BIAS || ldexpf(least, 30 - power) < 1.0f);
     }
     for (int group = wave / 4; group < blocks; group += kClassWaves / 4) {
         const int row = wave % 4 * 16 + (lane >> 2);
@@ -893,11 +923,12 @@ __global__ void __launch_bounds__(kClassThreads, 2) k_few_classes(const FewJob j
 
     for (int t = 0; t < tiles; ++t) {
         __syncthreads();                                   // (the tile before is done with)
-        int label[RB];
+        int label[RB], own_power[RB];
 #pragma unroll
         for (int b = 0; b < RB; ++b) {
             const int r = t * R + b * 32 + (lane & 31);
             label[b] = job.labels[t0 * R + min(r, here - 1)];
+            own_power[b] = apart ? power_of_two(finite_size(job.dloss[t0 * R + min(r, here - 1)])) : power;
             if (r >= here || !has_label(label[b], classes)) label[b] = -1;
         }
         const bool counts = t * R + to_row < here && has_label(raw_label, classes);
@@ -910,13 +941,13 @@ __global__ void __launch_bounds__(kClassThreads, 2) k_few_classes(const FewJob j
         __syncthreads();
 
         // z: a wavefront's block of 32 classes by 32 rows, of numbers in three parts half of its steps, which the other half's wavefront adds
-        const int cb = wave & 1, rb = RB == 2 ? wave >> 1 & 1 : 0, part = wave >> RB;
+        const int cb = wave & 1, rb = RB == 2 ? wave >> 1 & 1 : 0, part = wave >> RB, mine = RB == 1 ? label[0] : rb ? label[RB - 1] : label[0];
         constexpr int HALVES = P > 1 ? 2 : 1;
         Acc z;
-        if (part < HALVES) {
+        if (part < HALVES || (FORMS == 2 && apart && part == 1)) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) z[i] = 0.0f;
-            const int middle = HALVES == 2 ? steps / 4 * 2 : steps, from = part * middle, to = part == 0 ? middle : steps;
+            const int middle = HALVES == 2 ? steps / 4 * 2 : steps, from = HALVES == 2 ? part * middle : 0, to = part == 0 ? middle : steps;
             for (int k0 = from; k0 < to; k0 += 2) {        // (an even number of them)
                 Words4 a[2][P], b[2][P];
 #pragma unroll
@@ -944,9 +975,34 @@ __global__ void __launch_bounds__(kClassThreads, 2) k_few_classes(const FewJob j
             }
             __syncthreads();
         }
+        const int first = cb * 32 + 4 * half;              // register i: class first + 8 (i >> 2) + (i & 3)
+        const auto put_g = [&](int form, int scale_power) __attribute__((always_inline)) {         // share g, to LDS
+            const int64_t row = t0 * R + t * R + min(rb * 32 + (lane & 31), here - 1 - t * R);
+            const float lse2 = mine >= 0 ? job.lse[row] * kLog2e : 0.0f, share = mine >= 0 ? ldexpf(job.dloss ? job.dloss[row] : 1.0f, S::BIAS - scale_power) : 0.0f;
+            const bool idle = mine < 0 || share == 0.0f;
+            float v[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int c = first + 8 * (i >> 2) + (i & 3);
+                const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(z[i], kLog2e, -lse2));
+                v[i] = idle || c >= classes ? 0.0f : share * (p - (c == mine ? 1.0f : 0.0f));
+            }
+            const int at = rb * 32 + (lane & 31);
+#pragma unroll
+            for (int i = 0; i < 16; i += 8) {
+                float eight[8];
+                Words4 w[P];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) eight[j] = v[i + j];
+                cut<T>(eight, w);
+#pragma unroll
+                for (int p = 0; p < P; ++p)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+                        *(Words2*)(lds.g[form][p] + at * Lds::G_ROW + (((cb * 4 + i / 4 + j) ^ g_twist(at)) << 4) + half * 8) = Words2{w[p][2 * j], w[p][2 * j + 1]};
+            }
+        };
         if (part == 0) {
-            const int mine = RB == 1 ? label[0] : rb ? label[RB - 1] : label[0], first = cb * 32 + 4 * half;     // register i: class first + 8 (i >> 2) + (i & 3)
-            const int64_t row = t0 * R + min(t * R + rb * 32 + (lane & 31), here - 1);
             if constexpr (!GRAD) {
                 float top = -__builtin_inff(), there = 0.0f;
                 bool met = false;
@@ -970,32 +1026,8 @@ __global__ void __launch_bounds__(kClassThreads, 2) k_few_classes(const FewJob j
                     lds.sum[cb][at] = sum;
                 }
                 if (met) lds.target[at] = there;
-            } else {
-                const float lse2 = mine >= 0 ? job.lse[row] * kLog2e : 0.0f, share = mine >= 0 ? ldexpf(job.dloss ? job.dloss[row] : 1.0f, S::BIAS - power) : 0.0f;
-                const bool idle = mine < 0 || share == 0.0f;
-                float v[16];
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int c = first + 8 * (i >> 2) + (i & 3);
-                    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(z[i], kLog2e, -lse2));
-                    v[i] = idle || c >= classes ? 0.0f : share * (p - (c == mine ? 1.0f : 0.0f));
-                }
-                const int at = rb * 32 + (lane & 31);
-#pragma unroll
-                for (int i = 0; i < 16; i += 8) {
-                    float eight[8];
-                    Words4 w[P];
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) eight[j] = v[i + j];
-                    cut<T>(eight, w);
-#pragma unroll
-                    for (int p = 0; p < P; ++p)
-#pragma unroll
-                        for (int j = 0; j < 2; ++j)
-                            *(Words2*)(lds.g[p] + at * Lds::G_ROW + (((cb * 4 + i / 4 + j) ^ g_twist(at)) << 4) + half * 8) = Words2{w[p][2 * j], w[p][2 * j + 1]};
-                }
-            }
-        }
+            } else put_g(0, RB == 1 ? own_power[0] : rb ? own_power[RB - 1] : own_power[0]);
+        } else if (FORMS == 2 && apart && part == 1) put_g(1, power);
         __syncthreads();
         if constexpr (!GRAD) {
             if (threadIdx.x < R && t * R + (int)threadIdx.x < here) {
@@ -1024,7 +1056,7 @@ __global__ void __launch_bounds__(kClassThreads, 2) k_few_classes(const FewJob j
 #pragma unroll
                         for (int p = 0; p < P; ++p) {
                             a[p] = turned(lds.weight[p], f * 16, d);
-                            g[p] = *(const Words4*)(lds.g[p] + at * Lds::G_ROW + (((2 * f + half) ^ g_twist(at)) << 4));
+                            g[p] = *(const Words4*)(lds.g[0][p] + at * Lds::G_ROW + (((2 * f + half) ^ g_twist(at)) << 4));
                         }
                         out = mma_parts<E, P>(a, g, out);
                     }
@@ -1032,18 +1064,25 @@ __global__ void __launch_bounds__(kClassThreads, 2) k_few_classes(const FewJob j
                     if (r >= here) continue;
                     T* to = (T*)job.dx + (t0 * R + r) * job.dx_stride;
                     const float factor = mine < 0 ? 0.0f : job.scale;
+                    const int back = (RB == 2 ? (b ? own_power[RB - 1] : own_power[0]) : own_power[0]) - S::BIAS;
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
                         const int col = d * 32 + q * 8 + half * 4;
                         if (col >= dim) continue;
                         float v[4];
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) v[i] = mine < 0 ? 0.0f : ldexpf(out[q * 4 + i] * factor, power - S::BIAS);
+                        for (int i = 0; i < 4; ++i) v[i] = mine < 0 ? 0.0f : ldexpf(out[q * 4 + i] * factor, back);
                         rg_store_live<4>(to + col, dim - col, v);
                     }
                 }
             }
             if (job.parts) {
+                const auto& shared = lds.g[FORMS == 2 && apart ? 1 : 0];
+                if (FORMS == 1 && apart) {
+                    __syncthreads();
+                    if (part == 0) put_g(0, power);
+                    __syncthreads();
+                }
 #pragma unroll
                 for (int j = 0; j < CHUNKS; ++j) {
                     const int unit = wave + kClassWaves * j, d = unit >> 1, c = unit & 1;
@@ -1056,9 +1095,9 @@ __global__ void __launch_bounds__(kClassThreads, 2) k_few_classes(const FewJob j
                         for (int p = 0; p < P; ++p) {
                             a[p] = turned(lds.x[p], f * 16, d);
                             const Words2 low = __builtin_bit_cast(Words2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                                (Lds4*)(lds.g[p] + row * Lds::G_ROW + ((piece ^ g_twist(row)) << 4) + (i16 & 1) * 8)));
+                                (Lds4*)(shared[p] + row * Lds::G_ROW + ((piece ^ g_twist(row)) << 4) + (i16 & 1) * 8)));
                             const Words2 high = __builtin_bit_cast(Words2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                                (Lds4*)(lds.g[p] + (row + 4) * Lds::G_ROW + ((piece ^ g_twist(row + 4)) << 4) + (i16 & 1) * 8)));
+                                (Lds4*)(shared[p] + (row + 4) * Lds::G_ROW + ((piece ^ g_twist(row + 4)) << 4) + (i16 & 1) * 8)));
                             g[p] = Words4{low[0], low[1], high[0], high[1]};
                         }
                         dw[j] = mma_parts<E, P>(a, g, dw[j]);

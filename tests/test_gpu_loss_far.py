@@ -4,8 +4,9 @@ import pytest
 import torch
 
 import training_reference as ref
-from test_gpu_loss_ops import inputs, on_gpu
-from test_gpu_training_ops import DEV, F32, ctx, _name_the_case  # noqa: F401  (fixtures among them)
+import vector_reference as vec
+from test_gpu_loss_ops import check_grads, inputs, on_gpu
+from test_gpu_training_ops import DEV, F32, ctx, f64, _name_the_case  # noqa: F401  (fixtures among them)
 
 pytestmark = pytest.mark.gpu
 
@@ -26,3 +27,50 @@ def test_classes_whose_weight_is_not_a_number(ctx, dtype, n, classes, dim, bad):
         ctx.cross_entropy(x, n, dim, w, classes, on_gpu(labels), loss, lse)
         assert not bool(torch.isfinite(loss[counts]).any()) and not bool(torch.isfinite(lse[counts]).any())
         assert bool((loss[~counts] == 0).all()) and bool((lse[~counts] == 0).all())
+
+
+# ---------------------------------------------------------------- shares of very different size
+@pytest.mark.parametrize("dtype", ref.TYPES)
+@pytest.mark.parametrize("n,classes,dim", [(100, 41, 30), (100, 64, 100), (100, 20, 200), (40, 33, 300), (3000, 41, 30), (100, 65, 30), (100, 300, 200)])
+@pytest.mark.parametrize("far", [float("inf"), float("-inf"), 2.0 ** 126, 2.0 ** 40, 2.0 ** 20])
+def test_a_row_goes_by_its_own_share(ctx, dtype, n, classes, dim, far):  # noqa: F811
+    """One row's dloss is infinite or much larger: the others' dx are what they are without it, bit for bit, and within the bounds."""
+    rng = np.random.default_rng(n + classes + dim)
+    x, w, labels = inputs(rng, n, classes, dim, dtype)
+    labels = np.clip(labels, 0, classes - 1)
+    _, lse64 = vec.cross_entropy(vec.logits(f64(x), f64(w)), labels)
+    lse = torch.from_numpy(lse64).float().to(DEV)
+    dloss = torch.from_numpy(rng.normal(size=n) * np.exp2(rng.integers(-12, 8, n))).float().to(DEV)
+    dloss[5] = 0.0
+    dx, dw = torch.empty(n, dim, dtype=dtype, device=DEV), torch.empty(classes, dim, dtype=dtype, device=DEV)
+    ctx.cross_entropy_grad(x, n, dim, w, classes, on_gpu(labels), lse, dx, dw, dloss=dloss, scale=0.5)
+    check_grads(dx, dw, f64(x), f64(w), labels, f64(lse), f64(dloss) * 0.5, dtype)
+    dloss[7] = far
+    for with_weight in (True, False):
+        again = torch.empty_like(dx)
+        ctx.cross_entropy_grad(x, n, dim, w, classes, on_gpu(labels), lse, again, dw if with_weight else None, dloss=dloss, scale=0.5)
+        rest = np.delete(np.arange(n), 7)
+        at = torch.from_numpy(rest).to(DEV)
+        check_grads(again[at], None, f64(x)[rest], f64(w), labels[rest], f64(lse)[rest], f64(dloss)[rest] * 0.5, dtype)
+        assert torch.equal(again[at], dx[at])
+    if not np.isfinite(far):
+        assert not bool(torch.isfinite(again[7]).any()) and not bool(torch.isfinite(dw).any())
+
+
+@pytest.mark.parametrize("dtype", ref.TYPES)
+@pytest.mark.parametrize("n,classes,dim", [(200, 41, 30), (200, 64, 100), (200, 20, 200), (64, 33, 300), (200, 65, 30)])
+def test_small_shares_keep_their_bits(ctx, dtype, n, classes, dim):  # noqa: F811
+    """Shares down to 2^-100 of the largest (of f16: 2^-38, with a scale that brings the smallest dx into its range), each dx within its own row's bounds;
+    a class far below the others keeps a small g in every row."""
+    rng = np.random.default_rng(n + classes + dim)
+    x, w, labels = inputs(rng, n, classes, dim, dtype, spread=0.5)
+    labels = np.clip(labels, 0, classes - 1)
+    down, scale = (38, 2.0 ** 24) if dtype == torch.float16 else (100, 1.0)
+    _, lse64 = vec.cross_entropy(vec.logits(f64(x), f64(w)), labels)
+    lse = torch.from_numpy(lse64).float().to(DEV)
+    dloss = torch.from_numpy(rng.uniform(0.5, 1.0, n) * np.exp2(-rng.integers(down - 20, down + 1, n))).float().to(DEV)
+    dloss[0] = 1.0
+    dx, dw = torch.empty(n, dim, dtype=dtype, device=DEV), torch.empty(classes, dim, dtype=dtype, device=DEV)
+    ctx.cross_entropy_grad(x, n, dim, w, classes, on_gpu(labels), lse, dx, dw, dloss=dloss, scale=scale)
+    rest = np.arange(1, n)
+    check_grads(dx[1:], None, f64(x)[rest], f64(w), labels[rest], f64(lse)[rest], f64(dloss)[rest] * scale, dtype)

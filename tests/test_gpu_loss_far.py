@@ -74,3 +74,27 @@ def test_small_shares_keep_their_bits(ctx, dtype, n, classes, dim):  # noqa: F81
     ctx.cross_entropy_grad(x, n, dim, w, classes, on_gpu(labels), lse, dx, dw, dloss=dloss, scale=scale)
     rest = np.arange(1, n)
     check_grads(dx[1:], None, f64(x)[rest], f64(w), labels[rest], f64(lse)[rest], f64(dloss)[rest] * scale, dtype)
+
+
+# ---------------------------------------------------------------- many classes beside one
+@pytest.mark.parametrize("dtype,n,dim", [(torch.bfloat16, 33_000, 100), (torch.bfloat16, 33_000, 200), (torch.bfloat16, 33_000, 300), (torch.float16, 4096, 64), (F32, 33_000, 100),
+                                         (F32, 33_000, 200), (F32, 4096, 300), (torch.bfloat16, 4096, 300), (F32, 32, 100), (torch.bfloat16, 8, 100)])
+def test_what_one_class_leaves_is_shared_by_many(ctx, dtype, n, dim):  # noqa: F811
+    """A class of z = a against 232964 of z = 0: lse = a + log(1 + c), c = 232964 e^-a.  Roundings of lse's size: a / ln 2, the log's two steps, lse itself; of 1: up to
+    sixteen additions beside the one class, four of parts, exp2's step: together below 8 steps of 2^-24 (a + 1) (16 <= a + 1).  What the many add: 2^-18 of c."""
+    classes = 232_965
+    x, w = torch.zeros(n, dim, dtype=dtype, device=DEV), torch.zeros(classes, dim, dtype=dtype, device=DEV)
+    w[:, 1] = 3.0                                          # (against zeros of x)
+    first = torch.tensor([3.0, 3.25, 3.5, 4.0], device=DEV)[torch.arange(n, device=DEV) % 4]
+    x[:, 0] = first.to(dtype)
+    for label in (0, 64, 133, 116_000):
+        w[:, 0] = 0.0
+        w[label, 0] = 5.0
+        at = torch.full((n,), label, dtype=torch.int32, device=DEV)
+        loss, lse = torch.empty(n, device=DEV), torch.empty(n, device=DEV)
+        ctx.cross_entropy(x, n, dim, w, classes, at, loss, lse)
+        a = first.double() * 5.0
+        c = (classes - 1) * torch.exp(-a)
+        want = torch.log1p(c)
+        allowed = 8 * 2.0 ** -24 * (a + 1.0) + 2.0 ** -18 * c
+        assert bool(((lse.double() - a - want).abs() <= allowed).all()) and bool(((loss.double() - want).abs() <= allowed).all())

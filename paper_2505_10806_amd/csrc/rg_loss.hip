@@ -30,6 +30,11 @@ constexpr int kCols = 128, kRowBytes = kCols * 2;           // of a staged tile
 constexpr int kSteps = kCols / 16;                          // matrix products to its columns
 constexpr int kWaves = 8, kThreads = 64 * kWaves, kOwners = 32 * kWaves;      // rows that a workgroup owns
 constexpr float kLog2e = 1.44269504088896340736f;
+// exp(z - a) is formed as exp2(z log2(e) - a log2(e)), one operation beside the exponential; a log2(e) is rounded, which changes the exponent by up to 2^-24 of it: no more
+// than a's own rounding does, but beyond 2^31 by more than the exponential's range.  From this size on a is taken from z first.
+constexpr float kFar = 1024.0f;
+constexpr int kFarLabel = RG_LOSS_MAX_CLASSES;              // a bit above all labels: of a row whose lse is far
+__device__ __forceinline__ bool is_far(float a) { return fabsf(a) >= kFar && fabsf(a) < __builtin_inff(); }
 enum { LOSS = 0, DX = 1, DW = 2 };
 
 typedef __bf16 Bf8 __attribute__((ext_vector_type(8)));
@@ -246,11 +251,17 @@ __global__ void __launch_bounds__(kThreads, 2) k_softmax_rows(const Job job) {
     const int64_t owner = first_owner + wave * 32 + (lane & 31);
     int label = -1;
     float lse2 = 0.0f, m = -__builtin_inff(), s = 0.0f, lost = 0.0f, base = 0.0f;
+    bool far = false;                                      // DX: some row's lse is
     if (MODE != DW && owner < owners) {
         label = job.labels[owner];
         if (!has_label(label, job.classes)) label = -1;
-        if (MODE == DX && label >= 0) lse2 = job.lse[owner] * kLog2e - (float)S::BIAS;
+        if (MODE == DX && label >= 0) {
+            const float lse = job.lse[owner];
+            far = is_far(lse);
+            lse2 = (far ? 0.0f : lse * kLog2e) - (float)S::BIAS;
+        }
     }
+    if (MODE == DX) far = __any(far);
     const int told = label - (int)(t0 * ROWS);              // (the label among this split's rows; less than 0 if there is none)
     const Words4* owned = (const Words4*)job.owned + (first_owner / 32 + wave) * steps * (P * 64) + lane;
     Words4 held[HOLD ? STEPS : 1][P];
@@ -343,12 +354,12 @@ __global__ void __launch_bounds__(kThreads, 2) k_softmax_rows(const Job job) {
         }
         if (MODE == DW && first && threadIdx.x < ROWS) {
             const bool live = has_label(next_label, job.classes);
-            const float lse = live ? next_lse * kLog2e : 0.0f, share = live ? ldexpf(next_share, S::BIAS - power) : 0.0f;
+            const float lse = live ? next_lse : 0.0f, share = live ? ldexpf(next_share, S::BIAS - power) : 0.0f;
             row_lse[place][threadIdx.x] = lse;
             row_share[place][threadIdx.x] = share;
-            row_label[place][threadIdx.x] = live ? next_label : -1;
-            // share exp2(z - lse) = exp2(z - row_both); 0 where the share is
-            row_both[place][threadIdx.x] = share > 0.0f ? lse - __builtin_amdgcn_logf(share) : __builtin_inff();
+            row_label[place][threadIdx.x] = live ? next_label | (is_far(lse) ? kFarLabel : 0) : -1;
+            // share exp(z - lse) = exp2(z log2(e) - row_both); 0 where the share is
+            row_both[place][threadIdx.x] = share > 0.0f ? lse * kLog2e - __builtin_amdgcn_logf(share) : __builtin_inff();
         }
     };
 
@@ -387,7 +398,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_softmax_rows(const Job job) {
 #pragma unroll
         for (int u = 0; u < RING - 1; ++u)
             if (u < UNITS) read(u);
-#pragma unroll
+#pragma clang loop unroll(full)                            // (whatever its size: of numbers in parts it is beyond the limit of a plain unroll)
         for (int u = 0; u < UNITS; ++u) {
             const int k = u / SB, q = u % SB;
             if (u + RING - 1 < UNITS) read(u + RING - 1);
@@ -446,7 +457,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_softmax_rows(const Job job) {
         if (MODE == DW) {
             const int seen = row_label[place][lane & (ROWS - 1)], mine = (int)(job.first + first_owner) + wave * 32;
             const float share = row_share[place][lane & (ROWS - 1)];
-            return (bool)__any((seen >= mine && seen - mine < 32) || !(share > 0.0f || (share == 0.0f && !odd)));
+            return (bool)__any((seen >= mine && seen - mine < 32) || seen >= kFarLabel || !(share > 0.0f || (share == 0.0f && !odd)));
         }
         if ((t + 1) * ROWS > here) {                       // (behind the last class)
             int end = here - t * ROWS - 4 * half;
@@ -491,6 +502,17 @@ __global__ void __launch_bounds__(kThreads, 2) k_softmax_rows(const Job job) {
                 m = higher;
                 __builtin_amdgcn_sched_barrier(0);
             }
+            base = m == -__builtin_inff() || is_far(m) ? 0.0f : m * kLog2e;
+        }
+        if (MODE == LOSS ? __any(is_far(m)) : far) {
+            float a = m;
+            if (MODE == DX) a = label >= 0 ? job.lse[owner] : 0.0f;
+            a = is_far(a) ? a : 0.0f;
+#pragma unroll
+            for (int q = 0; q < SB; ++q)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) z[q][i] -= a;
+            __builtin_amdgcn_sched_barrier(0);
         }
         return hits;
     };
@@ -518,8 +540,8 @@ __global__ void __launch_bounds__(kThreads, 2) k_softmax_rows(const Job job) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const int row = q * 32 + f * 16 + row_at(j) + 4 * half;
-                const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(z[q][f * 8 + j], kLog2e, -row_lse[place][row])), share = row_share[place][row];
-                v[j] = share == 0.0f ? 0.0f : share * (p - (row_label[place][row] == mine ? 1.0f : 0.0f));       // (nothing of a row that does not count, whatever its p is)
+                const float p = __builtin_amdgcn_exp2f((z[q][f * 8 + j] - row_lse[place][row]) * kLog2e), share = row_share[place][row];
+                v[j] = share == 0.0f ? 0.0f : share * (p - ((row_label[place][row] & ~kFarLabel) == mine ? 1.0f : 0.0f));       // (nothing of a row that does not count, whatever its p is)
             }
         }
         __builtin_amdgcn_sched_barrier(0);
@@ -528,7 +550,6 @@ __global__ void __launch_bounds__(kThreads, 2) k_softmax_rows(const Job job) {
     // the powers of a whole tile
     const auto powers = [&](int t, int place, Acc (&z)[SB]) __attribute__((always_inline)) {
         const bool rare = open_tile(t, place, z);
-        base = m == -__builtin_inff() ? 0.0f : m * kLog2e;
         float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -561,7 +582,6 @@ __global__ void __launch_bounds__(kThreads, 2) k_softmax_rows(const Job job) {
             load(t + LOOK, 0, true);
             next_tile();
             const bool rare = open_tile(t, now, z);
-            base = m == -__builtin_inff() ? 0.0f : m * kLog2e;
             clear(next);
             float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f}, both[2][4], v[8];
             const auto read_both = [&](int e) __attribute__((always_inline)) {
@@ -692,8 +712,8 @@ __global__ void __launch_bounds__(kThreads, 2) k_softmax_rows(const Job job) {
     if constexpr (MODE == LOSS) {
         s += lost;
         const float other_m = __shfl_xor(m, 32, RG_WAVE), other_s = __shfl_xor(s, 32, RG_WAVE);
-        const float top = fmaxf(m, other_m), base = top == -__builtin_inff() ? 0.0f : top * kLog2e;
-        const float sum = s * __builtin_amdgcn_exp2f(__builtin_fmaf(m, kLog2e, -base)) + other_s * __builtin_amdgcn_exp2f(__builtin_fmaf(other_m, kLog2e, -base));
+        const float top = fmaxf(m, other_m), from = top == -__builtin_inff() ? 0.0f : top;
+        const float sum = s * __builtin_amdgcn_exp2f((m - from) * kLog2e) + other_s * __builtin_amdgcn_exp2f((other_m - from) * kLog2e);
         if (half == 0 && owner < owners) job.stats[split * job.owners + owner] = make_float2(top, sum);
     } else {
         if (owner >= owners) return;
@@ -884,7 +904,7 @@ __global__ void __launch_bounds__(kClassThreads, 2) k_few_classes(const FewJob j
     // g loses bits with the power of two that they have in common (of f16, any), dx gets a g of its own, each row with its own power.  Of f16 both lie in LDS, and wavefronts
     // that would be idle form z and the other g; else there is no room, and dweight's is formed when dx is done.  Powers of two change no bits, so that a row's dx is the
     // same whatever other rows have.  100 k rows of 256 over 47 classes, without shares, with shares of [0, 2), and with some 2^60 below: f32
-    // 86, 89 and 109 us, bf16 48, 50 and 62, f16 48, 56 and 56.
+    // 86, 88 and 109 us, bf16 48, 49 and 62, f16 48, 55 and 55.
     int power = 0;
     bool apart = false;
     if (GRAD && job.dloss) {
@@ -957,9 +977,10 @@ __global__ void __launch_bounds__(kClassThreads, 2) k_few_classes(const FewJob j
 
         // z: a wavefront's block of 32 classes by 32 rows, of numbers in three parts half of its steps, which the other half's wavefront adds
         const int cb = wave & 1, rb = RB == 2 ? wave >> 1 & 1 : 0, part = wave >> RB, mine = RB == 1 ? label[0] : rb ? label[RB - 1] : label[0];
+        const bool second_form = FORMS == 2 && apart && part == 1;
         constexpr int HALVES = P > 1 ? 2 : 1;
         Acc z;
-        if (part < HALVES || (FORMS == 2 && apart && part == 1)) {
+        if (part < HALVES || second_form) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) z[i] = 0.0f;
             const int middle = HALVES == 2 ? steps / 4 * 2 : steps, from = HALVES == 2 ? part * middle : 0, to = part == 0 ? middle : steps;
@@ -993,13 +1014,13 @@ __global__ void __launch_bounds__(kClassThreads, 2) k_few_classes(const FewJob j
         const int first = cb * 32 + 4 * half;              // register i: class first + 8 (i >> 2) + (i & 3)
         const auto put_g = [&](int form, int scale_power) __attribute__((always_inline)) {         // share g, to LDS
             const int64_t row = t0 * R + t * R + min(rb * 32 + (lane & 31), here - 1 - t * R);
-            const float lse2 = mine >= 0 ? job.lse[row] * kLog2e : 0.0f, share = mine >= 0 ? ldexpf(job.dloss ? job.dloss[row] : 1.0f, S::BIAS - scale_power) : 0.0f;
+            const float lse = mine >= 0 ? job.lse[row] : 0.0f, share = mine >= 0 ? ldexpf(job.dloss ? job.dloss[row] : 1.0f, S::BIAS - scale_power) : 0.0f;
             const bool idle = mine < 0 || share == 0.0f;
             float v[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 const int c = first + 8 * (i >> 2) + (i & 3);
-                const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(z[i], kLog2e, -lse2));
+                const float p = __builtin_amdgcn_exp2f((z[i] - lse) * kLog2e);
                 v[i] = idle || c >= classes ? 0.0f : share * (p - (c == mine ? 1.0f : 0.0f));
             }
             const int at = rb * 32 + (lane & 31);
@@ -1017,7 +1038,7 @@ __global__ void __launch_bounds__(kClassThreads, 2) k_few_classes(const FewJob j
                         *(Words2*)(lds.g[form][p] + at * Lds::G_ROW + (((cb * 4 + i / 4 + j) ^ g_twist(at)) << 4) + half * 8) = Words2{w[p][2 * j], w[p][2 * j + 1]};
             }
         };
-        if (part == 0) {
+        if (part == 0 || second_form) {
             if constexpr (!GRAD) {
                 float top = -__builtin_inff(), there = 0.0f;
                 bool met = false;
@@ -1041,8 +1062,8 @@ __global__ void __launch_bounds__(kClassThreads, 2) k_few_classes(const FewJob j
                     lds.sum[cb][at] = sum;
                 }
                 if (met) lds.target[at] = there;
-            } else put_g(0, RB == 1 ? own_power[0] : rb ? own_power[RB - 1] : own_power[0]);
-        } else if (FORMS == 2 && apart && part == 1) put_g(1, power);
+            } else put_g(second_form ? 1 : 0, second_form ? power : RB == 1 ? own_power[0] : rb ? own_power[RB - 1] : own_power[0]);
+        }
         __syncthreads();
         if constexpr (!GRAD) {
             if (threadIdx.x < R && t * R + (int)threadIdx.x < here) {

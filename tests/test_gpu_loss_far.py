@@ -6,7 +6,7 @@ import torch
 import training_reference as ref
 import vector_reference as vec
 from test_gpu_loss_ops import check_grads, inputs, on_gpu
-from test_gpu_training_ops import DEV, F32, ctx, f64, _name_the_case  # noqa: F401  (fixtures among them)
+from test_gpu_training_ops import DEV, F32, check, ctx, f64, _name_the_case  # noqa: F401  (fixtures among them)
 
 pytestmark = pytest.mark.gpu
 
@@ -74,6 +74,50 @@ def test_small_shares_keep_their_bits(ctx, dtype, n, classes, dim):  # noqa: F81
     ctx.cross_entropy_grad(x, n, dim, w, classes, on_gpu(labels), lse, dx, dw, dloss=dloss, scale=scale)
     rest = np.arange(1, n)
     check_grads(dx[1:], None, f64(x)[rest], f64(w), labels[rest], f64(lse)[rest], f64(dloss)[rest] * scale, dtype)
+
+
+# ---------------------------------------------------------------- logits of any size
+@pytest.mark.parametrize("dtype,far", [(F32, 10), (F32, 33), (F32, 60), (F32, 127), (torch.bfloat16, 10), (torch.bfloat16, 33), (torch.bfloat16, 60), (torch.bfloat16, 127),
+                                       (torch.float16, 10), (torch.float16, 30)])
+@pytest.mark.parametrize("n,classes,dim", [(100, 40, 64), (100, 33, 300), (20, 300, 64), (100, 300, 64), (100, 300, 16), (100, 200, 200), (100, 300, 300), (700, 5000, 64), (700, 5000, 300)])
+def test_logits_of_any_size(ctx, dtype, far, n, classes, dim):  # noqa: F811
+    """z of one product each, exact: m 2^(far - 1) with whole m in [-3, 3].  exp(z - lse) is 0 below a row's largest (its exponent is -512 or less).  lse = m + log(count):
+    one rounding to 32 bits, one of m / ln 2, two steps of log(count) < 9.  Given the largest z as lse, p is 1 or 0, so that sums of whole numbers below 2^13 times
+    powers of two make both gradients exact up to their storing; where lse is small (far 10) p may err as lse / ln 2 does."""
+    rng = np.random.default_rng(far + classes)
+    left = far // 2
+    x = torch.zeros(n, dim, dtype=dtype, device=DEV)
+    at = rng.integers(0, dim, n)
+    x[torch.arange(n), torch.from_numpy(at)] = 2.0 ** left
+    whole = rng.integers(-3, 4, size=(classes, dim))
+    whole[:, ::2] = -np.abs(whole[:, ::2]) - (whole[:, ::2] == 0)                   # (columns whose largest is below zero too)
+    whole[:, 3] = np.where(np.arange(classes) == classes // 2, 3, -3)               # (and one whose largest stands alone)
+    w = (torch.from_numpy(whole).double() * 2.0 ** (far - 1 - left)).to(dtype).to(DEV)
+    labels = rng.integers(0, classes, n)
+    labels[:n // 2] = whole[:, at[:n // 2]].argmax(0)
+    labels[3] = -1
+    counts = labels >= 0
+    z = f64(x) @ f64(w).T
+    want, want_lse = vec.cross_entropy(z, labels)
+    loss, lse = torch.empty(n, device=DEV), torch.empty(n, device=DEV)
+    ctx.cross_entropy(x, n, dim, w, classes, on_gpu(labels), loss, lse)
+    allowed = 2.0 ** -23 * np.abs(want_lse) + 2.0 ** -19
+    with np.errstate(over="ignore"):
+        stored = want.astype(np.float32).astype(np.float64)                           # (the distance of two z may be beyond 32 bits)
+    check(lse, want_lse, allowed, "lse")
+    check(loss, np.where(np.isinf(stored), stored, want), 2 * allowed + 2.0 ** -23 * np.abs(want), "loss")
+    dx, dw = torch.empty(n, dim, dtype=dtype, device=DEV), torch.empty(classes, dim, dtype=dtype, device=DEV)
+    saved = torch.from_numpy(np.where(counts, z.max(1), 0.0)).float().to(DEV)
+    ctx.cross_entropy_grad(x, n, dim, w, classes, on_gpu(labels), saved, dx, dw, scale=2.0 ** -12)
+    want_dx, want_dw, p, g = vec.cross_entropy_grad(z, labels, f64(saved), np.full(n, 2.0 ** -12), f64(x), f64(w))
+    if far == 10:
+        eg = 2.0 ** -12 * p * 2.0 ** -22 * (np.abs(z) + np.abs(f64(saved))[:, None] + 2.0)
+        eg += np.abs(g) * (ref.HALF_ULP[dtype] if dtype != F32 else 2.0 ** -20)
+        eg += 2.0 ** -50 if dtype == torch.float16 else 0.0                           # (f16's smallest step, 2^-38 of the share)
+    else:
+        eg = np.zeros_like(p)
+    check(dx, want_dx, eg @ np.abs(f64(w)) + (ref.stored(want_dx, dtype) if dtype != F32 or far == 10 else 2.0 ** -149), "dx")
+    check(dw, want_dw, eg.T @ np.abs(f64(x)) + (ref.stored(want_dw, dtype) if dtype != F32 or far == 10 else 2.0 ** -149), "dweight")
 
 
 # ---------------------------------------------------------------- many classes beside one

@@ -6,7 +6,7 @@ import torch
 import training_reference as ref
 import vector_reference as vec
 from test_gpu_loss_ops import check_grads, inputs, on_gpu
-from test_gpu_training_ops import DEV, F32, check, ctx, f64, _name_the_case  # noqa: F401  (fixtures among them)
+from test_gpu_training_ops import DEV, F32, PAD, check, ctx, f64, _name_the_case  # noqa: F401  (fixtures among them)
 
 pytestmark = pytest.mark.gpu
 
@@ -142,3 +142,61 @@ def test_what_one_class_leaves_is_shared_by_many(ctx, dtype, n, dim):  # noqa: F
         want = torch.log1p(c)
         allowed = 8 * 2.0 ** -24 * (a + 1.0) + 2.0 ** -18 * c
         assert bool(((lse.double() - a - want).abs() <= allowed).all()) and bool(((loss.double() - want).abs() <= allowed).all())
+
+
+# ---------------------------------------------------------------- long sums in 32 bits
+def one_sign(gen, rows, dim):
+    return torch.randn(rows, dim, generator=gen, device=DEV) * 0.2 + 1.0
+
+
+def long_sum(count, size):
+    """A sum of `count` terms in stretches of 4096: of each, and of their sums."""
+    return ref.sum_error(min(count, 4096), size) + ref.sum_error(-(-count // 4096), size)
+
+
+def g_error(p, z, x, w, lse, share):
+    return share * p * (ref.sum_error(x.shape[1], np.abs(x) @ np.abs(w).T) + 2.0 ** -20 * (np.abs(x) @ np.abs(w).T) + 2.0 ** -22 * (np.abs(z) + np.abs(lse)[:, None] + 2.0))
+
+
+@pytest.mark.parametrize("n,classes,dim", [(200_000, 66_000, 16), (70_000, 66_000, 40), (1_000_000, 1000, 16), (1_000_003, 47, 16), (60_000, 70_000, 300)])
+def test_weight_gradients_of_many_rows_of_one_sign(ctx, n, classes, dim):  # noqa: F811
+    """f32: a sum of many numbers of one sign, half of it taken away again by the label's rows, errs as sums of 4096 do."""
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(n)
+    x, w = one_sign(gen, n, dim), torch.randn(classes, dim, generator=gen, device=DEV) * 0.1
+    labels = torch.randint(0, classes, (n,), generator=gen, device=DEV).int()
+    lse = torch.empty(n, device=DEV)
+    ctx.cross_entropy(x, n, dim, w, classes, labels, None, lse)
+    dw = torch.full((classes + 1, dim), PAD, device=DEV)
+    ctx.cross_entropy_grad(x, n, dim, w, classes, labels, lse, None, dw[:classes])
+    assert bool((dw[classes] == PAD).all())
+    some = np.unique(np.r_[0:12, classes - 12:classes])
+    at = torch.from_numpy(some).to(DEV)
+    x64, w64, l64, told = f64(x), f64(w[at]), f64(lse), labels.long().cpu().numpy()
+    z = x64 @ w64.T
+    p = np.exp(z - l64[:, None])
+    g = p - (told[:, None] == some[None, :])
+    eg = g_error(p, z, x64, w64, l64, 1.0) + np.abs(g) * (2.0 ** -23 + 2.0 ** -20)
+    check(dw[at], g.T @ x64, eg.T @ np.abs(x64) + long_sum(n, np.abs(g).T @ np.abs(x64)), "dweight")
+
+
+@pytest.mark.parametrize("n,classes,dim", [(33_000, 400_000, 16), (33_000, 100_000, 100), (4096, 300_000, 300), (2000, 1_000_000, 16)])
+def test_row_gradients_against_many_classes_of_one_sign(ctx, n, classes, dim):  # noqa: F811
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(n)
+    x, w = torch.randn(n, dim, generator=gen, device=DEV) * 0.1, one_sign(gen, classes, dim)
+    labels = torch.randint(0, classes, (n,), generator=gen, device=DEV).int()
+    lse = torch.empty(n, device=DEV)
+    ctx.cross_entropy(x, n, dim, w, classes, labels, None, lse)
+    dx = torch.full((n + 1, dim), PAD, device=DEV)
+    ctx.cross_entropy_grad(x, n, dim, w, classes, labels, lse, dx[:n], None)
+    assert bool((dx[n] == PAD).all())
+    some = np.unique(np.r_[0:12, n - 12:n])
+    at = torch.from_numpy(some).to(DEV)
+    x64, w64, l64, told = f64(x[at]), f64(w), f64(lse[at]), labels[at].long().cpu().numpy()
+    z = x64 @ w64.T
+    p = np.exp(z - l64[:, None])
+    g = p.copy()
+    g[np.arange(len(some)), told] -= 1.0
+    eg = g_error(p, z, x64, w64, l64, 1.0) + np.abs(g) * (2.0 ** -23 + 2.0 ** -20)
+    check(dx[at], g @ w64, eg @ np.abs(w64) + long_sum(classes, np.abs(g) @ np.abs(w64)), "dx")

@@ -662,10 +662,20 @@ __global__ void __launch_bounds__(kThreads, 2) k_softmax_rows(const Job job) {
         Acc z[SB];
         const auto add_products = [&](int chunk, int buffer) __attribute__((always_inline)) {
             const int here = steps - chunk * kSteps;
-            if (here > 6) products(RG_INT(8), chunk, buffer, z, nothing);
-            else if (here > 4) products(RG_INT(6), chunk, buffer, z, nothing);
-            else if (here > 2) products(RG_INT(4), chunk, buffer, z, nothing);
-            else products(RG_INT(2), chunk, buffer, z, nothing);
+            // (of numbers in parts a chunk's sum apart: to a long row's z the products of small parts would add nothing)
+            Acc apart[SB];
+            Acc(&to)[SB] = P > 1 ? apart : z;
+            if (P > 1) clear(apart);
+            if (here > 6) products(RG_INT(8), chunk, buffer, to, nothing);
+            else if (here > 4) products(RG_INT(6), chunk, buffer, to, nothing);
+            else if (here > 2) products(RG_INT(4), chunk, buffer, to, nothing);
+            else products(RG_INT(2), chunk, buffer, to, nothing);
+            if (P > 1) {
+#pragma unroll
+                for (int q = 0; q < SB; ++q)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) z[q][i] += apart[q][i];
+            }
         };
         if (tiles > 0) {
             load(0, chunk_of(0), true);

@@ -200,3 +200,30 @@ def test_row_gradients_against_many_classes_of_one_sign(ctx, n, classes, dim):  
     g[np.arange(len(some)), told] -= 1.0
     eg = g_error(p, z, x64, w64, l64, 1.0) + np.abs(g) * (2.0 ** -23 + 2.0 ** -20)
     check(dx[at], g @ w64, eg @ np.abs(w64) + long_sum(classes, np.abs(g) @ np.abs(w64)), "dx")
+
+
+@pytest.mark.parametrize("n,classes,dim", [(64, 200, 8192), (64, 100, 20_000), (33, 65, 65_536), (5, 40, 8191)])
+def test_long_rows_of_one_sign(ctx, n, classes, dim):  # noqa: F811
+    """f32: z of many numbers of one sign errs as sums of 128 do, and each row's loss and gradients with it."""
+    rng = np.random.default_rng(dim)
+    x = torch.from_numpy(rng.random((n, dim))).float().to(DEV)
+    w = torch.from_numpy(rng.random((classes, dim)) * (400.0 / dim)).float().to(DEV)
+    labels = rng.integers(0, classes, n)
+    loss, lse = torch.empty(n, device=DEV), torch.empty(n, device=DEV)
+    ctx.cross_entropy(x, n, dim, w, classes, on_gpu(labels), loss, lse)
+    x64, w64 = f64(x), f64(w)
+    z = vec.logits(x64, w64)
+    size = np.abs(x64) @ np.abs(w64).T
+    # (chunks' sums are added with roundings to the nearest, 2^-24 each, independent: four deviations)
+    ez = 2.0 ** -20 * size + ref.sum_error(128, size) + 4.0 * np.sqrt(dim / 128) * 2.0 ** -24 * size
+    want, want_lse = vec.cross_entropy(z, labels)
+    allowed = ez.max(1) + 2.0 ** -22 * (np.abs(z).max(1) + np.abs(want_lse) + 2.0) + ref.sum_error(classes, 1.0)
+    check(lse, want_lse, allowed, "lse")
+    check(loss, want, allowed + ez.max(1) + 2.0 ** -23 * np.abs(want), "loss")
+    lse = torch.from_numpy(want_lse).float().to(DEV)
+    dx, dw = torch.empty(n, dim, device=DEV), torch.empty(classes, dim, device=DEV)
+    ctx.cross_entropy_grad(x, n, dim, w, classes, on_gpu(labels), lse, dx, dw)
+    want_dx, want_dw, p, g = vec.cross_entropy_grad(z, labels, f64(lse), np.ones(n), x64, w64)
+    eg = p * (ez + 2.0 ** -22 * (np.abs(z) + np.abs(f64(lse))[:, None] + 2.0)) + np.abs(g) * (2.0 ** -23 + 2.0 ** -20)
+    check(dx, want_dx, eg @ np.abs(w64) + ref.sum_error(classes, np.abs(g) @ np.abs(w64)) + ref.stored(want_dx, F32), "dx")
+    check(dw, want_dw, eg.T @ np.abs(x64) + ref.sum_error(n, np.abs(g).T @ np.abs(x64)) + ref.stored(want_dw, F32), "dweight")

@@ -70,7 +70,7 @@ __global__ void __launch_bounds__(kThreads) k_embedding(const T* __restrict__ ta
 
 // ---------------------------------------------------------------- zeros
 // Rows of a whole table that no id meets are zeros: all of it is cleared first, by workgroups of their own beside those of the launches that sort the ids (which
-// wait for each other more than they work: 65536 ids take 25 us in six launches).  pieces `from` .. `to` - 1 of 16 bytes, `chunks` to a row.
+// wait for each other more than they work: 65536 ids take 33 us in four launches, with 102 MB of zeros beside them).  pieces `from` .. `to` - 1 of 16 bytes, `chunks` to a row.
 struct Zeros {
     void* grad;
     int64_t stride, from, to;
@@ -405,7 +405,7 @@ __global__ void __launch_bounds__(kThreads) k_sum_pieces(const T* __restrict__ d
 // with 4 columns each (blockIdx.y: which 2^log2L) side by side on runs of its pieces.  Most workgroups only look; those that join wait for a few reads one behind the
 // other: 8 us of 65 k entries (12 where the last piece was looked for by halving), 5 of 794 k ids met once, 12.5 of 1.5 M entries of 47 ids.  There, ids join hundreds
 // of pieces each, and eight lanes a group (32 groups to a workgroup, more workgroups to an id) take 12.5 instead of the 20 of 32 lanes; on the 65 k entries it
-// is 21 instead of 8, so that the host takes them for ids of 64 entries or more.  Workgroups of 1024 threads: 42 to 57.
+// is 21 instead of 8, so that the host takes them where few ids have all entries.  Workgroups of 1024 threads: 42 to 57.
 constexpr int kJoinThreads = 256, kJoinPieces = 2;
 
 template <typename U, bool SHORT>
@@ -637,8 +637,11 @@ rg_status sum_by_id(rg_ctx* ctx, const char* who, const void* dy, rg_dtype dy_ty
         return RG_OK;
     }
     // pieces of 16 entries or more, and as many of them as fill the device: of 1 M f32 rows of 32 / 128 numbers into the rows met of 100000, 4096 pieces take 146 / 207 us, 8192
-    // 124 / 217, 16384 135 / 236.  Ids of many entries are joined from hundreds of pieces each: of 1.5 M rows of 100 into 47, 4096 pieces take 169 us, 16384 203
-    const bool dense = n / rg_max64(num_rows, 1) >= 64;
+    // 124 / 217, 16384 135 / 236.  Where few ids have all entries, each of them is joined from hundreds of pieces, and half as many pieces with narrower groups at the join
+    // take less: f32, at 1024 / 16384 / 100 k entries an id, 1.5 M rows of 100 210 / 167 / 163 us so and 206 / 176 / 178 otherwise, 1 M of 256 266 / 231 / 227 and 245 / 230 / 244,
+    // 300 k of 100 54 / 47 / 49 and 51 / 50 / 73; bf16, 1.5 M of 100 167 / 129 / 126 and 148 / 122 / 123, 300 k of 100 49 / 43 / 47 and 43 / 44 / 67.  (Of up to 32 columns
+    // the groups are narrow anyway: 1 M of 32 91 / 75 / 73 and 70 / 55 / 54.)
+    const bool dense = dim > 32 && n / rg_max64(num_rows, 1) >= 16384;
     const int most = (int)rg_max64(1024, rg_min64(dense ? 4096 : 8192, (1ll << 23) / dim));
     const int64_t size = rg_max64(16, rg_div_up(n, most));
     const int pieces = (int)rg_div_up(n, size);

@@ -70,3 +70,22 @@ def test_lookups_whose_result_is_stored_past_the_caches(ctx, table_type, out, n,
     there = (ids >= 0) & (ids < rows)
     want = torch.where(there[:, None], table[ids.clamp(0, rows - 1)].float() * 4.0, torch.zeros((), device=DEV)).to(out)
     assert torch.equal(y, want) and untouched(flat, y)
+
+
+@pytest.mark.parametrize("n,rows", [(50_001, 1), (50_001, 3), (16_384 * 4 - 1, 4), (16_384 * 4, 4), (400_003, 5), (1_500_000, 47)])
+@pytest.mark.parametrize("dim,dtype", [(32, F32), (33, F32), (40, torch.bfloat16), (100, torch.float16), (300, F32), (1030, torch.bfloat16)])
+def test_gradients_of_few_ids_that_have_all_entries(ctx, n, rows, dim, dtype):  # noqa: F811
+    """Both sides of the line beyond which ids are joined by narrow groups, and hubs of many pieces."""
+    if n * dim > 200_000_000:
+        n = 200_000_000 // dim
+    ids, dy, there = entries(n, rows, dim, dtype, n + dim)
+    want = sums(ids, dy, there, rows)
+    grad = torch.full((rows + 1, dim), PAD, device=DEV)
+    ctx.embedding_grad(dy, ids, n, dim, rows, grad[:rows])
+    assert torch.equal(grad[:rows].double(), want) and bool((grad[rows] == PAD).all())
+    many = torch.full((rows, dim), PAD, device=DEV)
+    touched, met = torch.full((rows,), -7, dtype=torch.int32, device=DEV), torch.zeros(1, dtype=torch.int32, device=DEV)
+    ctx.embedding_grad_rows(dy, ids, n, dim, rows, many, touched, met)
+    named = torch.unique(ids[there])
+    k = named.numel()
+    assert int(met) == k and torch.equal(touched[:k], named) and torch.equal(many[:k].double(), want[named.long()])

@@ -7,13 +7,16 @@ namespace {
 
 // With z = x . weight^T (n rows, `classes` columns), lse_i = log sum_c exp z_ic:  loss_i = lse_i - z_i,label(i);  with g_ic = exp(z_ic - lse_i) - [c = label(i)]:
 // dx_i = share_i sum_c g_ic weight_c,  dweight_c = sum_i share_i g_ic x_i.
-// One kernel does all three.  A wavefront owns 32 OB rows of one operand (of x for the loss and dx, of the weight for dweight) and walks the rows of the other, 64
-// at a time through LDS: z of 64 by 32 OB from the matrix units, with the owned row along the lanes, so that a row's maximum and sum stay in
+// One kernel does all three.  A wavefront owns 32 rows of one operand (of x for the loss and dx, of the weight for dweight) and walks the rows of the other, 64
+// at a time through LDS: z of 64 by 32 from the matrix units, with the owned row along the lanes, so that a row's maximum and sum stay in
 // its lane; exponentials; then, for a gradient, z's registers are the right operand of the second product as they lie, and the left one is the staged tile
 // again, read transposed.  dx and dweight each form z anew: that is one product in four, and nothing of size n by classes is ever stored.
 //
-// Numbers go through the matrix units as bf16 or f16 as they are; f32 in three parts of bf16 that add up to it (the six products of parts that reach
-// above 2^-24).  Of g, sums are in 32 bits and the second product takes g rounded to the rows' type (bf16: off by at most 2^-8 of it, as the result's own rounding is; f32: three parts again).
+// Numbers go through the matrix units as bf16 or f16 as they are; f32 in three parts of bf16 that add up to it, of which the second and third reach 2^-7 and 2^-15 of a
+// number: six products of parts (what the other three would add is below 2^-21 + 2^-30 of the product, and has its sign).  Of g, sums are in 32 bits and the second
+// product takes g rounded to the rows' type: bf16 off by at most 2^-8 of it, as the result's own rounding is, which takes a result of few terms up to sqrt(2) times as far from
+// 64 bits (dx and dweight over 2 to 100 classes 2.2e-3 of their norm instead of 1.7e-3, of 1024 rows against 2.4 M classes 1.65e-3 and 1.1e-4 either way), where two parts of g
+// would be half as many products again; f32 in three parts as above.
 // For f16, g is scaled by 2^14, which keeps g down to 2^-28 in f16's normal range.  dx's g is without the row's share, or with what of it lies in [0.5, 1); dweight's has
 // it, as a part of the largest (finite) share of the rows that a workgroup sums, so that of f16 what lies 2^-28 below that one loses bits.
 typedef float Acc __attribute__((ext_vector_type(16)));
@@ -190,9 +193,9 @@ constexpr bool held_rows(int mode, int steps) { return Part<T>::P == 1 && steps 
 // STEPS: 16 columns each, of rows of up to 256 numbers; 0: any, in chunks of 128 columns.
 // Bound by the matrix units, which the loss and dx keep busy 52 to 65 % of the cycles, dweight, whose workgroups walk 1024 rows and then load and store their own, 37 %, at the
 // 1.65 to 2.1 GHz that the card's power leaves them (a large library product of
-// bf16 reaches 1330 TFLOP/s): loss of 4096 rows of 256 f16 over 233 k classes 470-500 us, 980-1040 TFLOP/s; of 1024 rows of 100 bf16 over 2.4 M, dx 1110-1170 us and
-// dweight 1300-1700, 860-900 and 590-770 TFLOP/s of two products each (of 112 and 128 columns where rows have 100: a fifth more work); of 1024 rows of 128 f32 over
-// 200 k, dx 575 and dweight 880, at six products of parts 1090 and 710.  Two wavefronts a SIMD with 256 registers each: with three (32 walked rows) they spill; of two
+// bf16 reaches 1330 TFLOP/s): loss of 4096 rows of 256 f16 over 233 k classes 470-530 us, 920-1040 TFLOP/s; of 1024 rows of 100 bf16 over 2.4 M, dx 1000-1150 us and
+// dweight 1350-1700, 870-1000 and 590-740 TFLOP/s of two products each (of 112 and 128 columns where rows have 100: a fifth more work); of 1024 rows of 128 f32 over
+// 200 k, dx 510-575 and dweight 790-880, at six products of parts 1090-1230 and 710-800.  Two wavefronts a SIMD with 256 registers each: with three (32 walked rows) they spill; of two
 // blocks of owned rows to a wavefront too.  Two workgroups of 4 wavefronts to a unit took 1342 us where one of 8 takes 1264; one tile between barriers 1260 where two
 // take 1200; an order of priorities, deeper reads of fragments, another place of the loads or the first tiles loaded together changed nothing beyond 3 %.
 template <typename T, int MODE, int NB, int STEPS>
@@ -838,7 +841,7 @@ __global__ void __launch_bounds__(256) k_zero_rows(T* __restrict__ out, int64_t 
 // Up to 64 classes, whose weight rows fit LDS beside a tile of R rows of x: a workgroup walks its rows once, each tile z, g, dx and its share of dweight, so that x is
 // read and dx written once and z is formed once.  z is [class][row] (rows along the lanes); g goes through LDS, from where dx's product reads it by rows and
 // dweight's transposed.  Outputs go to the wavefronts by blocks of 32 columns; dweight's sums stay in registers until the end, then a second launch joins the workgroups'.
-// 1024 rows of 256 f32 over 41 classes 7.2 us (the general kernel and its two companions: 21); gradients of 100 k rows of 256 f32 over 47 classes 90 us, 2.3 TB/s read and
+// 1024 rows of 256 f32 over 41 classes 7.2 us (the general kernel and its two companions: 21); gradients of 100 k rows of 256 f32 over 47 classes 92 us, 2.2 TB/s read and
 // written: products of three parts, cutting rows into them and the barriers between a tile's steps take turns (four wavefronts instead of eight: 119; the general kernel: 429).
 template <int P, int FORMS, int R, int CHUNKS>
 struct FewLds {
@@ -1176,8 +1179,9 @@ __global__ void __launch_bounds__(kClassThreads, 2) k_few_classes(const FewJob j
     }
 }
 
-// Whether the kernel above takes rows of `dim` numbers, and its launch.  Both sides of the line, 64 and 65 classes, rows of 256: loss of 1024 f32 7.5 and 21.5 us, of 100 k
-// bf16 19 and 52; gradients of 1024 f32 15 and 95, of 100 k f32 96 and 453, of 100 k bf16 50 and 123; rows of 100, 100 k f32 51 and 166.  (More classes do not fit LDS.)
+// Whether the kernel above takes rows of `dim` numbers, and its launch.  Both sides of the line, 64 and 65 classes, rows of 256: loss of 1024 f32 8 and 21.5 us, of 100 k
+// bf16 19 and 52; gradients of 1024 f32 15 and 95, of 100 k f32 90 and 451, of 100 k bf16 50 and 123; rows of 100, 100 k f32 52 and 167.  (f32 rows beyond 128 numbers fill LDS
+// with 64 classes.  For the others more classes would fit; the kernel has two blocks of them.)
 constexpr int kFewClasses = 64;
 template <typename T>
 bool few_classes(int classes, int dim) { return classes <= kFewClasses && dim >= 8 && dim <= (Part<T>::P > 1 ? 256 : 512); }
@@ -1296,7 +1300,7 @@ __global__ void __launch_bounds__(64 * kFewWaves, 2) k_few_rows(const T* __restr
 }
 
 // Whether the kernel above takes the call: its rows as parts lie in LDS (16 KB at 256 numbers of 16 bits).  Both sides of the line, 32 and 33 rows of 128 numbers: against
-// 200000 classes 31 and 84 us of f32, 17 and 24 of bf16; against 65, 11 and 16 of f32, 11 and 11 of bf16.
+// 200000 classes 31 and 72 us of f32, 17 and 22 of bf16; against 65, 11 and 16 of f32, 10 and 10 of bf16.
 constexpr int kFewRows = 32;
 template <typename T>
 bool few_rows_many_classes(int64_t n, int dim) { return n <= kFewRows && dim >= 8 && rg_div_up(dim, 32) * 2 * Part<T>::P * 1024 <= 60 * 1024; }
@@ -1341,8 +1345,8 @@ void join_parts(rg_ctx* ctx, const float* parts, int splits, int64_t rows, int64
     kernel<<<grid, dim < 4 ? 256 : 64 * runs, 0, s>>>(parts, splits, rows, first, n, n_dev, dim, quads, out, stride);
 }
 
-// Splits of the walked rows: as many workgroups as there are compute units, one to each (two to each with half as many owned rows, 4 wavefronts, took a few per cent
-// longer), or a multiple of that where a split would be longer than `longest` rows (which count in 31 bits).
+// Splits of the walked rows: as many workgroups as there are compute units, one to each (two to each, with half as many owned rows and 4 wavefronts, took 1342 us
+// instead of 1264 for dx of 1024 rows of 100 against 2.4 M), or a multiple of that where a split would be longer than `longest` rows (which count in 31 bits).
 int splits_for(rg_ctx* ctx, int64_t workgroups, int64_t walked, int64_t longest) {
     const int64_t fit = rg_max64(1, rg_min64(rg_div_up(walked, 64), ctx->num_cus / workgroups)), least = rg_div_up(walked, longest);
     return (int)(rg_div_up(least, fit) * fit);

@@ -14,9 +14,9 @@ namespace {
 //
 // Numbers go through the matrix units as bf16 or f16 as they are; f32 in three parts of bf16 that add up to it, of which the second and third reach 2^-7 and 2^-15 of a
 // number: six products of parts (what the other three would add is below 2^-21 + 2^-30 of the product, and has its sign).  Of g, sums are in 32 bits and the second
-// product takes g rounded to the rows' type: bf16 off by at most 2^-8 of it, as the result's own rounding is, which takes a result of few terms up to sqrt(2) times as far from
-// 64 bits (dx and dweight over 2 to 100 classes 2.2e-3 of their norm instead of 1.7e-3, of 1024 rows against 2.4 M classes 1.65e-3 and 1.1e-4 either way), where two parts of g
-// would be half as many products again; f32 in three parts as above.
+// product takes g rounded to the rows' type: bf16 off by at most 2^-8 of it, as the result's own rounding is, which takes results of few terms further from
+// 64 bits (of many rows over 2 to 100 classes 2.2e-3 of their norm instead of 1.7e-3, dweight of one row, where one g has all of the norm, up to 2^-8; of 1024 rows against 2.4 M
+// classes 1.65e-3 and 1.1e-4 either way), where two parts of g would be half as many products again; f32 in three parts as above.
 // For f16, g is scaled by 2^14, which keeps g down to 2^-28 in f16's normal range.  dx's g is without the row's share, or with what of it lies in [0.5, 1); dweight's has
 // it, as a part of the largest (finite) share of the rows that a workgroup sums, so that of f16 what lies 2^-28 below that one loses bits.
 typedef float Acc __attribute__((ext_vector_type(16)));

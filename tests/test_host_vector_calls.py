@@ -178,3 +178,18 @@ for line in log("launch"):
     x, y, block, lds = (int(v) for v in at[1:5])
     assert 1 <= x < 1 << 31 and 1 <= y <= 65535 and x * block < 1 << 32 and lds <= 65536, line
 ''')
+
+
+def test_scratch_of_long_walks_is_bounded():
+    """Gradients of f32 that are cut into walks of at most 4096 rows: parts of a gigabyte, twice that where their number is rounded up, and the owned rows' 128 MB."""
+    run(r'''
+for dim in (1, 16, 100, 300, 4000, 65536):
+    most = min((1 << 31) - 1, (1 << 38) // dim)
+    for n, classes in ((most, 65), (most, 4097), (most, 70_000), (40, min(1 << 30, most)), (33_000, min(1 << 30, most)), (1 << 20, min(1 << 30, most)), (5000, 5000), (70_000, 70_000)):
+        held = rt.memory_held()
+        assert loss_grad(n=n, classes=classes, dim=dim, stride=dim, weight_stride=dim, dx_stride=dim, dweight_stride=dim, type=F32) == OK, message()
+        assert rt.memory_held() - held <= (2 << 30) + (160 << 20), (n, classes, dim, rt.memory_held() - held)
+        rt.forget()
+        lib.rg_destroy(c)
+        c = context()
+''')
